@@ -1,15 +1,16 @@
 """Python binding of the MI355X CGTP library (libcgtp.so): argument marshalling only.
 
 Every step of the tensor products runs in the HIP kernels behind the C ABI
-declared in ``include/cgtp.h`` (full CGTP) and ``include/istp.h`` (the MIMO
-Gaunt and vector signal products); this module passes raw device pointers and
+declared in ``include/cgtp.h`` (full CGTP), ``include/istp.h`` (the MIMO
+Gaunt and vector signal products) and ``include/ffn.h`` (the feed-forward
+sublayer around them, bound in ``_ffn.py``); this module passes raw device pointers and
 a HIP stream through ctypes.  PyTorch is used for device memory and streams.
 There is no CPU fallback: if the shared library is missing or the GPU is
 absent, the calls raise.
 
 The functions carry the C names (``cgtp_plan``, ``cgtp_forward``,
-``istp_plan``, ...); ``Plan`` and ``IstpPlan`` are small convenience wrappers
-around them.
+``istp_plan``, ``ffn_plan``, ...); ``Plan``, ``IstpPlan``, ``FfnPlan`` and
+``NormPlan`` are small convenience wrappers around them.
 """
 from __future__ import annotations
 
@@ -18,7 +19,9 @@ import os
 
 import numpy as np
 
+from . import _ffn
 from ._build import LIB as _LIB_PATH
+from ._ffn import *  # noqa: F401,F403  (the feed-forward sublayer's names)
 
 CGTP_OK, CGTP_EINVAL, CGTP_EGRID, CGTP_EDTYPE, CGTP_ENOMEM, CGTP_EHIP, CGTP_EUNSUP = 0, -1, -2, -3, -4, -5, -6
 CGTP_ESCRATCH = -7
@@ -110,6 +113,7 @@ def _load():
         "istp_backward": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, i64, vp]),
         "istp_backward_query": (ctypes.c_int, [vp, ctypes.POINTER(i32), dp, dp]),
     }
+    sig.update(_ffn.SIGNATURES)
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
         fn.restype = res
@@ -128,7 +132,7 @@ def exported_symbols():
             "istp_plan", "istp_forward", "istp_forward_weighted", "istp_num_labels", "istp_label_index",
             "istp_forward_real", "istp_real_workspace_bytes", "istp_forward_real_static", "istp_backward_real",
             "istp_real_backward_workspace_bytes", "istp_backward_weighted", "istp_destroy", "istp_num_inputs", "istp_num_outputs", "istp_label_offset",
-            "istp_plan_query", "istp_plan_describe", "istp_backward", "istp_backward_query"]
+            "istp_plan_query", "istp_plan_describe", "istp_backward", "istp_backward_query"] + list(_ffn.SIGNATURES)
 
 
 def _check(rc: int, where: str):

@@ -1,0 +1,394 @@
+"""Binding of include/ffn.h: the gated feed-forward block, the norms around it
+with gate and residual scale, and counter-based dropout.
+
+As in the package itself: the functions carry the C names and take device
+pointers and a HIP stream; ``FfnPlan``, ``NormPlan`` and ``dropout`` take and
+return CUDA (HIP) torch tensors.  Outputs and workspaces that the caller does
+not give are allocated here, for the stream that uses them.
+"""
+from __future__ import annotations
+
+import ctypes
+
+FFN_FP32, FFN_BF16, FFN_FP16 = 0, 2, 3
+FFN_SILU, FFN_GELU, FFN_RELU = 0, 1, 2
+FFN_MAX_WIDTH, FFN_MAX_ROWS = 1 << 20, 1 << 30
+__all__ = ["FFN_FP32", "FFN_BF16", "FFN_FP16", "FFN_SILU", "FFN_GELU", "FFN_RELU", "FFN_MAX_WIDTH", "FFN_MAX_ROWS",
+           "ffn_norm", "ffn_plan", "ffn_destroy", "ffn_workspace_bytes", "ffn_backward_workspace_bytes", "ffn_forward",
+           "ffn_backward", "ffn_norm_forward", "ffn_norm_backward", "ffn_norm_workspace_bytes", "ffn_residual_forward",
+           "ffn_residual_backward", "ffn_dropout", "FfnPlan", "NormPlan", "dropout"]
+_DTYPES = {"fp32": FFN_FP32, "bf16": FFN_BF16, "fp16": FFN_FP16}
+_ACTIVATIONS = {"silu": FFN_SILU, "gelu": FFN_GELU, "relu": FFN_RELU}
+
+
+class ffn_norm(ctypes.Structure):
+    _fields_ = [("width", ctypes.c_int64), ("rows_per_gate", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("dropout", ctypes.c_double), ("seed", ctypes.c_uint64),
+                ("offset", ctypes.c_uint64)]
+
+
+_i32, _i64, _u64, _vp, _int = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_int
+_np = ctypes.POINTER(ffn_norm)
+SIGNATURES = {
+    "ffn_plan": (_int, [_i64, _i64, _i64, _i32, _i32, ctypes.POINTER(_vp)]),
+    "ffn_destroy": (_int, [_vp]),
+    "ffn_workspace_bytes": (_i64, [_vp, _i64]),
+    "ffn_backward_workspace_bytes": (_i64, [_vp, _i64]),
+    "ffn_forward": (_int, [_vp, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "ffn_backward": (_int, [_vp, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "ffn_norm_forward": (_int, [_np, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "ffn_norm_backward": (_int, [_np, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "ffn_residual_forward": (_int, [_np] + [_vp] * 9 + [_i64, _vp]),
+    "ffn_residual_backward": (_int, [_np] + [_vp] * 15 + [_i64, _vp, _i64, _vp]),
+    "ffn_norm_workspace_bytes": (_i64, [_np, _i64, _i32]),
+    "ffn_dropout": (_int, [_vp, _i64, _vp, _i64, _i64, _i64, _i32, ctypes.c_double, _u64, _u64, _vp]),
+}
+
+
+def _call(name, *args):
+    from . import _check, _load
+    rc = getattr(_load(), name)(*args)
+    if rc:
+        _check(rc, name)
+
+
+def _code(table, value, what):
+    if value in table:
+        return table[value]
+    if isinstance(value, int):
+        return value
+    raise ValueError("%s must be one of %s" % (what, ", ".join(table)))
+
+
+# ---------------------------------------------------------------- C names
+
+def ffn_plan(d_in: int, d_ff: int, d_out: int, activation="silu", dtype="fp32") -> ctypes.c_void_p:
+    h = ctypes.c_void_p()
+    _call("ffn_plan", int(d_in), int(d_ff), int(d_out), _code(_ACTIVATIONS, activation, "activation"),
+          _code(_DTYPES, dtype, "dtype"), ctypes.byref(h))
+    return h
+
+
+def ffn_destroy(plan) -> None:
+    _call("ffn_destroy", plan)
+
+
+def ffn_workspace_bytes(plan, N: int) -> int:
+    from . import _load
+    return int(_load().ffn_workspace_bytes(plan, N))
+
+
+def ffn_backward_workspace_bytes(plan, N: int) -> int:
+    from . import _load
+    return int(_load().ffn_backward_workspace_bytes(plan, N))
+
+
+def ffn_forward(plan, x_ptr, ldx, w_in_ptr, w_out_ptr, y_ptr, saved_ptr, N, ws_ptr, ws_bytes, stream_ptr=None) -> None:
+    _call("ffn_forward", plan, x_ptr, ldx, w_in_ptr, w_out_ptr, y_ptr, saved_ptr, N, ws_ptr, ws_bytes, stream_ptr)
+
+
+def ffn_backward(plan, x_ptr, ldx, w_in_ptr, w_out_ptr, saved_ptr, g_ptr, ldg, gx_ptr, gw_in_ptr, gw_out_ptr, N,
+                 ws_ptr, ws_bytes, stream_ptr=None) -> None:
+    _call("ffn_backward", plan, x_ptr, ldx, w_in_ptr, w_out_ptr, saved_ptr, g_ptr, ldg, gx_ptr, gw_in_ptr, gw_out_ptr,
+          N, ws_ptr, ws_bytes, stream_ptr)
+
+
+def ffn_norm_forward(norm, x_ptr, ldx, w_ptr, u_ptr, ldu, rstd_ptr, N, stream_ptr=None) -> None:
+    _call("ffn_norm_forward", norm, x_ptr, ldx, w_ptr, u_ptr, ldu, rstd_ptr, N, stream_ptr)
+
+
+def ffn_norm_backward(norm, x_ptr, ldx, w_ptr, rstd_ptr, gu_ptr, ldg, gx_ptr, gw_ptr, N, ws_ptr, ws_bytes,
+                      stream_ptr=None) -> None:
+    _call("ffn_norm_backward", norm, x_ptr, ldx, w_ptr, rstd_ptr, gu_ptr, ldg, gx_ptr, gw_ptr, N, ws_ptr, ws_bytes,
+          stream_ptr)
+
+
+def ffn_norm_workspace_bytes(norm, N: int, residual: int) -> int:
+    from . import _load
+    return int(_load().ffn_norm_workspace_bytes(norm, N, residual))
+
+
+def ffn_residual_forward(norm, x_ptr, h_ptr, w_ptr, gate_ptr, scale_ptr, w_next_ptr, y_ptr, u_ptr, stats_ptr, N,
+                         stream_ptr=None) -> None:
+    _call("ffn_residual_forward", norm, x_ptr, h_ptr, w_ptr, gate_ptr, scale_ptr, w_next_ptr, y_ptr, u_ptr, stats_ptr,
+          N, stream_ptr)
+
+
+def ffn_residual_backward(norm, h_ptr, y_ptr, w_ptr, gate_ptr, scale_ptr, w_next_ptr, stats_ptr, gy_ptr, gu_ptr,
+                          gx_ptr, gh_ptr, gw_ptr, ggate_ptr, gscale_ptr, gw_next_ptr, N, ws_ptr, ws_bytes,
+                          stream_ptr=None) -> None:
+    _call("ffn_residual_backward", norm, h_ptr, y_ptr, w_ptr, gate_ptr, scale_ptr, w_next_ptr, stats_ptr, gy_ptr,
+          gu_ptr, gx_ptr, gh_ptr, gw_ptr, ggate_ptr, gscale_ptr, gw_next_ptr, N, ws_ptr, ws_bytes, stream_ptr)
+
+
+def ffn_dropout(x_ptr, ldx, y_ptr, ldy, N, width, dtype, p, seed, offset, stream_ptr=None) -> None:
+    _call("ffn_dropout", x_ptr, ldx, y_ptr, ldy, N, width, _code(_DTYPES, dtype, "dtype"), p, seed, offset, stream_ptr)
+
+
+# ---------------------------------------------------------------- convenience
+
+_U64 = (1 << 64) - 1
+
+
+def _torch_dtype(dtype):
+    import torch
+    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+
+
+def _rows(t, tdt, rows, width, what):
+    """Row stride of t, which must be a [rows, width] tensor whose rows do not overlap (rows None: any number)."""
+    if not t.is_cuda or t.dtype != tdt or t.dim() != 2 or t.shape[1] != width or (rows is not None and t.shape[0] != rows):
+        raise ValueError("%s must be a %s CUDA tensor [%s, %d]" % (what, tdt, "N" if rows is None else rows, width))
+    ld = t.stride(0)
+    if t.shape[0] <= 1:
+        ld = max(ld, width)
+    if (width > 1 and t.stride(1) != 1) or ld < width:
+        raise ValueError("%s must have adjacent values in each row and rows that do not overlap" % what)
+    return ld
+
+
+def _whole(t, tdt, shape, what):
+    """Pointer of t, a contiguous CUDA tensor of this shape (None where t is None)."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != tdt or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s CUDA tensor %s" % (what, tdt, list(shape)))
+    return t.data_ptr()
+
+
+def _on_one_device(x, *others):
+    for t in others:
+        if t is not None and t.device != x.device:
+            raise ValueError("all tensors must be on %s" % x.device)
+
+
+def _stream(stream, device):
+    """The HIP stream's handle, and the torch stream where it is not the current one."""
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream(device).cuda_stream, None
+    return stream.cuda_stream, stream
+
+
+def _new(shape, dtype, device, other):
+    """A new tensor of the stream `other` (None: the current one), so that its memory is reused in that stream's order."""
+    import torch
+    if other is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(other):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _workspace(workspace, need, device, other):
+    import torch
+    if workspace is None:
+        return _new((max(need, 1),), torch.uint8, device, other)
+    if workspace.dtype != torch.uint8 or workspace.device != device or not workspace.is_contiguous() or \
+            workspace.numel() < need:
+        raise ValueError("workspace must be a contiguous uint8 tensor of at least %d bytes on %s" % (need, device))
+    return workspace
+
+
+class FfnPlan:
+    """Owns an ffn plan: Y = (act(X Wg^T) * (X Wu^T)) Wo^T for X [N, d_in]."""
+
+    def __init__(self, d_in: int, d_ff: int, d_out: int | None = None, dtype: str = "fp32", activation: str = "silu"):
+        self.d_in, self.d_ff = int(d_in), int(d_ff)
+        self.d_out = self.d_in if d_out is None else int(d_out)
+        self.dtype, self.activation = dtype, activation
+        self._h = ffn_plan(self.d_in, self.d_ff, self.d_out, activation, dtype)
+        self._tdt = _torch_dtype(dtype)
+
+    def forward(self, x, w_in, w_out, save=False, out=None, saved=None, workspace=None, stream=None):
+        """x: [N, d_in], rows may be strided; w_in: [2 d_ff, d_in], the gate's rows, then the up projection's;
+        w_out: [d_out, d_ff].  Returns [N, d_out]; with save=True (or `saved`, a [N, 2 d_ff] fp32 tensor to write)
+        also the values that backward() reads."""
+        import torch
+        tdt, di, df, do = self._tdt, self.d_in, self.d_ff, self.d_out
+        ldx = _rows(x, tdt, None, di, "x")
+        N, dev = x.shape[0], x.device
+        wi, wo = _whole(w_in, tdt, (2 * df, di), "w_in"), _whole(w_out, tdt, (do, df), "w_out")
+        _on_one_device(x, w_in, w_out, out, saved)
+        sp, other = _stream(stream, dev)
+        if out is None:
+            out = _new((N, do), tdt, dev, other)
+        if save and saved is None:
+            saved = _new((N, 2 * df), torch.float32, dev, other)
+        ws = _workspace(workspace, ffn_workspace_bytes(self._h, N), dev, other)
+        ffn_forward(self._h, x.data_ptr(), ldx, wi, wo, _whole(out, tdt, (N, do), "out"),
+                    _whole(saved, torch.float32, (N, 2 * df), "saved"), N, ws.data_ptr(), ws.numel(), sp)
+        return out if saved is None else (out, saved)
+
+    def backward(self, x, w_in, w_out, saved, grad_out, need_x=True, need_w_in=True, need_w_out=True, workspace=None,
+                 stream=None):
+        """(grad_x, grad_w_in, grad_w_out) of sum(grad_out * forward(x, w_in, w_out)); one not asked for is None.
+        saved: what forward() returned beside Y; x and grad_out may have strided rows."""
+        import torch
+        tdt, di, df, do = self._tdt, self.d_in, self.d_ff, self.d_out
+        ldx = _rows(x, tdt, None, di, "x")
+        N, dev = x.shape[0], x.device
+        ldg = _rows(grad_out, tdt, N, do, "grad_out")
+        wi, wo = _whole(w_in, tdt, (2 * df, di), "w_in"), _whole(w_out, tdt, (do, df), "w_out")
+        sv = _whole(saved, torch.float32, (N, 2 * df), "saved")
+        _on_one_device(x, w_in, w_out, saved, grad_out)
+        if not (need_x or need_w_in or need_w_out):
+            return None, None, None
+        sp, other = _stream(stream, dev)
+        gx = _new((N, di), tdt, dev, other) if need_x else None
+        gwi = _new((2 * df, di), tdt, dev, other) if need_w_in else None
+        gwo = _new((do, df), tdt, dev, other) if need_w_out else None
+        ws = _workspace(workspace, ffn_backward_workspace_bytes(self._h, N), dev, other)
+        ptr = lambda t: t.data_ptr() if t is not None else None
+        ffn_backward(self._h, x.data_ptr(), ldx, wi, wo, sv, grad_out.data_ptr(), ldg, ptr(gx), ptr(gwi), ptr(gwo), N,
+                     ws.data_ptr(), ws.numel(), sp)
+        return gx, gwi, gwo
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            ffn_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class NormPlan:
+    """The norms before and after a block: N(v; w) = v / sqrt(mean(v^2) + eps) * w over rows of `width` values.
+
+    rows_per_gate consecutive rows share one row of the gate; `dropout` is the probability of dropping a value of
+    the block's normed output."""
+
+    def __init__(self, width: int, dtype: str = "fp32", eps: float = 1e-6, rows_per_gate: int = 1,
+                 dropout: float = 0.0):
+        self.width, self.dtype, self.eps = int(width), dtype, float(eps)
+        self.rows_per_gate, self.dropout = int(rows_per_gate), float(dropout)
+        self._code = _code(_DTYPES, dtype, "dtype")
+        self._tdt = _torch_dtype(dtype)
+        if ffn_norm_workspace_bytes(self._norm(), 0, 0) < 0:
+            raise ValueError("width must be 1 .. %d, eps positive, rows_per_gate at least 1 and dropout within [0, 1]"
+                             % FFN_MAX_WIDTH)
+
+    def _norm(self, seed=0, offset=0):
+        return ffn_norm(self.width, self.rows_per_gate, self._code, self.eps, self.dropout, seed & _U64, offset & _U64)
+
+    def forward(self, x, w=None, out=None, rstd=None, stream=None):
+        """(u, rstd): u = N(x; w) for x [N, width], rows may be strided, and the rows' 1 / sqrt(mean + eps)."""
+        import torch
+        tdt, D = self._tdt, self.width
+        ldx = _rows(x, tdt, None, D, "x")
+        N, dev = x.shape[0], x.device
+        wp = _whole(w, tdt, (D,), "w")
+        _on_one_device(x, w, out, rstd)
+        sp, other = _stream(stream, dev)
+        if out is None:
+            out = _new((N, D), tdt, dev, other)
+        if rstd is None:
+            rstd = _new((N,), torch.float32, dev, other)
+        ffn_norm_forward(self._norm(), x.data_ptr(), ldx, wp, out.data_ptr(), _rows(out, tdt, N, D, "out"),
+                         _whole(rstd, torch.float32, (N,), "rstd"), N, sp)
+        return out, rstd
+
+    def backward(self, x, w, rstd, grad_out, need_x=True, need_w=True, workspace=None, stream=None):
+        """(grad_x, grad_w) of sum(grad_out * N(x; w)); one not asked for is None."""
+        import torch
+        tdt, D = self._tdt, self.width
+        ldx = _rows(x, tdt, None, D, "x")
+        N, dev = x.shape[0], x.device
+        ldg = _rows(grad_out, tdt, N, D, "grad_out")
+        wp, rp = _whole(w, tdt, (D,), "w"), _whole(rstd, torch.float32, (N,), "rstd")
+        _on_one_device(x, w, rstd, grad_out)
+        if not (need_x or need_w):
+            return None, None
+        sp, other = _stream(stream, dev)
+        norm = self._norm()
+        gx = _new((N, D), tdt, dev, other) if need_x else None
+        gw = _new((D,), tdt, dev, other) if need_w else None
+        ws = _workspace(workspace, ffn_norm_workspace_bytes(norm, N, 0), dev, other)
+        ffn_norm_backward(norm, x.data_ptr(), ldx, wp, rp, grad_out.data_ptr(), ldg,
+                          gx.data_ptr() if need_x else None, gw.data_ptr() if need_w else None, N, ws.data_ptr(),
+                          ws.numel(), sp)
+        return gx, gw
+
+    def _gates(self, N):
+        return -(-N // self.rows_per_gate)
+
+    def residual(self, x, h, w=None, gate=None, scale=None, w_next=None, next_norm=True, seed=0, offset=0, out=None,
+                 stream=None):
+        """(y, u, stats): y = x + scale * gate * drop(N(h; w)) and u = N(y; w_next) (None with next_norm=False).
+
+        x, h: [N, width]; gate: [ceil(N / rows_per_gate), width]; scale, w, w_next: [width]; each of the four may be
+        None (ones).  seed and offset choose the dropout's draws (see dropout()).  stats [2, N] holds the
+        1 / sqrt(mean + eps) of h's and of y's rows, for residual_backward().  out may be x."""
+        import torch
+        tdt, D = self._tdt, self.width
+        if not x.is_cuda or x.dim() != 2:
+            raise ValueError("x must be a %s CUDA tensor [N, %d]" % (tdt, D))
+        N, dev = x.shape[0], x.device
+        xp, hp = _whole(x, tdt, (N, D), "x"), _whole(h, tdt, (N, D), "h")
+        wp, sc = _whole(w, tdt, (D,), "w"), _whole(scale, tdt, (D,), "scale")
+        gp, np_ = _whole(gate, tdt, (self._gates(N), D), "gate"), _whole(w_next, tdt, (D,), "w_next")
+        _on_one_device(x, h, w, gate, scale, w_next, out)
+        sp, other = _stream(stream, dev)
+        if out is None:
+            out = _new((N, D), tdt, dev, other)
+        u = _new((N, D), tdt, dev, other) if next_norm else None
+        stats = _new((2, N), torch.float32, dev, other)
+        ffn_residual_forward(self._norm(seed, offset), xp, hp, wp, gp, sc, np_, _whole(out, tdt, (N, D), "out"),
+                             u.data_ptr() if next_norm else None, stats.data_ptr(), N, sp)
+        return out, u, stats
+
+    def residual_backward(self, h, y, w, stats, grad_y, grad_u, gate=None, scale=None, w_next=None, seed=0, offset=0,
+                          workspace=None, stream=None):
+        """(grad_x, grad_h, grad_w, grad_gate, grad_scale, grad_w_next) of sum(grad_y * y) + sum(grad_u * u) for
+        residual() with the same arguments; those of arguments that are None are None.  grad_y or grad_u may be
+        None (zero), not both."""
+        import torch
+        tdt, D = self._tdt, self.width
+        if not h.is_cuda or h.dim() != 2:
+            raise ValueError("h must be a %s CUDA tensor [N, %d]" % (tdt, D))
+        if grad_y is None and grad_u is None:
+            raise ValueError("one of grad_y and grad_u must be given")
+        N, dev = h.shape[0], h.device
+        hp, yp = _whole(h, tdt, (N, D), "h"), _whole(y, tdt, (N, D), "y")
+        wp, sc = _whole(w, tdt, (D,), "w"), _whole(scale, tdt, (D,), "scale")
+        gp, np_ = _whole(gate, tdt, (self._gates(N), D), "gate"), _whole(w_next, tdt, (D,), "w_next")
+        st = _whole(stats, torch.float32, (2, N), "stats")
+        gyp, gup = _whole(grad_y, tdt, (N, D), "grad_y"), _whole(grad_u, tdt, (N, D), "grad_u")
+        _on_one_device(h, y, w, gate, scale, w_next, stats, grad_y, grad_u)
+        sp, other = _stream(stream, dev)
+        gx, gh = _new((N, D), tdt, dev, other), _new((N, D), tdt, dev, other)
+        gw, gs, gn = (None if t is None else _new((D,), tdt, dev, other) for t in (w, scale, w_next))
+        gg = None if gate is None else _new(tuple(gate.shape), tdt, dev, other)
+        norm = self._norm(seed, offset)
+        ws = _workspace(workspace, ffn_norm_workspace_bytes(norm, N, 1), dev, other)
+        ptr = lambda t: t.data_ptr() if t is not None else None
+        ffn_residual_backward(norm, hp, yp, wp, gp, sc, np_, st, gyp, gup, gx.data_ptr(), gh.data_ptr(), ptr(gw), ptr(gg),
+                              ptr(gs), ptr(gn), N, ws.data_ptr(), ws.numel(), sp)
+        return gx, gh, gw, gg, gs, gn
+
+
+def dropout(x, p: float, seed: int, offset: int = 0, out=None, stream=None):
+    """Dropout of x [..., width] by a counter-based generator: the values kept, scaled by 1 / (1 - p) with p rounded
+    to a multiple of 2^-16.  Which are kept depends on (seed, offset, row, column) alone, with the leading dimensions
+    flattened to rows; the gradient is the same call on the gradient.  x: contiguous, or [N, width] with strided
+    rows; out may be x."""
+    import torch
+    name = {torch.float32: "fp32", torch.bfloat16: "bf16", torch.float16: "fp16"}.get(x.dtype)
+    if name is None or not x.is_cuda or x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x must be an fp32, bf16 or fp16 CUDA tensor [..., width]")
+    width, dev = x.shape[-1], x.device
+    if x.dim() != 2 and not x.is_contiguous():
+        raise ValueError("x must be contiguous, or [N, width] with strided rows")
+    N = x.numel() // width
+    ldx = _rows(x, x.dtype, N, width, "x") if x.dim() == 2 else width
+    sp, other = _stream(stream, dev)
+    if out is None:
+        out = _new(tuple(x.shape), x.dtype, dev, other)
+    elif out.shape != x.shape or out.device != dev or (out.dim() != 2 and not out.is_contiguous()):
+        raise ValueError("out must have the shape and device of x")
+    ldy = _rows(out, x.dtype, N, width, "out") if out.dim() == 2 else _whole(out, x.dtype, tuple(x.shape), "out") and width
+    ffn_dropout(x.data_ptr(), ldx, out.data_ptr(), ldy or width, N, width, name, float(p), seed & _U64, offset & _U64, sp)
+    return out

@@ -1,0 +1,77 @@
+// Device helpers of the feed-forward sublayer's kernels: conversions,
+// activations and their derivatives, the counter-based generator, and
+// reductions over a work-group.  Internal; included by the ffn_*.hip sources.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "ffn_internal.h"
+
+namespace ffn {
+namespace dev {
+
+typedef __bf16 bf16;
+typedef _Float16 fp16;
+
+template <typename T> __device__ __forceinline__ float to_f32(T v) { return (float)v; }
+
+// act(g) and act'(g), 32 bits
+__device__ __forceinline__ void activate(int act, float g, float& v, float& dv) {
+    if (act == FFN_SILU) {
+        const float s = 1.0f / (1.0f + expf(-g));
+        v = g * s;
+        dv = s * (1.0f + g * (1.0f - s));
+    } else if (act == FFN_GELU) {
+        const float c = 0.5f * (1.0f + erff(g * 0.70710678118654752440f));
+        v = g * c;
+        dv = c + g * 0.39894228040143267794f * expf(-0.5f * g * g);
+    } else {
+        v = g > 0.0f ? g : 0.0f;
+        dv = g > 0.0f ? 1.0f : 0.0f;
+    }
+}
+
+// Philox 4x32, 10 rounds (Salmon et al. 2011): two 32 x 32 -> 64 bit products a round
+// mix the four counter words; the key steps by fixed constants (the golden ratio, sqrt 3 - 1).
+struct Words { uint32_t w[4]; };
+__device__ __forceinline__ Words philox(uint32_t c0, uint32_t c1, uint64_t offset, uint64_t seed) {
+    uint32_t c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
+    uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t p = (uint64_t)0xD2511F53u * c0, q = (uint64_t)0xCD9E8D57u * c2;
+        const uint32_t n0 = (uint32_t)(q >> 32) ^ c1 ^ k0, n2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
+        c1 = (uint32_t)q;
+        c3 = (uint32_t)p;
+        c0 = n0;
+        c2 = n2;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return Words{{c0, c1, c2, c3}};
+}
+
+// Whether column (8 b + i) of the block's eight is kept.
+__device__ __forceinline__ bool kept(const Words& q, int i, uint32_t threshold) {
+    const uint32_t v = q.w[i >> 1];
+    return ((i & 1) ? v >> 16 : v & 0xFFFFu) >= threshold;
+}
+
+// Sum over the work-group, returned to every thread; `s` holds one float per wave.
+__device__ __forceinline__ float group_sum(float v, float* s) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
+    const int waves = blockDim.x >> 6;
+    if (waves == 1) return v;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float t = s[0];
+    for (int i = 1; i < waves; ++i) t += s[i];
+    return t;
+}
+
+}  // namespace dev
+}  // namespace ffn

@@ -1,0 +1,505 @@
+"""The feed-forward sublayer (include/ffn.h) on the GPU against its definitions in 64 bits.
+
+Tolerances follow from the roundings.  With e the unit roundoff of the arrays'
+type (2^-24, 2^-9, 2^-12) an output that is rounded once from 32-bit arithmetic
+is within e of itself in every value; a product's intermediates (H, dG, dU)
+are rounded too, each adding at most a few e relative to the
+norms of the factors.  Errors are 2-norms over 2-norms per output: a rounding
+contributes at most e, and no output here passes more than six of them
+(H or dG / dU and the output in the arrays' type; G and U are saved in 32 bits): 8 e.
+32-bit sums of K terms add at most K 2^-24 of the sum of magnitudes; with random
+signs that is below 2^-24 sqrt(K) sqrt(K) / sqrt(K), and 4e-6 covers it and the
+elementary functions' errors up to the K used here.
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+ROUND = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -9, "fp16": 2.0 ** -12}
+
+
+def _setup():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2602_21466_amd as lib
+    return torch, lib
+
+
+def _tol(dtype, roundings):
+    return roundings * ROUND[dtype] + 4e-6
+
+
+def _dt(torch, dtype):
+    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+
+
+def _rel(got, want):
+    """2-norm of the difference over that of `want`; none where every value is the nearest its type has."""
+    if got.shape == want.shape and bool((got.cpu() == want.to(got.dtype).cpu()).all()):
+        return 0.0
+    got, want = got.double().cpu(), want.double().cpu()
+    assert got.shape == want.shape
+    assert bool((got.isfinite() == want.isfinite()).all())
+    return float((got - want).norm() / max(float(want.norm()), 1e-300))
+
+
+def _randn(torch, g, shape, dtype, scale=1.0, mean=0.0):
+    return (torch.randn(shape, generator=g, dtype=torch.float64) * scale + mean).to(_dt(torch, dtype))
+
+
+# ---------------------------------------------------------------- feed-forward block
+
+def _act64(torch, name, v):
+    if name == "silu":
+        return v * torch.sigmoid(v)
+    if name == "gelu":
+        return v * 0.5 * (1.0 + torch.erf(v / math.sqrt(2.0)))
+    return torch.relu(v)
+
+
+def _ffn64(torch, x, w_in, w_out, act):
+    z = x @ w_in.T
+    df = w_in.shape[0] // 2
+    return (_act64(torch, act, z[:, :df]) * z[:, df:]) @ w_out.T
+
+
+def _ffn_case(torch, N, di, df, do, dtype, seed=0):
+    g = torch.Generator().manual_seed(1000 + seed)
+    return (_randn(torch, g, (N, di), dtype), _randn(torch, g, (2 * df, di), dtype, di ** -0.5),
+            _randn(torch, g, (do, df), dtype, df ** -0.5), _randn(torch, g, (N, do), dtype))
+
+
+# rows, d_in, d_ff, d_out: one token, below and across tile edges, odd strides, long sums, wide outputs
+FFN_SIZES = [(1, 1, 1, 1), (1, 64, 128, 64), (1, 81, 324, 489), (3, 17, 5, 31), (16, 256, 512, 256), (17, 96, 200, 40),
+             (33, 128, 64, 8), (64, 289, 130, 75), (65, 72, 136, 264), (129, 264, 72, 129), (200, 40, 1000, 16),
+             (257, 520, 264, 136), (300, 1089, 100, 77), (513, 64, 256, 320), (1000, 32, 48, 56), (2, 2048, 40, 24),
+             (31, 1000, 2056, 8), (128, 512, 1024, 512)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("N,di,df,do", FFN_SIZES)
+def test_ffn_forward_and_gradients(N, di, df, do, dtype):
+    torch, lib = _setup()
+    act = ("silu", "gelu", "relu")[(N + di) % 3]
+    x, wi, wo, gy = _ffn_case(torch, N, di, df, do, dtype, N)
+    plan = lib.FfnPlan(di, df, do, dtype=dtype, activation=act)
+    dev = [t.cuda() for t in (x, wi, wo)]
+    y = plan.forward(*dev)
+    y2, saved = plan.forward(*dev, save=True)
+    assert torch.equal(y, y2)
+    grads = plan.backward(*dev, saved, gy.cuda())
+    ref = [t.double().requires_grad_(True) for t in (x, wi, wo)]
+    want = _ffn64(torch, *ref, act)
+    want_g = torch.autograd.grad(want, ref, gy.double())
+    z = ref[0] @ ref[1].T
+    assert _rel(saved, z.detach()) <= _tol(dtype, 1)
+    assert _rel(y, want.detach()) <= _tol(dtype, 4)
+    # relu'(g) jumps at 0: a G that rounds across it changes one term of a sum
+    slack = 8 if act != "relu" else 16
+    for got, w in zip(grads, want_g):
+        assert got.dtype == x.dtype and _rel(got, w) <= _tol(dtype, slack)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_ffn_single_gradients_and_determinism(dtype):
+    torch, lib = _setup()
+    x, wi, wo, gy = (t.cuda() for t in _ffn_case(torch, 70, 48, 96, 56, dtype))
+    plan = lib.FfnPlan(48, 96, 56, dtype=dtype)
+    _, saved = plan.forward(x, wi, wo, save=True)
+    whole = plan.backward(x, wi, wo, saved, gy)
+    for k in range(3):
+        need = [j == k for j in range(3)]
+        part = plan.backward(x, wi, wo, saved, gy, *need)
+        assert [p is not None for p in part] == need and torch.equal(part[k], whole[k])
+    assert plan.backward(x, wi, wo, saved, gy, False, False, False) == (None, None, None)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("N", [1, 5, 150])
+def test_ffn_strided_and_unaligned_rows(dtype, N):
+    """Rows inside wider ones, from an odd first column: the same values as from packed rows, bit for bit."""
+    torch, lib = _setup()
+    di, df, do = 80, 64, 72
+    x, wi, wo, gy = (t.cuda() for t in _ffn_case(torch, N, di, df, do, dtype))
+    plan = lib.FfnPlan(di, df, do, dtype=dtype)
+    want, saved = plan.forward(x, wi, wo, save=True)
+    want_g = plan.backward(x, wi, wo, saved, gy)
+    wide = torch.full((N, di + 11), float("nan"), dtype=x.dtype, device="cuda")
+    gwide = torch.full((N, do + 5), float("nan"), dtype=x.dtype, device="cuda")
+    wide[:, 3:3 + di] = x
+    gwide[:, 1:1 + do] = gy
+    got, saved2 = plan.forward(wide[:, 3:3 + di], wi, wo, save=True)
+    assert torch.equal(got, want) and torch.equal(saved, saved2)
+    for a, b in zip(plan.backward(wide[:, 3:3 + di], wi, wo, saved2, gwide[:, 1:1 + do]), want_g):
+        assert torch.equal(a, b)
+
+
+def test_ffn_rows_do_not_mix():
+    """A row of infinities and one of NaN leave the other rows' outputs as they were."""
+    torch, lib = _setup()
+    x, wi, wo, _ = (t.cuda() for t in _ffn_case(torch, 40, 64, 96, 64, "bf16"))
+    for dtype in ("bf16", "fp32"):
+        t = _dt(torch, dtype)
+        plan = lib.FfnPlan(64, 96, 64, dtype=dtype)
+        want = plan.forward(x.to(t), wi.to(t), wo.to(t))
+        bad = x.to(t).clone()
+        bad[7, 3], bad[21] = float("inf"), float("nan")
+        got = plan.forward(bad, wi.to(t), wo.to(t))
+        keep = [i for i in range(40) if i not in (7, 21)]
+        assert torch.equal(got[keep], want[keep])
+        assert not got[7].isfinite().any() and got[21].isnan().all()
+
+
+def test_ffn_gradients_against_differences():
+    """Central differences of sum(grad * Y) along random directions, in fp32 arrays at a small size: the step 2^-6
+    leaves a third-order term of about 2^-12 relative and rounding of about 2^-24 * 2^6 relative to |Y|."""
+    torch, lib = _setup()
+    N, di, df, do = 9, 12, 20, 7
+    x, wi, wo, gy = _ffn_case(torch, N, di, df, do, "fp32", 3)
+    for act in ("silu", "gelu"):
+        plan = lib.FfnPlan(di, df, do, activation=act)
+        args = [t.cuda() for t in (x, wi, wo)]
+        y, saved = plan.forward(*args, save=True)
+        grads = plan.backward(*args, saved, gy.cuda())
+        g = torch.Generator().manual_seed(5)
+        for k in range(3):
+            d = torch.randn(args[k].shape, generator=g).cuda()
+            d = d / d.norm() * args[k].norm()
+            h = 2.0 ** -6
+            up, dn = list(args), list(args)
+            up[k], dn[k] = args[k] + h * d, args[k] - h * d
+            num = float(((plan.forward(*up).double() - plan.forward(*dn).double()) * gy.cuda().double()).sum()) / (2 * h)
+            ana = float((grads[k].double() * d.double()).sum())
+            size = float(grads[k].double().norm() * d.double().norm())
+            assert abs(num - ana) <= 2e-3 * size
+
+
+def test_ffn_zero_rows():
+    torch, lib = _setup()
+    plan = lib.FfnPlan(16, 24, 8, dtype="bf16")
+    _, wi, wo, _ = (t.cuda() for t in _ffn_case(torch, 1, 16, 24, 8, "bf16"))
+    x = torch.empty(0, 16, dtype=torch.bfloat16, device="cuda")
+    y, saved = plan.forward(x, wi, wo, save=True)
+    assert y.shape == (0, 8)
+    gx, gwi, gwo = plan.backward(x, wi, wo, saved, torch.empty(0, 8, dtype=torch.bfloat16, device="cuda"))
+    assert gx.shape == (0, 16) and not gwi.any() and not gwo.any()
+
+
+def test_ffn_on_another_stream():
+    torch, lib = _setup()
+    x, wi, wo, gy = (t.cuda() for t in _ffn_case(torch, 90, 64, 128, 64, "bf16"))
+    plan = lib.FfnPlan(64, 128, 64, dtype="bf16")
+    want, saved = plan.forward(x, wi, wo, save=True)
+    want_g = plan.backward(x, wi, wo, saved, gy)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        got, saved2 = plan.forward(x, wi, wo, save=True, stream=s)
+        grads = plan.backward(x, wi, wo, saved2, gy, stream=s)
+        s.synchronize()
+        assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(grads, want_g))
+
+
+def test_ffn_and_norms_in_a_graph():
+    """Captured once, replayed on changing inputs with eager work between the replays."""
+    torch, lib = _setup()
+    N, d, df = 40, 64, 96
+    x, wi, wo, gy = (t.cuda() for t in _ffn_case(torch, N, d, df, d, "bf16"))
+    plan, norm = lib.FfnPlan(d, df, d, dtype="bf16"), lib.NormPlan(d, dtype="bf16", dropout=0.25)
+    w = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        u, rstd = norm.forward(x, w)
+        h, saved = plan.forward(u, wi, wo, save=True)
+        y, un, stats = norm.residual(x, h, w, w_next=w, seed=3)
+        gx, gh, gw, _, _, gn = norm.residual_backward(h, y, w, stats, gy, gy, w_next=w, seed=3)
+        gu, gwi, gwo = plan.backward(u, wi, wo, saved, gh)
+        return (y, un, gx, gw, gn, gwi, gwo) + norm.backward(x, w, rstd, gu)
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(4):
+        x.copy_(_ffn_case(torch, N, d, df, d, "bf16", 50 + k)[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        for a, b in zip(got, step()):
+            assert torch.equal(a, b)
+
+
+# ---------------------------------------------------------------- norms, gate, residual scale
+
+def _keep64(rows, width, p, seed, offset):
+    """Factors of the dropout, from the definition in include/ffn.h."""
+    t = math.floor(p * 65536 + 0.5)
+    if t == 65536:
+        return np.zeros((rows, width))
+    out = np.zeros((rows, width))
+    for r in range(rows):
+        for b in range(-(-width // 8)):
+            words = _philox((b, r, offset & 0xFFFFFFFF, offset >> 32), (seed & 0xFFFFFFFF, seed >> 32))
+            for i in range(min(8, width - 8 * b)):
+                draw = words[i // 2] >> (16 * (i % 2)) & 0xFFFF
+                out[r, 8 * b + i] = 65536 / (65536 - t) if draw >= t else 0.0
+    return out
+
+
+def _philox(counter, key):
+    c, k = list(counter), list(key)
+    for _ in range(10):
+        p, q = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
+        c = [(q >> 32) ^ c[1] ^ k[0], q & 0xFFFFFFFF, (p >> 32) ^ c[3] ^ k[1], p & 0xFFFFFFFF]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return c
+
+
+def _norm64(v, w, eps):
+    n = v / (v.square().mean(1, keepdim=True) + eps).sqrt()
+    return n if w is None else n * w
+
+
+NORM_SIZES = [(1, 1), (1, 4096), (3, 7), (5, 289), (64, 256), (70, 1089), (130, 64), (9, 5000), (33, 2056), (2, 20001),
+              (4, 16384), (600, 40)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("N,D", NORM_SIZES)
+def test_norm_before(N, D, dtype):
+    torch, lib = _setup()
+    g = torch.Generator().manual_seed(N * 7 + D)
+    x, gu = _randn(torch, g, (N, D), dtype), _randn(torch, g, (N, D), dtype)
+    w = _randn(torch, g, (D,), dtype, 0.1, 1.0)
+    plan = lib.NormPlan(D, dtype=dtype, eps=1e-5)
+    for weight in (w, None):
+        wd = None if weight is None else weight.cuda()
+        u, rstd = plan.forward(x.cuda(), wd)
+        gx, gw = plan.backward(x.cuda(), wd, rstd, gu.cuda())
+        xr, wr = x.double().requires_grad_(True), w.double().requires_grad_(True)
+        want = _norm64(xr, None if weight is None else wr, 1e-5)
+        grads = torch.autograd.grad((want * gu.double()).sum(), (xr, wr) if weight is not None else (xr,))
+        assert _rel(u, want.detach()) <= _tol(dtype, 1)
+        # where a row has one value its gradient cancels: what is left is rounding of 32-bit terms of size |gu| rstd
+        if D > 1:
+            assert _rel(gx, grads[0]) <= _tol(dtype, 1)
+        if weight is not None:
+            assert _rel(gw, grads[1]) <= _tol(dtype, 1)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("N,D,rpg,p", [(1, 1, 1, 0.0), (1, 4096, 1, 0.0), (5, 289, 1, 0.25), (70, 1089, 7, 0.0),
+                                       (67, 40, 64, 0.5), (300, 24, 128, 0.1), (33, 2056, 1000, 0.1), (3, 20001, 2, 0.25),
+                                       (130, 512, 3, 0.0), (4, 16384, 1, 0.1), (257, 64, 16, 0.0), (1030, 16, 2, 0.25)])
+def test_residual(N, D, rpg, p, dtype):
+    torch, lib = _setup()
+    g = torch.Generator().manual_seed(N * 11 + D)
+    gates = -(-N // rpg)
+    x, h, gy, gu = (_randn(torch, g, (N, D), dtype) for _ in range(4))
+    w, scale, wn = (_randn(torch, g, (D,), dtype, 0.2, 1.0) for _ in range(3))
+    gate = _randn(torch, g, (gates, D), dtype)
+    seed, offset = 0x123456789ABCDEF0 + N, 0xFEDCBA9876543210 - D
+    plan = lib.NormPlan(D, dtype=dtype, rows_per_gate=rpg, dropout=p)
+    args = {"gate": gate.cuda(), "scale": scale.cuda(), "w_next": wn.cuda(), "seed": seed, "offset": offset}
+    y, u, stats = plan.residual(x.cuda(), h.cuda(), w.cuda(), **args)
+    grads = plan.residual_backward(h.cuda(), y, w.cuda(), stats, gy.cuda(), gu.cuda(), **args)
+    leaves = [t.double().requires_grad_(True) for t in (x, h, w, gate, scale, wn)]
+    xr, hr, wr, gr, sr, nr = leaves
+    keep = torch.from_numpy(_keep64(N, D, p, seed, offset)) if p else 1.0
+    yr = xr + sr * gr[torch.arange(N) // rpg] * keep * _norm64(hr, wr, 1e-6)
+    ur = _norm64(yr, nr, 1e-6)
+    want = torch.autograd.grad((yr * gy.double()).sum() + (ur * gu.double()).sum(), leaves)
+    assert _rel(y, yr.detach()) <= _tol(dtype, 1) and _rel(u, ur.detach()) <= _tol(dtype, 1)
+    if D > 1:
+        for got, wt in zip(grads, want):
+            assert _rel(got, wt) <= _tol(dtype, 3)  # y is read back rounded
+    # a mask decided as written: dropped values leave x as it was
+    if p:
+        dropped = (keep == 0).cuda()
+        assert torch.equal(y[dropped], x.cuda()[dropped])
+        assert 0 < int(dropped.sum()) < N * D
+    # without the next norm, and without gate, scale and weight
+    y1, u1, st1 = plan.residual(x.cuda(), h.cuda(), next_norm=False, seed=seed, offset=offset)
+    assert u1 is None
+    yr1 = x.double() + (keep * _norm64(h.double(), None, 1e-6))
+    assert _rel(y1, yr1) <= _tol(dtype, 1)
+    gx, gh, gw, gg, gs, gn = plan.residual_backward(h.cuda(), y1, None, st1, gy.cuda(), None, seed=seed, offset=offset)
+    assert gw is None and gg is None and gs is None and gn is None and torch.equal(gx, gy.cuda())
+    hr1 = h.double().requires_grad_(True)
+    if D > 1:
+        w1 = torch.autograd.grad((keep * _norm64(hr1, None, 1e-6) * gy.double()).sum(), hr1)[0]
+        assert _rel(gh, w1) <= _tol(dtype, 2)
+    # the gradient arriving through u alone
+    only_u = plan.residual_backward(h.cuda(), y, w.cuda(), stats, None, gu.cuda(), **args)
+    want_u = torch.autograd.grad((_norm64(xr + sr * gr[torch.arange(N) // rpg] * keep * _norm64(hr, wr, 1e-6), nr, 1e-6)
+                                  * gu.double()).sum(), leaves)
+    if D > 1:
+        for got, wt in zip(only_u, want_u):
+            assert _rel(got, wt) <= _tol(dtype, 3)
+
+
+def test_norm_of_zero_rows_and_of_large_values():
+    """A row of zeros gives zeros (rstd = 1 / sqrt(eps)); values whose squares fit 32 bits stay finite."""
+    torch, lib = _setup()
+    plan = lib.NormPlan(96, dtype="bf16", eps=1e-6)
+    x = torch.zeros(3, 96, dtype=torch.bfloat16, device="cuda")
+    x[1] = 1e18
+    u, rstd = plan.forward(x)
+    assert not u[0].any() and not u[2].any() and bool((u[1] == 1).all())
+    assert abs(float(rstd[0]) - 1000.0) < 1e-3
+    gx, gw = plan.backward(x, torch.ones(96, dtype=torch.bfloat16, device="cuda"), rstd, torch.ones_like(x))
+    assert gx.isfinite().all() and bool((gx[0] == 1000.0).all())
+
+
+def test_norm_strided_in_place_and_zero_rows():
+    torch, lib = _setup()
+    plan = lib.NormPlan(45, dtype="fp16")
+    g = torch.Generator().manual_seed(2)
+    wide = _randn(torch, g, (20, 64), "fp16").cuda()
+    x = wide[:, 7:52]
+    want, rstd = plan.forward(x.contiguous())
+    got, r2 = plan.forward(x)
+    assert torch.equal(got, want) and torch.equal(rstd, r2)
+    gu = _randn(torch, g, (20, 90), "fp16").cuda()[:, 1:46]
+    for a, b in zip(plan.backward(x, None, rstd, gu), plan.backward(x.contiguous(), None, rstd, gu.contiguous())):
+        assert torch.equal(a, b)
+    before = wide.clone()
+    plan.forward(x, out=x)
+    assert torch.equal(x, want) and torch.equal(wide[:, :7], before[:, :7]) and torch.equal(wide[:, 52:], before[:, 52:])
+    e = torch.empty(0, 45, dtype=torch.float16, device="cuda")
+    u, r = plan.forward(e)
+    gx, gw = plan.backward(e, None, r, e)
+    assert gx.shape == (0, 45) and not gw.any()
+    # y in place of x, grad_x in place of grad_y (C entry)
+    a, h = _randn(torch, g, (20, 45), "fp16").cuda(), _randn(torch, g, (20, 45), "fp16").cuda()
+    y, u, _ = plan.residual(a, h)
+    b = a.clone()
+    y2, u2, _ = plan.residual(b, h, out=b)
+    assert y2.data_ptr() == b.data_ptr() and torch.equal(y, y2) and torch.equal(u, u2)
+
+
+# ---------------------------------------------------------------- dropout
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("N,D,p", [(1, 1, 0.5), (3, 7, 0.25), (5, 64, 0.1), (1, 1001, 0.5), (40, 289, 0.25), (17, 24, 0.9),
+                                   (6, 33, 1.0), (6, 33, 0.0)])
+def test_dropout_is_the_defined_mask(N, D, p, dtype):
+    torch, lib = _setup()
+    g = torch.Generator().manual_seed(N + D)
+    x = _randn(torch, g, (N, D), dtype)
+    seed, offset = 0xDEADBEEFCAFEF00D, 0x0123456789ABCDEF + N
+    got = lib.dropout(x.cuda(), p, seed=seed, offset=offset)
+    keep = _keep64(N, D, p, seed, offset) if p else np.ones((N, D))
+    # one multiplication in 32 bits and one rounding: the same as the same two here
+    want = (x.float() * torch.from_numpy(keep).float()).to(x.dtype)
+    assert torch.equal(got.cpu().abs(), want.abs()) and bool((got.cpu()[torch.from_numpy(keep) == 0] == 0).all())
+
+
+def test_dropout_masks_what_is_not_finite_and_strides():
+    torch, lib = _setup()
+    wide = torch.full((9, 50), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide[3] = float("inf")
+    x = wide[:, 5:38]
+    y = lib.dropout(x, 0.5, seed=1)
+    keep = torch.from_numpy(_keep64(9, 33, 0.5, 1, 0)).cuda()
+    assert bool((y[keep == 0] == 0).all()) and not bool(y[keep != 0].isfinite().any())
+    z = torch.randn(9, 33, device="cuda")
+    out = torch.zeros(9, 41, device="cuda")
+    lib.dropout(z, 0.5, seed=1, out=out[:, 2:35])
+    assert torch.equal(out[:, 2:35], lib.dropout(z, 0.5, seed=1)) and not out[:, :2].any() and not out[:, 35:].any()
+    w = z.clone()
+    assert lib.dropout(w, 0.5, seed=1, out=w) is w and torch.equal(w, out[:, 2:35])
+    assert torch.equal(lib.dropout(z.reshape(3, 3, 33), 0.5, seed=1).reshape(9, 33), w)
+    assert not torch.equal(lib.dropout(z, 0.5, seed=2), w) and not torch.equal(lib.dropout(z, 0.5, seed=1, offset=1), w)
+    assert lib.dropout(z[:0], 0.5, seed=1).shape == (0, 33)
+
+
+def test_dropout_share_and_independence():
+    """The share dropped over 2^22 draws is within 5 standard deviations of t / 65536, and so is that of pairs of
+    draws that are neighbours in a row, in a column, and at the next offset."""
+    torch, lib = _setup()
+    x = torch.ones(2048, 2048, device="cuda")
+    n = x.numel()
+    for p in (0.1, 0.5):
+        t = math.floor(p * 65536 + 0.5) / 65536
+        a = (lib.dropout(x, p, seed=9) == 0).double()
+        b = (lib.dropout(x, p, seed=9, offset=1) == 0).double()
+        assert abs(float(a.mean()) - t) <= 5 * math.sqrt(t * (1 - t) / n)
+        for u, v in ((a[:, 1:], a[:, :-1]), (a[1:], a[:-1]), (a, b)):
+            both = float((u * v).mean())
+            assert abs(both - t * t) <= 6 * math.sqrt(t * t * (1 - t * t) / u.numel())
+
+
+# ---------------------------------------------------------------- refusals
+
+def test_refusals():
+    torch, lib = _setup()
+    f = lib._load()
+    plan = lib.FfnPlan(16, 24, 8, dtype="bf16")
+    x, wi, wo, gy = (t.cuda() for t in _ffn_case(torch, 4, 16, 24, 8, "bf16"))
+    for args in ((x.float(), wi, wo), (x[:, :8], wi, wo), (x, wi[:24], wo), (x, wi, wo.T), (x.cpu(), wi, wo),
+                 (x[:1].expand(4, 16), wi, wo), (x.T.contiguous().T, wi, wo)):
+        with pytest.raises(ValueError):
+            plan.forward(*args)
+    with pytest.raises(ValueError):
+        plan.forward(x, wi, wo, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+    y = torch.empty(4, 8, dtype=x.dtype, device="cuda")
+    need = lib.ffn_workspace_bytes(plan._h, 4)
+    ws = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
+    p = lambda t: t.data_ptr()
+    ok = [plan._h, p(x), 16, p(wi), p(wo), p(y), None, 4, p(ws), need, None]
+    assert f.ffn_forward(*ok) == lib.CGTP_OK
+    for i, v, rc in ((1, None, lib.CGTP_EINVAL), (2, 15, lib.CGTP_EINVAL), (2, (1 << 22) + 1, lib.CGTP_EUNSUP),
+                     (1, p(x) + 1, lib.CGTP_EINVAL), (5, p(x), lib.CGTP_EINVAL), (5, p(wo), lib.CGTP_EINVAL),
+                     (6, p(ws), lib.CGTP_EINVAL), (7, -1, lib.CGTP_EINVAL), (7, (1 << 30) + 1, lib.CGTP_EUNSUP),
+                     (8, None, lib.CGTP_EINVAL), (8, p(ws) + 16, lib.CGTP_EINVAL), (9, need - 1, lib.CGTP_EINVAL)):
+        bad = list(ok)
+        bad[i] = v
+        assert f.ffn_forward(*bad) == rc, (i, v)
+    saved = torch.empty(4, 48, device="cuda")
+    gx, gwi, gwo = torch.empty_like(x), torch.empty_like(wi), torch.empty_like(wo)
+    need = lib.ffn_backward_workspace_bytes(plan._h, 4)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    ok = [plan._h, p(x), 16, p(wi), p(wo), p(saved), p(gy), 8, p(gx), p(gwi), p(gwo), 4, p(ws), need, None]
+    assert f.ffn_backward(*ok) == lib.CGTP_OK
+    for i, v, rc in ((5, None, lib.CGTP_EINVAL), (7, 7, lib.CGTP_EINVAL), (8, p(x), lib.CGTP_EINVAL), (9, p(gwo), lib.CGTP_EINVAL),
+                     (10, p(saved), lib.CGTP_EINVAL), (13, 0, lib.CGTP_EINVAL), (11, -3, lib.CGTP_EINVAL)):
+        bad = list(ok)
+        bad[i] = v
+        assert f.ffn_backward(*bad) == rc, (i, v)
+    bad = list(ok)
+    bad[8] = bad[9] = bad[10] = None
+    assert f.ffn_backward(*bad) == lib.CGTP_EINVAL
+    norm = lib.NormPlan(16, dtype="bf16", rows_per_gate=2)
+    h = torch.randn(4, 16, device="cuda").bfloat16()
+    for kw in ({"gate": h}, {"scale": h}, {"w": h[0, :8]}, {"w_next": h[0].float()}):
+        with pytest.raises(ValueError):
+            norm.residual(x, h, **kw)
+    with pytest.raises(ValueError):
+        norm.residual(x, h[:3])
+    with pytest.raises(lib.CgtpError):
+        norm.residual(x, h, out=h)
+    y, u, st = norm.residual(x, h)
+    with pytest.raises(ValueError):
+        norm.residual_backward(h, y, None, st, None, None)
+    with pytest.raises(ValueError):
+        norm.forward(x[:, :15])
+    with pytest.raises(lib.CgtpError):
+        norm.forward(wi[:4], out=wi[1:5])
+    with pytest.raises(ValueError):
+        lib.dropout(x.double(), 0.5, seed=1)
+    with pytest.raises(ValueError):
+        lib.dropout(x.reshape(2, 2, 16).transpose(0, 1), 0.5, seed=1)
+    for q in (-0.1, 1.1, float("nan")):
+        with pytest.raises(lib.CgtpError):
+            lib.dropout(x, q, seed=1)
+    with pytest.raises(lib.CgtpError):
+        lib.dropout(wi[:4], 0.5, seed=1, out=wi[1:5])
