@@ -12,9 +12,9 @@
  * 32 bits; what is stored is rounded to the arrays' type once, to nearest.
  *
  * Row strides (ldx, ...) count elements and must be >= the row's width; the
- * elements of a row are adjacent.  Arrays need the alignment of their element
- * (arrays whose base and row stride are multiples of 16 bytes are read in
- * wider loads).  No output may overlap an input, the workspace or another
+ * elements of a row are adjacent.  Arrays that have a row stride, and those of
+ * the norms and of dropout, need the alignment of their element; the weights
+ * and results of ffn_forward and ffn_backward start on 16 bytes (CGTP_EINVAL).  No output may overlap an input, the workspace or another
  * output (CGTP_EINVAL), except where a call says so.
  *
  * Every call runs asynchronously on hip_stream (NULL: the default stream),
@@ -81,7 +81,7 @@ int64_t ffn_backward_workspace_bytes(ffn_plan_t plan, int64_t N);
  * gradient).  CGTP_EINVAL for NULL or
  * misaligned arrays, N < 0, ldx < d_in, overlaps, a workspace that is too
  * small, or another current device than the plan's; CGTP_EUNSUP for
- * N > FFN_MAX_ROWS or ldx > 2^22.
+ * N > FFN_MAX_ROWS or ldx > 2^21.
  */
 int ffn_forward(ffn_plan_t plan, const void *x, int64_t ldx, const void *w_in, const void *w_out, void *y,
                 void *saved, int64_t N, void *workspace, int64_t workspace_bytes, void *hip_stream);

@@ -9,27 +9,44 @@
 namespace ffn {
 
 // ---------------------------------------------------------------- matrix products
-// C[m, n] = sum_k A(m, k) B(n, k).  A stored [M, K] (row stride lda) or, with
-// a_cols, [K, M]; likewise B.
+// C(m, n) = sum_k A(m, k) B(n, k) of 16-bit operands; see ffn_tile.h.
 enum Epilogue : int32_t {
     kStore = 0,      // C
     kGate = 1,       // B holds the gate's N rows, then the up projection's: H = act(G) * U; G, U kept in `saved`
-    kGateGrad = 2,   // acc is dH: dG, dU into C [M, 2 N], H into `h`
+    kGateGrad = 2,   // the sum is dH: dG, dU into C [M, 2 N], H into `h`
+    kPartial = 3,    // 32-bit partial sums of one split of k
 };
 
-struct GemmArgs {
+// Operands and results of one launch.  Strides in elements; operands start on 16 bytes, with strides that are
+// multiples of 8, and, along k, zeros up to the next multiple of 8.
+struct TileArgs {
     const void *a, *b;
-    int64_t lda, ldb;
-    int32_t a_cols, b_cols;
+    int64_t lda, ldb, plane_a, plane_b;   // plane: elements from one plane of a 32-bit array to the next
     int64_t M, N, K;
-    void* c;
-    int64_t ldc;
-    int32_t epilogue, act;
-    void* saved;     // kGate: output or NULL; kGateGrad: input; [M, 2 N] floats
-    void* h;         // kGateGrad: [M, N]
+    int32_t planes;                       // 1, or 3 for 32-bit arrays
+    int32_t act;
+    int32_t tiles_m, tiles_n, splits;
+    void* c;                              // kStore: C; kPartial: floats [splits, M, ldc]; kGate: H; kGateGrad: [dG dU]
+    int64_t ldc, plane_c;
+    float* saved;                         // [M, 2 N]
+    void* h;                              // kGateGrad: H
+    int64_t ldh, plane_h;
+    int32_t wide;                         // rows of c, h and saved start on a multiple of four elements of theirs
 };
 
-int launch_gemm(const GemmArgs& a, int32_t dtype, void* stream);
+int launch_tile_bf16(const TileArgs& p, int32_t epilogue, bool a_cols, bool b_cols, int32_t tile, void* stream);
+int launch_tile_fp16(const TileArgs& p, int32_t epilogue, bool a_cols, bool b_cols, int32_t tile, void* stream);
+int launch_tile_fp32(const TileArgs& p, int32_t epilogue, bool a_cols, bool b_cols, int32_t tile, void* stream);
+
+// out[i, j] = sum over splits of partial[s, i, j] (rows of ld floats), N columns, out contiguous.
+int launch_join(const float* partial, int64_t ld, int32_t splits, int64_t M, int64_t N, void* out, int32_t dtype, void* stream);
+
+int launch_zero(void* p, int64_t bytes, void* stream);
+
+// [rows, width] of `dtype` with row stride ld -> 16-bit operand with row stride `to_ld` (zeros from width on): a copy,
+// or three planes, `plane` elements apart, of 32-bit values.
+int launch_pack(const void* from, int64_t ld, int64_t rows, int64_t width, int32_t dtype, void* to, int64_t to_ld,
+                int64_t plane, void* stream);
 
 // ---------------------------------------------------------------- norms and dropout
 

@@ -16,7 +16,7 @@ struct ffn_plan_s {
 
 namespace {
 
-constexpr int64_t kMaxStride = 1LL << 22;
+constexpr int64_t kMaxStride = 1LL << 21;   // byte offsets within a tile of 256 rows stay below 2^31
 
 struct Range { const void* p; int64_t bytes; };
 
@@ -91,14 +91,119 @@ int check_norm(const ffn_norm* n, int64_t N, ffn::NormArgs* a) {
     return CGTP_OK;
 }
 
-// Byte offsets of the block's intermediates in its workspace.
-struct Layout { int64_t h, dgu, total; };
+int64_t up8(int64_t n) { return (n + 7) & ~7LL; }
+int64_t tiles(int64_t n, int64_t t) { return (n + t - 1) / t; }
+
+// How a product is cut up: work-groups of `tile` x `tile` outputs, k in `splits` parts.
+struct Cut { int32_t tile, splits; };
+
+// The shortest by this count, in steps of a 256-wide tile (64 k): a compute unit takes one such work-group, or two of
+// the 128-wide, whose steps cost 0.33 of it each when both run (a quarter of the arithmetic, twice the operands read
+// for it); parts of k cost their partial sums, written and read once.
+Cut choose(int64_t M, int64_t N, int64_t steps, bool gate, bool may_split) {
+    Cut best = {256, 1};
+    double least = 1e300;
+    for (int32_t tile : {256, 128}) {
+        const int64_t groups = tiles(M, tile) * tiles(gate ? 2 * N : N, tile);
+        for (int32_t s = 1; s <= 64 && (s == 1 || (may_split && steps / s >= 4)); s *= 2) {
+            const double rounds = (double)tiles(groups * s, tile == 256 ? 256 : 512);
+            const double t = rounds * ((double)tiles(steps, s) + 4) * (tile == 256 ? 1.0 : 0.66) +
+                             (s > 1 ? 8.0 + (double)(M * N * s) * 8.0 / 4e6 : 0.0);
+            if (t < least) { least = t; best = {tile, s}; }
+        }
+    }
+    return best;
+}
+
+int64_t steps_of(int64_t K, int32_t dtype) { return tiles(K, 64) * (dtype == FFN_FP32 ? 6 : 1); }
+
+int64_t partial_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype) {
+    const Cut c = choose(M, N, steps_of(K, dtype), false, true);
+    return c.splits > 1 ? aligned(c.splits * M * ((N + 3) & ~3LL) * 4) : 0;
+}
+
+int launch_tile(const ffn::TileArgs& t, int32_t epilogue, bool ac, bool bc, int32_t dtype, int32_t tile, void* stream) {
+    switch (dtype) {
+        case FFN_FP32: return ffn::launch_tile_fp32(t, epilogue, ac, bc, tile, stream);
+        case FFN_BF16: return ffn::launch_tile_bf16(t, epilogue, ac, bc, tile, stream);
+        default: return ffn::launch_tile_fp16(t, epilogue, ac, bc, tile, stream);
+    }
+}
+
+// Runs the product whose operands, sizes and results `t` describes; `partial` is scratch of partial_bytes().
+int product(ffn::TileArgs t, int32_t epilogue, bool ac, bool bc, int32_t dtype, void* partial, void* stream) {
+    t.planes = dtype == FFN_FP32 ? 3 : 1;
+    const Cut c = choose(t.M, t.N, steps_of(t.K, dtype), epilogue == ffn::kGate, epilogue == ffn::kStore);
+    const int64_t tm = tiles(t.M, c.tile), tn = tiles(epilogue == ffn::kGate ? 2 * t.N : t.N, c.tile);
+    if (tm * tn > 0x7FFFFFFF / 512) return CGTP_EUNSUP;   // threads of a launch
+    t.tiles_m = (int32_t)tm;
+    t.tiles_n = (int32_t)tn;
+    t.splits = c.splits;
+    if (c.splits == 1) return status(launch_tile(t, epilogue, ac, bc, dtype, c.tile, stream));
+    void* out = t.c;
+    t.c = partial;
+    t.ldc = (t.N + 3) & ~3LL;
+    const int rc = status(launch_tile(t, ffn::kPartial, ac, bc, dtype, c.tile, stream));
+    if (rc != CGTP_OK) return rc;
+    return status(ffn::launch_join((const float*)partial, t.ldc, c.splits, t.M, t.N, out, dtype, stream));
+}
+
+// A matrix as the products read it: 16-bit values (or three planes of them) on 16 bytes.
+struct Operand { const void* p; int64_t ld, plane; };
+
+// Elements of 16 bits of a packed [rows, width] matrix (one plane).
+int64_t packed(int64_t rows, int64_t width) { return rows * up8(width); }
+int64_t packed_bytes(int64_t rows, int64_t width, int32_t dtype) {
+    return aligned(packed(rows, width) * 2 * (dtype == FFN_FP32 ? 3 : 1));
+}
+
+// 16-bit matrices whose rows start on 16 bytes and hold whole chunks of 16 are read where they are.
+bool as_is(const void* p, int64_t ld, int64_t rows, int64_t width, int32_t dtype) {
+    return dtype != FFN_FP32 && ((uintptr_t)p & 15) == 0 && width % 8 == 0 && (ld % 8 == 0 || rows == 1);
+}
+
+int operand(const void* p, int64_t ld, int64_t rows, int64_t width, int32_t dtype, void* scratch, void* stream, Operand* o) {
+    if (as_is(p, ld, rows, width, dtype)) {
+        *o = {p, ld % 8 == 0 ? ld : up8(ld), 0};
+        return CGTP_OK;
+    }
+    *o = {scratch, up8(width), packed(rows, width)};
+    return status(ffn::launch_pack(p, ld, rows, width, dtype, scratch, o->ld, o->plane, stream));
+}
+
+// Byte offsets in the block's workspace: intermediates, operands to be packed, partial sums.
+struct Layout { int64_t h, dgu, x, w_in, w_out, gy, partial, total; };
 Layout layout(const ffn_plan_s* p, int64_t N, bool backward) {
-    const int64_t e = size_of(p->dtype);
+    const int64_t di = p->d_in, df = p->d_ff, d_o = p->d_out;
+    const int32_t t = p->dtype;
     Layout l = {};
-    l.dgu = aligned(N * p->d_ff * e);
-    l.total = l.dgu + (backward ? aligned(N * 2 * p->d_ff * e) : 0);
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) { const int64_t o = at; at += bytes; return o; };
+    // weights are contiguous and start on 16 bytes: they need packing by their width alone
+    l.h = take(packed_bytes(N, df, t));
+    l.x = take(packed_bytes(N, di, t));
+    l.w_in = take(t == FFN_FP32 || di % 8 ? packed_bytes(2 * df, di, t) : 0);
+    l.w_out = take(t == FFN_FP32 || df % 8 ? packed_bytes(d_o, df, t) : 0);
+    int64_t partial = 0;
+    auto also = [&](int64_t bytes) { partial = bytes > partial ? bytes : partial; };
+    if (backward) {
+        l.dgu = take(packed_bytes(N, 2 * df, t));
+        l.gy = take(packed_bytes(N, d_o, t));
+        also(partial_bytes(N, di, 2 * df, t));
+        also(partial_bytes(2 * df, di, N, t));
+        also(partial_bytes(d_o, df, N, t));
+    } else {
+        also(partial_bytes(N, d_o, df, t));
+    }
+    l.partial = take(partial);
+    l.total = at;
     return l;
+}
+
+bool wide4(std::initializer_list<const void*> ps, std::initializer_list<int64_t> widths) {
+    int64_t all = 0;
+    for (int64_t w : widths) all |= w;
+    return !misaligned(ps, 16) && (all & 3) == 0;
 }
 
 }  // namespace
@@ -141,7 +246,7 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
     if (!x || !w_in || !w_out || !y || ldx < plan->d_in) return CGTP_EINVAL;
     if (N > FFN_MAX_ROWS || ldx > kMaxStride) return CGTP_EUNSUP;
     const int64_t e = size_of(plan->dtype), di = plan->d_in, df = plan->d_ff, d_o = plan->d_out;
-    if (misaligned({x, w_in, w_out, y}, e) || misaligned({saved}, 4)) return CGTP_EINVAL;
+    if (misaligned({x}, e) || misaligned({w_in, w_out, y, saved}, 16)) return CGTP_EINVAL;
     const Layout l = layout(plan, N, false);
     int rc = workspace_ok(workspace, workspace_bytes, l.total);
     if (rc != CGTP_OK) return rc;
@@ -151,18 +256,27 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
     rc = current_device_is(plan->device);
     if (rc != CGTP_OK) return rc;
     char* ws = (char*)workspace;
-    ffn::GemmArgs g = {};
-    g.a = x; g.lda = ldx; g.b = w_in; g.ldb = di;
-    g.M = N; g.N = df; g.K = di;
-    g.c = ws + l.h; g.ldc = df;
-    g.epilogue = ffn::kGate; g.act = plan->act; g.saved = saved;
-    rc = status(ffn::launch_gemm(g, plan->dtype, hip_stream));
+    Operand X, Wi, Wo;
+    rc = operand(x, ldx, N, di, plan->dtype, ws + l.x, hip_stream, &X);
+    if (rc == CGTP_OK) rc = operand(w_in, di, 2 * df, di, plan->dtype, ws + l.w_in, hip_stream, &Wi);
+    if (rc == CGTP_OK) rc = operand(w_out, df, d_o, df, plan->dtype, ws + l.w_out, hip_stream, &Wo);
     if (rc != CGTP_OK) return rc;
-    ffn::GemmArgs o = {};
-    o.a = ws + l.h; o.lda = df; o.b = w_out; o.ldb = df;
+    ffn::TileArgs g = {};
+    g.a = X.p; g.lda = X.ld; g.plane_a = X.plane;
+    g.b = Wi.p; g.ldb = Wi.ld; g.plane_b = Wi.plane;
+    g.M = N; g.N = df; g.K = di;
+    g.c = ws + l.h; g.ldc = up8(df); g.plane_c = packed(N, df);
+    g.act = plan->act; g.saved = (float*)saved;
+    g.wide = wide4({saved}, {df});
+    rc = product(g, ffn::kGate, false, false, plan->dtype, nullptr, hip_stream);
+    if (rc != CGTP_OK) return rc;
+    ffn::TileArgs o = {};
+    o.a = ws + l.h; o.lda = up8(df); o.plane_a = packed(N, df);
+    o.b = Wo.p; o.ldb = Wo.ld; o.plane_b = Wo.plane;
     o.M = N; o.N = d_o; o.K = df;
     o.c = y; o.ldc = d_o;
-    return status(ffn::launch_gemm(o, plan->dtype, hip_stream));
+    o.wide = wide4({y}, {d_o});
+    return product(o, ffn::kStore, false, false, plan->dtype, ws + l.partial, hip_stream);
 }
 
 int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, const void* w_out, const void* saved,
@@ -172,7 +286,7 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
     const int64_t e = size_of(plan->dtype), di = plan->d_in, df = plan->d_ff, d_o = plan->d_out;
     if (N > 0 && (!x || !w_in || !w_out || !saved || !grad_y || ldx < di || ldg < d_o)) return CGTP_EINVAL;
     if (N > FFN_MAX_ROWS || ldx > kMaxStride || ldg > kMaxStride) return CGTP_EUNSUP;
-    if (misaligned({x, w_in, w_out, grad_y, grad_x, grad_w_in, grad_w_out}, e) || misaligned({saved}, 4)) return CGTP_EINVAL;
+    if (misaligned({x, grad_y}, e) || misaligned({w_in, w_out, saved, grad_x, grad_w_in, grad_w_out}, 16)) return CGTP_EINVAL;
     const Layout l = layout(plan, N, true);
     int rc = workspace_ok(workspace, workspace_bytes, l.total);
     if (rc != CGTP_OK) return rc;
@@ -183,38 +297,58 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
     if (any_overlap(outs, ins)) return CGTP_EINVAL;
     rc = current_device_is(plan->device);
     if (rc != CGTP_OK) return rc;
+    if (N == 0) {
+        // sums over no rows
+        hipStream_t s = (hipStream_t)hip_stream;
+        if (grad_w_in) rc = status(ffn::launch_zero(grad_w_in, 2 * df * di * e, s));
+        if (rc == CGTP_OK && grad_w_out) rc = status(ffn::launch_zero(grad_w_out, d_o * df * e, s));
+        return rc;
+    }
     char* ws = (char*)workspace;
-    if (N > 0) {
-        ffn::GemmArgs g = {};
-        g.a = grad_y; g.lda = ldg; g.b = w_out; g.ldb = df; g.b_cols = 1;
-        g.M = N; g.N = df; g.K = d_o;
-        g.c = ws + l.dgu; g.ldc = 2 * df;
-        g.epilogue = ffn::kGateGrad; g.act = plan->act; g.saved = const_cast<void*>(saved); g.h = ws + l.h;
-        rc = status(ffn::launch_gemm(g, plan->dtype, hip_stream));
+    Operand X, Wi, Wo, Gy;
+    rc = operand(grad_y, ldg, N, d_o, plan->dtype, ws + l.gy, hip_stream, &Gy);
+    if (rc == CGTP_OK) rc = operand(w_out, df, d_o, df, plan->dtype, ws + l.w_out, hip_stream, &Wo);
+    if (rc != CGTP_OK) return rc;
+    const Operand H = {ws + l.h, up8(df), packed(N, df)}, D = {ws + l.dgu, up8(2 * df), packed(N, 2 * df)};
+    ffn::TileArgs g = {};
+    g.a = Gy.p; g.lda = Gy.ld; g.plane_a = Gy.plane;
+    g.b = Wo.p; g.ldb = Wo.ld; g.plane_b = Wo.plane;
+    g.M = N; g.N = df; g.K = d_o;
+    g.c = ws + l.dgu; g.ldc = D.ld; g.plane_c = D.plane;
+    g.h = ws + l.h; g.ldh = H.ld; g.plane_h = H.plane;
+    g.act = plan->act; g.saved = (float*)const_cast<void*>(saved);
+    g.wide = wide4({saved}, {df});
+    rc = product(g, ffn::kGateGrad, false, true, plan->dtype, nullptr, hip_stream);
+    if (rc == CGTP_OK && grad_x) {
+        rc = operand(w_in, di, 2 * df, di, plan->dtype, ws + l.w_in, hip_stream, &Wi);
         if (rc != CGTP_OK) return rc;
+        ffn::TileArgs t = {};
+        t.a = D.p; t.lda = D.ld; t.plane_a = D.plane;
+        t.b = Wi.p; t.ldb = Wi.ld; t.plane_b = Wi.plane;
+        t.M = N; t.N = di; t.K = 2 * df;
+        t.c = grad_x; t.ldc = di;
+        t.wide = wide4({grad_x}, {di});
+        rc = product(t, ffn::kStore, false, true, plan->dtype, ws + l.partial, hip_stream);
     }
-    if (grad_x && N > 0) {
-        ffn::GemmArgs g = {};
-        g.a = ws + l.dgu; g.lda = 2 * df; g.b = w_in; g.ldb = di; g.b_cols = 1;
-        g.M = N; g.N = di; g.K = 2 * df;
-        g.c = grad_x; g.ldc = di;
-        rc = status(ffn::launch_gemm(g, plan->dtype, hip_stream));
+    if (rc == CGTP_OK && grad_w_in) {
+        rc = operand(x, ldx, N, di, plan->dtype, ws + l.x, hip_stream, &X);
         if (rc != CGTP_OK) return rc;
+        ffn::TileArgs t = {};
+        t.a = D.p; t.lda = D.ld; t.plane_a = D.plane;
+        t.b = X.p; t.ldb = X.ld; t.plane_b = X.plane;
+        t.M = 2 * df; t.N = di; t.K = N;
+        t.c = grad_w_in; t.ldc = di;
+        t.wide = wide4({grad_w_in}, {di});
+        rc = product(t, ffn::kStore, true, true, plan->dtype, ws + l.partial, hip_stream);
     }
-    if (grad_w_in) {
-        ffn::GemmArgs g = {};
-        g.a = ws + l.dgu; g.lda = 2 * df; g.a_cols = 1; g.b = x; g.ldb = ldx; g.b_cols = 1;
-        g.M = 2 * df; g.N = di; g.K = N;
-        g.c = grad_w_in; g.ldc = di;
-        rc = status(ffn::launch_gemm(g, plan->dtype, hip_stream));
-        if (rc != CGTP_OK) return rc;
-    }
-    if (grad_w_out) {
-        ffn::GemmArgs g = {};
-        g.a = grad_y; g.lda = ldg; g.a_cols = 1; g.b = ws + l.h; g.ldb = df; g.b_cols = 1;
-        g.M = d_o; g.N = df; g.K = N;
-        g.c = grad_w_out; g.ldc = df;
-        rc = status(ffn::launch_gemm(g, plan->dtype, hip_stream));
+    if (rc == CGTP_OK && grad_w_out) {
+        ffn::TileArgs t = {};
+        t.a = Gy.p; t.lda = Gy.ld; t.plane_a = Gy.plane;
+        t.b = H.p; t.ldb = H.ld; t.plane_b = H.plane;
+        t.M = d_o; t.N = df; t.K = N;
+        t.c = grad_w_out; t.ldc = df;
+        t.wide = wide4({grad_w_out}, {df});
+        rc = product(t, ffn::kStore, true, true, plan->dtype, ws + l.partial, hip_stream);
     }
     return rc;
 }

@@ -1,0 +1,390 @@
+// Tiled matrix product on the 16-bit matrix instructions, with the feed-forward
+// block's epilogues.  Internal; instantiated once per array type (ffn_tile_*.hip).
+//
+// C(m, n) = sum_k A(m, k) B(n, k), A and B each stored with k adjacent ("rows")
+// or with m / n adjacent ("columns").  A work-group of BM x BN outputs walks k in
+// steps of 64: operands go from memory to LDS directly (16 bytes a lane, no
+// registers), one step ahead of the step that is multiplied, in two buffers.
+// Waves hold 16 x 16 accumulators of a (BM / WM) x 64 block.
+//
+// LDS layouts, chosen so that the direct loads write whole 1 KB runs and the
+// reads meet no bank twice:
+//   rows:    [row][64 k], 16-byte chunk c of row r kept at chunk c ^ (r & 7);
+//            fragments by 16-byte reads
+//   columns: [k][BM or BN], 32-byte unit u of row k kept at u ^ s(k),
+//            s(k) = (k & 3) | ((k >> 3) & 1) << 2; fragments by the transposing
+//            8-byte read (16 lanes give four k-rows of 16 values and get back one
+//            column of four k each)
+//
+// 32-bit arrays run as three bf16 planes, x = x0 + x1 + x2 exactly (8 bits of the
+// significand each, cut, not rounded, so that no plane overflows), by the six
+// products x_i y_j with i + j <= 2: what is left out is below 2^-24 of |x| |y|.
+#pragma once
+
+#include "ffn_device.h"
+
+namespace ffn {
+
+namespace dev {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef fp16 fp16x4 __attribute__((ext_vector_type(4)));
+typedef fp16 fp16x8 __attribute__((ext_vector_type(8)));
+#define FFN_LDS __attribute__((address_space(3)))
+
+__device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c, bf16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c, fp16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(fp16x8, a), __builtin_bit_cast(fp16x8, b), c, 0, 0, 0);
+}
+
+// x cut to its upper 16 bits; the rest follows exactly.  What is not finite goes to the first plane alone.
+__device__ __forceinline__ float cut(float x) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xFFFF0000u); }
+__device__ __forceinline__ void planes_of(float x, uint16_t (&p)[3]) {
+    if ((__builtin_bit_cast(uint32_t, x) & 0x7F800000u) == 0x7F800000u) {
+        // a NaN whose set bits are all cut away would read as infinite
+        p[0] = (uint16_t)((__builtin_bit_cast(uint32_t, x) >> 16) | (x != x ? 0x40u : 0u));
+        p[1] = p[2] = 0;
+        return;
+    }
+    const float x0 = cut(x), r1 = x - x0, x1 = cut(r1), x2 = cut(r1 - x1);
+    p[0] = (uint16_t)(__builtin_bit_cast(uint32_t, x0) >> 16);
+    p[1] = (uint16_t)(__builtin_bit_cast(uint32_t, x1) >> 16);
+    p[2] = (uint16_t)(__builtin_bit_cast(uint32_t, x2) >> 16);
+}
+
+// Four adjacent values of a row, columns n .. n + 3, in the arrays' type; whoever stores column N - 1 also
+// writes zeros up to column `pad`, for products that read whole 16-byte chunks of the row.
+template <typename Out> __device__ __forceinline__ void store4(Out* p, int64_t n, int64_t N, int64_t pad, f32x4 v, bool wide) {
+    typedef Out Out4 __attribute__((ext_vector_type(4)));
+    if (wide && n + 3 < N) {
+        Out4 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = (Out)v[j];
+        *(Out4*)(p + n) = o;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (n + j < N) p[n + j] = (Out)v[j];
+    }
+    if (n < N && n + 4 >= N)
+        for (int64_t c = N; c < pad; ++c) p[c] = (Out)0.0f;
+}
+
+// The same for a 32-bit intermediate kept as three planes.
+__device__ __forceinline__ void store4_planes(uint16_t* p, int64_t plane, int64_t n, int64_t N, int64_t pad, f32x4 v, bool wide) {
+    uint16_t q[4][3];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) planes_of(v[j], q[j]);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        uint16_t* r = p + i * plane;
+        if (wide && n + 3 < N) {
+            *(s16x4*)(r + n) = s16x4{(short)q[0][i], (short)q[1][i], (short)q[2][i], (short)q[3][i]};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (n + j < N) r[n + j] = q[j][i];
+        }
+        if (n < N && n + 4 >= N)
+            for (int64_t c = N; c < pad; ++c) r[c] = 0;
+    }
+}
+
+// An intermediate (H, dG, dU): in T, or as planes of T where the arrays hold 32 bits.
+template <typename T, typename Out> __device__ __forceinline__ void store_mid(void* base, int64_t row, int64_t ld, int64_t plane, int64_t n,
+                                                                              int64_t N, int64_t pad, f32x4 v, bool wide) {
+    if constexpr (sizeof(Out) == 4) store4_planes((uint16_t*)base + row * ld, plane, n, N, pad, v, wide);
+    else store4<T>((T*)base + row * ld, n, N, pad, v, wide);
+}
+
+__device__ __forceinline__ f32x4 load4(const float* p, int64_t n, int64_t N, bool wide) {
+    if (wide && n + 3 < N) return *(const f32x4*)(p + n);
+    f32x4 v = {};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (n + j < N) v[j] = p[n + j];
+    return v;
+}
+
+constexpr uint32_t kOut = 0x80000000u;    // beyond every buffer: a direct load from there writes zeros
+
+// The direct loads of one operand: `R` rows of C's index a tile, 64 k a step, by NW waves.
+template <int R, int NW, bool COLS, bool GATE> struct Loader {
+    static constexpr int kLoads = R * 128 / 1024 / NW;
+    __amdgpu_buffer_rsrc_t rsrc[GATE ? 2 : 1];
+    const char* base[GATE ? 2 : 1];
+    uint32_t voff[kLoads];
+    uint32_t kpos;       // first k of this lane's chunk (rows) or k row of its first load (columns)
+    int64_t step;
+
+    static __device__ __forceinline__ int swizzle(int k) {
+        const int s = (k & 3) | ((k >> 3) & 1) << 2;
+        return R >= 128 ? s : s & (R / 16 - 1);
+    }
+
+    __device__ __forceinline__ void init(const void* p, int64_t ld, int64_t r0, int64_t rows, int64_t half, int wave, int lane) {
+        if constexpr (!COLS) {
+            const int sub = lane >> 3, c = (lane & 7) ^ sub;
+            kpos = c * 8;
+            step = 128;
+            if constexpr (GATE) {
+                // blocks of 64 tile rows: 32 of the gate's rows, then the same 32 of the up projection's
+                base[0] = (const char*)p + r0 * ld * 2;
+                base[1] = base[0] + half * ld * 2;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int t = (i * NW + wave) * 8 + sub;
+                    int64_t r = (t >> 6) * 32 + (t & 31);
+                    if (r0 + r >= rows) r = rows - 1 - r0;
+                    voff[i] = (uint32_t)(r * ld * 2 + c * 16);
+                }
+            } else {
+                base[0] = (const char*)p + r0 * ld * 2;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    int64_t r = (i * NW + wave) * 8 + sub;
+                    if (r0 + r >= rows) r = rows - 1 - r0;
+                    voff[i] = (uint32_t)(r * ld * 2 + c * 16);
+                }
+            }
+        } else {
+            constexpr int kRows = 1024 / (R * 2) ? 1024 / (R * 2) : 1;   // k rows a load
+            constexpr int kChunks = 64 / kRows;
+            base[0] = (const char*)p + r0 * 2;
+            step = 64 * ld * 2;
+            kpos = wave * kRows + lane / kChunks;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int k = i * NW * kRows + (int)kpos, pos = lane % kChunks;
+                int c = (((pos >> 1) ^ swizzle(k)) << 1) | (pos & 1);
+                if (r0 + c * 8 >= rows) c = 0;
+                voff[i] = (uint32_t)(k * ld * 2 + c * 16);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void seek(int64_t bytes) {
+#pragma unroll
+        for (int g = 0; g < (GATE ? 2 : 1); ++g)
+            rsrc[g] = __builtin_amdgcn_make_buffer_rsrc((void*)(base[g] + bytes), 0, (int)0x7FFFFFFF, 0x00020000);
+    }
+
+    // k left from this step's first on; `whole`: at least 64 of them
+    __device__ __forceinline__ void issue(char* lds, int wave, int left) const {
+        constexpr int kRows = COLS ? (1024 / (R * 2) ? 1024 / (R * 2) : 1) : 0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int k = COLS ? (int)kpos + i * NW * kRows : (int)kpos;
+            const uint32_t v = k < left ? voff[i] : kOut;
+            FFN_LDS void* to = (FFN_LDS void*)(lds + (i * NW + wave) * 1024);
+            if constexpr (GATE) {
+                if ((((i * NW + wave) * 8) & 63) < 32) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc[0], to, 16, v, 0, 0, 0);
+                else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc[1], to, 16, v, 0, 0, 0);
+            } else {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc[0], to, 16, v, 0, 0, 0);
+            }
+        }
+    }
+};
+
+// The fragment of 16 rows from `r` on and 32 k from 32 kk on: lane l gets row r + l % 16, k = 8 (l / 16) .. + 7.
+template <int R, bool COLS> __device__ __forceinline__ s16x8 fragment(const char* lds, int r, int kk, int lane) {
+    const int q = lane >> 4, i = lane & 15;
+    if constexpr (!COLS) {
+        const int row = r + i, c = (kk * 4 + q) ^ (row & 7);
+        return *(const s16x8*)(lds + row * 128 + c * 16);
+    } else {
+        const int k = kk * 32 + q * 8 + (i >> 2);
+        const int s = Loader<R, 1, true, false>::swizzle(k);
+        const int at = k * R * 2 + (((r >> 4) ^ s) << 5) + (i & 3) * 8;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FFN_LDS s16x4*)(lds + at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FFN_LDS s16x4*)(lds + at + 4 * R * 2));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+}
+
+// Which tile a work-group takes.  Consecutive work-groups go to the eight dies in turn; each die gets a run of
+// consecutive tiles, and a run walks down eight rows of tiles before it moves one column on, so that a die's L2
+// holds what its tiles share.
+__device__ __forceinline__ void place(int id, int total, int tm, int tn, int& m, int& n) {
+    const int die = id & 7, per = total >> 3, more = total & 7;
+    const int t = die * per + (die < more ? die : more) + (id >> 3);
+    constexpr int kGroup = 8;
+    const int band = t / (kGroup * tn), r = t - band * kGroup * tn;
+    const int rows = tm - band * kGroup < kGroup ? tm - band * kGroup : kGroup;
+    m = band * kGroup + r % rows;
+    n = r / rows;
+}
+
+template <typename T, typename Out, int BM, int BN, int WM, int WN, bool AC, bool BC, int EPI>
+__global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
+#ifdef __HIP_DEVICE_COMPILE__   // (the host's pass needs the launch stub alone)
+    constexpr int NW = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16;
+    static_assert(EPI != kGate || NT == 4, "a wave holds 32 gate columns and 32 of the up projection");
+    __shared__ __align__(1024) char sa0[BM * 128], sb0[BN * 128];
+    __shared__ __align__(1024) char sa1[BM * 128], sb1[BN * 128];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+    const int total = p.tiles_m * p.tiles_n;
+    int tm, tn;
+    place(blockIdx.x, total, p.tiles_m, p.tiles_n, tm, tn);
+    constexpr int kCols = EPI == kGate ? BN / 2 : BN;      // columns of C a tile covers
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * kCols;
+
+    Loader<BM, NW, AC, false> la;
+    Loader<BN, NW, BC, EPI == kGate> lb;
+    la.init(p.a, p.lda, m0, p.M, 0, wave, lane);
+    lb.init(p.b, p.ldb, n0, p.N, p.N, wave, lane);
+
+    // this split's steps, of 64 k each, one product of planes after the other
+    const int nk = (int)((p.K + 63) >> 6), pairs = p.planes == 3 ? 6 : 1, steps = nk * pairs;
+    const int s0 = (int)((int64_t)steps * blockIdx.y / p.splits), s1 = (int)((int64_t)steps * (blockIdx.y + 1) / p.splits);
+    int pair = s0 / nk, ks = s0 - pair * nk;
+
+    auto issue = [&](char* a, char* b) {
+        // products (0, 2), (2, 0), (1, 1), (0, 1), (1, 0), (0, 0): the smallest first
+        const int pa = p.planes == 3 ? (0x010120 >> (4 * pair)) & 3 : 0, pb = p.planes == 3 ? (0x001102 >> (4 * pair)) & 3 : 0;
+        la.seek(pa * p.plane_a * 2 + ks * la.step);
+        lb.seek(pb * p.plane_b * 2 + ks * lb.step);
+        const int64_t rest = p.K - (int64_t)ks * 64;
+        const int left = rest < 64 ? (int)rest : 64;
+        la.issue(a, wave, left);
+        lb.issue(b, wave, left);
+        if (++ks == nk) { ks = 0; ++pair; }
+    };
+
+    f32x4 acc[MT][NT] = {};
+    auto multiply = [&](const char* a, const char* b) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            s16x8 fb[NT], fa[MT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) fb[j] = fragment<BN, BC>(b, wn + j * 16, kk, lane);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) fa[i] = fragment<BM, AC>(a, wm + i * 16, kk, lane);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = mfma16(fb[j], fa[i], acc[i][j], T());
+        }
+    };
+
+    if (s0 < s1) issue(sa0, sb0);
+    __syncthreads();
+    int s = s0;
+    for (; s + 1 < s1; s += 2) {
+        issue(sa1, sb1);
+        multiply(sa0, sb0);
+        __syncthreads();
+        if (s + 2 < s1) issue(sa0, sb0);
+        multiply(sa1, sb1);
+        __syncthreads();
+    }
+    if (s < s1) multiply(sa0, sb0);
+
+    // acc[i][j][e] is row m = .. + lane % 16, column n = .. + 4 (lane / 16) + e.  Each wave turns 32 rows at a time in
+    // LDS of its own, so that memory is read and written along the rows: 16 lanes a row of 64 columns.
+    __syncthreads();
+    constexpr int kRow = 68, kTurn = 32 * kRow * 4;        // floats a row (four more than it holds: no bank twice)
+    constexpr int kFit = BM * 128 / kTurn;
+    static_assert(kFit >= 1 && 4 * kFit >= NW && BM == BN, "a turn buffer for every wave");
+    float* turn = (float*)((wave / kFit == 0 ? sa0 : wave / kFit == 1 ? sb0 : wave / kFit == 2 ? sa1 : sb1) + wave % kFit * kTurn);
+    const bool wide = p.wide;
+#pragma unroll
+    for (int i = 0; i < MT; i += 2) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                *(f32x4*)(turn + (x * 16 + (lane & 15)) * kRow + j * 16 + (lane >> 4) * 4) = acc[i + x][j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const int64_t mb = m0 + wm + i * 16;
+        if constexpr (EPI == kGate) {
+            const int64_t n = n0 + wn / 2 + (lane & 7) * 4;
+            for (int r = lane >> 3; r < 32; r += 8) {
+                const int64_t m = mb + r;
+                if (m >= p.M) break;
+                const f32x4 g = *(const f32x4*)(turn + r * kRow + (lane & 7) * 4), u = *(const f32x4*)(turn + r * kRow + 32 + (lane & 7) * 4);
+                f32x4 h;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float v, dv;
+                    activate(p.act, g[e], v, dv);
+                    h[e] = v * u[e];
+                }
+                store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, p.ldc, h, wide);
+                if (p.saved) {
+                    store4<float>(p.saved + m * 2 * p.N, n, p.N, 0, g, wide);
+                    store4<float>(p.saved + m * 2 * p.N + p.N, n, p.N, 0, u, wide);
+                }
+            }
+        } else {
+            const int64_t n = n0 + wn + (lane & 15) * 4;
+            for (int r = lane >> 4; r < 32; r += 4) {
+                const int64_t m = mb + r;
+                if (m >= p.M) break;
+                const f32x4 v = *(const f32x4*)(turn + r * kRow + (lane & 15) * 4);
+                if constexpr (EPI == kStore) {
+                    store4<Out>((Out*)p.c + m * p.ldc, n, p.N, 0, v, wide);
+                } else if constexpr (EPI == kPartial) {
+                    store4<float>((float*)p.c + ((int64_t)blockIdx.y * p.M + m) * p.ldc, n, p.N, 0, v, true);
+                } else {
+                    const f32x4 g = load4(p.saved + m * 2 * p.N, n, p.N, wide), u = load4(p.saved + m * 2 * p.N + p.N, n, p.N, wide);
+                    f32x4 dg, du, h;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float a, da;
+                        activate(p.act, g[e], a, da);
+                        dg[e] = v[e] * u[e] * da;
+                        du[e] = v[e] * a;
+                        h[e] = a * u[e];
+                    }
+                    store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, 0, dg, wide);
+                    if constexpr (sizeof(Out) == 4)
+                        store4_planes((uint16_t*)p.c + m * p.ldc + p.N, p.plane_c, n, p.N, p.ldc - p.N, du, wide);
+                    else
+                        store4<T>((T*)p.c + m * p.ldc + p.N, n, p.N, p.ldc - p.N, du, wide);
+                    store_mid<T, Out>(p.h, m, p.ldh, p.plane_h, n, p.N, p.ldh, h, wide);
+                }
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+#endif
+}
+
+template <typename T, typename Out, int BM, int WM, bool AC, bool BC, int EPI> int run_tile(const TileArgs& p, hipStream_t s) {
+    constexpr int WN = BM / 64;
+    tile_kernel<T, Out, BM, BM, WM, WN, AC, BC, EPI><<<dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), 64 * WM * WN, 0, s>>>(p);
+    return (int)hipGetLastError();
+}
+
+// tile: 256 or 128 (outputs a side of a work-group)
+template <typename T, typename Out> int run_product(const TileArgs& p, int32_t epilogue, bool ac, bool bc, int32_t tile, hipStream_t s) {
+#define FFN_RUN(AC, BC, EPI) (tile == 256 ? run_tile<T, Out, 256, 2, AC, BC, EPI>(p, s) : run_tile<T, Out, 128, 2, AC, BC, EPI>(p, s))
+    if (epilogue == kGate && !ac && !bc) return FFN_RUN(false, false, kGate);
+    if (epilogue == kGateGrad && !ac && bc) return FFN_RUN(false, true, kGateGrad);
+    if (epilogue == kStore) {
+        if (!ac && !bc) return FFN_RUN(false, false, kStore);
+        if (!ac && bc) return FFN_RUN(false, true, kStore);
+        if (ac && bc) return FFN_RUN(true, true, kStore);
+    }
+    if (epilogue == kPartial) {
+        if (!ac && !bc) return FFN_RUN(false, false, kPartial);
+        if (!ac && bc) return FFN_RUN(false, true, kPartial);
+        if (ac && bc) return FFN_RUN(true, true, kPartial);
+    }
+#undef FFN_RUN
+    return (int)hipErrorInvalidValue;
+}
+
+}  // namespace dev
+}  // namespace ffn
