@@ -62,75 +62,280 @@ __global__ __launch_bounds__(kThreads) void norm_forward_kernel(NormArgs p) {
     }
 }
 
-// Terms of one value of the backward pass, given the row's means.
-struct Terms { float gx, ny, nh, f, g, s; };
-template <typename T> __device__ __forceinline__ Terms terms(const NormArgs& p, int64_t row, int64_t c, float ry, float rh, float c1) {
-    Terms t = {};
-    t.gx = p.gy ? to_f32(((const T*)p.gy)[row * p.width + c]) : 0.0f;
-    if (p.gu) {
-        t.ny = to_f32(((const T*)p.y)[row * p.ldx + c]) * ry;
-        t.gx += ry * (to_f32(((const T*)p.gu)[row * p.ldg + c]) * load<T>(p.wn, c, 1.0f) - t.ny * c1);
+// ---------------------------------------------------------------- rows held in registers
+//
+// A worker of TPR threads takes a row, eight adjacent values (one block of the generator) a thread and turn, I turns:
+// every array is read and written once, and the row's sums stay in registers.  Workers of 64 threads or fewer reduce by
+// shuffles alone; a wider worker is a work-group and passes its waves' sums through LDS.
+
+template <typename T> struct Raw { typedef T V __attribute__((ext_vector_type(8))); };
+
+// Values c .. c + 7 of a row of D (zeros beyond it).  Rows may start on any element.
+template <typename T> __device__ __forceinline__ typename Raw<T>::V load8(const T* row, int64_t c, int64_t D) {
+    typename Raw<T>::V v;
+    if (c + 8 <= D) {
+        __builtin_memcpy(&v, row + c, sizeof(v));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < D ? row[c + j] : (T)0.0f;
     }
-    if (p.h) {
-        t.f = factor(p.drop, row, c);
-        t.g = load<T>(p.gate, row / p.rows_per_gate * p.width + c, 1.0f);
-        t.s = load<T>(p.scale, c, 1.0f);
-        t.nh = to_f32(((const T*)p.h)[row * p.width + c]) * rh;
+    return v;
+}
+template <typename T> __device__ __forceinline__ void store8(T* row, int64_t c, int64_t D, const float (&f)[8]) {
+    if (c + 8 <= D) {
+        typename Raw<T>::V v;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (T)f[j];
+        __builtin_memcpy(row + c, &v, sizeof(v));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < D) row[c + j] = (T)f[j];
     }
-    return t;
+}
+// A row of factors; ones where there is none.
+template <typename T> __device__ __forceinline__ void factors8(const void* p, int64_t c, int64_t D, float (&f)[8]) {
+    if (p) {
+        const typename Raw<T>::V v = load8((const T*)p, c, D);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = to_f32(v[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = 1.0f;
+    }
+}
+__device__ __forceinline__ void drop8(const DropArgs& d, int64_t row, int64_t c, float (&f)[8]) {
+    if (d.threshold == 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = 1.0f;
+        return;
+    }
+    const Words q = philox((uint32_t)(c >> 3), (uint32_t)row, d.offset, d.seed);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = kept(q, j, d.threshold) ? d.scale : 0.0f;
 }
 
-// The two means of each row: of (gu w_next) n_y, and of (d/dN(h)) w n_h.
+// Sums of K values over a worker, returned to all its threads.  `s` is LDS for two calls in turn (`turn` alternates):
+// one barrier a call keeps both the values and the next but one call's writes in order.
+template <int TPR, int K> __device__ __forceinline__ void worker_sum(float (&v)[K], float* s, int turn) {
+#pragma unroll
+    for (int o = (TPR < 64 ? TPR : 64) / 2; o; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o, 64);
+    if constexpr (TPR > 64) {
+        constexpr int W = TPR / 64;
+        float* t = s + turn * W * K;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int k = 0; k < K; ++k) t[(threadIdx.x >> 6) * K + k] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            float a = t[k];
+#pragma unroll
+            for (int w = 1; w < W; ++w) a += t[w * K + k];
+            v[k] = a;
+        }
+    }
+}
+
+constexpr int group_of(int tpr) { return tpr > 64 ? tpr : 256; }
+
+template <typename T, int TPR, int I>
+__global__ __launch_bounds__(group_of(TPR)) void norm_forward_rows(NormArgs p) {
+    __shared__ float s[2 * (TPR > 64 ? TPR / 64 : 1)];
+    constexpr int kWorkers = group_of(TPR) / TPR;
+    const int64_t D = p.width;
+    const int t = threadIdx.x % TPR;
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * kWorkers + threadIdx.x / TPR; row < p.N; row += (int64_t)gridDim.x * kWorkers) {
+    typename Raw<T>::V xr[I], hr[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const int64_t c = (int64_t)(t + i * TPR) * 8;
+        xr[i] = load8((const T*)p.x + row * p.ldx, c, D);
+        if (p.h) hr[i] = load8((const T*)p.h + row * D, c, D);
+    }
+    float v[I][8];
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = to_f32(xr[i][j]);
+    if (p.h) {
+        float sum[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[0] += to_f32(hr[i][j]) * to_f32(hr[i][j]);
+        worker_sum<TPR, 1>(sum, s, turn);
+        turn ^= 1;
+        const float rh = 1.0f / sqrtf(sum[0] / (float)D + p.eps);
+        if (p.rstd_h && t == 0) p.rstd_h[row] = rh;
+        const T* gate = p.gate ? (const T*)p.gate + (int64_t)((uint32_t)row / (uint32_t)p.rows_per_gate) * D : nullptr;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t c = (int64_t)(t + i * TPR) * 8;
+            if (c >= D) continue;
+            float f[8], g[8], w[8], sc[8];
+            drop8(p.drop, row, c, f);
+            factors8<T>(p.w, c, D, w);
+            factors8<T>(gate, c, D, g);
+            factors8<T>(p.scale, c, D, sc);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float n = to_f32(hr[i][j]) * rh * w[j];
+                v[i][j] += sc[j] * g[j] * (f[j] == 0.0f ? 0.0f : n * f[j]);
+            }
+            if (p.y) store8((T*)p.y + row * D, c, D, v[i]);
+        }
+    }
+    if (!p.u) continue;
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const int64_t c = (int64_t)(t + i * TPR) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < D) sum[0] += v[i][j] * v[i][j];
+    }
+    worker_sum<TPR, 1>(sum, s, turn);
+    turn ^= 1;
+    const float ry = 1.0f / sqrtf(sum[0] / (float)D + p.eps);
+    if (p.rstd_y && t == 0) p.rstd_y[row] = ry;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const int64_t c = (int64_t)(t + i * TPR) * 8;
+        if (c >= D) continue;
+        float w[8], o[8];
+        factors8<T>(p.wn, c, D, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = v[i][j] * ry * w[j];
+        store8((T*)p.u + row * p.ldu, c, D, o);
+    }
+    }
+}
+
+// Rows too wide for that: the two means of each row first, then a thread eight columns of kChunk rows.
+
+struct Terms { float gx[8], ny[8], nh[8], f[8], g[8], s[8], w[8], gu[8]; };
+template <typename T> __device__ __forceinline__ void terms8(const NormArgs& p, int64_t row, int64_t c, float ry, float rh, float c1, Terms& t) {
+    const int64_t D = p.width;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t.gx[j] = t.ny[j] = t.gu[j] = 0.0f;
+    if (p.gy) factors8<T>((const T*)p.gy + row * D, c, D, t.gx);
+    if (p.gu) {
+        float wn[8];
+        factors8<T>(p.wn, c, D, wn);
+        factors8<T>((const T*)p.y + row * p.ldx, c, D, t.ny);
+        factors8<T>((const T*)p.gu + row * p.ldg, c, D, t.gu);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            t.ny[j] *= ry;
+            t.gx[j] += ry * (t.gu[j] * wn[j] - t.ny[j] * c1);
+        }
+    }
+    if (p.h) {
+        drop8(p.drop, row, c, t.f);
+        factors8<T>(p.gate ? (const T*)p.gate + (int64_t)((uint32_t)row / (uint32_t)p.rows_per_gate) * D : nullptr, c, D, t.g);
+        factors8<T>(p.scale, c, D, t.s);
+        factors8<T>(p.w, c, D, t.w);
+        factors8<T>((const T*)p.h + row * D, c, D, t.nh);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t.nh[j] *= rh;
+    }
+}
+
+// The means of (gu w_next) n_y and of (d/dN(h)) w n_h.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_means_kernel(NormArgs p) {
     __shared__ float s[kThreads / 64];
     const int64_t D = p.width;
     for (int64_t row = blockIdx.x; row < p.N; row += gridDim.x) {
-    const float ry = p.gu ? p.rstd_y[row] : 0.0f, rh = p.h ? p.rstd_h[row] : 0.0f;
-    float c1 = 0.0f, c2 = 0.0f;
-    if (p.gu) {
-        for (int64_t c = threadIdx.x; c < D; c += kThreads)
-            c1 += to_f32(((const T*)p.gu)[row * p.ldg + c]) * load<T>(p.wn, c, 1.0f) * (to_f32(((const T*)p.y)[row * p.ldx + c]) * ry);
-        c1 = group_sum(c1, s) / (float)D;
-    }
-    if (p.h) {
-        for (int64_t c = threadIdx.x; c < D; c += kThreads) {
-            const Terms t = terms<T>(p, row, c, ry, rh, c1);
-            if (t.f != 0.0f) c2 += t.gx * t.s * t.g * t.f * load<T>(p.w, c, 1.0f) * t.nh;
+        const float ry = p.gu ? p.rstd_y[row] : 0.0f, rh = p.h ? p.rstd_h[row] : 0.0f;
+        float c1 = 0.0f, c2 = 0.0f;
+        if (p.gu) {
+            for (int64_t c = threadIdx.x * 8; c < D; c += kThreads * 8) {
+                float wn[8], y[8], gu[8];
+                factors8<T>(p.wn, c, D, wn);
+                factors8<T>((const T*)p.y + row * p.ldx, c, D, y);
+                factors8<T>((const T*)p.gu + row * p.ldg, c, D, gu);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < D) c1 += gu[j] * wn[j] * (y[j] * ry);
+            }
+            c1 = group_sum(c1, s) / (float)D;
         }
-        c2 = group_sum(c2, s) / (float)D;
-    }
-    if (threadIdx.x == 0) {
-        p.partial[row] = c1;
-        p.partial[p.N + row] = c2;
-    }
+        if (p.h) {
+            for (int64_t c = threadIdx.x * 8; c < D; c += kThreads * 8) {
+                Terms t;
+                terms8<T>(p, row, c, ry, rh, c1, t);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < D && t.f[j] != 0.0f) c2 += t.gx[j] * t.s[j] * t.g[j] * t.f[j] * t.w[j] * t.nh[j];
+            }
+            c2 = group_sum(c2, s) / (float)D;
+        }
+        if (threadIdx.x == 0) {
+            p.partial[row] = c1;
+            p.partial[p.N + row] = c2;
+        }
     }
 }
 
-// A thread a column: the rows' gradients, and the column sums of kChunk rows (of one gate row's where ggate is asked for).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormArgs p) {
-    const int64_t D = p.width, c = (int64_t)blockIdx.y * kThreads + threadIdx.x;
+    const int64_t D = p.width, c = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * 8;
     if (c >= D) return;
     const int64_t r0 = (int64_t)blockIdx.x * kChunk, r1 = r0 + kChunk < p.N ? r0 + kChunk : p.N;
-    float w = load<T>(p.w, c, 1.0f), sw = 0.0f, ss = 0.0f, sn = 0.0f;
+    float sw[8] = {}, ss[8] = {}, sn[8] = {};
     for (int64_t row = r0; row < r1; ++row) {
         const float ry = p.gu ? p.rstd_y[row] : 0.0f, rh = p.h ? p.rstd_h[row] : 0.0f;
         const float c1 = p.partial[row], c2 = p.partial[p.N + row];
-        const Terms t = terms<T>(p, row, c, ry, rh, c1);
-        if (p.gx) ((T*)p.gx)[row * D + c] = (T)t.gx;
-        if (p.gu) sn += to_f32(((const T*)p.gu)[row * p.ldg + c]) * t.ny;
+        Terms t;
+        terms8<T>(p, row, c, ry, rh, c1, t);
+        if (p.gx) store8((T*)p.gx + row * D, c, D, t.gx);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sn[j] += t.gu[j] * t.ny[j];
         if (p.h) {
-            const float gv = t.f == 0.0f ? 0.0f : t.gx * t.s * t.g * t.f;
-            ((T*)p.gh)[row * D + c] = (T)(rh * (gv * w - t.nh * c2));
-            sw += gv * t.nh;
-            if (t.f != 0.0f) ss += t.gx * t.g * t.f * (t.nh * w);
+            float gh[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float gv = t.f[j] == 0.0f ? 0.0f : t.gx[j] * t.s[j] * t.g[j] * t.f[j];
+                gh[j] = rh * (gv * t.w[j] - t.nh[j] * c2);
+                sw[j] += gv * t.nh[j];
+                if (t.f[j] != 0.0f) ss[j] += t.gx[j] * t.g[j] * t.f[j] * (t.nh[j] * t.w[j]);
+            }
+            store8((T*)p.gh + row * D, c, D, gh);
         }
     }
-    float* out = p.partial + 2 * p.N + (int64_t)blockIdx.x * 3 * D;
-    out[c] = sw;
-    out[D + c] = ss;
-    out[2 * D + c] = sn;
+    float* out = p.partial + 2 * p.N + (int64_t)blockIdx.x * 3 * D + c;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (c + j < D) {
+            out[j] = sw[j];
+            out[D + j] = ss[j];
+            out[2 * D + j] = sn[j];
+        }
+}
+
+// The gate's gradient: a thread eight columns of one gate row, over the rows that share it.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void gate_grad_kernel(NormArgs p) {
+    const int64_t D = p.width, c = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * 8;
+    if (c >= D) return;
+    const int64_t gates = (p.N + p.rows_per_gate - 1) / p.rows_per_gate;
+    for (int64_t k = blockIdx.x; k < gates; k += gridDim.x) {
+        const int64_t r0 = k * p.rows_per_gate, r1 = r0 + p.rows_per_gate < p.N ? r0 + p.rows_per_gate : p.N;
+        float v[8] = {};
+        for (int64_t row = r0; row < r1; ++row) {
+            Terms t;
+            terms8<T>(p, row, c, p.gu ? p.rstd_y[row] : 0.0f, p.rstd_h[row], p.partial[row], t);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (t.f[j] != 0.0f) v[j] += t.gx[j] * t.s[j] * t.f[j] * (t.nh[j] * t.w[j]);
+        }
+        store8((T*)p.ggate + k * D, c, D, v);
+    }
 }
 
 template <typename T>
@@ -146,63 +351,369 @@ __global__ __launch_bounds__(kThreads) void norm_sum_kernel(NormArgs p, int64_t 
     }
 }
 
-// The gate's gradient: a thread a column of one gate row, over the rows that share it.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void gate_grad_kernel(NormArgs p) {
-    const int64_t D = p.width, c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (c >= D) return;
-    const int64_t gates = (p.N + p.rows_per_gate - 1) / p.rows_per_gate;
-    for (int64_t k = blockIdx.y; k < gates; k += gridDim.y) {
-        const int64_t r0 = k * p.rows_per_gate, r1 = r0 + p.rows_per_gate < p.N ? r0 + p.rows_per_gate : p.N;
-        float v = 0.0f;
-        for (int64_t row = r0; row < r1; ++row) {
-            const Terms t = terms<T>(p, row, c, p.gu ? p.rstd_y[row] : 0.0f, p.rstd_h[row], p.partial[row]);
-            if (t.f != 0.0f) v += t.gx * t.s * t.f * (t.nh * load<T>(p.w, c, 1.0f));
+// How the backward pass divides the rows: worker k takes `rows` of them from first(k) on, all of one gate row where
+// parts > 1 (that gate row's gradient is then the sum of `parts` workers'), else of whole gate rows.
+struct Rows { int64_t rows, parts, workers; };
+
+// One pass over the rows: gx, gh, the gate's gradient, and each work-group's column sums (of w, scale, w_next).
+// With q = scale gate drop w n_h, the two means of a row need three sums and no second pass:
+//   c1 = mean(gu w_next n_y),  c2 = mean((gy + r_y gu w_next) q) - r_y c1 mean(n_y q)
+template <typename T, int TPR, int I, bool H>
+__global__ __launch_bounds__(group_of(TPR)) void norm_backward_rows(NormArgs p, Rows rw) {
+    constexpr int kGroup = group_of(TPR), kWorkers = kGroup / TPR, kSums = H ? 3 : 1;
+    __shared__ float s[2 * 3 * (TPR > 64 ? TPR / 64 : 1)];
+    __shared__ float cols[kWorkers > 1 ? kWorkers * TPR * I * 8 : 1];
+    const int64_t D = p.width, worker = (int64_t)blockIdx.x * kWorkers + threadIdx.x / TPR;
+    const int t = threadIdx.x % TPR;
+    int64_t r0, r1;
+    if (rw.parts > 1) {
+        const int64_t gate = worker / rw.parts, part = worker - gate * rw.parts;
+        r0 = gate * p.rows_per_gate + part * rw.rows;
+        r1 = r0 + rw.rows;
+        if (r1 > (gate + 1) * p.rows_per_gate) r1 = (gate + 1) * p.rows_per_gate;
+    } else {
+        r0 = worker * rw.rows;
+        r1 = r0 + rw.rows;
+    }
+    if (r1 > p.N) r1 = p.N;
+    if (worker >= rw.workers) r1 = r0;
+
+    float sw[H ? I : 1][8] = {}, ss[H ? I : 1][8] = {}, sg[H ? I : 1][8] = {}, sn[I][8] = {};
+    typedef typename Raw<T>::V V;
+    V gyr[I], gur[I], yr[I], hr[H ? I : 1], gr[H ? I : 1];
+    int64_t gate_row = r0 < r1 ? r0 / p.rows_per_gate : 0, gate_end = (gate_row + 1) * p.rows_per_gate;
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t c = (int64_t)(t + i * TPR) * 8;
+            if (p.gy) gyr[i] = load8((const T*)p.gy + row * D, c, D);
+            if (p.gu) {
+                gur[i] = load8((const T*)p.gu + row * p.ldg, c, D);
+                yr[i] = load8((const T*)p.y + row * p.ldx, c, D);
+            }
+            if constexpr (H) {
+                hr[i] = load8((const T*)p.h + row * D, c, D);
+                if (p.gate) gr[i] = load8((const T*)p.gate + gate_row * D, c, D);
+            }
         }
-        ((T*)p.ggate)[k * D + c] = (T)v;
+    };
+    if (r0 < r1) fetch(r0);
+    int turn = 0;
+    for (int64_t row = r0; row < r1; ++row, turn ^= 1) {
+        const float ry = p.gu ? p.rstd_y[row] : 0.0f, rh = H ? p.rstd_h[row] : 0.0f;
+        // per value: a = gy + r_y gu w_next, ny, and for the block's side q / w and n_h
+        float a[I][8], ny[I][8], b[H ? I : 1][8], nh[H ? I : 1][8];
+        uint32_t dropped[H ? I : 1];
+        float sum[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t c = (int64_t)(t + i * TPR) * 8;
+            if constexpr (H) dropped[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                a[i][j] = p.gy ? to_f32(gyr[i][j]) : 0.0f;
+                ny[i][j] = 0.0f;
+            }
+            if (p.gu) {
+                float wn[8];
+                factors8<T>(p.wn, c, D, wn);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float gu = to_f32(gur[i][j]), gw = gu * wn[j];
+                    ny[i][j] = to_f32(yr[i][j]) * ry;
+                    sum[0] += gw * ny[i][j];
+                    sn[i][j] += gu * ny[i][j];
+                    a[i][j] += ry * gw;
+                }
+            }
+            if constexpr (H) {
+                float f[8], sc[8], w[8];
+                drop8(p.drop, row, c, f);
+                factors8<T>(p.scale, c, D, sc);
+                factors8<T>(p.w, c, D, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float g = p.gate ? to_f32(gr[i][j]) : 1.0f;
+                    nh[i][j] = to_f32(hr[i][j]) * rh;
+                    b[i][j] = sc[j] * g * f[j];
+                    if (f[j] == 0.0f) dropped[i] |= 1u << j;
+                    const float q = f[j] == 0.0f ? 0.0f : b[i][j] * w[j] * nh[i][j];
+                    sum[1] += a[i][j] * q;
+                    sum[2] += ny[i][j] * q;
+                }
+            }
+        }
+        V gate_now[H ? I : 1];
+        if constexpr (H) {
+#pragma unroll
+            for (int i = 0; i < I; ++i) gate_now[i] = gr[i];
+        }
+        const bool last = row + 1 == r1 || row + 1 == gate_end;   // of this gate row, or of this worker
+        const int64_t gate_at = gate_row;
+        if (row + 1 < r1) {
+            if (row + 1 == gate_end) { ++gate_row; gate_end += p.rows_per_gate; }
+            fetch(row + 1);
+        }
+        if constexpr (H) {
+            worker_sum<TPR, 3>(sum, s, turn);
+        } else {
+            float one[1] = {sum[0]};
+            worker_sum<TPR, 1>(one, s, turn);
+            sum[0] = one[0];
+        }
+        const float c1 = sum[0] / (float)D, c2 = (sum[1] - ry * c1 * sum[2]) / (float)D;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t c = (int64_t)(t + i * TPR) * 8;
+            if (c >= D) continue;
+            float gx[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) gx[j] = a[i][j] - ry * ny[i][j] * c1;
+            if (p.gx) store8((T*)p.gx + row * D, c, D, gx);
+            if constexpr (H) {
+                float gh[8], sc[8], w[8];
+                factors8<T>(p.scale, c, D, sc);
+                factors8<T>(p.w, c, D, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool off = dropped[i] >> j & 1;
+                    const float f = off ? 0.0f : p.drop.threshold ? p.drop.scale : 1.0f;
+                    const float g = p.gate ? to_f32(gate_now[i][j]) : 1.0f;
+                    const float gv = off ? 0.0f : gx[j] * b[i][j], v = off ? 0.0f : gx[j] * f * (nh[i][j] * w[j]);
+                    gh[j] = rh * (gv * w[j] - nh[i][j] * c2);
+                    sw[i][j] += gv * nh[i][j];
+                    ss[i][j] += v * g;
+                    sg[i][j] += v * sc[j];
+                }
+                store8((T*)p.gh + row * D, c, D, gh);
+                if (p.ggate && last) {
+                    if (rw.parts > 1) {
+                        float* to = p.partial + worker * D;   // gate rows' parts come first
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (c + j < D) to[c + j] = sg[i][j];
+                    } else {
+                        store8((T*)p.ggate + gate_at * D, c, D, sg[i]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sg[i][j] = 0.0f;
+                }
+            }
+        }
+    }
+
+    // column sums of the work-group
+    const int64_t gates_at = H && rw.parts > 1 ? rw.workers * D : 0;
+    float* out = p.partial + gates_at + (int64_t)blockIdx.x * kSums * D;
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        if constexpr (kWorkers > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    cols[(threadIdx.x / TPR) * (TPR * I * 8) + (t + i * TPR) * 8 + j] = k == kSums - 1 ? sn[i][j] : k == 0 ? sw[H ? i : 0][j] : ss[H ? i : 0][j];
+            __syncthreads();
+            for (int c = threadIdx.x; c < D; c += kGroup) {
+                float v = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWorkers; ++w) v += cols[w * (TPR * I * 8) + c];
+                out[k * D + c] = v;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                const int64_t c = (int64_t)(t + i * TPR) * 8;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < D) out[k * D + c + j] = k == kSums - 1 ? sn[i][j] : k == 0 ? sw[H ? i : 0][j] : ss[H ? i : 0][j];
+            }
+        }
     }
 }
 
+// The work-groups' column sums added up, 64 columns a work-group, sixteen strands of rows; then, by the work-groups
+// after those, the parts of each gate row.  Every sum is taken in a fixed order.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs p, Rows rw, int64_t groups, int sums) {
+    const int64_t D = p.width, blocks = (D + 63) / 64, c = (int64_t)(blockIdx.x % blocks) * 64 + (threadIdx.x & 63);
+    const int strand = threadIdx.x >> 6;
+    const int64_t job = blockIdx.x / blocks;
+    const bool gates = job >= sums;
+    const float* from;
+    int64_t n;
+    const bool split = sums == 3 && rw.parts > 1;
+    if (gates) {
+        const int64_t gate = job - sums;
+        from = p.partial + gate * rw.parts * D + c;
+        // the last gate row may have fewer rows: the workers beyond them wrote nothing
+        const int64_t left = (p.N - gate * p.rows_per_gate + rw.rows - 1) / rw.rows;
+        n = left < rw.parts ? left : rw.parts;
+    } else {
+        from = p.partial + (split ? rw.workers * D : 0) + job * D + c;
+        n = groups;
+    }
+    const int64_t step = gates ? D : sums * D;
+    float v = 0.0f;
+    if (c < D)
+        for (int64_t i = strand; i < n; i += 16) v += from[i * step];
+    __shared__ float s[16][64];
+    s[strand][threadIdx.x & 63] = v;
+    __syncthreads();
+    if (strand || c >= D) return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k) v += s[k][threadIdx.x];
+    if (gates) {
+        ((T*)p.ggate)[(job - sums) * D + c] = (T)v;
+    } else {
+        void* to = job == sums - 1 ? p.gwn : job == 0 ? p.gw : p.gscale;
+        if (to) ((T*)to)[c] = (T)v;
+    }
+}
+
+// Threads a row and turns for a width; none above what registers hold.  The backward pass of a block's side carries
+// four column sums and ten values a column and takes one turn (190 registers); the others take two.
+enum Pass { kForward, kBackward, kBackwardBlock };
+struct Shape { int tpr, turns; };
+inline Shape shape_of(int64_t width, Pass pass) {
+    const int64_t chunks = (width + 7) / 8;
+    for (int t : {8, 16, 32, 64})
+        if (chunks <= t) return {t, 1};
+    if (pass == kBackwardBlock) {
+        for (int t : {128, 256, 512})
+            if (chunks <= t) return {t, 1};
+        return {0, 0};
+    }
+    if (chunks <= 128) return {64, 2};
+    if (chunks <= 256) return {256, 1};
+    for (int t : {256, 512, 1024})
+        if (chunks <= 2 * t) return {t, 2};
+    return {0, 0};
+}
+
+inline Rows rows_of(const Shape& sh, int64_t N, int64_t rows_per_gate) {
+    const int64_t want = 512 * 256 / sh.tpr;   // eight waves a compute unit
+    int64_t r = (N + want - 1) / want;
+    if (r < 4) r = 4;
+    Rows out;
+    if (rows_per_gate > r) {
+        out.parts = (rows_per_gate + r - 1) / r;
+        out.rows = (rows_per_gate + out.parts - 1) / out.parts;
+        out.workers = (N + rows_per_gate - 1) / rows_per_gate * out.parts;
+    } else {
+        out.parts = 1;
+        out.rows = r / rows_per_gate * rows_per_gate;
+        out.workers = (N + out.rows - 1) / out.rows;
+    }
+    return out;
+}
+
+inline int64_t groups_for(const Rows& r, const Shape& sh) {
+    const int64_t per = group_of(sh.tpr) / sh.tpr;
+    return (r.workers + per - 1) / per;
+}
+
+// A thread a block of eight columns (one call of the generator) and turn; the row and block of its next turn follow
+// from the last one's without a division.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(const T* x, int64_t ldx, T* y, int64_t ldy, int64_t N, int64_t width,
-                                                           DropArgs d) {
-    const int64_t blocks = (width + 7) / 8, total = N * blocks;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t row = i / blocks, b = i - row * blocks;
+                                                           DropArgs d, int64_t step_rows, int64_t step_blocks) {
+    const int64_t blocks = (width + 7) / 8;
+    const int64_t first = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    int64_t row = first / blocks, b = first - row * blocks;
+    while (row < N) {
+        const typename Raw<T>::V v = load8(x + row * ldx, b * 8, width);
         const Words q = philox((uint32_t)b, (uint32_t)row, d.offset, d.seed);
-        for (int j = 0; j < 8 && b * 8 + j < width; ++j) {
-            const float v = to_f32(x[row * ldx + b * 8 + j]);
-            y[row * ldy + b * 8 + j] = (T)(kept(q, j, d.threshold) ? v * d.scale : 0.0f);
-        }
+        float o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = kept(q, j, d.threshold) ? to_f32(v[j]) * d.scale : 0.0f;
+        store8(y + row * ldy, b * 8, width, o);
+        row += step_rows;
+        b += step_blocks;
+        if (b >= blocks) { b -= blocks; ++row; }
     }
 }
 
 inline unsigned row_groups(int64_t N) { return (unsigned)(N < (1 << 20) ? N : 1 << 20); }
 
+#define FFN_SHAPES(RUN)                                  \
+    switch (sh.tpr * 8 + sh.turns) {                     \
+        case 8 * 8 + 1: RUN(8, 1); break;                \
+        case 16 * 8 + 1: RUN(16, 1); break;              \
+        case 32 * 8 + 1: RUN(32, 1); break;              \
+        case 64 * 8 + 1: RUN(64, 1); break;              \
+        case 64 * 8 + 2: RUN(64, 2); break;              \
+        case 256 * 8 + 1: RUN(256, 1); break;            \
+        case 256 * 8 + 2: RUN(256, 2); break;            \
+        case 512 * 8 + 2: RUN(512, 2); break;            \
+        default: RUN(1024, 2); break;                    \
+    }
+
 template <typename T> int forward(const NormArgs& a, hipStream_t s) {
-    norm_forward_kernel<T><<<dim3(row_groups(a.N)), kThreads, 0, s>>>(a);
+    const Shape sh = shape_of(a.width, kForward);
+    if (sh.tpr == 0) {
+        norm_forward_kernel<T><<<dim3(row_groups(a.N)), kThreads, 0, s>>>(a);
+        return (int)hipGetLastError();
+    }
+#define FFN_FORWARD(TPR, I) \
+    norm_forward_rows<T, TPR, I><<<dim3(row_groups((a.N + group_of(TPR) / TPR - 1) / (group_of(TPR) / TPR))), group_of(TPR), 0, s>>>(a)
+    FFN_SHAPES(FFN_FORWARD)
+#undef FFN_FORWARD
     return (int)hipGetLastError();
 }
 
 template <typename T> int backward(const NormArgs& a, hipStream_t s) {
-    const int64_t chunks = (a.N + kChunk - 1) / kChunk;
-    const unsigned cols = (unsigned)((a.width + kThreads - 1) / kThreads);
-    if (a.N > 0) {
-        norm_means_kernel<T><<<dim3(row_groups(a.N)), kThreads, 0, s>>>(a);
-        if (a.ggate) {
-            const int64_t gates = (a.N + a.rows_per_gate - 1) / a.rows_per_gate;
-            gate_grad_kernel<T><<<dim3(cols, (unsigned)(gates < 65535 ? gates : 65535)), kThreads, 0, s>>>(a);
+    const bool block = a.h != nullptr;
+    const Shape sh = shape_of(a.width, block ? kBackwardBlock : kBackward);
+    if (sh.tpr == 0) {
+        const int64_t chunks = (a.N + kChunk - 1) / kChunk;
+        const unsigned cols = (unsigned)((a.width + 8 * kThreads - 1) / (8 * kThreads));
+        if (a.N > 0) {
+            norm_means_kernel<T><<<dim3(row_groups(a.N)), kThreads, 0, s>>>(a);
+            if (a.ggate) {
+                const int64_t gates = (a.N + a.rows_per_gate - 1) / a.rows_per_gate;
+                gate_grad_kernel<T><<<dim3(row_groups(gates), cols), kThreads, 0, s>>>(a);
+            }
+            norm_grad_kernel<T><<<dim3((unsigned)chunks, cols), kThreads, 0, s>>>(a);
         }
-        norm_grad_kernel<T><<<dim3((unsigned)chunks, cols), kThreads, 0, s>>>(a);
+        norm_sum_kernel<T><<<dim3((unsigned)((a.width + kThreads - 1) / kThreads)), kThreads, 0, s>>>(a, chunks);
+        return (int)hipGetLastError();
     }
-    norm_sum_kernel<T><<<dim3(cols), kThreads, 0, s>>>(a, chunks);
+    const Rows rw = rows_of(sh, a.N, block ? a.rows_per_gate : 1);
+    const int64_t groups = groups_for(rw, sh);
+    if (groups > 0 && block) {
+#define FFN_BLOCK(TPR) norm_backward_rows<T, TPR, 1, true><<<dim3((unsigned)groups), group_of(TPR), 0, s>>>(a, rw)
+        switch (sh.tpr) {
+            case 8: FFN_BLOCK(8); break;
+            case 16: FFN_BLOCK(16); break;
+            case 32: FFN_BLOCK(32); break;
+            case 64: FFN_BLOCK(64); break;
+            case 128: FFN_BLOCK(128); break;
+            case 256: FFN_BLOCK(256); break;
+            default: FFN_BLOCK(512); break;
+        }
+#undef FFN_BLOCK
+    } else if (groups > 0) {
+#define FFN_BACKWARD(TPR, I) norm_backward_rows<T, TPR, I, false><<<dim3((unsigned)groups), group_of(TPR), 0, s>>>(a, rw)
+        FFN_SHAPES(FFN_BACKWARD)
+#undef FFN_BACKWARD
+    }
+    if (a.gw || a.gscale || a.gwn || (a.ggate && rw.parts > 1)) {
+        const int sums = block ? 3 : 1;
+        const int64_t jobs = sums + (a.ggate && rw.parts > 1 ? (a.N + a.rows_per_gate - 1) / a.rows_per_gate : 0);
+        norm_join_kernel<T><<<dim3((unsigned)(jobs * ((a.width + 63) / 64))), 1024, 0, s>>>(a, rw, groups, sums);
+    }
     return (int)hipGetLastError();
 }
 
 }  // namespace
 
-int64_t norm_workspace_floats(int64_t width, int64_t N, int64_t, bool) {
-    return 2 * N + (N + kChunk - 1) / kChunk * 3 * width;
+int64_t norm_workspace_floats(int64_t width, int64_t N, int64_t rows_per_gate, bool residual) {
+    const Shape sh = shape_of(width, residual ? kBackwardBlock : kBackward);
+    if (sh.tpr == 0) return 2 * N + (N + kChunk - 1) / kChunk * 3 * width;
+    const Rows rw = rows_of(sh, N, residual ? rows_per_gate : 1);
+    return (residual && rw.parts > 1 ? rw.workers * width : 0) + groups_for(rw, sh) * (residual ? 3 : 1) * width;
 }
 
 int launch_norm_forward(const NormArgs& a, int32_t dtype, void* stream) {
@@ -218,11 +729,12 @@ int launch_norm_backward(const NormArgs& a, int32_t dtype, void* stream) {
 int launch_dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t N, int64_t width, int32_t dtype,
                    const DropArgs& d, void* stream) {
     hipStream_t s = (hipStream_t)stream;
-    const int64_t groups = (N * ((width + 7) / 8) + kThreads - 1) / kThreads;
-    const dim3 grid((unsigned)(groups < 65536 ? groups : 65536));
-    if (dtype == FFN_FP32) dropout_kernel<float><<<grid, kThreads, 0, s>>>((const float*)x, ldx, (float*)y, ldy, N, width, d);
-    else if (dtype == FFN_BF16) dropout_kernel<bf16><<<grid, kThreads, 0, s>>>((const bf16*)x, ldx, (bf16*)y, ldy, N, width, d);
-    else dropout_kernel<fp16><<<grid, kThreads, 0, s>>>((const fp16*)x, ldx, (fp16*)y, ldy, N, width, d);
+    const int64_t blocks = (width + 7) / 8, groups = (N * blocks + kThreads - 1) / kThreads;
+    const dim3 grid((unsigned)(groups < 4096 ? groups : 4096));
+    const int64_t stride = (int64_t)grid.x * kThreads, dr = stride / blocks, db = stride % blocks;
+    if (dtype == FFN_FP32) dropout_kernel<float><<<grid, kThreads, 0, s>>>((const float*)x, ldx, (float*)y, ldy, N, width, d, dr, db);
+    else if (dtype == FFN_BF16) dropout_kernel<bf16><<<grid, kThreads, 0, s>>>((const bf16*)x, ldx, (bf16*)y, ldy, N, width, d, dr, db);
+    else dropout_kernel<fp16><<<grid, kThreads, 0, s>>>((const fp16*)x, ldx, (fp16*)y, ldy, N, width, d, dr, db);
     return (int)hipGetLastError();
 }
 

@@ -86,7 +86,7 @@ int check_norm(const ffn_norm* n, int64_t N, ffn::NormArgs* a) {
     if (n->width > FFN_MAX_WIDTH || N > FFN_MAX_ROWS) return CGTP_EUNSUP;
     a->width = n->width;
     a->N = N;
-    a->rows_per_gate = n->rows_per_gate;
+    a->rows_per_gate = n->rows_per_gate < FFN_MAX_ROWS ? n->rows_per_gate : FFN_MAX_ROWS;   // (32 bits)
     a->eps = n->eps;
     return CGTP_OK;
 }
