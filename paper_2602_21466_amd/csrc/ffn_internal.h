@@ -72,11 +72,16 @@ struct NormArgs {
     float* partial;       // workspace
 };
 
-int launch_norm_forward(const NormArgs& a, int32_t dtype, void* stream);
-int launch_norm_backward(const NormArgs& a, int32_t dtype, void* stream);
 int64_t norm_workspace_floats(int64_t width, int64_t N, int64_t rows_per_gate, bool residual);
 
-int launch_dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t N, int64_t width, int32_t dtype,
-                   const DropArgs& d, void* stream);
+#define FFN_NORM_LAUNCHERS(TYPE)                                                                                     \
+    int launch_norm_forward_##TYPE(const NormArgs& a, void* stream);                                                 \
+    int launch_norm_backward_##TYPE(const NormArgs& a, void* stream);                                                \
+    int launch_dropout_##TYPE(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t N, int64_t width,            \
+                              const DropArgs& d, void* stream);
+FFN_NORM_LAUNCHERS(fp32)
+FFN_NORM_LAUNCHERS(bf16)
+FFN_NORM_LAUNCHERS(fp16)
+#undef FFN_NORM_LAUNCHERS
 
 }  // namespace ffn

@@ -1,4 +1,7 @@
-// Norms before and after a block with its gate and residual scale, and dropout.
+// Kernels of the norms before and after a block with its gate and residual scale, and of dropout.  Internal;
+// instantiated once per array type (ffn_norm_*.hip).
+#pragma once
+
 #include "ffn_device.h"
 
 namespace ffn {
@@ -139,79 +142,147 @@ template <int TPR, int K> __device__ __forceinline__ void worker_sum(float (&v)[
     }
 }
 
+// Values c .. c + 7 of a row of D >= 8 (zeros beyond it).  TAIL: D is no multiple of 8; the last thread reads the
+// row's last eight values and moves them down, so that no lane reads beside the row and no load is by single values.
+template <typename T, bool TAIL> __device__ __forceinline__ typename Raw<T>::V row8(const T* row, int c, int D) {
+    typename Raw<T>::V v = {};
+    if (c < D) {
+        const int at = TAIL && c > D - 8 ? D - 8 : c;
+        __builtin_memcpy(&v, row + at, sizeof(v));
+        if constexpr (TAIL) {
+            const int by = c - at;
+            if (by) {
+                constexpr int W = sizeof(v) / 4;
+                typedef uint32_t U __attribute__((ext_vector_type(W)));
+                U u = __builtin_bit_cast(U, v);
+#pragma unroll
+                for (int b = 4; b; b >>= 1) {
+                    const bool move = by & b;
+                    const int words = b * (int)sizeof(T) / 4;
+#pragma unroll
+                    for (int k = 0; k < W; ++k) {
+                        const uint32_t next = words ? (k + words < W ? u[k + words < W ? k + words : 0] : 0u)
+                                                    : (u[k] >> 16 | (k + 1 < W ? u[k + 1 < W ? k + 1 : 0] << 16 : 0u));
+                        u[k] = move ? next : u[k];
+                    }
+                }
+                v = __builtin_bit_cast(typename Raw<T>::V, u);
+            }
+        }
+    }
+    return v;
+}
+template <typename T, bool TAIL> __device__ __forceinline__ void put8(T* row, int c, int D, const float (&f)[8]) {
+    if (!TAIL || c + 8 <= D) {
+        typename Raw<T>::V v;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (T)f[j];
+        __builtin_memcpy(row + c, &v, sizeof(v));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < D) row[c + j] = (T)f[j];
+    }
+}
+// A row of factors, ones where there is none.
+template <typename T, bool TAIL> __device__ __forceinline__ typename Raw<T>::V ones8(const void* p, int c, int D) {
+    if (p) return row8<T, TAIL>((const T*)p, c, D);
+    typename Raw<T>::V v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (T)1.0f;
+    return v;
+}
+
 constexpr int group_of(int tpr) { return tpr > 64 ? tpr : 256; }
 
-template <typename T, int TPR, int I>
+// BLOCK: y = x + scale gate drop(N(h; w)) first.  A worker walks its rows with the next one's loads in flight, the
+// factors shared by all rows in registers.
+template <typename T, int TPR, int I, bool TAIL, bool BLOCK>
 __global__ __launch_bounds__(group_of(TPR)) void norm_forward_rows(NormArgs p) {
     __shared__ float s[2 * (TPR > 64 ? TPR / 64 : 1)];
-    constexpr int kWorkers = group_of(TPR) / TPR;
-    const int64_t D = p.width;
-    const int t = threadIdx.x % TPR;
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * kWorkers + threadIdx.x / TPR; row < p.N; row += (int64_t)gridDim.x * kWorkers) {
-    typename Raw<T>::V xr[I], hr[I];
+    constexpr int kWorkers = group_of(TPR) / TPR, B = BLOCK ? I : 1;
+    typedef typename Raw<T>::V V;
+    const int D = (int)p.width, t = threadIdx.x % TPR;
+    const int64_t step = (int64_t)gridDim.x * kWorkers;
+    int64_t row = (int64_t)blockIdx.x * kWorkers + threadIdx.x / TPR;
+    if (row >= p.N) return;
+    V wn[I], w[B], sc[B], xr[I], hr[B], gr[B];
+    auto fetch = [&](int64_t r) {
+        const T* gate = BLOCK && p.gate ? (const T*)p.gate + (int64_t)((uint32_t)r / (uint32_t)p.rows_per_gate) * D : nullptr;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int c = (t + i * TPR) * 8;
+            xr[i] = row8<T, TAIL>((const T*)p.x + r * p.ldx, c, D);
+            if constexpr (BLOCK) {
+                hr[i] = row8<T, TAIL>((const T*)p.h + r * D, c, D);
+                gr[i] = ones8<T, TAIL>(gate, c, D);
+            }
+        }
+    };
+    fetch(row);
 #pragma unroll
     for (int i = 0; i < I; ++i) {
-        const int64_t c = (int64_t)(t + i * TPR) * 8;
-        xr[i] = load8((const T*)p.x + row * p.ldx, c, D);
-        if (p.h) hr[i] = load8((const T*)p.h + row * D, c, D);
+        const int c = (t + i * TPR) * 8;
+        wn[i] = ones8<T, TAIL>(p.wn, c, D);
+        if constexpr (BLOCK) {
+            w[i] = ones8<T, TAIL>(p.w, c, D);
+            sc[i] = ones8<T, TAIL>(p.scale, c, D);
+        }
     }
-    float v[I][8];
+    for (int turn = 0; row < p.N; row += step) {
+        float v[I][8];
+        V h[B], g[B];
 #pragma unroll
-    for (int i = 0; i < I; ++i)
+        for (int i = 0; i < I; ++i) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = to_f32(xr[i][j]);
-    if (p.h) {
+            for (int j = 0; j < 8; ++j) v[i][j] = to_f32(xr[i][j]);
+            if constexpr (BLOCK) {
+                h[i] = hr[i];
+                g[i] = gr[i];
+            }
+        }
+        if (row + step < p.N) fetch(row + step);
+        if constexpr (BLOCK) {
+            float sum[1] = {0.0f};
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[0] += to_f32(h[i][j]) * to_f32(h[i][j]);
+            worker_sum<TPR, 1>(sum, s, turn);
+            turn ^= 1;
+            const float rh = 1.0f / sqrtf(sum[0] / (float)D + p.eps);
+            if (p.rstd_h && t == 0) p.rstd_h[row] = rh;
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                const int c = (t + i * TPR) * 8;
+                float f[8];
+                drop8(p.drop, row, c, f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float n = to_f32(h[i][j]) * rh * to_f32(w[i][j]);
+                    v[i][j] += to_f32(sc[i][j]) * to_f32(g[i][j]) * (f[j] == 0.0f ? 0.0f : n * f[j]);
+                }
+                if (c < D) put8<T, TAIL>((T*)p.y + row * D, c, D, v[i]);
+            }
+        }
+        if (BLOCK && !p.u) continue;
         float sum[1] = {0.0f};
 #pragma unroll
         for (int i = 0; i < I; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[0] += to_f32(hr[i][j]) * to_f32(hr[i][j]);
+            for (int j = 0; j < 8; ++j) sum[0] += (t + i * TPR) * 8 + j < D ? v[i][j] * v[i][j] : 0.0f;
         worker_sum<TPR, 1>(sum, s, turn);
         turn ^= 1;
-        const float rh = 1.0f / sqrtf(sum[0] / (float)D + p.eps);
-        if (p.rstd_h && t == 0) p.rstd_h[row] = rh;
-        const T* gate = p.gate ? (const T*)p.gate + (int64_t)((uint32_t)row / (uint32_t)p.rows_per_gate) * D : nullptr;
+        const float ry = 1.0f / sqrtf(sum[0] / (float)D + p.eps);
+        if (p.rstd_y && t == 0) p.rstd_y[row] = ry;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int64_t c = (int64_t)(t + i * TPR) * 8;
-            if (c >= D) continue;
-            float f[8], g[8], w[8], sc[8];
-            drop8(p.drop, row, c, f);
-            factors8<T>(p.w, c, D, w);
-            factors8<T>(gate, c, D, g);
-            factors8<T>(p.scale, c, D, sc);
+            const int c = (t + i * TPR) * 8;
+            float o[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float n = to_f32(hr[i][j]) * rh * w[j];
-                v[i][j] += sc[j] * g[j] * (f[j] == 0.0f ? 0.0f : n * f[j]);
-            }
-            if (p.y) store8((T*)p.y + row * D, c, D, v[i]);
+            for (int j = 0; j < 8; ++j) o[j] = v[i][j] * ry * to_f32(wn[i][j]);
+            if (c < D) put8<T, TAIL>((T*)p.u + row * p.ldu, c, D, o);
         }
-    }
-    if (!p.u) continue;
-    float sum[1] = {0.0f};
-#pragma unroll
-    for (int i = 0; i < I; ++i) {
-        const int64_t c = (int64_t)(t + i * TPR) * 8;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (c + j < D) sum[0] += v[i][j] * v[i][j];
-    }
-    worker_sum<TPR, 1>(sum, s, turn);
-    turn ^= 1;
-    const float ry = 1.0f / sqrtf(sum[0] / (float)D + p.eps);
-    if (p.rstd_y && t == 0) p.rstd_y[row] = ry;
-#pragma unroll
-    for (int i = 0; i < I; ++i) {
-        const int64_t c = (int64_t)(t + i * TPR) * 8;
-        if (c >= D) continue;
-        float w[8], o[8];
-        factors8<T>(p.wn, c, D, w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = v[i][j] * ry * w[j];
-        store8((T*)p.u + row * p.ldu, c, D, o);
-    }
     }
 }
 
@@ -358,95 +429,90 @@ struct Rows { int64_t rows, parts, workers; };
 // One pass over the rows: gx, gh, the gate's gradient, and each work-group's column sums (of w, scale, w_next).
 // With q = scale gate drop w n_h, the two means of a row need three sums and no second pass:
 //   c1 = mean(gu w_next n_y),  c2 = mean((gy + r_y gu w_next) q) - r_y c1 mean(n_y q)
-template <typename T, int TPR, int I, bool H>
+template <typename T, int TPR, int I, bool TAIL, bool H>
 __global__ __launch_bounds__(group_of(TPR)) void norm_backward_rows(NormArgs p, Rows rw) {
-    constexpr int kGroup = group_of(TPR), kWorkers = kGroup / TPR, kSums = H ? 3 : 1;
+    constexpr int kGroup = group_of(TPR), kWorkers = kGroup / TPR, kSums = H ? 3 : 1, B = H ? I : 1;
     __shared__ float s[2 * 3 * (TPR > 64 ? TPR / 64 : 1)];
     __shared__ float cols[kWorkers > 1 ? kWorkers * TPR * I * 8 : 1];
-    const int64_t D = p.width, worker = (int64_t)blockIdx.x * kWorkers + threadIdx.x / TPR;
-    const int t = threadIdx.x % TPR;
-    int64_t r0, r1;
+    typedef typename Raw<T>::V V;
+    const int D = (int)p.width, t = threadIdx.x % TPR;
+    const int64_t worker = (int64_t)blockIdx.x * kWorkers + threadIdx.x / TPR;
+    int64_t r0, r1, gate_row = 0;
     if (rw.parts > 1) {
-        const int64_t gate = worker / rw.parts, part = worker - gate * rw.parts;
-        r0 = gate * p.rows_per_gate + part * rw.rows;
+        gate_row = worker / rw.parts;
+        r0 = gate_row * p.rows_per_gate + (worker - gate_row * rw.parts) * rw.rows;
         r1 = r0 + rw.rows;
-        if (r1 > (gate + 1) * p.rows_per_gate) r1 = (gate + 1) * p.rows_per_gate;
+        if (r1 > (gate_row + 1) * p.rows_per_gate) r1 = (gate_row + 1) * p.rows_per_gate;
     } else {
         r0 = worker * rw.rows;
         r1 = r0 + rw.rows;
+        gate_row = r0 / p.rows_per_gate;
     }
     if (r1 > p.N) r1 = p.N;
     if (worker >= rw.workers) r1 = r0;
+    int64_t gate_end = (gate_row + 1) * p.rows_per_gate;
 
-    float sw[H ? I : 1][8] = {}, ss[H ? I : 1][8] = {}, sg[H ? I : 1][8] = {}, sn[I][8] = {};
-    typedef typename Raw<T>::V V;
-    V gyr[I], gur[I], yr[I], hr[H ? I : 1], gr[H ? I : 1];
-    int64_t gate_row = r0 < r1 ? r0 / p.rows_per_gate : 0, gate_end = (gate_row + 1) * p.rows_per_gate;
+    float sw[B][8] = {}, ss[B][8] = {}, sg[B][8] = {}, sn[I][8] = {};
+    V gyr[I], gur[I], yr[I], hr[B], gr[B], wn[I], w[B], sc[B];
+    float ryr = 0.0f, rhr = 0.0f;
+#pragma unroll
+    for (int i = 0; i < I; ++i) gyr[i] = gur[i] = yr[i] = V{};
     auto fetch = [&](int64_t row) {
+        const T* gate = H && p.gate ? (const T*)p.gate + gate_row * D : nullptr;
+        if (p.gu) ryr = p.rstd_y[row];
+        if constexpr (H) rhr = p.rstd_h[row];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int64_t c = (int64_t)(t + i * TPR) * 8;
-            if (p.gy) gyr[i] = load8((const T*)p.gy + row * D, c, D);
+            const int c = (t + i * TPR) * 8;
+            if (p.gy) gyr[i] = row8<T, TAIL>((const T*)p.gy + row * D, c, D);
             if (p.gu) {
-                gur[i] = load8((const T*)p.gu + row * p.ldg, c, D);
-                yr[i] = load8((const T*)p.y + row * p.ldx, c, D);
+                gur[i] = row8<T, TAIL>((const T*)p.gu + row * p.ldg, c, D);
+                yr[i] = row8<T, TAIL>((const T*)p.y + row * p.ldx, c, D);
             }
             if constexpr (H) {
-                hr[i] = load8((const T*)p.h + row * D, c, D);
-                if (p.gate) gr[i] = load8((const T*)p.gate + gate_row * D, c, D);
+                hr[i] = row8<T, TAIL>((const T*)p.h + row * D, c, D);
+                gr[i] = ones8<T, TAIL>(gate, c, D);
             }
         }
     };
     if (r0 < r1) fetch(r0);
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const int c = (t + i * TPR) * 8;
+        wn[i] = ones8<T, TAIL>(p.wn, c, D);
+        if constexpr (H) {
+            w[i] = ones8<T, TAIL>(p.w, c, D);
+            sc[i] = ones8<T, TAIL>(p.scale, c, D);
+        }
+    }
     int turn = 0;
     for (int64_t row = r0; row < r1; ++row, turn ^= 1) {
-        const float ry = p.gu ? p.rstd_y[row] : 0.0f, rh = H ? p.rstd_h[row] : 0.0f;
-        // per value: a = gy + r_y gu w_next, ny, and for the block's side q / w and n_h
-        float a[I][8], ny[I][8], b[H ? I : 1][8], nh[H ? I : 1][8];
-        uint32_t dropped[H ? I : 1];
+        // per value: a = gy + r_y gu w_next, n_y, and for the block's side n_h and the dropout's factor
+        const float ry = ryr, rh = rhr;
+        float a[I][8], ny[I][8], nh[B][8], f[B][8];
+        V g[B];
         float sum[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int64_t c = (int64_t)(t + i * TPR) * 8;
-            if constexpr (H) dropped[i] = 0;
+            const int c = (t + i * TPR) * 8;
+            if constexpr (H) {
+                g[i] = gr[i];
+                drop8(p.drop, row, c, f[i]);
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                a[i][j] = p.gy ? to_f32(gyr[i][j]) : 0.0f;
-                ny[i][j] = 0.0f;
-            }
-            if (p.gu) {
-                float wn[8];
-                factors8<T>(p.wn, c, D, wn);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float gu = to_f32(gur[i][j]), gw = gu * wn[j];
-                    ny[i][j] = to_f32(yr[i][j]) * ry;
-                    sum[0] += gw * ny[i][j];
-                    sn[i][j] += gu * ny[i][j];
-                    a[i][j] += ry * gw;
-                }
-            }
-            if constexpr (H) {
-                float f[8], sc[8], w[8];
-                drop8(p.drop, row, c, f);
-                factors8<T>(p.scale, c, D, sc);
-                factors8<T>(p.w, c, D, w);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float g = p.gate ? to_f32(gr[i][j]) : 1.0f;
+                const float gu = to_f32(gur[i][j]), gw = gu * to_f32(wn[i][j]);
+                ny[i][j] = to_f32(yr[i][j]) * ry;
+                sum[0] += gw * ny[i][j];
+                sn[i][j] += gu * ny[i][j];
+                a[i][j] = to_f32(gyr[i][j]) + ry * gw;
+                if constexpr (H) {
                     nh[i][j] = to_f32(hr[i][j]) * rh;
-                    b[i][j] = sc[j] * g * f[j];
-                    if (f[j] == 0.0f) dropped[i] |= 1u << j;
-                    const float q = f[j] == 0.0f ? 0.0f : b[i][j] * w[j] * nh[i][j];
+                    const float q = f[i][j] == 0.0f ? 0.0f : to_f32(sc[i][j]) * to_f32(g[i][j]) * f[i][j] * to_f32(w[i][j]) * nh[i][j];
                     sum[1] += a[i][j] * q;
                     sum[2] += ny[i][j] * q;
                 }
             }
-        }
-        V gate_now[H ? I : 1];
-        if constexpr (H) {
-#pragma unroll
-            for (int i = 0; i < I; ++i) gate_now[i] = gr[i];
         }
         const bool last = row + 1 == r1 || row + 1 == gate_end;   // of this gate row, or of this worker
         const int64_t gate_at = gate_row;
@@ -464,28 +530,26 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_backward_rows(NormArgs p, 
         const float c1 = sum[0] / (float)D, c2 = (sum[1] - ry * c1 * sum[2]) / (float)D;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int64_t c = (int64_t)(t + i * TPR) * 8;
+            const int c = (t + i * TPR) * 8;
             if (c >= D) continue;
             float gx[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) gx[j] = a[i][j] - ry * ny[i][j] * c1;
-            if (p.gx) store8((T*)p.gx + row * D, c, D, gx);
+            if (p.gx) put8<T, TAIL>((T*)p.gx + row * D, c, D, gx);
             if constexpr (H) {
-                float gh[8], sc[8], w[8];
-                factors8<T>(p.scale, c, D, sc);
-                factors8<T>(p.w, c, D, w);
+                float gh[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const bool off = dropped[i] >> j & 1;
-                    const float f = off ? 0.0f : p.drop.threshold ? p.drop.scale : 1.0f;
-                    const float g = p.gate ? to_f32(gate_now[i][j]) : 1.0f;
-                    const float gv = off ? 0.0f : gx[j] * b[i][j], v = off ? 0.0f : gx[j] * f * (nh[i][j] * w[j]);
-                    gh[j] = rh * (gv * w[j] - nh[i][j] * c2);
-                    sw[i][j] += gv * nh[i][j];
-                    ss[i][j] += v * g;
-                    sg[i][j] += v * sc[j];
+                    const float wj = to_f32(w[i][j]), gj = to_f32(g[i][j]), sj = to_f32(sc[i][j]);
+                    const float d = f[i][j] == 0.0f ? 0.0f : gx[j] * f[i][j];     // with respect to scale gate N(h)
+                    const float m = f[i][j] == 0.0f ? 0.0f : d * nh[i][j];
+                    const float gv = d * sj * gj;
+                    gh[j] = rh * (gv * wj - nh[i][j] * c2);
+                    sw[i][j] += m * sj * gj;
+                    ss[i][j] += m * wj * gj;
+                    sg[i][j] += m * wj * sj;
                 }
-                store8((T*)p.gh + row * D, c, D, gh);
+                put8<T, TAIL>((T*)p.gh + row * D, c, D, gh);
                 if (p.ggate && last) {
                     if (rw.parts > 1) {
                         float* to = p.partial + worker * D;   // gate rows' parts come first
@@ -493,7 +557,7 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_backward_rows(NormArgs p, 
                         for (int j = 0; j < 8; ++j)
                             if (c + j < D) to[c + j] = sg[i][j];
                     } else {
-                        store8((T*)p.ggate + gate_at * D, c, D, sg[i]);
+                        put8<T, TAIL>((T*)p.ggate + gate_at * D, c, D, sg[i]);
                     }
 #pragma unroll
                     for (int j = 0; j < 8; ++j) sg[i][j] = 0.0f;
@@ -519,15 +583,15 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_backward_rows(NormArgs p, 
                 float v = 0.0f;
 #pragma unroll
                 for (int w = 0; w < kWorkers; ++w) v += cols[w * (TPR * I * 8) + c];
-                out[k * D + c] = v;
+                out[(int64_t)k * D + c] = v;
             }
         } else {
 #pragma unroll
             for (int i = 0; i < I; ++i) {
-                const int64_t c = (int64_t)(t + i * TPR) * 8;
+                const int c = (t + i * TPR) * 8;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (c + j < D) out[k * D + c + j] = k == kSums - 1 ? sn[i][j] : k == 0 ? sw[H ? i : 0][j] : ss[H ? i : 0][j];
+                    if (c + j < D) out[(int64_t)k * D + c + j] = k == kSums - 1 ? sn[i][j] : k == 0 ? sw[H ? i : 0][j] : ss[H ? i : 0][j];
             }
         }
     }
@@ -555,9 +619,16 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs p, Rows rw, in
         n = groups;
     }
     const int64_t step = gates ? D : sums * D;
-    float v = 0.0f;
-    if (c < D)
-        for (int64_t i = strand; i < n; i += 16) v += from[i * step];
+    float v = 0.0f, u[8] = {};
+    if (c < D) {
+        int64_t i = strand;
+        for (; i + 112 < n; i += 128)   // eight loads in flight
+#pragma unroll
+            for (int k = 0; k < 8; ++k) u[k] += from[(i + 16 * k) * step];
+        for (; i < n; i += 16) v += from[i * step];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v += u[k];
+    }
     __shared__ float s[16][64];
     s[strand][threadIdx.x & 63] = v;
     __syncthreads();
@@ -572,12 +643,13 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs p, Rows rw, in
     }
 }
 
-// Threads a row and turns for a width; none above what registers hold.  The backward pass of a block's side carries
+// Threads a row and turns for a width; none below a chunk and above what registers hold.  The backward pass of a block's side carries
 // four column sums and ten values a column and takes one turn (190 registers); the others take two.
 enum Pass { kForward, kBackward, kBackwardBlock };
 struct Shape { int tpr, turns; };
 inline Shape shape_of(int64_t width, Pass pass) {
     const int64_t chunks = (width + 7) / 8;
+    if (width < 8) return {0, 0};   // row8 reads eight values
     for (int t : {8, 16, 32, 64})
         if (chunks <= t) return {t, 1};
     if (pass == kBackwardBlock) {
@@ -656,15 +728,22 @@ template <typename T> int forward(const NormArgs& a, hipStream_t s) {
         norm_forward_kernel<T><<<dim3(row_groups(a.N)), kThreads, 0, s>>>(a);
         return (int)hipGetLastError();
     }
-#define FFN_FORWARD(TPR, I) \
-    norm_forward_rows<T, TPR, I><<<dim3(row_groups((a.N + group_of(TPR) / TPR - 1) / (group_of(TPR) / TPR))), group_of(TPR), 0, s>>>(a)
+    const bool tail = a.width % 8 != 0, block = a.h != nullptr;
+    // up to sixteen waves a compute unit walk the rows
+    const int64_t per = group_of(sh.tpr) / sh.tpr, all = (a.N + per - 1) / per, most = 256 * 1024 / group_of(sh.tpr);
+    const dim3 grid((unsigned)(all < most ? all : most));
+#define FFN_FORWARD(TPR, I)                                                                              \
+    if (block && tail) norm_forward_rows<T, TPR, I, true, true><<<grid, group_of(TPR), 0, s>>>(a);      \
+    else if (block) norm_forward_rows<T, TPR, I, false, true><<<grid, group_of(TPR), 0, s>>>(a);        \
+    else if (tail) norm_forward_rows<T, TPR, I, true, false><<<grid, group_of(TPR), 0, s>>>(a);         \
+    else norm_forward_rows<T, TPR, I, false, false><<<grid, group_of(TPR), 0, s>>>(a)
     FFN_SHAPES(FFN_FORWARD)
 #undef FFN_FORWARD
     return (int)hipGetLastError();
 }
 
 template <typename T> int backward(const NormArgs& a, hipStream_t s) {
-    const bool block = a.h != nullptr;
+    const bool block = a.h != nullptr, tail = a.width % 8 != 0;
     const Shape sh = shape_of(a.width, block ? kBackwardBlock : kBackward);
     if (sh.tpr == 0) {
         const int64_t chunks = (a.N + kChunk - 1) / kChunk;
@@ -683,7 +762,9 @@ template <typename T> int backward(const NormArgs& a, hipStream_t s) {
     const Rows rw = rows_of(sh, a.N, block ? a.rows_per_gate : 1);
     const int64_t groups = groups_for(rw, sh);
     if (groups > 0 && block) {
-#define FFN_BLOCK(TPR) norm_backward_rows<T, TPR, 1, true><<<dim3((unsigned)groups), group_of(TPR), 0, s>>>(a, rw)
+#define FFN_BLOCK(TPR)                                                                                              \
+    if (tail) norm_backward_rows<T, TPR, 1, true, true><<<dim3((unsigned)groups), group_of(TPR), 0, s>>>(a, rw);    \
+    else norm_backward_rows<T, TPR, 1, false, true><<<dim3((unsigned)groups), group_of(TPR), 0, s>>>(a, rw)
         switch (sh.tpr) {
             case 8: FFN_BLOCK(8); break;
             case 16: FFN_BLOCK(16); break;
@@ -695,7 +776,9 @@ template <typename T> int backward(const NormArgs& a, hipStream_t s) {
         }
 #undef FFN_BLOCK
     } else if (groups > 0) {
-#define FFN_BACKWARD(TPR, I) norm_backward_rows<T, TPR, I, false><<<dim3((unsigned)groups), group_of(TPR), 0, s>>>(a, rw)
+#define FFN_BACKWARD(TPR, I)                                                                                        \
+    if (tail) norm_backward_rows<T, TPR, I, true, false><<<dim3((unsigned)groups), group_of(TPR), 0, s>>>(a, rw);   \
+    else norm_backward_rows<T, TPR, I, false, false><<<dim3((unsigned)groups), group_of(TPR), 0, s>>>(a, rw)
         FFN_SHAPES(FFN_BACKWARD)
 #undef FFN_BACKWARD
     }
@@ -707,35 +790,20 @@ template <typename T> int backward(const NormArgs& a, hipStream_t s) {
     return (int)hipGetLastError();
 }
 
-}  // namespace
+template <typename T> int drop(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t N, int64_t width, const DropArgs& d, hipStream_t s) {
+    const int64_t blocks = (width + 7) / 8, groups = (N * blocks + kThreads - 1) / kThreads;
+    const dim3 grid((unsigned)(groups < 4096 ? groups : 4096));
+    const int64_t stride = (int64_t)grid.x * kThreads, dr = stride / blocks, db = stride % blocks;
+    dropout_kernel<T><<<grid, kThreads, 0, s>>>((const T*)x, ldx, (T*)y, ldy, N, width, d, dr, db);
+    return (int)hipGetLastError();
+}
 
-int64_t norm_workspace_floats(int64_t width, int64_t N, int64_t rows_per_gate, bool residual) {
+inline int64_t workspace_floats(int64_t width, int64_t N, int64_t rows_per_gate, bool residual) {
     const Shape sh = shape_of(width, residual ? kBackwardBlock : kBackward);
     if (sh.tpr == 0) return 2 * N + (N + kChunk - 1) / kChunk * 3 * width;
     const Rows rw = rows_of(sh, N, residual ? rows_per_gate : 1);
     return (residual && rw.parts > 1 ? rw.workers * width : 0) + groups_for(rw, sh) * (residual ? 3 : 1) * width;
 }
 
-int launch_norm_forward(const NormArgs& a, int32_t dtype, void* stream) {
-    hipStream_t s = (hipStream_t)stream;
-    return dtype == FFN_FP32 ? forward<float>(a, s) : dtype == FFN_BF16 ? forward<bf16>(a, s) : forward<fp16>(a, s);
-}
-
-int launch_norm_backward(const NormArgs& a, int32_t dtype, void* stream) {
-    hipStream_t s = (hipStream_t)stream;
-    return dtype == FFN_FP32 ? backward<float>(a, s) : dtype == FFN_BF16 ? backward<bf16>(a, s) : backward<fp16>(a, s);
-}
-
-int launch_dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t N, int64_t width, int32_t dtype,
-                   const DropArgs& d, void* stream) {
-    hipStream_t s = (hipStream_t)stream;
-    const int64_t blocks = (width + 7) / 8, groups = (N * blocks + kThreads - 1) / kThreads;
-    const dim3 grid((unsigned)(groups < 4096 ? groups : 4096));
-    const int64_t stride = (int64_t)grid.x * kThreads, dr = stride / blocks, db = stride % blocks;
-    if (dtype == FFN_FP32) dropout_kernel<float><<<grid, kThreads, 0, s>>>((const float*)x, ldx, (float*)y, ldy, N, width, d, dr, db);
-    else if (dtype == FFN_BF16) dropout_kernel<bf16><<<grid, kThreads, 0, s>>>((const bf16*)x, ldx, (bf16*)y, ldy, N, width, d, dr, db);
-    else dropout_kernel<fp16><<<grid, kThreads, 0, s>>>((const fp16*)x, ldx, (fp16*)y, ldy, N, width, d, dr, db);
-    return (int)hipGetLastError();
-}
-
+}  // namespace
 }  // namespace ffn

@@ -200,6 +200,23 @@ Layout layout(const ffn_plan_s* p, int64_t N, bool backward) {
     return l;
 }
 
+int norm_forward(const ffn::NormArgs& a, int32_t dtype, void* stream) {
+    return dtype == FFN_FP32   ? ffn::launch_norm_forward_fp32(a, stream)
+           : dtype == FFN_BF16 ? ffn::launch_norm_forward_bf16(a, stream)
+                               : ffn::launch_norm_forward_fp16(a, stream);
+}
+int norm_backward(const ffn::NormArgs& a, int32_t dtype, void* stream) {
+    return dtype == FFN_FP32   ? ffn::launch_norm_backward_fp32(a, stream)
+           : dtype == FFN_BF16 ? ffn::launch_norm_backward_bf16(a, stream)
+                               : ffn::launch_norm_backward_fp16(a, stream);
+}
+int dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t N, int64_t width, int32_t dtype, const ffn::DropArgs& d,
+            void* stream) {
+    return dtype == FFN_FP32   ? ffn::launch_dropout_fp32(x, ldx, y, ldy, N, width, d, stream)
+           : dtype == FFN_BF16 ? ffn::launch_dropout_bf16(x, ldx, y, ldy, N, width, d, stream)
+                               : ffn::launch_dropout_fp16(x, ldx, y, ldy, N, width, d, stream);
+}
+
 bool wide4(std::initializer_list<const void*> ps, std::initializer_list<int64_t> widths) {
     int64_t all = 0;
     for (int64_t w : widths) all |= w;
@@ -370,7 +387,7 @@ int ffn_norm_forward(const ffn_norm* norm, const void* x, int64_t ldx, const voi
     if (any_overlap(outs, in_x) || any_overlap(stat, also)) return CGTP_EINVAL;
     a.x = x; a.ldx = ldx;
     a.u = u; a.ldu = ldu; a.wn = w; a.rstd_y = rstd;
-    return status(ffn::launch_norm_forward(a, norm->dtype, hip_stream));
+    return status(norm_forward(a, norm->dtype, hip_stream));
 }
 
 int64_t ffn_norm_workspace_bytes(const ffn_norm* norm, int64_t N, int32_t residual) {
@@ -399,7 +416,7 @@ int ffn_norm_backward(const ffn_norm* norm, const void* x, int64_t ldx, const vo
     a.y = const_cast<void*>(x); a.ldx = ldx; a.wn = w; a.rstd_y = const_cast<float*>(rstd);
     a.gu = grad_u; a.ldg = ldg; a.gx = grad_x; a.gwn = grad_w;
     a.partial = (float*)workspace;
-    return status(ffn::launch_norm_backward(a, norm->dtype, hip_stream));
+    return status(norm_backward(a, norm->dtype, hip_stream));
 }
 
 int ffn_residual_forward(const ffn_norm* norm, const void* x, const void* h, const void* w, const void* gate,
@@ -421,7 +438,7 @@ int ffn_residual_forward(const ffn_norm* norm, const void* x, const void* h, con
     a.y = y; a.u = u; a.ldu = D;
     a.rstd_h = stats;
     a.rstd_y = stats ? stats + N : nullptr;
-    return status(ffn::launch_norm_forward(a, norm->dtype, hip_stream));
+    return status(norm_forward(a, norm->dtype, hip_stream));
 }
 
 int ffn_residual_backward(const ffn_norm* norm, const void* h, const void* y, const void* w, const void* gate,
@@ -454,7 +471,7 @@ int ffn_residual_backward(const ffn_norm* norm, const void* h, const void* y, co
     a.gy = grad_y; a.gu = grad_u; a.ldg = D;
     a.gx = grad_x; a.gh = grad_h; a.gw = grad_w; a.ggate = N > 0 ? grad_gate : nullptr; a.gscale = grad_scale; a.gwn = grad_w_next;
     a.partial = (float*)workspace;
-    return status(ffn::launch_norm_backward(a, norm->dtype, hip_stream));
+    return status(norm_backward(a, norm->dtype, hip_stream));
 }
 
 int ffn_dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t N, int64_t width, int32_t dtype, double p,
@@ -474,7 +491,7 @@ int ffn_dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t N, int
     const Range ins[] = {{y == x && ldy == ldx ? nullptr : x, span(N, ldx, width, e)}};
     const Range outs[] = {{y, span(N, ldy, width, e)}};
     if (any_overlap(outs, ins)) return CGTP_EINVAL;
-    return status(ffn::launch_dropout(x, ldx, y, ldy, N, width, dtype, d, hip_stream));
+    return status(dropout(x, ldx, y, ldy, N, width, dtype, d, hip_stream));
 }
 
 }  // extern "C"
