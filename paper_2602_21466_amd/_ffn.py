@@ -45,10 +45,21 @@ SIGNATURES = {
 }
 
 
+_fn = {}   # entry points by name, once the library is loaded
+
+
+def _entry(name):
+    f = _fn.get(name)
+    if f is None:
+        from . import _load
+        f = _fn[name] = getattr(_load(), name)
+    return f
+
+
 def _call(name, *args):
-    from . import _check, _load
-    rc = getattr(_load(), name)(*args)
+    rc = _entry(name)(*args)
     if rc:
+        from . import _check
         _check(rc, name)
 
 
@@ -74,13 +85,11 @@ def ffn_destroy(plan) -> None:
 
 
 def ffn_workspace_bytes(plan, N: int) -> int:
-    from . import _load
-    return int(_load().ffn_workspace_bytes(plan, N))
+    return _entry("ffn_workspace_bytes")(plan, N)
 
 
 def ffn_backward_workspace_bytes(plan, N: int) -> int:
-    from . import _load
-    return int(_load().ffn_backward_workspace_bytes(plan, N))
+    return _entry("ffn_backward_workspace_bytes")(plan, N)
 
 
 def ffn_forward(plan, x_ptr, ldx, w_in_ptr, w_out_ptr, y_ptr, saved_ptr, N, ws_ptr, ws_bytes, stream_ptr=None) -> None:
@@ -104,8 +113,7 @@ def ffn_norm_backward(norm, x_ptr, ldx, w_ptr, rstd_ptr, gu_ptr, ldg, gx_ptr, gw
 
 
 def ffn_norm_workspace_bytes(norm, N: int, residual: int) -> int:
-    from . import _load
-    return int(_load().ffn_norm_workspace_bytes(norm, N, residual))
+    return _entry("ffn_norm_workspace_bytes")(norm, N, residual)
 
 
 def ffn_residual_forward(norm, x_ptr, h_ptr, w_ptr, gate_ptr, scale_ptr, w_next_ptr, y_ptr, u_ptr, stats_ptr, N,
@@ -135,57 +143,63 @@ def _torch_dtype(dtype):
     return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
 
 
-def _rows(t, tdt, rows, width, what):
-    """Row stride of t, which must be a [rows, width] tensor whose rows do not overlap (rows None: any number)."""
+def _rows(t, tdt, rows, width, what, dev=None):
+    """Row stride of t, which must be a [rows, width] tensor on GPU `dev` whose rows do not overlap (None: any)."""
     if not t.is_cuda or t.dtype != tdt or t.dim() != 2 or t.shape[1] != width or (rows is not None and t.shape[0] != rows):
         raise ValueError("%s must be a %s CUDA tensor [%s, %d]" % (what, tdt, "N" if rows is None else rows, width))
-    ld = t.stride(0)
+    if dev is not None and t.get_device() != dev:
+        raise ValueError("all tensors must be on GPU %d: %s is not" % (dev, what))
+    ld, one = t.stride()
     if t.shape[0] <= 1:
         ld = max(ld, width)
-    if (width > 1 and t.stride(1) != 1) or ld < width:
+    if (width > 1 and one != 1) or ld < width:
         raise ValueError("%s must have adjacent values in each row and rows that do not overlap" % what)
     return ld
 
 
-def _whole(t, tdt, shape, what):
-    """Pointer of t, a contiguous CUDA tensor of this shape (None where t is None)."""
+def _whole(t, tdt, shape, what, dev):
+    """Pointer of t, a contiguous tensor of this shape on GPU `dev` (None where t is None)."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != tdt or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s CUDA tensor %s" % (what, tdt, list(shape)))
+    if t.get_device() != dev or t.dtype != tdt or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor %s on GPU %d" % (what, tdt, list(shape), dev))
     return t.data_ptr()
 
 
-def _on_one_device(x, *others):
-    for t in others:
-        if t is not None and t.device != x.device:
-            raise ValueError("all tensors must be on %s" % x.device)
-
-
-def _stream(stream, device):
+def _stream(stream, dev):
     """The HIP stream's handle, and the torch stream where it is not the current one."""
-    import torch
     if stream is None:
-        return torch.cuda.current_stream(device).cuda_stream, None
+        import torch
+        return torch._C._cuda_getCurrentRawStream(dev), None
     return stream.cuda_stream, stream
 
 
-def _new(shape, dtype, device, other):
+def _new(shape, dtype, dev, other):
     """A new tensor of the stream `other` (None: the current one), so that its memory is reused in that stream's order."""
     import torch
     if other is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(shape, dtype=dtype, device=_devices[dev])
     with torch.cuda.stream(other):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(shape, dtype=dtype, device=_devices[dev])
 
 
-def _workspace(workspace, need, device, other):
+class _Devices(dict):
+    def __missing__(self, dev):
+        import torch
+        d = self[dev] = torch.device("cuda", dev)
+        return d
+
+
+_devices = _Devices()
+
+
+def _workspace(workspace, need, dev, other):
     import torch
     if workspace is None:
-        return _new((max(need, 1),), torch.uint8, device, other)
-    if workspace.dtype != torch.uint8 or workspace.device != device or not workspace.is_contiguous() or \
+        return _new((max(need, 1),), torch.uint8, dev, other)
+    if workspace.dtype != torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous() or \
             workspace.numel() < need:
-        raise ValueError("workspace must be a contiguous uint8 tensor of at least %d bytes on %s" % (need, device))
+        raise ValueError("workspace must be a contiguous uint8 tensor of at least %d bytes on GPU %d" % (need, dev))
     return workspace
 
 
@@ -206,17 +220,16 @@ class FfnPlan:
         import torch
         tdt, di, df, do = self._tdt, self.d_in, self.d_ff, self.d_out
         ldx = _rows(x, tdt, None, di, "x")
-        N, dev = x.shape[0], x.device
-        wi, wo = _whole(w_in, tdt, (2 * df, di), "w_in"), _whole(w_out, tdt, (do, df), "w_out")
-        _on_one_device(x, w_in, w_out, out, saved)
+        N, dev = x.shape[0], x.get_device()
+        wi, wo = _whole(w_in, tdt, (2 * df, di), "w_in", dev), _whole(w_out, tdt, (do, df), "w_out", dev)
         sp, other = _stream(stream, dev)
         if out is None:
             out = _new((N, do), tdt, dev, other)
         if save and saved is None:
             saved = _new((N, 2 * df), torch.float32, dev, other)
         ws = _workspace(workspace, ffn_workspace_bytes(self._h, N), dev, other)
-        ffn_forward(self._h, x.data_ptr(), ldx, wi, wo, _whole(out, tdt, (N, do), "out"),
-                    _whole(saved, torch.float32, (N, 2 * df), "saved"), N, ws.data_ptr(), ws.numel(), sp)
+        ffn_forward(self._h, x.data_ptr(), ldx, wi, wo, _whole(out, tdt, (N, do), "out", dev),
+                    _whole(saved, torch.float32, (N, 2 * df), "saved", dev), N, ws.data_ptr(), ws.numel(), sp)
         return out if saved is None else (out, saved)
 
     def backward(self, x, w_in, w_out, saved, grad_out, need_x=True, need_w_in=True, need_w_out=True, workspace=None,
@@ -226,11 +239,10 @@ class FfnPlan:
         import torch
         tdt, di, df, do = self._tdt, self.d_in, self.d_ff, self.d_out
         ldx = _rows(x, tdt, None, di, "x")
-        N, dev = x.shape[0], x.device
-        ldg = _rows(grad_out, tdt, N, do, "grad_out")
-        wi, wo = _whole(w_in, tdt, (2 * df, di), "w_in"), _whole(w_out, tdt, (do, df), "w_out")
-        sv = _whole(saved, torch.float32, (N, 2 * df), "saved")
-        _on_one_device(x, w_in, w_out, saved, grad_out)
+        N, dev = x.shape[0], x.get_device()
+        ldg = _rows(grad_out, tdt, N, do, "grad_out", dev)
+        wi, wo = _whole(w_in, tdt, (2 * df, di), "w_in", dev), _whole(w_out, tdt, (do, df), "w_out", dev)
+        sv = _whole(saved, torch.float32, (N, 2 * df), "saved", dev)
         if not (need_x or need_w_in or need_w_out):
             return None, None, None
         sp, other = _stream(stream, dev)
@@ -279,16 +291,15 @@ class NormPlan:
         import torch
         tdt, D = self._tdt, self.width
         ldx = _rows(x, tdt, None, D, "x")
-        N, dev = x.shape[0], x.device
-        wp = _whole(w, tdt, (D,), "w")
-        _on_one_device(x, w, out, rstd)
+        N, dev = x.shape[0], x.get_device()
+        wp = _whole(w, tdt, (D,), "w", dev)
         sp, other = _stream(stream, dev)
         if out is None:
             out = _new((N, D), tdt, dev, other)
         if rstd is None:
             rstd = _new((N,), torch.float32, dev, other)
-        ffn_norm_forward(self._norm(), x.data_ptr(), ldx, wp, out.data_ptr(), _rows(out, tdt, N, D, "out"),
-                         _whole(rstd, torch.float32, (N,), "rstd"), N, sp)
+        ffn_norm_forward(self._norm(), x.data_ptr(), ldx, wp, out.data_ptr(), _rows(out, tdt, N, D, "out", dev),
+                         _whole(rstd, torch.float32, (N,), "rstd", dev), N, sp)
         return out, rstd
 
     def backward(self, x, w, rstd, grad_out, need_x=True, need_w=True, workspace=None, stream=None):
@@ -296,10 +307,9 @@ class NormPlan:
         import torch
         tdt, D = self._tdt, self.width
         ldx = _rows(x, tdt, None, D, "x")
-        N, dev = x.shape[0], x.device
-        ldg = _rows(grad_out, tdt, N, D, "grad_out")
-        wp, rp = _whole(w, tdt, (D,), "w"), _whole(rstd, torch.float32, (N,), "rstd")
-        _on_one_device(x, w, rstd, grad_out)
+        N, dev = x.shape[0], x.get_device()
+        ldg = _rows(grad_out, tdt, N, D, "grad_out", dev)
+        wp, rp = _whole(w, tdt, (D,), "w", dev), _whole(rstd, torch.float32, (N,), "rstd", dev)
         if not (need_x or need_w):
             return None, None
         sp, other = _stream(stream, dev)
@@ -326,17 +336,16 @@ class NormPlan:
         tdt, D = self._tdt, self.width
         if not x.is_cuda or x.dim() != 2:
             raise ValueError("x must be a %s CUDA tensor [N, %d]" % (tdt, D))
-        N, dev = x.shape[0], x.device
-        xp, hp = _whole(x, tdt, (N, D), "x"), _whole(h, tdt, (N, D), "h")
-        wp, sc = _whole(w, tdt, (D,), "w"), _whole(scale, tdt, (D,), "scale")
-        gp, np_ = _whole(gate, tdt, (self._gates(N), D), "gate"), _whole(w_next, tdt, (D,), "w_next")
-        _on_one_device(x, h, w, gate, scale, w_next, out)
+        N, dev = x.shape[0], x.get_device()
+        xp, hp = _whole(x, tdt, (N, D), "x", dev), _whole(h, tdt, (N, D), "h", dev)
+        wp, sc = _whole(w, tdt, (D,), "w", dev), _whole(scale, tdt, (D,), "scale", dev)
+        gp, np_ = _whole(gate, tdt, (self._gates(N), D), "gate", dev), _whole(w_next, tdt, (D,), "w_next", dev)
         sp, other = _stream(stream, dev)
         if out is None:
             out = _new((N, D), tdt, dev, other)
         u = _new((N, D), tdt, dev, other) if next_norm else None
         stats = _new((2, N), torch.float32, dev, other)
-        ffn_residual_forward(self._norm(seed, offset), xp, hp, wp, gp, sc, np_, _whole(out, tdt, (N, D), "out"),
+        ffn_residual_forward(self._norm(seed, offset), xp, hp, wp, gp, sc, np_, _whole(out, tdt, (N, D), "out", dev),
                              u.data_ptr() if next_norm else None, stats.data_ptr(), N, sp)
         return out, u, stats
 
@@ -351,13 +360,12 @@ class NormPlan:
             raise ValueError("h must be a %s CUDA tensor [N, %d]" % (tdt, D))
         if grad_y is None and grad_u is None:
             raise ValueError("one of grad_y and grad_u must be given")
-        N, dev = h.shape[0], h.device
-        hp, yp = _whole(h, tdt, (N, D), "h"), _whole(y, tdt, (N, D), "y")
-        wp, sc = _whole(w, tdt, (D,), "w"), _whole(scale, tdt, (D,), "scale")
-        gp, np_ = _whole(gate, tdt, (self._gates(N), D), "gate"), _whole(w_next, tdt, (D,), "w_next")
-        st = _whole(stats, torch.float32, (2, N), "stats")
-        gyp, gup = _whole(grad_y, tdt, (N, D), "grad_y"), _whole(grad_u, tdt, (N, D), "grad_u")
-        _on_one_device(h, y, w, gate, scale, w_next, stats, grad_y, grad_u)
+        N, dev = h.shape[0], h.get_device()
+        hp, yp = _whole(h, tdt, (N, D), "h", dev), _whole(y, tdt, (N, D), "y", dev)
+        wp, sc = _whole(w, tdt, (D,), "w", dev), _whole(scale, tdt, (D,), "scale", dev)
+        gp, np_ = _whole(gate, tdt, (self._gates(N), D), "gate", dev), _whole(w_next, tdt, (D,), "w_next", dev)
+        st = _whole(stats, torch.float32, (2, N), "stats", dev)
+        gyp, gup = _whole(grad_y, tdt, (N, D), "grad_y", dev), _whole(grad_u, tdt, (N, D), "grad_u", dev)
         sp, other = _stream(stream, dev)
         gx, gh = _new((N, D), tdt, dev, other), _new((N, D), tdt, dev, other)
         gw, gs, gn = (None if t is None else _new((D,), tdt, dev, other) for t in (w, scale, w_next))
@@ -379,7 +387,7 @@ def dropout(x, p: float, seed: int, offset: int = 0, out=None, stream=None):
     name = {torch.float32: "fp32", torch.bfloat16: "bf16", torch.float16: "fp16"}.get(x.dtype)
     if name is None or not x.is_cuda or x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("x must be an fp32, bf16 or fp16 CUDA tensor [..., width]")
-    width, dev = x.shape[-1], x.device
+    width, dev = x.shape[-1], x.get_device()
     if x.dim() != 2 and not x.is_contiguous():
         raise ValueError("x must be contiguous, or [N, width] with strided rows")
     N = x.numel() // width
@@ -387,8 +395,8 @@ def dropout(x, p: float, seed: int, offset: int = 0, out=None, stream=None):
     sp, other = _stream(stream, dev)
     if out is None:
         out = _new(tuple(x.shape), x.dtype, dev, other)
-    elif out.shape != x.shape or out.device != dev or (out.dim() != 2 and not out.is_contiguous()):
+    elif out.shape != x.shape or out.get_device() != dev or (out.dim() != 2 and not out.is_contiguous()):
         raise ValueError("out must have the shape and device of x")
-    ldy = _rows(out, x.dtype, N, width, "out") if out.dim() == 2 else _whole(out, x.dtype, tuple(x.shape), "out") and width
+    ldy = _rows(out, x.dtype, N, width, "out", dev) if out.dim() == 2 else _whole(out, x.dtype, tuple(x.shape), "out", dev) and width
     ffn_dropout(x.data_ptr(), ldx, out.data_ptr(), ldy or width, N, width, name, float(p), seed & _U64, offset & _U64, sp)
     return out

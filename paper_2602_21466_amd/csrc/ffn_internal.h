@@ -38,6 +38,22 @@ int launch_tile_bf16(const TileArgs& p, int32_t epilogue, bool a_cols, bool b_co
 int launch_tile_fp16(const TileArgs& p, int32_t epilogue, bool a_cols, bool b_cols, int32_t tile, void* stream);
 int launch_tile_fp32(const TileArgs& p, int32_t epilogue, bool a_cols, bool b_cols, int32_t tile, void* stream);
 
+// The forward products for few rows (M <= kFewRows): C = X W^T (kStore) or the gated form (kGate: W holds the gate's
+// N rows, then the up projection's).  Strides in elements of the arrays' type; any alignment.  See ffn_few.h.
+constexpr int64_t kFewRows = 64;
+struct FewArgs {
+    const void *x, *w;
+    int64_t ldx, ldw, M, N, K;
+    void* c;
+    int64_t ldc;
+    float* saved;                         // kGate: [M, 2 N] or NULL
+    int32_t act;
+    int32_t wide;                         // as TileArgs::wide
+};
+int launch_few_bf16(const FewArgs& p, int32_t epilogue, int32_t nr, int32_t waves, void* stream);
+int launch_few_fp16(const FewArgs& p, int32_t epilogue, int32_t nr, int32_t waves, void* stream);
+int launch_few_fp32(const FewArgs& p, int32_t epilogue, int32_t nr, int32_t waves, void* stream);
+
 // out[i, j] = sum over splits of partial[s, i, j] (rows of ld floats), N columns, out contiguous.
 int launch_join(const float* partial, int64_t ld, int32_t splits, int64_t M, int64_t N, void* out, int32_t dtype, void* stream);
 

@@ -148,6 +148,24 @@ int product(ffn::TileArgs t, int32_t epilogue, bool ac, bool bc, int32_t dtype, 
     return status(ffn::launch_join((const float*)partial, t.ldc, c.splits, t.M, t.N, out, dtype, stream));
 }
 
+// A product for few rows: weight rows a work-group, and waves (parts of k).  Measured, bf16: below one work-group of
+// 16 a compute unit 8 rows are faster for up to 16 rows of x (2048 x 8192, one row: 10.3 against 12.5 us); 32 where
+// x's rows are read as often as the weights and two work-groups a unit are left (16384 x 4096 gated, 24 rows: 55
+// against 61 us).
+int few_product(const ffn::FewArgs& p, int32_t epilogue, int32_t dtype, void* stream) {
+    const bool gate = epilogue == ffn::kGate;
+    const int32_t nr = p.N < 16 * 256 && p.M <= 16 ? 8 : gate && p.M > 16 && p.N >= 32 * 512 ? 32 : 16;
+    const int32_t mt = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4, per = (nr > 16 ? 2 : 1) * (gate ? 2 : 1) * mt;
+    int32_t waves = nr == 8 ? 4 : 8;
+    const int64_t blocks = tiles(p.K, dtype == FFN_FP32 ? 32 : 64);
+    while (waves > 1 && (waves * per > 64 || waves > blocks)) waves /= 2;
+    switch (dtype) {
+        case FFN_FP32: return status(ffn::launch_few_fp32(p, epilogue, nr, waves, stream));
+        case FFN_BF16: return status(ffn::launch_few_bf16(p, epilogue, nr, waves, stream));
+        default: return status(ffn::launch_few_fp16(p, epilogue, nr, waves, stream));
+    }
+}
+
 // A matrix as the products read it: 16-bit values (or three planes of them) on 16 bytes.
 struct Operand { const void* p; int64_t ld, plane; };
 
@@ -223,6 +241,17 @@ bool wide4(std::initializer_list<const void*> ps, std::initializer_list<int64_t>
     return !misaligned(ps, 16) && (all & 3) == 0;
 }
 
+// Y = H Wo^T by tiles.
+int down(const ffn_plan_s* plan, const void* h, const Operand& w, void* y, int64_t N, void* partial, void* stream) {
+    ffn::TileArgs o = {};
+    o.a = h; o.lda = up8(plan->d_ff); o.plane_a = packed(N, plan->d_ff);
+    o.b = w.p; o.ldb = w.ld; o.plane_b = w.plane;
+    o.M = N; o.N = plan->d_out; o.K = plan->d_ff;
+    o.c = y; o.ldc = plan->d_out;
+    o.wide = wide4({y}, {plan->d_out});
+    return product(o, ffn::kStore, false, false, plan->dtype, partial, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -273,6 +302,25 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
     rc = current_device_is(plan->device);
     if (rc != CGTP_OK) return rc;
     char* ws = (char*)workspace;
+    if (N <= ffn::kFewRows) {
+        ffn::FewArgs g = {};
+        g.x = x; g.ldx = ldx; g.w = w_in; g.ldw = di;
+        g.M = N; g.N = df; g.K = di;
+        g.c = ws + l.h; g.ldc = up8(df);
+        g.act = plan->act; g.saved = (float*)saved;
+        g.wide = wide4({saved}, {df});
+        rc = few_product(g, ffn::kGate, plan->dtype, hip_stream);
+        if (rc != CGTP_OK) return rc;
+        // from here on the weights alone are many: 16-bit ones that need no packing go through LDS in 128-wide tiles with
+        // k in parts, which passes 16 rows of x (4096 x 16384, 24 rows: 38 us with the joining, against 44)
+        if (N > 16 && as_is(w_out, df, d_o, df, plan->dtype)) return down(plan, ws + l.h, {w_out, df, 0}, y, N, ws + l.partial, hip_stream);
+        ffn::FewArgs o = {};
+        o.x = ws + l.h; o.ldx = up8(df); o.w = w_out; o.ldw = df;
+        o.M = N; o.N = d_o; o.K = df;
+        o.c = y; o.ldc = d_o;
+        o.wide = wide4({y}, {d_o});
+        return few_product(o, ffn::kStore, plan->dtype, hip_stream);
+    }
     Operand X, Wi, Wo;
     rc = operand(x, ldx, N, di, plan->dtype, ws + l.x, hip_stream, &X);
     if (rc == CGTP_OK) rc = operand(w_in, di, 2 * df, di, plan->dtype, ws + l.w_in, hip_stream, &Wi);
@@ -287,13 +335,7 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
     g.wide = wide4({saved}, {df});
     rc = product(g, ffn::kGate, false, false, plan->dtype, nullptr, hip_stream);
     if (rc != CGTP_OK) return rc;
-    ffn::TileArgs o = {};
-    o.a = ws + l.h; o.lda = up8(df); o.plane_a = packed(N, df);
-    o.b = Wo.p; o.ldb = Wo.ld; o.plane_b = Wo.plane;
-    o.M = N; o.N = d_o; o.K = df;
-    o.c = y; o.ldc = d_o;
-    o.wide = wide4({y}, {d_o});
-    return product(o, ffn::kStore, false, false, plan->dtype, ws + l.partial, hip_stream);
+    return down(plan, ws + l.h, Wo, y, N, ws + l.partial, hip_stream);
 }
 
 int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, const void* w_out, const void* saved,
