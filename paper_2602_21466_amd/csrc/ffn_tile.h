@@ -5,7 +5,10 @@
 // or with m / n adjacent ("columns").  A work-group of BM x BN outputs walks k in
 // steps of 64: operands go from memory to LDS directly (16 bytes a lane, no
 // registers), one step ahead of the step that is multiplied, in two buffers.
-// Waves hold 16 x 16 accumulators of a (BM / WM) x 64 block.
+// Each of the WM x WN waves holds the 16 x 16 accumulators of a (BM / WM) x (BN / WN) block.  A step is two halves of
+// 32 k: while the matrix instructions of one half run, the fragments of the next are read from LDS.  Between the halves
+// all waves meet: by then each has read the last of this step's buffer, which takes the step after next from memory,
+// and the next step's data, asked for a whole step earlier, is there.
 //
 // LDS layouts, chosen so that the direct loads write whole 1 KB runs and the
 // reads meet no bank twice:
@@ -114,8 +117,9 @@ __device__ __forceinline__ f32x4 load4(const float* p, int64_t n, int64_t N, boo
 
 constexpr uint32_t kOut = 0x80000000u;    // beyond every buffer: a direct load from there writes zeros
 
-// The direct loads of one operand: `R` rows of C's index a tile, 64 k a step, by NW waves.
-template <int R, int NW, bool COLS, bool GATE> struct Loader {
+// The direct loads of one operand: `R` rows of C's index a tile, 64 k a step, by NW waves.  GATE: in blocks of GATE
+// tile rows, half of the gate's rows, then the same half of the up projection's.
+template <int R, int NW, bool COLS, int GATE> struct Loader {
     static constexpr int kLoads = R * 128 / 1024 / NW;
     __amdgpu_buffer_rsrc_t rsrc[GATE ? 2 : 1];
     const char* base[GATE ? 2 : 1];
@@ -134,13 +138,12 @@ template <int R, int NW, bool COLS, bool GATE> struct Loader {
             kpos = c * 8;
             step = 128;
             if constexpr (GATE) {
-                // blocks of 64 tile rows: 32 of the gate's rows, then the same 32 of the up projection's
                 base[0] = (const char*)p + r0 * ld * 2;
                 base[1] = base[0] + half * ld * 2;
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
                     const int t = (i * NW + wave) * 8 + sub;
-                    int64_t r = (t >> 6) * 32 + (t & 31);
+                    int64_t r = t / GATE * (GATE / 2) + t % (GATE / 2);
                     if (r0 + r >= rows) r = rows - 1 - r0;
                     voff[i] = (uint32_t)(r * ld * 2 + c * 16);
                 }
@@ -184,7 +187,7 @@ template <int R, int NW, bool COLS, bool GATE> struct Loader {
             const uint32_t v = k < left ? voff[i] : kOut;
             FFN_LDS void* to = (FFN_LDS void*)(lds + (i * NW + wave) * 1024);
             if constexpr (GATE) {
-                if ((((i * NW + wave) * 8) & 63) < 32) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc[0], to, 16, v, 0, 0, 0);
+                if ((i * NW + wave) * 8 % GATE < GATE / 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc[0], to, 16, v, 0, 0, 0);
                 else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc[1], to, 16, v, 0, 0, 0);
             } else {
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc[0], to, 16, v, 0, 0, 0);
@@ -193,21 +196,25 @@ template <int R, int NW, bool COLS, bool GATE> struct Loader {
     }
 };
 
-// The fragment of 16 rows from `r` on and 32 k from 32 kk on: lane l gets row r + l % 16, k = 8 (l / 16) .. + 7.
-template <int R, bool COLS> __device__ __forceinline__ s16x8 fragment(const char* lds, int r, int kk, int lane) {
-    const int q = lane >> 4, i = lane & 15;
-    if constexpr (!COLS) {
-        const int row = r + i, c = (kk * 4 + q) ^ (row & 7);
-        return *(const s16x8*)(lds + row * 128 + c * 16);
-    } else {
-        const int k = kk * 32 + q * 8 + (i >> 2);
-        const int s = Loader<R, 1, true, false>::swizzle(k);
-        const int at = k * R * 2 + (((r >> 4) ^ s) << 5) + (i & 3) * 8;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FFN_LDS s16x4*)(lds + at));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FFN_LDS s16x4*)(lds + at + 4 * R * 2));
+// Fragments: 16 rows and 32 k (half kk of the step) of an operand; lane l gets row l % 16, k = 8 (l / 16) .. + 7.  The
+// swizzles are exclusive ors of fields that hold nothing else, so that one lane offset serves all fragments: base()
+// for the wave's first row r0, then an exclusive or and a constant.
+template <int R, bool COLS> struct Fragments {
+    static __device__ __forceinline__ int base(int r0, int lane) {
+        const int q = lane >> 4, i = lane & 15;
+        if constexpr (!COLS) return (r0 + i) * 128 + ((q ^ (i & 7)) << 4);
+        const int k = q * 8 + (i >> 2);
+        return k * R * 2 + (((r0 >> 4) ^ Loader<R, 1, true, 0>::swizzle(k)) << 5) + (i & 3) * 8;
+    }
+    // tile i of the wave's; r0 is a multiple of its tiles' rows
+    static __device__ __forceinline__ s16x8 get(const char* lds, int base, int i, int kk) {
+        if constexpr (!COLS) return *(const s16x8*)(lds + (base ^ (kk << 6)) + i * 2048);
+        const char* at = lds + (base ^ (i << 5)) + kk * 64 * R;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FFN_LDS s16x4*)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FFN_LDS s16x4*)(at + 8 * R));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
-}
+};
 
 // Which tile a work-group takes.  Consecutive work-groups go to the eight dies in turn; each die gets a run of
 // consecutive tiles, and a run walks down eight rows of tiles before it moves one column on, so that a die's L2
@@ -225,20 +232,19 @@ __device__ __forceinline__ void place(int id, int total, int tm, int tn, int& m,
 template <typename T, typename Out, int BM, int BN, int WM, int WN, bool AC, bool BC, int EPI>
 __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
 #ifdef __HIP_DEVICE_COMPILE__   // (the host's pass needs the launch stub alone)
-    constexpr int NW = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16;
-    static_assert(EPI != kGate || NT == 4, "a wave holds 32 gate columns and 32 of the up projection");
+    constexpr int NW = WM * WN, MT = BM / WM / 16, CW = BN / WN, NT = CW / 16;
     __shared__ __align__(1024) char sa0[BM * 128], sb0[BN * 128];
     __shared__ __align__(1024) char sa1[BM * 128], sb1[BN * 128];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+    const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * CW;
     const int total = p.tiles_m * p.tiles_n;
     int tm, tn;
     place(blockIdx.x, total, p.tiles_m, p.tiles_n, tm, tn);
     constexpr int kCols = EPI == kGate ? BN / 2 : BN;      // columns of C a tile covers
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * kCols;
 
-    Loader<BM, NW, AC, false> la;
-    Loader<BN, NW, BC, EPI == kGate> lb;
+    Loader<BM, NW, AC, 0> la;
+    Loader<BN, NW, BC, EPI == kGate ? CW : 0> lb;
     la.init(p.a, p.lda, m0, p.M, 0, wave, lane);
     lb.init(p.b, p.ldb, n0, p.N, p.N, wave, lane);
 
@@ -260,44 +266,94 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
     };
 
     f32x4 acc[MT][NT] = {};
-    auto multiply = [&](const char* a, const char* b) {
+    s16x8 fa[2][MT], fb[2][NT];
+    const int base_a = Fragments<BM, AC>::base(wm, lane), base_b = Fragments<BN, BC>::base(wn, lane);
+    auto read = [&](const char* a, const char* b, int kk) {
+        // (the offsets are made anew at every reading: kept over the loop they would not fit the registers)
+        int oa = base_a, ob = base_b;
+        asm volatile("" : "+v"(oa), "+v"(ob));
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            s16x8 fb[NT], fa[MT];
+        for (int j = 0; j < NT; ++j) fb[kk][j] = Fragments<BN, BC>::get(b, ob, j, kk);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) fb[j] = fragment<BN, BC>(b, wn + j * 16, kk, lane);
+        for (int i = 0; i < MT; ++i) fa[kk][i] = Fragments<BM, AC>::get(a, oa, i, kk);
+    };
+    auto multiply = [&](int kk) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) fa[i] = fragment<BM, AC>(a, wm + i * 16, kk, lane);
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mfma16(fb[j], fa[i], acc[i][j], T());
-        }
+            for (int j = 0; j < NT; ++j) acc[i][j] = mfma16(fb[kk][j], fa[kk][i], acc[i][j], T());
+    };
+    // one step out of (a, b), the next one's first half out of (an, bn)
+    auto step = [&](char* a, char* b, char* an, char* bn, bool more) {
+        read(a, b, 1);
+        multiply(0);
+        __syncthreads();
+        if (more) issue(a, b);
+        read(an, bn, 0);
+        multiply(1);
     };
 
-    if (s0 < s1) issue(sa0, sb0);
-    __syncthreads();
-    int s = s0;
-    for (; s + 1 < s1; s += 2) {
-        issue(sa1, sb1);
-        multiply(sa0, sb0);
+    const int n = s1 - s0;
+    if constexpr (NW == 8) {
+        // Two waves a SIMD, of which one reads fragments while the other multiplies: waves 4 - 7 run one phase behind.
+        auto meet = [] {
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto phases = [&](char* a, char* b, char* an, char* bn, bool more) {
+            if (more) issue(an, bn);
+            read(a, b, 0);
+            __builtin_amdgcn_s_waitcnt(0xC07F);     // own LDS reads done
+            meet();
+            __builtin_amdgcn_s_setprio(1);
+            multiply(0);
+            __builtin_amdgcn_s_setprio(0);
+            meet();
+            read(a, b, 1);
+            __builtin_amdgcn_s_waitcnt(0x0070);     // own LDS reads done, own direct loads landed
+            meet();
+            __builtin_amdgcn_s_setprio(1);
+            multiply(1);
+            __builtin_amdgcn_s_setprio(0);
+            meet();
+        };
+        if (n > 0) issue(sa0, sb0);
         __syncthreads();
-        if (s + 2 < s1) issue(sa0, sb0);
-        multiply(sa1, sb1);
+        if (wave >= 4) meet();
+        int s = 0;
+        for (; s + 1 < n; s += 2) {
+            phases(sa0, sb0, sa1, sb1, true);
+            phases(sa1, sb1, sa0, sb0, s + 2 < n);
+        }
+        if (s < n) phases(sa0, sb0, sa1, sb1, false);
+        if (wave < 4) meet();
+    } else {
+        if (n > 0) issue(sa0, sb0);
+        if (n > 1) issue(sa1, sb1);
         __syncthreads();
+        read(sa0, sb0, 0);
+        int s = 0;
+        for (; s + 1 < n; s += 2) {
+            step(sa0, sb0, sa1, sb1, s + 2 < n);
+            step(sa1, sb1, sa0, sb0, s + 3 < n);
+        }
+        if (s < n) step(sa0, sb0, sa1, sb1, false);
     }
-    if (s < s1) multiply(sa0, sb0);
 
     // acc[i][j][e] is row m = .. + lane % 16, column n = .. + 4 (lane / 16) + e.  Each wave turns 32 rows at a time in
-    // LDS of its own, so that memory is read and written along the rows: 16 lanes a row of 64 columns.
+    // LDS of its own, so that memory is read and written along the rows.
     __syncthreads();
-    constexpr int kRow = 68, kTurn = 32 * kRow * 4;        // floats a row (four more than it holds: no bank twice)
-    constexpr int kFit = BM * 128 / kTurn;
-    static_assert(kFit >= 1 && 4 * kFit >= NW && BM == BN, "a turn buffer for every wave");
+    constexpr int kRow = CW + 4, kTurn = 32 * kRow * 4;    // floats a row (four more than it holds: no bank twice)
+    constexpr int kFit = (BM < BN ? BM : BN) * 128 / kTurn;
+    static_assert(kFit >= 1 && 4 * kFit >= NW, "a turn buffer for every wave");
     float* turn = (float*)((wave / kFit == 0 ? sa0 : wave / kFit == 1 ? sb0 : wave / kFit == 2 ? sa1 : sb1) + wave % kFit * kTurn);
     const bool wide = p.wide;
+    constexpr int kLanes = EPI == kGate ? CW / 8 : CW / 4, kTake = 64 / kLanes;      // lanes a row, rows a turn
+    const int tc = (lane % kLanes) * 4;
 #pragma unroll
     for (int i = 0; i < MT; i += 2) {
+        const int64_t mb = m0 + wm + i * 16, n = n0 + (EPI == kGate ? wn / 2 : wn) + tc;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -305,55 +361,65 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
                 *(f32x4*)(turn + (x * 16 + (lane & 15)) * kRow + j * 16 + (lane >> 4) * 4) = acc[i + x][j];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        const int64_t mb = m0 + wm + i * 16;
-        if constexpr (EPI == kGate) {
-            const int64_t n = n0 + wn / 2 + (lane & 7) * 4;
-            for (int r = lane >> 3; r < 32; r += 8) {
-                const int64_t m = mb + r;
-                if (m >= p.M) break;
-                const f32x4 g = *(const f32x4*)(turn + r * kRow + (lane & 7) * 4), u = *(const f32x4*)(turn + r * kRow + 32 + (lane & 7) * 4);
+        // (kGateGrad: G and U of kAhead turns are asked for together)
+        constexpr int kTurns = 32 / kTake, kAhead = EPI == kGateGrad ? 4 : 1;
+#pragma unroll 1
+        for (int k0 = 0; k0 < kTurns; k0 += kAhead) {
+        f32x4 gs[kAhead], us[kAhead];
+        if constexpr (EPI == kGateGrad) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int64_t m = mb + lane / kLanes + (k0 + k) * kTake;
+                gs[k] = us[k] = f32x4{};
+                if (m < p.M) {
+                    gs[k] = load4(p.saved + m * 2 * p.N, n, p.N, wide);
+                    us[k] = load4(p.saved + m * 2 * p.N + p.N, n, p.N, wide);
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int r = lane / kLanes + (k0 + k) * kTake;
+            const int64_t m = mb + r;
+            if (m >= p.M) continue;
+            const f32x4 v = *(const f32x4*)(turn + r * kRow + tc);
+            if constexpr (EPI == kGate) {
+                const f32x4 u = *(const f32x4*)(turn + r * kRow + CW / 2 + tc);
                 f32x4 h;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float v, dv;
-                    activate(p.act, g[e], v, dv);
-                    h[e] = v * u[e];
+                    float a, da;
+                    activate(p.act, v[e], a, da);
+                    h[e] = a * u[e];
                 }
                 store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, p.ldc, h, wide);
                 if (p.saved) {
-                    store4<float>(p.saved + m * 2 * p.N, n, p.N, 0, g, wide);
+                    store4<float>(p.saved + m * 2 * p.N, n, p.N, 0, v, wide);
                     store4<float>(p.saved + m * 2 * p.N + p.N, n, p.N, 0, u, wide);
                 }
-            }
-        } else {
-            const int64_t n = n0 + wn + (lane & 15) * 4;
-            for (int r = lane >> 4; r < 32; r += 4) {
-                const int64_t m = mb + r;
-                if (m >= p.M) break;
-                const f32x4 v = *(const f32x4*)(turn + r * kRow + (lane & 15) * 4);
-                if constexpr (EPI == kStore) {
-                    store4<Out>((Out*)p.c + m * p.ldc, n, p.N, 0, v, wide);
-                } else if constexpr (EPI == kPartial) {
-                    store4<float>((float*)p.c + ((int64_t)blockIdx.y * p.M + m) * p.ldc, n, p.N, 0, v, true);
-                } else {
-                    const f32x4 g = load4(p.saved + m * 2 * p.N, n, p.N, wide), u = load4(p.saved + m * 2 * p.N + p.N, n, p.N, wide);
-                    f32x4 dg, du, h;
+            } else if constexpr (EPI == kStore) {
+                store4<Out>((Out*)p.c + m * p.ldc, n, p.N, 0, v, wide);
+            } else if constexpr (EPI == kPartial) {
+                store4<float>((float*)p.c + ((int64_t)blockIdx.y * p.M + m) * p.ldc, n, p.N, 0, v, true);
+            } else {
+                const f32x4 g = gs[k], u = us[k];
+                f32x4 dg, du, h;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float a, da;
-                        activate(p.act, g[e], a, da);
-                        dg[e] = v[e] * u[e] * da;
-                        du[e] = v[e] * a;
-                        h[e] = a * u[e];
-                    }
-                    store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, 0, dg, wide);
-                    if constexpr (sizeof(Out) == 4)
-                        store4_planes((uint16_t*)p.c + m * p.ldc + p.N, p.plane_c, n, p.N, p.ldc - p.N, du, wide);
-                    else
-                        store4<T>((T*)p.c + m * p.ldc + p.N, n, p.N, p.ldc - p.N, du, wide);
-                    store_mid<T, Out>(p.h, m, p.ldh, p.plane_h, n, p.N, p.ldh, h, wide);
+                for (int e = 0; e < 4; ++e) {
+                    float a, da;
+                    activate(p.act, g[e], a, da);
+                    dg[e] = v[e] * u[e] * da;
+                    du[e] = v[e] * a;
+                    h[e] = a * u[e];
                 }
+                store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, 0, dg, wide);
+                if constexpr (sizeof(Out) == 4)
+                    store4_planes((uint16_t*)p.c + m * p.ldc + p.N, p.plane_c, n, p.N, p.ldc - p.N, du, wide);
+                else
+                    store4<T>((T*)p.c + m * p.ldc + p.N, n, p.N, p.ldc - p.N, du, wide);
+                store_mid<T, Out>(p.h, m, p.ldh, p.plane_h, n, p.N, p.ldh, h, wide);
             }
+        }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -361,15 +427,15 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
 #endif
 }
 
-template <typename T, typename Out, int BM, int WM, bool AC, bool BC, int EPI> int run_tile(const TileArgs& p, hipStream_t s) {
-    constexpr int WN = BM / 64;
+template <typename T, typename Out, int BM, bool AC, bool BC, int EPI> int run_tile(const TileArgs& p, hipStream_t s) {
+    constexpr int WM = 2, WN = BM == 256 ? 4 : 2;
     tile_kernel<T, Out, BM, BM, WM, WN, AC, BC, EPI><<<dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), 64 * WM * WN, 0, s>>>(p);
     return (int)hipGetLastError();
 }
 
 // tile: 256 or 128 (outputs a side of a work-group)
 template <typename T, typename Out> int run_product(const TileArgs& p, int32_t epilogue, bool ac, bool bc, int32_t tile, hipStream_t s) {
-#define FFN_RUN(AC, BC, EPI) (tile == 256 ? run_tile<T, Out, 256, 2, AC, BC, EPI>(p, s) : run_tile<T, Out, 128, 2, AC, BC, EPI>(p, s))
+#define FFN_RUN(AC, BC, EPI) (tile == 256 ? run_tile<T, Out, 256, AC, BC, EPI>(p, s) : run_tile<T, Out, 128, AC, BC, EPI>(p, s))
     if (epilogue == kGate && !ac && !bc) return FFN_RUN(false, false, kGate);
     if (epilogue == kGateGrad && !ac && bc) return FFN_RUN(false, true, kGateGrad);
     if (epilogue == kStore) {
