@@ -8,36 +8,47 @@ using namespace dev;
 
 constexpr int kThreads = 256;
 
-// A thread a chunk of eight values of the packed rows.
+// A thread a chunk of eight values of the packed rows; the work-groups are dealt to the matrices in turn.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void pack_kernel(const T* from, int64_t ld, int64_t rows, int64_t width, uint16_t* to,
-                                                        int64_t to_ld, int64_t plane) {
-    const int64_t chunks = to_ld >> 3, total = rows * chunks;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t row = i / chunks, c = (i - row * chunks) * 8;
-        const T* f = from + row * ld + c;
-        T v[8];
+__global__ __launch_bounds__(kThreads) void pack_kernel(PackJobs jobs) {
+    int k = 0, first = 0;
+    while (k + 1 < jobs.n && (int)blockIdx.x >= jobs.job[k].end) first = jobs.job[k++].end;
+    const PackJob& j = jobs.job[k];
+    const int64_t stride = (int64_t)(j.end - first) * kThreads;
+    const int64_t chunks = j.to_ld >> 3, total = j.rows * chunks;
+    int64_t i = (int64_t)((int)blockIdx.x - first) * kThreads + threadIdx.x;
+    int64_t row = i / chunks, at = i - row * chunks;
+    const int64_t dr = stride / chunks, da = stride - dr * chunks;
+    for (; i < total; i += stride) {
+        const int64_t c = at * 8;
+        const T* f = (const T*)j.from + row * j.ld + c;
+        typedef T V __attribute__((ext_vector_type(8)));
+        V v;
+        if (c + 8 <= j.width) {
+            __builtin_memcpy(&v, f, sizeof(v));
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c + j < width ? f[j] : (T)0.0f;
-        uint16_t* t = to + row * to_ld + c;
+            for (int e = 0; e < 8; ++e) v[e] = c + e < j.width ? f[e] : (T)0.0f;
+        }
+        uint16_t* t = (uint16_t*)j.to + row * j.to_ld + c;
         if constexpr (sizeof(T) == 4) {
             s16x8 o[3];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int e = 0; e < 8; ++e) {
                 uint16_t q[3];
-                planes_of(v[j], q);
-                o[0][j] = (short)q[0];
-                o[1][j] = (short)q[1];
-                o[2][j] = (short)q[2];
+                planes_of(v[e], q);
+                o[0][e] = (short)q[0];
+                o[1][e] = (short)q[1];
+                o[2][e] = (short)q[2];
             }
 #pragma unroll
-            for (int k = 0; k < 3; ++k) *(s16x8*)(t + k * plane) = o[k];
+            for (int e = 0; e < 3; ++e) *(s16x8*)(t + e * j.plane) = o[e];
         } else {
-            s16x8 o;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = __builtin_bit_cast(short, v[j]);
-            *(s16x8*)t = o;
+            *(s16x8*)t = __builtin_bit_cast(s16x8, v);
         }
+        row += dr;
+        at += da;
+        if (at >= chunks) { at -= chunks; ++row; }
     }
 }
 
@@ -53,6 +64,50 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float* partial, in
     }
 }
 
+// The joining of split sums with the gate's epilogues; the same arithmetic as the tiles' own.  kGate: the sums hold
+// [G U] (2 N columns); kGateGrad: dH.
+template <typename T, typename Out, int EPI>
+__global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const float* partial, int64_t ld) {
+    const int64_t quads = (p.N + 3) >> 2, total = p.M * quads;
+    const bool wide = p.wide;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t m = i / quads, n = (i - m * quads) * 4;
+        f32x4 v = {}, u = {};
+        for (int s = 0; s < p.splits; ++s) {
+            const float* from = partial + ((int64_t)s * p.M + m) * ld;
+            v += *(const f32x4*)(from + n);
+            if constexpr (EPI == kGate) u += load4(from + p.N, n, p.N, wide);
+        }
+        f32x4 h;
+        if constexpr (EPI == kGate) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float a, da;
+                activate(p.act, v[e], a, da);
+                h[e] = a * u[e];
+            }
+            store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, p.ldc, h, wide);
+            if (p.saved) {
+                store4<float>(p.saved + m * 2 * p.N, n, p.N, 0, v, wide);
+                store4<float>(p.saved + m * 2 * p.N + p.N, n, p.N, 0, u, wide);
+            }
+        } else {
+            const f32x4 g = load4(p.saved + m * 2 * p.N, n, p.N, wide);
+            u = load4(p.saved + m * 2 * p.N + p.N, n, p.N, wide);
+            f32x4 dg, du;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float a, da;
+                activate(p.act, g[e], a, da);
+                dg[e] = v[e] * u[e] * da;
+                du[e] = v[e] * a;
+                h[e] = a * u[e];
+            }
+            store_gate_grad<T, Out>(p, m, n, dg, du, h, wide);
+        }
+    }
+}
+
 // (a kernel, not a memset: it may be captured in a graph)
 __global__ __launch_bounds__(kThreads) void zero_kernel(uint16_t* p, int64_t n) {
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) p[i] = 0;
@@ -65,12 +120,29 @@ unsigned groups(int64_t n) {
 
 }  // namespace
 
-int launch_pack(const void* from, int64_t ld, int64_t rows, int64_t width, int32_t dtype, void* to, int64_t to_ld, int64_t plane,
-                void* stream) {
+int launch_pack(PackJobs jobs, int32_t dtype, void* stream) {
+    if (jobs.n == 0) return 0;
+    int end = 0;
+    for (int k = 0; k < jobs.n; ++k) {
+        const int64_t n = (jobs.job[k].rows * (jobs.job[k].to_ld >> 3) + kThreads - 1) / kThreads;
+        jobs.job[k].end = end += (int)(n < 4096 ? n : 4096);
+    }
     hipStream_t s = (hipStream_t)stream;
-    const unsigned g = groups(rows * (to_ld >> 3));
-    if (dtype == FFN_FP32) pack_kernel<float><<<g, kThreads, 0, s>>>((const float*)from, ld, rows, width, (uint16_t*)to, to_ld, plane);
-    else pack_kernel<bf16><<<g, kThreads, 0, s>>>((const bf16*)from, ld, rows, width, (uint16_t*)to, to_ld, plane);   // bits alone
+    if (dtype == FFN_FP32) pack_kernel<float><<<end, kThreads, 0, s>>>(jobs);
+    else pack_kernel<bf16><<<end, kThreads, 0, s>>>(jobs);   // bits alone
+    return (int)hipGetLastError();
+}
+
+int launch_join_gate(const TileArgs& p, int32_t epilogue, const float* partial, int64_t ld, int32_t dtype, void* stream) {
+    hipStream_t s = (hipStream_t)stream;
+    const unsigned g = groups(p.M * ((p.N + 3) >> 2));
+#define FFN_JOIN(T, OUT)                                                                                       \
+    if (epilogue == kGate) join_gate_kernel<T, OUT, kGate><<<g, kThreads, 0, s>>>(p, partial, ld);             \
+    else join_gate_kernel<T, OUT, kGateGrad><<<g, kThreads, 0, s>>>(p, partial, ld)
+    if (dtype == FFN_FP32) { FFN_JOIN(bf16, float); }
+    else if (dtype == FFN_BF16) { FFN_JOIN(bf16, bf16); }
+    else { FFN_JOIN(fp16, fp16); }
+#undef FFN_JOIN
     return (int)hipGetLastError();
 }
 

@@ -59,10 +59,22 @@ int launch_join(const float* partial, int64_t ld, int32_t splits, int64_t M, int
 
 int launch_zero(void* p, int64_t bytes, void* stream);
 
+// The same for the gate's epilogues (p as for the tile launch: p.c is H or [dG dU], p.splits the parts).
+int launch_join_gate(const TileArgs& p, int32_t epilogue, const float* partial, int64_t ld, int32_t dtype, void* stream);
+
 // [rows, width] of `dtype` with row stride ld -> 16-bit operand with row stride `to_ld` (zeros from width on): a copy,
-// or three planes, `plane` elements apart, of 32-bit values.
-int launch_pack(const void* from, int64_t ld, int64_t rows, int64_t width, int32_t dtype, void* to, int64_t to_ld,
-                int64_t plane, void* stream);
+// or three planes, `plane` elements apart, of 32-bit values.  Up to four matrices a launch.
+struct PackJob {
+    const void* from;
+    void* to;
+    int64_t ld, rows, width, to_ld, plane;
+    int32_t end;                          // work-groups up to here; set by the launcher
+};
+struct PackJobs {
+    PackJob job[4];
+    int32_t n;
+};
+int launch_pack(PackJobs jobs, int32_t dtype, void* stream);
 
 // ---------------------------------------------------------------- norms and dropout
 

@@ -97,18 +97,18 @@ int64_t tiles(int64_t n, int64_t t) { return (n + t - 1) / t; }
 // How a product is cut up: work-groups of `tile` x `tile` outputs, k in `splits` parts.
 struct Cut { int32_t tile, splits; };
 
-// The shortest by this count, in steps of a 256-wide tile (64 k): a compute unit takes one such work-group, or two of
-// the 128-wide, whose steps cost 0.33 of it each when both run (a quarter of the arithmetic, twice the operands read
-// for it); parts of k cost their partial sums, written and read once.
-Cut choose(int64_t M, int64_t N, int64_t steps, bool gate, bool may_split) {
+// The shortest by this count, in steps of a 256-wide tile (64 k; 1.6 us): a compute unit takes one such work-group, or
+// two of the 128-wide, whose steps take 0.66 of it when both run (measured on large bf16 products: 1.33 PFLOP/s with
+// 256-wide tiles, 1.0 with 128-wide); four steps stand for a tile's start and end.  Parts of k cost a launch (three
+// microseconds) and their sums, written and read once at 4 TB/s.
+Cut choose(int64_t M, int64_t N, int64_t steps) {
     Cut best = {256, 1};
     double least = 1e300;
     for (int32_t tile : {256, 128}) {
-        const int64_t groups = tiles(M, tile) * tiles(gate ? 2 * N : N, tile);
-        for (int32_t s = 1; s <= 64 && (s == 1 || (may_split && steps / s >= 4)); s *= 2) {
-            const double rounds = (double)tiles(groups * s, tile == 256 ? 256 : 512);
-            const double t = rounds * ((double)tiles(steps, s) + 4) * (tile == 256 ? 1.0 : 0.66) +
-                             (s > 1 ? 8.0 + (double)(M * N * s) * 8.0 / 4e6 : 0.0);
+        const int64_t groups = tiles(M, tile) * tiles(N, tile), slots = tile == 256 ? 256 : 512;
+        for (int32_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); ++s) {
+            const double t = (double)tiles(groups * s, slots) * ((double)tiles(steps, s) + 4) * (tile == 256 ? 1.6 : 1.06) +
+                             (s > 1 ? 3.0 + (double)(M * N * s) * 8.0 / 4e6 : 0.0);
             if (t < least) { least = t; best = {tile, s}; }
         }
     }
@@ -117,8 +117,9 @@ Cut choose(int64_t M, int64_t N, int64_t steps, bool gate, bool may_split) {
 
 int64_t steps_of(int64_t K, int32_t dtype) { return tiles(K, 64) * (dtype == FFN_FP32 ? 6 : 1); }
 
+// Bytes of the partial sums of an [M, N] product.
 int64_t partial_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype) {
-    const Cut c = choose(M, N, steps_of(K, dtype), false, true);
+    const Cut c = choose(M, N, steps_of(K, dtype));
     return c.splits > 1 ? aligned(c.splits * M * ((N + 3) & ~3LL) * 4) : 0;
 }
 
@@ -130,22 +131,27 @@ int launch_tile(const ffn::TileArgs& t, int32_t epilogue, bool ac, bool bc, int3
     }
 }
 
-// Runs the product whose operands, sizes and results `t` describes; `partial` is scratch of partial_bytes().
+// Runs the product whose operands, sizes and results `t` describes; `partial` is scratch of partial_bytes() (for kGate,
+// of 2 N columns).
 int product(ffn::TileArgs t, int32_t epilogue, bool ac, bool bc, int32_t dtype, void* partial, void* stream) {
     t.planes = dtype == FFN_FP32 ? 3 : 1;
-    const Cut c = choose(t.M, t.N, steps_of(t.K, dtype), epilogue == ffn::kGate, epilogue == ffn::kStore);
-    const int64_t tm = tiles(t.M, c.tile), tn = tiles(epilogue == ffn::kGate ? 2 * t.N : t.N, c.tile);
+    const int64_t columns = epilogue == ffn::kGate ? 2 * t.N : t.N;
+    const Cut c = choose(t.M, columns, steps_of(t.K, dtype));
+    const int64_t tm = tiles(t.M, c.tile), tn = tiles(columns, c.tile);
     if (tm * tn > 0x7FFFFFFF / 512) return CGTP_EUNSUP;   // threads of a launch
     t.tiles_m = (int32_t)tm;
     t.tiles_n = (int32_t)tn;
     t.splits = c.splits;
     if (c.splits == 1) return status(launch_tile(t, epilogue, ac, bc, dtype, c.tile, stream));
-    void* out = t.c;
-    t.c = partial;
-    t.ldc = (t.N + 3) & ~3LL;
-    const int rc = status(launch_tile(t, ffn::kPartial, ac, bc, dtype, c.tile, stream));
+    ffn::TileArgs s = t;
+    s.c = partial;
+    s.N = columns;
+    s.ldc = (columns + 3) & ~3LL;
+    const int rc = status(launch_tile(s, ffn::kPartial, ac, bc, dtype, c.tile, stream));
     if (rc != CGTP_OK) return rc;
-    return status(ffn::launch_join((const float*)partial, t.ldc, c.splits, t.M, t.N, out, dtype, stream));
+    if (epilogue == ffn::kStore)
+        return status(ffn::launch_join((const float*)partial, s.ldc, c.splits, t.M, t.N, t.c, dtype, stream));
+    return status(ffn::launch_join_gate(t, epilogue, (const float*)partial, s.ldc, dtype, stream));
 }
 
 // A product for few rows: weight rows a work-group, and waves (parts of k).  Measured, bf16: below one work-group of
@@ -180,13 +186,11 @@ bool as_is(const void* p, int64_t ld, int64_t rows, int64_t width, int32_t dtype
     return dtype != FFN_FP32 && ((uintptr_t)p & 15) == 0 && width % 8 == 0 && (ld % 8 == 0 || rows == 1);
 }
 
-int operand(const void* p, int64_t ld, int64_t rows, int64_t width, int32_t dtype, void* scratch, void* stream, Operand* o) {
-    if (as_is(p, ld, rows, width, dtype)) {
-        *o = {p, ld % 8 == 0 ? ld : up8(ld), 0};
-        return CGTP_OK;
-    }
-    *o = {scratch, up8(width), packed(rows, width)};
-    return status(ffn::launch_pack(p, ld, rows, width, dtype, scratch, o->ld, o->plane, stream));
+Operand operand(const void* p, int64_t ld, int64_t rows, int64_t width, int32_t dtype, void* scratch, ffn::PackJobs* jobs) {
+    if (as_is(p, ld, rows, width, dtype)) return {p, ld % 8 == 0 ? ld : up8(width), 0};
+    const Operand o = {scratch, up8(width), packed(rows, width)};
+    jobs->job[jobs->n++] = {p, scratch, ld, rows, width, o.ld, o.plane, 0};
+    return o;
 }
 
 // Byte offsets in the block's workspace: intermediates, operands to be packed, partial sums.
@@ -207,10 +211,12 @@ Layout layout(const ffn_plan_s* p, int64_t N, bool backward) {
     if (backward) {
         l.dgu = take(packed_bytes(N, 2 * df, t));
         l.gy = take(packed_bytes(N, d_o, t));
+        also(partial_bytes(N, df, d_o, t));
         also(partial_bytes(N, di, 2 * df, t));
         also(partial_bytes(2 * df, di, N, t));
         also(partial_bytes(d_o, df, N, t));
     } else {
+        also(partial_bytes(N, 2 * df, di, t));
         also(partial_bytes(N, d_o, df, t));
     }
     l.partial = take(partial);
@@ -321,10 +327,10 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
         o.wide = wide4({y}, {d_o});
         return few_product(o, ffn::kStore, plan->dtype, hip_stream);
     }
-    Operand X, Wi, Wo;
-    rc = operand(x, ldx, N, di, plan->dtype, ws + l.x, hip_stream, &X);
-    if (rc == CGTP_OK) rc = operand(w_in, di, 2 * df, di, plan->dtype, ws + l.w_in, hip_stream, &Wi);
-    if (rc == CGTP_OK) rc = operand(w_out, df, d_o, df, plan->dtype, ws + l.w_out, hip_stream, &Wo);
+    ffn::PackJobs jobs = {};
+    const Operand X = operand(x, ldx, N, di, plan->dtype, ws + l.x, &jobs), Wi = operand(w_in, di, 2 * df, di, plan->dtype, ws + l.w_in, &jobs),
+                  Wo = operand(w_out, df, d_o, df, plan->dtype, ws + l.w_out, &jobs);
+    rc = status(ffn::launch_pack(jobs, plan->dtype, hip_stream));
     if (rc != CGTP_OK) return rc;
     ffn::TileArgs g = {};
     g.a = X.p; g.lda = X.ld; g.plane_a = X.plane;
@@ -333,7 +339,7 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
     g.c = ws + l.h; g.ldc = up8(df); g.plane_c = packed(N, df);
     g.act = plan->act; g.saved = (float*)saved;
     g.wide = wide4({saved}, {df});
-    rc = product(g, ffn::kGate, false, false, plan->dtype, nullptr, hip_stream);
+    rc = product(g, ffn::kGate, false, false, plan->dtype, ws + l.partial, hip_stream);
     if (rc != CGTP_OK) return rc;
     return down(plan, ws + l.h, Wo, y, N, ws + l.partial, hip_stream);
 }
@@ -364,9 +370,12 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
         return rc;
     }
     char* ws = (char*)workspace;
-    Operand X, Wi, Wo, Gy;
-    rc = operand(grad_y, ldg, N, d_o, plan->dtype, ws + l.gy, hip_stream, &Gy);
-    if (rc == CGTP_OK) rc = operand(w_out, df, d_o, df, plan->dtype, ws + l.w_out, hip_stream, &Wo);
+    ffn::PackJobs jobs = {};
+    const Operand Gy = operand(grad_y, ldg, N, d_o, plan->dtype, ws + l.gy, &jobs), Wo = operand(w_out, df, d_o, df, plan->dtype, ws + l.w_out, &jobs);
+    Operand X = {}, Wi = {};
+    if (grad_x) Wi = operand(w_in, di, 2 * df, di, plan->dtype, ws + l.w_in, &jobs);
+    if (grad_w_in) X = operand(x, ldx, N, di, plan->dtype, ws + l.x, &jobs);
+    rc = status(ffn::launch_pack(jobs, plan->dtype, hip_stream));
     if (rc != CGTP_OK) return rc;
     const Operand H = {ws + l.h, up8(df), packed(N, df)}, D = {ws + l.dgu, up8(2 * df), packed(N, 2 * df)};
     ffn::TileArgs g = {};
@@ -377,10 +386,8 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
     g.h = ws + l.h; g.ldh = H.ld; g.plane_h = H.plane;
     g.act = plan->act; g.saved = (float*)const_cast<void*>(saved);
     g.wide = wide4({saved}, {df});
-    rc = product(g, ffn::kGateGrad, false, true, plan->dtype, nullptr, hip_stream);
+    rc = product(g, ffn::kGateGrad, false, true, plan->dtype, ws + l.partial, hip_stream);
     if (rc == CGTP_OK && grad_x) {
-        rc = operand(w_in, di, 2 * df, di, plan->dtype, ws + l.w_in, hip_stream, &Wi);
-        if (rc != CGTP_OK) return rc;
         ffn::TileArgs t = {};
         t.a = D.p; t.lda = D.ld; t.plane_a = D.plane;
         t.b = Wi.p; t.ldb = Wi.ld; t.plane_b = Wi.plane;
@@ -390,8 +397,6 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
         rc = product(t, ffn::kStore, false, true, plan->dtype, ws + l.partial, hip_stream);
     }
     if (rc == CGTP_OK && grad_w_in) {
-        rc = operand(x, ldx, N, di, plan->dtype, ws + l.x, hip_stream, &X);
-        if (rc != CGTP_OK) return rc;
         ffn::TileArgs t = {};
         t.a = D.p; t.lda = D.ld; t.plane_a = D.plane;
         t.b = X.p; t.ldb = X.ld; t.plane_b = X.plane;

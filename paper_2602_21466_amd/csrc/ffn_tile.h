@@ -106,6 +106,17 @@ template <typename T, typename Out> __device__ __forceinline__ void store_mid(vo
     else store4<T>((T*)base + row * ld, n, N, pad, v, wide);
 }
 
+// dG and dU side by side (zeros behind dU), and H
+template <typename T, typename Out> __device__ __forceinline__ void store_gate_grad(const TileArgs& p, int64_t m, int64_t n, f32x4 dg,
+                                                                                   f32x4 du, f32x4 h, bool wide) {
+    store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, 0, dg, wide);
+    if constexpr (sizeof(Out) == 4)
+        store4_planes((uint16_t*)p.c + m * p.ldc + p.N, p.plane_c, n, p.N, p.ldc - p.N, du, wide);
+    else
+        store4<T>((T*)p.c + m * p.ldc + p.N, n, p.N, p.ldc - p.N, du, wide);
+    store_mid<T, Out>(p.h, m, p.ldh, p.plane_h, n, p.N, p.ldh, h, wide);
+}
+
 __device__ __forceinline__ f32x4 load4(const float* p, int64_t n, int64_t N, bool wide) {
     if (wide && n + 3 < N) return *(const f32x4*)(p + n);
     f32x4 v = {};
@@ -412,12 +423,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
                     du[e] = v[e] * a;
                     h[e] = a * u[e];
                 }
-                store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, 0, dg, wide);
-                if constexpr (sizeof(Out) == 4)
-                    store4_planes((uint16_t*)p.c + m * p.ldc + p.N, p.plane_c, n, p.N, p.ldc - p.N, du, wide);
-                else
-                    store4<T>((T*)p.c + m * p.ldc + p.N, n, p.N, p.ldc - p.N, du, wide);
-                store_mid<T, Out>(p.h, m, p.ldh, p.plane_h, n, p.N, p.ldh, h, wide);
+                store_gate_grad<T, Out>(p, m, n, dg, du, h, wide);
             }
         }
         }
