@@ -162,13 +162,13 @@ __global__ __launch_bounds__(512) void few_kernel(FewArgs p) {
                 activate(p.act, v[e], a, da);
                 h[e] = a * u[e];
             }
-            store4<T>((T*)p.c + r * p.ldc, n, p.N, p.ldc, h, p.wide);
+            store4<T>((T*)p.c + r * p.ldc, n, p.N, p.ldc, h);
             if (p.saved) {
-                store4<float>(p.saved + r * 2 * p.N, n, p.N, 0, v, p.wide);
-                store4<float>(p.saved + r * 2 * p.N + p.N, n, p.N, 0, u, p.wide);
+                store4<float>(p.saved + r * 2 * p.N, n, p.N, 0, v);
+                store4<float>(p.saved + r * 2 * p.N + p.N, n, p.N, 0, u);
             }
         } else {
-            store4<T>((T*)p.c + r * p.ldc, n, p.N, 0, v, p.wide);
+            store4<T>((T*)p.c + r * p.ldc, n, p.N, 0, v);
         }
     }
 #endif

@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float* partial, in
         const int64_t row = i / quads, c = (i - row * quads) * 4;
         f32x4 v = {};
         for (int s = 0; s < splits; ++s) v += *(const f32x4*)(partial + ((int64_t)s * M + row) * ld + c);
-        store4<Out>(out + row * N, c, N, 0, v, (N & 3) == 0);
+        store4<Out>(out + row * N, c, N, 0, v);
     }
 }
 
@@ -69,14 +69,13 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float* partial, in
 template <typename T, typename Out, int EPI>
 __global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const float* partial, int64_t ld) {
     const int64_t quads = (p.N + 3) >> 2, total = p.M * quads;
-    const bool wide = p.wide;
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
         const int64_t m = i / quads, n = (i - m * quads) * 4;
         f32x4 v = {}, u = {};
         for (int s = 0; s < p.splits; ++s) {
             const float* from = partial + ((int64_t)s * p.M + m) * ld;
             v += *(const f32x4*)(from + n);
-            if constexpr (EPI == kGate) u += load4(from + p.N, n, p.N, wide);
+            if constexpr (EPI == kGate) u += load4(from + p.N, n, p.N);
         }
         f32x4 h;
         if constexpr (EPI == kGate) {
@@ -86,14 +85,14 @@ __global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const f
                 activate(p.act, v[e], a, da);
                 h[e] = a * u[e];
             }
-            store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, p.ldc, h, wide);
+            store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, p.ldc, h);
             if (p.saved) {
-                store4<float>(p.saved + m * 2 * p.N, n, p.N, 0, v, wide);
-                store4<float>(p.saved + m * 2 * p.N + p.N, n, p.N, 0, u, wide);
+                store4<float>(p.saved + m * 2 * p.N, n, p.N, 0, v);
+                store4<float>(p.saved + m * 2 * p.N + p.N, n, p.N, 0, u);
             }
         } else {
-            const f32x4 g = load4(p.saved + m * 2 * p.N, n, p.N, wide);
-            u = load4(p.saved + m * 2 * p.N + p.N, n, p.N, wide);
+            const f32x4 g = load4(p.saved + m * 2 * p.N, n, p.N);
+            u = load4(p.saved + m * 2 * p.N + p.N, n, p.N);
             f32x4 dg, du;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -103,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const f
                 du[e] = v[e] * a;
                 h[e] = a * u[e];
             }
-            store_gate_grad<T, Out>(p, m, n, dg, du, h, wide);
+            store_gate_grad<T, Out>(p, m, n, dg, du, h);
         }
     }
 }

@@ -31,7 +31,6 @@ struct TileArgs {
     float* saved;                         // [M, 2 N]
     void* h;                              // kGateGrad: H
     int64_t ldh, plane_h;
-    int32_t wide;                         // rows of c, h and saved start on a multiple of four elements of theirs
 };
 
 int launch_tile_bf16(const TileArgs& p, int32_t epilogue, bool a_cols, bool b_cols, int32_t tile, void* stream);
@@ -48,7 +47,6 @@ struct FewArgs {
     int64_t ldc;
     float* saved;                         // kGate: [M, 2 N] or NULL
     int32_t act;
-    int32_t wide;                         // as TileArgs::wide
 };
 int launch_few_bf16(const FewArgs& p, int32_t epilogue, int32_t nr, int32_t waves, void* stream);
 int launch_few_fp16(const FewArgs& p, int32_t epilogue, int32_t nr, int32_t waves, void* stream);

@@ -138,7 +138,7 @@ int product(ffn::TileArgs t, int32_t epilogue, bool ac, bool bc, int32_t dtype, 
     const int64_t columns = epilogue == ffn::kGate ? 2 * t.N : t.N;
     const Cut c = choose(t.M, columns, steps_of(t.K, dtype));
     const int64_t tm = tiles(t.M, c.tile), tn = tiles(columns, c.tile);
-    if (tm * tn > 0x7FFFFFFF / 512) return CGTP_EUNSUP;   // threads of a launch
+    if (tm * tn * c.splits > 0x7FFFFFFF / 512) return CGTP_EUNSUP;   // threads of a launch
     t.tiles_m = (int32_t)tm;
     t.tiles_n = (int32_t)tn;
     t.splits = c.splits;
@@ -241,12 +241,6 @@ int dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t N, int64_t
                                : ffn::launch_dropout_fp16(x, ldx, y, ldy, N, width, d, stream);
 }
 
-bool wide4(std::initializer_list<const void*> ps, std::initializer_list<int64_t> widths) {
-    int64_t all = 0;
-    for (int64_t w : widths) all |= w;
-    return !misaligned(ps, 16) && (all & 3) == 0;
-}
-
 // Y = H Wo^T by tiles.
 int down(const ffn_plan_s* plan, const void* h, const Operand& w, void* y, int64_t N, void* partial, void* stream) {
     ffn::TileArgs o = {};
@@ -254,7 +248,6 @@ int down(const ffn_plan_s* plan, const void* h, const Operand& w, void* y, int64
     o.b = w.p; o.ldb = w.ld; o.plane_b = w.plane;
     o.M = N; o.N = plan->d_out; o.K = plan->d_ff;
     o.c = y; o.ldc = plan->d_out;
-    o.wide = wide4({y}, {plan->d_out});
     return product(o, ffn::kStore, false, false, plan->dtype, partial, stream);
 }
 
@@ -314,7 +307,6 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
         g.M = N; g.N = df; g.K = di;
         g.c = ws + l.h; g.ldc = up8(df);
         g.act = plan->act; g.saved = (float*)saved;
-        g.wide = wide4({saved}, {df});
         rc = few_product(g, ffn::kGate, plan->dtype, hip_stream);
         if (rc != CGTP_OK) return rc;
         // from here on the weights alone are many: 16-bit ones that need no packing go through LDS in 128-wide tiles with
@@ -324,7 +316,6 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
         o.x = ws + l.h; o.ldx = up8(df); o.w = w_out; o.ldw = df;
         o.M = N; o.N = d_o; o.K = df;
         o.c = y; o.ldc = d_o;
-        o.wide = wide4({y}, {d_o});
         return few_product(o, ffn::kStore, plan->dtype, hip_stream);
     }
     ffn::PackJobs jobs = {};
@@ -338,7 +329,6 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
     g.M = N; g.N = df; g.K = di;
     g.c = ws + l.h; g.ldc = up8(df); g.plane_c = packed(N, df);
     g.act = plan->act; g.saved = (float*)saved;
-    g.wide = wide4({saved}, {df});
     rc = product(g, ffn::kGate, false, false, plan->dtype, ws + l.partial, hip_stream);
     if (rc != CGTP_OK) return rc;
     return down(plan, ws + l.h, Wo, y, N, ws + l.partial, hip_stream);
@@ -385,7 +375,6 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
     g.c = ws + l.dgu; g.ldc = D.ld; g.plane_c = D.plane;
     g.h = ws + l.h; g.ldh = H.ld; g.plane_h = H.plane;
     g.act = plan->act; g.saved = (float*)const_cast<void*>(saved);
-    g.wide = wide4({saved}, {df});
     rc = product(g, ffn::kGateGrad, false, true, plan->dtype, ws + l.partial, hip_stream);
     if (rc == CGTP_OK && grad_x) {
         ffn::TileArgs t = {};
@@ -393,7 +382,6 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
         t.b = Wi.p; t.ldb = Wi.ld; t.plane_b = Wi.plane;
         t.M = N; t.N = di; t.K = 2 * df;
         t.c = grad_x; t.ldc = di;
-        t.wide = wide4({grad_x}, {di});
         rc = product(t, ffn::kStore, false, true, plan->dtype, ws + l.partial, hip_stream);
     }
     if (rc == CGTP_OK && grad_w_in) {
@@ -402,7 +390,6 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
         t.b = X.p; t.ldb = X.ld; t.plane_b = X.plane;
         t.M = 2 * df; t.N = di; t.K = N;
         t.c = grad_w_in; t.ldc = di;
-        t.wide = wide4({grad_w_in}, {di});
         rc = product(t, ffn::kStore, true, true, plan->dtype, ws + l.partial, hip_stream);
     }
     if (rc == CGTP_OK && grad_w_out) {
@@ -411,7 +398,6 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
         t.b = H.p; t.ldb = H.ld; t.plane_b = H.plane;
         t.M = d_o; t.N = df; t.K = N;
         t.c = grad_w_out; t.ldc = df;
-        t.wide = wide4({grad_w_out}, {df});
         rc = product(t, ffn::kStore, true, true, plan->dtype, ws + l.partial, hip_stream);
     }
     return rc;

@@ -61,15 +61,16 @@ __device__ __forceinline__ void planes_of(float x, uint16_t (&p)[3]) {
     p[2] = (uint16_t)(__builtin_bit_cast(uint32_t, x2) >> 16);
 }
 
-// Four adjacent values of a row, columns n .. n + 3, in the arrays' type; whoever stores column N - 1 also
-// writes zeros up to column `pad`, for products that read whole 16-byte chunks of the row.
-template <typename Out> __device__ __forceinline__ void store4(Out* p, int64_t n, int64_t N, int64_t pad, f32x4 v, bool wide) {
+// Four adjacent values of a row, columns n .. n + 3, in the arrays' type, by one store where all are inside (rows may
+// start on any element: memory takes wide accesses at any address); whoever stores column N - 1 also writes zeros up to
+// column `pad`, for products that read whole 16-byte chunks of the row.
+template <typename Out> __device__ __forceinline__ void store4(Out* p, int64_t n, int64_t N, int64_t pad, f32x4 v) {
     typedef Out Out4 __attribute__((ext_vector_type(4)));
-    if (wide && n + 3 < N) {
+    if (n + 3 < N) {
         Out4 o;
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = (Out)v[j];
-        *(Out4*)(p + n) = o;
+        __builtin_memcpy(p + n, &o, sizeof(o));
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -80,15 +81,16 @@ template <typename Out> __device__ __forceinline__ void store4(Out* p, int64_t n
 }
 
 // The same for a 32-bit intermediate kept as three planes.
-__device__ __forceinline__ void store4_planes(uint16_t* p, int64_t plane, int64_t n, int64_t N, int64_t pad, f32x4 v, bool wide) {
+__device__ __forceinline__ void store4_planes(uint16_t* p, int64_t plane, int64_t n, int64_t N, int64_t pad, f32x4 v) {
     uint16_t q[4][3];
 #pragma unroll
     for (int j = 0; j < 4; ++j) planes_of(v[j], q[j]);
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
         uint16_t* r = p + i * plane;
-        if (wide && n + 3 < N) {
-            *(s16x4*)(r + n) = s16x4{(short)q[0][i], (short)q[1][i], (short)q[2][i], (short)q[3][i]};
+        if (n + 3 < N) {
+            const s16x4 o = {(short)q[0][i], (short)q[1][i], (short)q[2][i], (short)q[3][i]};
+            __builtin_memcpy(r + n, &o, sizeof(o));
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -101,28 +103,31 @@ __device__ __forceinline__ void store4_planes(uint16_t* p, int64_t plane, int64_
 
 // An intermediate (H, dG, dU): in T, or as planes of T where the arrays hold 32 bits.
 template <typename T, typename Out> __device__ __forceinline__ void store_mid(void* base, int64_t row, int64_t ld, int64_t plane, int64_t n,
-                                                                              int64_t N, int64_t pad, f32x4 v, bool wide) {
-    if constexpr (sizeof(Out) == 4) store4_planes((uint16_t*)base + row * ld, plane, n, N, pad, v, wide);
-    else store4<T>((T*)base + row * ld, n, N, pad, v, wide);
+                                                                              int64_t N, int64_t pad, f32x4 v) {
+    if constexpr (sizeof(Out) == 4) store4_planes((uint16_t*)base + row * ld, plane, n, N, pad, v);
+    else store4<T>((T*)base + row * ld, n, N, pad, v);
 }
 
 // dG and dU side by side (zeros behind dU), and H
 template <typename T, typename Out> __device__ __forceinline__ void store_gate_grad(const TileArgs& p, int64_t m, int64_t n, f32x4 dg,
-                                                                                   f32x4 du, f32x4 h, bool wide) {
-    store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, 0, dg, wide);
+                                                                                   f32x4 du, f32x4 h) {
+    store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, 0, dg);
     if constexpr (sizeof(Out) == 4)
-        store4_planes((uint16_t*)p.c + m * p.ldc + p.N, p.plane_c, n, p.N, p.ldc - p.N, du, wide);
+        store4_planes((uint16_t*)p.c + m * p.ldc + p.N, p.plane_c, n, p.N, p.ldc - p.N, du);
     else
-        store4<T>((T*)p.c + m * p.ldc + p.N, n, p.N, p.ldc - p.N, du, wide);
-    store_mid<T, Out>(p.h, m, p.ldh, p.plane_h, n, p.N, p.ldh, h, wide);
+        store4<T>((T*)p.c + m * p.ldc + p.N, n, p.N, p.ldc - p.N, du);
+    store_mid<T, Out>(p.h, m, p.ldh, p.plane_h, n, p.N, p.ldh, h);
 }
 
-__device__ __forceinline__ f32x4 load4(const float* p, int64_t n, int64_t N, bool wide) {
-    if (wide && n + 3 < N) return *(const f32x4*)(p + n);
+__device__ __forceinline__ f32x4 load4(const float* p, int64_t n, int64_t N) {
     f32x4 v = {};
+    if (n + 3 < N) {
+        __builtin_memcpy(&v, p + n, sizeof(v));
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (n + j < N) v[j] = p[n + j];
+        for (int j = 0; j < 4; ++j)
+            if (n + j < N) v[j] = p[n + j];
+    }
     return v;
 }
 
@@ -227,12 +232,14 @@ template <int R, bool COLS> struct Fragments {
     }
 };
 
-// Which tile a work-group takes.  Consecutive work-groups go to the eight dies in turn; each die gets a run of
-// consecutive tiles, and a run walks down eight rows of tiles before it moves one column on, so that a die's L2
-// holds what its tiles share.
-__device__ __forceinline__ void place(int id, int total, int tm, int tn, int& m, int& n) {
-    const int die = id & 7, per = total >> 3, more = total & 7;
-    const int t = die * per + (die < more ? die : more) + (id >> 3);
+// Which part of k and which tile a work-group takes.  Consecutive work-groups go to the eight dies in turn; each die gets
+// a run of consecutive tiles of one part, and a run walks down eight rows of tiles before it moves one column on, so
+// that a die's L2 holds what its tiles share (down projection, 8192 x 4096 x 16384: 1.28 against 0.99 PFLOP/s without).
+__device__ __forceinline__ void place(int id, int tm, int tn, int splits, int& m, int& n, int& split) {
+    const int tiles = tm * tn, total = tiles * splits, die = id & 7, per = total >> 3, more = total & 7;
+    int t = die * per + (die < more ? die : more) + (id >> 3);
+    split = t / tiles;
+    t -= split * tiles;
     constexpr int kGroup = 8;
     const int band = t / (kGroup * tn), r = t - band * kGroup * tn;
     const int rows = tm - band * kGroup < kGroup ? tm - band * kGroup : kGroup;
@@ -248,9 +255,8 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
     __shared__ __align__(1024) char sa1[BM * 128], sb1[BN * 128];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * CW;
-    const int total = p.tiles_m * p.tiles_n;
-    int tm, tn;
-    place(blockIdx.x, total, p.tiles_m, p.tiles_n, tm, tn);
+    int tm, tn, split;
+    place(blockIdx.x, p.tiles_m, p.tiles_n, p.splits, tm, tn, split);
     constexpr int kCols = EPI == kGate ? BN / 2 : BN;      // columns of C a tile covers
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * kCols;
 
@@ -261,7 +267,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
 
     // this split's steps, of 64 k each, one product of planes after the other
     const int nk = (int)((p.K + 63) >> 6), pairs = p.planes == 3 ? 6 : 1, steps = nk * pairs;
-    const int s0 = (int)((int64_t)steps * blockIdx.y / p.splits), s1 = (int)((int64_t)steps * (blockIdx.y + 1) / p.splits);
+    const int s0 = (int)((int64_t)steps * split / p.splits), s1 = (int)((int64_t)steps * (split + 1) / p.splits);
     int pair = s0 / nk, ks = s0 - pair * nk;
 
     auto issue = [&](char* a, char* b) {
@@ -359,7 +365,6 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
     constexpr int kFit = (BM < BN ? BM : BN) * 128 / kTurn;
     static_assert(kFit >= 1 && 4 * kFit >= NW, "a turn buffer for every wave");
     float* turn = (float*)((wave / kFit == 0 ? sa0 : wave / kFit == 1 ? sb0 : wave / kFit == 2 ? sa1 : sb1) + wave % kFit * kTurn);
-    const bool wide = p.wide;
     constexpr int kLanes = EPI == kGate ? CW / 8 : CW / 4, kTake = 64 / kLanes;      // lanes a row, rows a turn
     const int tc = (lane % kLanes) * 4;
 #pragma unroll
@@ -383,8 +388,8 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
                 const int64_t m = mb + lane / kLanes + (k0 + k) * kTake;
                 gs[k] = us[k] = f32x4{};
                 if (m < p.M) {
-                    gs[k] = load4(p.saved + m * 2 * p.N, n, p.N, wide);
-                    us[k] = load4(p.saved + m * 2 * p.N + p.N, n, p.N, wide);
+                    gs[k] = load4(p.saved + m * 2 * p.N, n, p.N);
+                    us[k] = load4(p.saved + m * 2 * p.N + p.N, n, p.N);
                 }
             }
         }
@@ -403,15 +408,15 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
                     activate(p.act, v[e], a, da);
                     h[e] = a * u[e];
                 }
-                store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, p.ldc, h, wide);
+                store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, p.ldc, h);
                 if (p.saved) {
-                    store4<float>(p.saved + m * 2 * p.N, n, p.N, 0, v, wide);
-                    store4<float>(p.saved + m * 2 * p.N + p.N, n, p.N, 0, u, wide);
+                    store4<float>(p.saved + m * 2 * p.N, n, p.N, 0, v);
+                    store4<float>(p.saved + m * 2 * p.N + p.N, n, p.N, 0, u);
                 }
             } else if constexpr (EPI == kStore) {
-                store4<Out>((Out*)p.c + m * p.ldc, n, p.N, 0, v, wide);
+                store4<Out>((Out*)p.c + m * p.ldc, n, p.N, 0, v);
             } else if constexpr (EPI == kPartial) {
-                store4<float>((float*)p.c + ((int64_t)blockIdx.y * p.M + m) * p.ldc, n, p.N, 0, v, true);
+                store4<float>((float*)p.c + ((int64_t)split * p.M + m) * p.ldc, n, p.N, 0, v);
             } else {
                 const f32x4 g = gs[k], u = us[k];
                 f32x4 dg, du, h;
@@ -423,7 +428,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
                     du[e] = v[e] * a;
                     h[e] = a * u[e];
                 }
-                store_gate_grad<T, Out>(p, m, n, dg, du, h, wide);
+                store_gate_grad<T, Out>(p, m, n, dg, du, h);
             }
         }
         }
@@ -435,7 +440,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
 
 template <typename T, typename Out, int BM, bool AC, bool BC, int EPI> int run_tile(const TileArgs& p, hipStream_t s) {
     constexpr int WM = 2, WN = BM == 256 ? 4 : 2;
-    tile_kernel<T, Out, BM, BM, WM, WN, AC, BC, EPI><<<dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), 64 * WM * WN, 0, s>>>(p);
+    tile_kernel<T, Out, BM, BM, WM, WN, AC, BC, EPI><<<dim3((unsigned)(p.tiles_m * p.tiles_n * p.splits)), 64 * WM * WN, 0, s>>>(p);
     return (int)hipGetLastError();
 }
 
