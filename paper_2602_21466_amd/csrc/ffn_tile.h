@@ -265,13 +265,14 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
     la.init(p.a, p.lda, m0, p.M, 0, wave, lane);
     lb.init(p.b, p.ldb, n0, p.N, p.N, wave, lane);
 
-    // this split's steps, of 64 k each, one product of planes after the other
+    // this split's steps, of 64 k each; the six products of planes of one 64 follow each other, while their operands are
+    // in L2
     const int nk = (int)((p.K + 63) >> 6), pairs = p.planes == 3 ? 6 : 1, steps = nk * pairs;
     const int s0 = (int)((int64_t)steps * split / p.splits), s1 = (int)((int64_t)steps * (split + 1) / p.splits);
-    int pair = s0 / nk, ks = s0 - pair * nk;
+    int ks = s0 / pairs, pair = s0 - ks * pairs;
 
     auto issue = [&](char* a, char* b) {
-        // products (0, 2), (2, 0), (1, 1), (0, 1), (1, 0), (0, 0): the smallest first
+        // planes (0, 2), (2, 0), (1, 1), (0, 1), (1, 0), (0, 0)
         const int pa = p.planes == 3 ? (0x010120 >> (4 * pair)) & 3 : 0, pb = p.planes == 3 ? (0x001102 >> (4 * pair)) & 3 : 0;
         la.seek(pa * p.plane_a * 2 + ks * la.step);
         lb.seek(pb * p.plane_b * 2 + ks * lb.step);
@@ -279,7 +280,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
         const int left = rest < 64 ? (int)rest : 64;
         la.issue(a, wave, left);
         lb.issue(b, wave, left);
-        if (++ks == nk) { ks = 0; ++pair; }
+        if (++pair == pairs) { pair = 0; ++ks; }
     };
 
     f32x4 acc[MT][NT] = {};
