@@ -138,9 +138,20 @@ def ffn_dropout(x_ptr, ldx, y_ptr, ldy, N, width, dtype, p, seed, offset, stream
 _U64 = (1 << 64) - 1
 
 
-def _torch_dtype(dtype):
-    import torch
-    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+class _Torch:
+    """What the calls below need of torch, imported with the first of them."""
+
+    def __getattr__(self, name):
+        import torch
+        self.empty, self.empty_like, self.float32, self.uint8 = torch.empty, torch.empty_like, torch.float32, torch.uint8
+        self.raw_stream, self.on_stream = torch._C._cuda_getCurrentRawStream, torch.cuda.stream
+        self.dtypes = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+        self.codes = {t: _DTYPES[name] for name, t in self.dtypes.items()}
+        self.devices = [torch.device("cuda", i) for i in range(max(torch.cuda.device_count(), 1))]
+        return self.__dict__[name]
+
+
+_t = _Torch()
 
 
 def _rows(t, tdt, rows, width, what, dev=None):
@@ -169,35 +180,22 @@ def _whole(t, tdt, shape, what, dev):
 def _stream(stream, dev):
     """The HIP stream's handle, and the torch stream where it is not the current one."""
     if stream is None:
-        import torch
-        return torch._C._cuda_getCurrentRawStream(dev), None
+        return _t.raw_stream(dev), None
     return stream.cuda_stream, stream
 
 
 def _new(shape, dtype, dev, other):
     """A new tensor of the stream `other` (None: the current one), so that its memory is reused in that stream's order."""
-    import torch
     if other is None:
-        return torch.empty(shape, dtype=dtype, device=_devices[dev])
-    with torch.cuda.stream(other):
-        return torch.empty(shape, dtype=dtype, device=_devices[dev])
-
-
-class _Devices(dict):
-    def __missing__(self, dev):
-        import torch
-        d = self[dev] = torch.device("cuda", dev)
-        return d
-
-
-_devices = _Devices()
+        return _t.empty(shape, dtype=dtype, device=_t.devices[dev])
+    with _t.on_stream(other):
+        return _t.empty(shape, dtype=dtype, device=_t.devices[dev])
 
 
 def _workspace(workspace, need, dev, other):
-    import torch
     if workspace is None:
-        return _new((max(need, 1),), torch.uint8, dev, other)
-    if workspace.dtype != torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous() or \
+        return _new((max(need, 1),), _t.uint8, dev, other)
+    if workspace.dtype != _t.uint8 or workspace.get_device() != dev or not workspace.is_contiguous() or \
             workspace.numel() < need:
         raise ValueError("workspace must be a contiguous uint8 tensor of at least %d bytes on GPU %d" % (need, dev))
     return workspace
@@ -210,14 +208,14 @@ class FfnPlan:
         self.d_in, self.d_ff = int(d_in), int(d_ff)
         self.d_out = self.d_in if d_out is None else int(d_out)
         self.dtype, self.activation = dtype, activation
+        _code(_DTYPES, dtype, "dtype")
         self._h = ffn_plan(self.d_in, self.d_ff, self.d_out, activation, dtype)
-        self._tdt = _torch_dtype(dtype)
+        self._tdt = _t.dtypes[dtype]
 
     def forward(self, x, w_in, w_out, save=False, out=None, saved=None, workspace=None, stream=None):
         """x: [N, d_in], rows may be strided; w_in: [2 d_ff, d_in], the gate's rows, then the up projection's;
         w_out: [d_out, d_ff].  Returns [N, d_out]; with save=True (or `saved`, a [N, 2 d_ff] fp32 tensor to write)
         also the values that backward() reads."""
-        import torch
         tdt, di, df, do = self._tdt, self.d_in, self.d_ff, self.d_out
         ldx = _rows(x, tdt, None, di, "x")
         N, dev = x.shape[0], x.get_device()
@@ -226,23 +224,22 @@ class FfnPlan:
         if out is None:
             out = _new((N, do), tdt, dev, other)
         if save and saved is None:
-            saved = _new((N, 2 * df), torch.float32, dev, other)
+            saved = _new((N, 2 * df), _t.float32, dev, other)
         ws = _workspace(workspace, ffn_workspace_bytes(self._h, N), dev, other)
         ffn_forward(self._h, x.data_ptr(), ldx, wi, wo, _whole(out, tdt, (N, do), "out", dev),
-                    _whole(saved, torch.float32, (N, 2 * df), "saved", dev), N, ws.data_ptr(), ws.numel(), sp)
+                    _whole(saved, _t.float32, (N, 2 * df), "saved", dev), N, ws.data_ptr(), ws.numel(), sp)
         return out if saved is None else (out, saved)
 
     def backward(self, x, w_in, w_out, saved, grad_out, need_x=True, need_w_in=True, need_w_out=True, workspace=None,
                  stream=None):
         """(grad_x, grad_w_in, grad_w_out) of sum(grad_out * forward(x, w_in, w_out)); one not asked for is None.
         saved: what forward() returned beside Y; x and grad_out may have strided rows."""
-        import torch
         tdt, di, df, do = self._tdt, self.d_in, self.d_ff, self.d_out
         ldx = _rows(x, tdt, None, di, "x")
         N, dev = x.shape[0], x.get_device()
         ldg = _rows(grad_out, tdt, N, do, "grad_out", dev)
         wi, wo = _whole(w_in, tdt, (2 * df, di), "w_in", dev), _whole(w_out, tdt, (do, df), "w_out", dev)
-        sv = _whole(saved, torch.float32, (N, 2 * df), "saved", dev)
+        sv = _whole(saved, _t.float32, (N, 2 * df), "saved", dev)
         if not (need_x or need_w_in or need_w_out):
             return None, None, None
         sp, other = _stream(stream, dev)
@@ -278,17 +275,22 @@ class NormPlan:
         self.width, self.dtype, self.eps = int(width), dtype, float(eps)
         self.rows_per_gate, self.dropout = int(rows_per_gate), float(dropout)
         self._code = _code(_DTYPES, dtype, "dtype")
-        self._tdt = _torch_dtype(dtype)
-        if ffn_norm_workspace_bytes(self._norm(), 0, 0) < 0:
+        self._tdt = _t.dtypes[dtype]
+        self._plain = self._describe(0, 0)
+        if ffn_norm_workspace_bytes(self._plain, 0, 0) < 0:
             raise ValueError("width must be 1 .. %d, eps positive, rows_per_gate at least 1 and dropout within [0, 1]"
                              % FFN_MAX_WIDTH)
 
     def _norm(self, seed=0, offset=0):
+        if self.dropout == 0.0:   # the generator is not asked
+            return self._plain
+        return self._describe(seed, offset)
+
+    def _describe(self, seed, offset):
         return ffn_norm(self.width, self.rows_per_gate, self._code, self.eps, self.dropout, seed & _U64, offset & _U64)
 
     def forward(self, x, w=None, out=None, rstd=None, stream=None):
         """(u, rstd): u = N(x; w) for x [N, width], rows may be strided, and the rows' 1 / sqrt(mean + eps)."""
-        import torch
         tdt, D = self._tdt, self.width
         ldx = _rows(x, tdt, None, D, "x")
         N, dev = x.shape[0], x.get_device()
@@ -297,23 +299,22 @@ class NormPlan:
         if out is None:
             out = _new((N, D), tdt, dev, other)
         if rstd is None:
-            rstd = _new((N,), torch.float32, dev, other)
-        ffn_norm_forward(self._norm(), x.data_ptr(), ldx, wp, out.data_ptr(), _rows(out, tdt, N, D, "out", dev),
-                         _whole(rstd, torch.float32, (N,), "rstd", dev), N, sp)
+            rstd = _new((N,), _t.float32, dev, other)
+        _call("ffn_norm_forward", self._plain, x.data_ptr(), ldx, wp, out.data_ptr(), _rows(out, tdt, N, D, "out", dev),
+                         _whole(rstd, _t.float32, (N,), "rstd", dev), N, sp)
         return out, rstd
 
     def backward(self, x, w, rstd, grad_out, need_x=True, need_w=True, workspace=None, stream=None):
         """(grad_x, grad_w) of sum(grad_out * N(x; w)); one not asked for is None."""
-        import torch
         tdt, D = self._tdt, self.width
         ldx = _rows(x, tdt, None, D, "x")
         N, dev = x.shape[0], x.get_device()
         ldg = _rows(grad_out, tdt, N, D, "grad_out", dev)
-        wp, rp = _whole(w, tdt, (D,), "w", dev), _whole(rstd, torch.float32, (N,), "rstd", dev)
+        wp, rp = _whole(w, tdt, (D,), "w", dev), _whole(rstd, _t.float32, (N,), "rstd", dev)
         if not (need_x or need_w):
             return None, None
         sp, other = _stream(stream, dev)
-        norm = self._norm()
+        norm = self._plain
         gx = _new((N, D), tdt, dev, other) if need_x else None
         gw = _new((D,), tdt, dev, other) if need_w else None
         ws = _workspace(workspace, ffn_norm_workspace_bytes(norm, N, 0), dev, other)
@@ -332,7 +333,6 @@ class NormPlan:
         x, h: [N, width]; gate: [ceil(N / rows_per_gate), width]; scale, w, w_next: [width]; each of the four may be
         None (ones).  seed and offset choose the dropout's draws (see dropout()).  stats [2, N] holds the
         1 / sqrt(mean + eps) of h's and of y's rows, for residual_backward().  out may be x."""
-        import torch
         tdt, D = self._tdt, self.width
         if not x.is_cuda or x.dim() != 2:
             raise ValueError("x must be a %s CUDA tensor [N, %d]" % (tdt, D))
@@ -344,8 +344,8 @@ class NormPlan:
         if out is None:
             out = _new((N, D), tdt, dev, other)
         u = _new((N, D), tdt, dev, other) if next_norm else None
-        stats = _new((2, N), torch.float32, dev, other)
-        ffn_residual_forward(self._norm(seed, offset), xp, hp, wp, gp, sc, np_, _whole(out, tdt, (N, D), "out", dev),
+        stats = _new((2, N), _t.float32, dev, other)
+        _call("ffn_residual_forward", self._norm(seed, offset), xp, hp, wp, gp, sc, np_, _whole(out, tdt, (N, D), "out", dev),
                              u.data_ptr() if next_norm else None, stats.data_ptr(), N, sp)
         return out, u, stats
 
@@ -354,7 +354,6 @@ class NormPlan:
         """(grad_x, grad_h, grad_w, grad_gate, grad_scale, grad_w_next) of sum(grad_y * y) + sum(grad_u * u) for
         residual() with the same arguments; those of arguments that are None are None.  grad_y or grad_u may be
         None (zero), not both."""
-        import torch
         tdt, D = self._tdt, self.width
         if not h.is_cuda or h.dim() != 2:
             raise ValueError("h must be a %s CUDA tensor [N, %d]" % (tdt, D))
@@ -364,7 +363,7 @@ class NormPlan:
         hp, yp = _whole(h, tdt, (N, D), "h", dev), _whole(y, tdt, (N, D), "y", dev)
         wp, sc = _whole(w, tdt, (D,), "w", dev), _whole(scale, tdt, (D,), "scale", dev)
         gp, np_ = _whole(gate, tdt, (self._gates(N), D), "gate", dev), _whole(w_next, tdt, (D,), "w_next", dev)
-        st = _whole(stats, torch.float32, (2, N), "stats", dev)
+        st = _whole(stats, _t.float32, (2, N), "stats", dev)
         gyp, gup = _whole(grad_y, tdt, (N, D), "grad_y", dev), _whole(grad_u, tdt, (N, D), "grad_u", dev)
         sp, other = _stream(stream, dev)
         gx, gh = _new((N, D), tdt, dev, other), _new((N, D), tdt, dev, other)
@@ -383,20 +382,27 @@ def dropout(x, p: float, seed: int, offset: int = 0, out=None, stream=None):
     to a multiple of 2^-16.  Which are kept depends on (seed, offset, row, column) alone, with the leading dimensions
     flattened to rows; the gradient is the same call on the gradient.  x: contiguous, or [N, width] with strided
     rows; out may be x."""
-    import torch
-    name = {torch.float32: "fp32", torch.bfloat16: "bf16", torch.float16: "fp16"}.get(x.dtype)
-    if name is None or not x.is_cuda or x.dim() < 1 or x.shape[-1] < 1:
+    code = _t.codes.get(x.dtype)
+    if code is None or not x.is_cuda or x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("x must be an fp32, bf16 or fp16 CUDA tensor [..., width]")
     width, dev = x.shape[-1], x.get_device()
-    if x.dim() != 2 and not x.is_contiguous():
-        raise ValueError("x must be contiguous, or [N, width] with strided rows")
     N = x.numel() // width
-    ldx = _rows(x, x.dtype, N, width, "x") if x.dim() == 2 else width
+    if x.is_contiguous():
+        ldx = width
+    elif x.dim() == 2:
+        ldx = _rows(x, x.dtype, N, width, "x")
+    else:
+        raise ValueError("x must be contiguous, or [N, width] with strided rows")
     sp, other = _stream(stream, dev)
     if out is None:
-        out = _new(tuple(x.shape), x.dtype, dev, other)
-    elif out.shape != x.shape or out.get_device() != dev or (out.dim() != 2 and not out.is_contiguous()):
-        raise ValueError("out must have the shape and device of x")
-    ldy = _rows(out, x.dtype, N, width, "out", dev) if out.dim() == 2 else _whole(out, x.dtype, tuple(x.shape), "out", dev) and width
-    ffn_dropout(x.data_ptr(), ldx, out.data_ptr(), ldy or width, N, width, name, float(p), seed & _U64, offset & _U64, sp)
+        out, ldy = _new(x.shape, x.dtype, dev, other), width
+    elif out.shape != x.shape or out.get_device() != dev or out.dtype != x.dtype:
+        raise ValueError("out must have the shape, type and device of x")
+    elif out.is_contiguous():
+        ldy = width
+    elif out.dim() == 2:
+        ldy = _rows(out, x.dtype, N, width, "out", dev)
+    else:
+        raise ValueError("out must be contiguous, or [N, width] with strided rows")
+    _call("ffn_dropout", x.data_ptr(), ldx, out.data_ptr(), ldy, N, width, code, float(p), seed & _U64, offset & _U64, sp)
     return out

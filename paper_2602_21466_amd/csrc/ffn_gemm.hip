@@ -59,6 +59,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float* partial, in
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
         const int64_t row = i / quads, c = (i - row * quads) * 4;
         f32x4 v = {};
+#pragma unroll 8
         for (int s = 0; s < splits; ++s) v += *(const f32x4*)(partial + ((int64_t)s * M + row) * ld + c);
         store4<Out>(out + row * N, c, N, 0, v);
     }
@@ -72,6 +73,7 @@ __global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const f
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
         const int64_t m = i / quads, n = (i - m * quads) * 4;
         f32x4 v = {}, u = {};
+#pragma unroll 4
         for (int s = 0; s < p.splits; ++s) {
             const float* from = partial + ((int64_t)s * p.M + m) * ld;
             v += *(const f32x4*)(from + n);

@@ -10,7 +10,6 @@ namespace {
 using namespace dev;
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 64;   // rows whose column sums one work-group of the backward pass holds
 
 template <typename T> __device__ __forceinline__ float load(const void* p, int64_t i, float missing) {
     return p ? to_f32(((const T*)p)[i]) : missing;
@@ -196,7 +195,7 @@ template <typename T, bool TAIL> __device__ __forceinline__ typename Raw<T>::V o
 constexpr int group_of(int tpr) { return tpr > 64 ? tpr : 256; }
 
 // BLOCK: y = x + scale gate drop(N(h; w)) first.  A worker walks its rows with the next one's loads in flight, the
-// factors shared by all rows in registers.
+// factors shared by all rows in registers; workers of 1024 threads have 128 registers each and do neither.
 template <typename T, int TPR, int I, bool TAIL, bool BLOCK>
 __global__ __launch_bounds__(group_of(TPR)) void norm_forward_rows(NormArgs p) {
     __shared__ float s[2 * (TPR > 64 ? TPR / 64 : 1)];
@@ -219,17 +218,22 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_forward_rows(NormArgs p) {
             }
         }
     };
-    fetch(row);
-#pragma unroll
-    for (int i = 0; i < I; ++i) {
+    constexpr bool kLean = TPR == 1024;
+    auto factors = [&](int i) {
         const int c = (t + i * TPR) * 8;
         wn[i] = ones8<T, TAIL>(p.wn, c, D);
         if constexpr (BLOCK) {
             w[i] = ones8<T, TAIL>(p.w, c, D);
             sc[i] = ones8<T, TAIL>(p.scale, c, D);
         }
+    };
+    if constexpr (!kLean) {
+        fetch(row);
+#pragma unroll
+        for (int i = 0; i < I; ++i) factors(i);
     }
     for (int turn = 0; row < p.N; row += step) {
+        if constexpr (kLean) fetch(row);
         float v[I][8];
         V h[B], g[B];
 #pragma unroll
@@ -241,7 +245,7 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_forward_rows(NormArgs p) {
                 g[i] = gr[i];
             }
         }
-        if (row + step < p.N) fetch(row + step);
+        if (!kLean && row + step < p.N) fetch(row + step);
         if constexpr (BLOCK) {
             float sum[1] = {0.0f};
 #pragma unroll
@@ -257,6 +261,7 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_forward_rows(NormArgs p) {
                 const int c = (t + i * TPR) * 8;
                 float f[8];
                 drop8(p.drop, row, c, f);
+                if constexpr (kLean) factors(i);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float n = to_f32(h[i][j]) * rh * to_f32(w[i][j]);
@@ -279,6 +284,7 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_forward_rows(NormArgs p) {
         for (int i = 0; i < I; ++i) {
             const int c = (t + i * TPR) * 8;
             float o[8];
+            if constexpr (kLean) factors(i);
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[j] = v[i][j] * ry * to_f32(wn[i][j]);
             if (c < D) put8<T, TAIL>((T*)p.u + row * p.ldu, c, D, o);
@@ -289,7 +295,7 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_forward_rows(NormArgs p) {
 // Rows too wide for that: the two means of each row first, then a thread eight columns of kChunk rows.
 
 struct Terms { float gx[8], ny[8], nh[8], f[8], g[8], s[8], w[8], gu[8]; };
-template <typename T> __device__ __forceinline__ void terms8(const NormArgs& p, int64_t row, int64_t c, float ry, float rh, float c1, Terms& t) {
+template <typename T> __device__ __forceinline__ void terms8(const NormArgs& p, int64_t row, int64_t gate_row, int64_t c, float ry, float rh, float c1, Terms& t) {
     const int64_t D = p.width;
 #pragma unroll
     for (int j = 0; j < 8; ++j) t.gx[j] = t.ny[j] = t.gu[j] = 0.0f;
@@ -307,7 +313,7 @@ template <typename T> __device__ __forceinline__ void terms8(const NormArgs& p, 
     }
     if (p.h) {
         drop8(p.drop, row, c, t.f);
-        factors8<T>(p.gate ? (const T*)p.gate + (int64_t)((uint32_t)row / (uint32_t)p.rows_per_gate) * D : nullptr, c, D, t.g);
+        factors8<T>(p.gate ? (const T*)p.gate + gate_row * D : nullptr, c, D, t.g);
         factors8<T>(p.scale, c, D, t.s);
         factors8<T>(p.w, c, D, t.w);
         factors8<T>((const T*)p.h + row * D, c, D, t.nh);
@@ -316,9 +322,13 @@ template <typename T> __device__ __forceinline__ void terms8(const NormArgs& p, 
     }
 }
 
+// How the backward pass divides the rows: worker k takes `rows` of them from first(k) on, all of one gate row where
+// parts > 1 (that gate row's gradient is then the sum of `parts` workers'), else of whole gate rows.
+struct Rows { int64_t rows, parts, workers; };
+
 // The means of (gu w_next) n_y and of (d/dN(h)) w n_h.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void norm_means_kernel(NormArgs p) {
+__global__ __launch_bounds__(kThreads) void norm_means_kernel(NormArgs p, Rows rw) {
     __shared__ float s[kThreads / 64];
     const int64_t D = p.width;
     for (int64_t row = blockIdx.x; row < p.N; row += gridDim.x) {
@@ -339,7 +349,7 @@ __global__ __launch_bounds__(kThreads) void norm_means_kernel(NormArgs p) {
         if (p.h) {
             for (int64_t c = threadIdx.x * 8; c < D; c += kThreads * 8) {
                 Terms t;
-                terms8<T>(p, row, c, ry, rh, c1, t);
+                terms8<T>(p, row, (uint32_t)row / (uint32_t)p.rows_per_gate, c, ry, rh, c1, t);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     if (c + j < D && t.f[j] != 0.0f) c2 += t.gx[j] * t.s[j] * t.g[j] * t.f[j] * t.w[j] * t.nh[j];
@@ -347,23 +357,40 @@ __global__ __launch_bounds__(kThreads) void norm_means_kernel(NormArgs p) {
             c2 = group_sum(c2, s) / (float)D;
         }
         if (threadIdx.x == 0) {
-            p.partial[row] = c1;
-            p.partial[p.N + row] = c2;
+            float* means = p.partial + (p.h && rw.parts > 1 ? rw.workers * D : 0) + rw.workers * (p.h ? 3 : 1) * D;
+            means[row] = c1;
+            means[p.N + row] = c2;
         }
     }
 }
 
+
+// A thread eight columns of one worker's rows: gx, gh, the gate's gradient and the column sums, given the means.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormArgs p) {
-    const int64_t D = p.width, c = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * 8;
+__global__ __launch_bounds__(kThreads) void norm_columns_kernel(NormArgs p, Rows rw) {
+    const int64_t D = p.width, c = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * 8, worker = blockIdx.x;
     if (c >= D) return;
-    const int64_t r0 = (int64_t)blockIdx.x * kChunk, r1 = r0 + kChunk < p.N ? r0 + kChunk : p.N;
-    float sw[8] = {}, ss[8] = {}, sn[8] = {};
+    int64_t r0, r1, gate_row;
+    if (rw.parts > 1) {
+        gate_row = worker / rw.parts;
+        r0 = gate_row * p.rows_per_gate + (worker - gate_row * rw.parts) * rw.rows;
+        r1 = r0 + rw.rows;
+        if (r1 > (gate_row + 1) * p.rows_per_gate) r1 = (gate_row + 1) * p.rows_per_gate;
+    } else {
+        r0 = worker * rw.rows;
+        r1 = r0 + rw.rows;
+        gate_row = r0 / p.rows_per_gate;
+    }
+    if (r1 > p.N) r1 = p.N;
+    int64_t gate_end = (gate_row + 1) * p.rows_per_gate;
+    // the means of the rows lie behind the sums
+    const float* means = p.partial + (p.h && rw.parts > 1 ? rw.workers * D : 0) + rw.workers * (p.h ? 3 : 1) * D;
+    float sw[8] = {}, ss[8] = {}, sn[8] = {}, sg[8] = {};
     for (int64_t row = r0; row < r1; ++row) {
         const float ry = p.gu ? p.rstd_y[row] : 0.0f, rh = p.h ? p.rstd_h[row] : 0.0f;
-        const float c1 = p.partial[row], c2 = p.partial[p.N + row];
         Terms t;
-        terms8<T>(p, row, c, ry, rh, c1, t);
+        terms8<T>(p, row, gate_row, c, ry, rh, means[row], t);
+        const float c2 = means[p.N + row];
         if (p.gx) store8((T*)p.gx + row * D, c, D, t.gx);
 #pragma unroll
         for (int j = 0; j < 8; ++j) sn[j] += t.gu[j] * t.ny[j];
@@ -371,60 +398,40 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormArgs p) {
             float gh[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float gv = t.f[j] == 0.0f ? 0.0f : t.gx[j] * t.s[j] * t.g[j] * t.f[j];
-                gh[j] = rh * (gv * t.w[j] - t.nh[j] * c2);
-                sw[j] += gv * t.nh[j];
-                if (t.f[j] != 0.0f) ss[j] += t.gx[j] * t.g[j] * t.f[j] * (t.nh[j] * t.w[j]);
+                const float d = t.f[j] == 0.0f ? 0.0f : t.gx[j] * t.f[j], m = t.f[j] == 0.0f ? 0.0f : d * t.nh[j];
+                gh[j] = rh * (d * t.s[j] * t.g[j] * t.w[j] - t.nh[j] * c2);
+                sw[j] += m * t.s[j] * t.g[j];
+                ss[j] += m * t.w[j] * t.g[j];
+                sg[j] += m * t.w[j] * t.s[j];
             }
             store8((T*)p.gh + row * D, c, D, gh);
+            if (p.ggate && (row + 1 == r1 || row + 1 == gate_end)) {
+                if (rw.parts > 1) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (c + j < D) p.partial[worker * D + c + j] = sg[j];
+                } else {
+                    store8((T*)p.ggate + gate_row * D, c, D, sg);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sg[j] = 0.0f;
+            }
         }
+        if (row + 1 == gate_end) { ++gate_row; gate_end += p.rows_per_gate; }
     }
-    float* out = p.partial + 2 * p.N + (int64_t)blockIdx.x * 3 * D + c;
+    float* out = p.partial + (p.h && rw.parts > 1 ? rw.workers * D : 0) + worker * (p.h ? 3 : 1) * D + c;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         if (c + j < D) {
-            out[j] = sw[j];
-            out[D + j] = ss[j];
-            out[2 * D + j] = sn[j];
+            if (p.h) {
+                out[j] = sw[j];
+                out[D + j] = ss[j];
+                out[2 * D + j] = sn[j];
+            } else {
+                out[j] = sn[j];
+            }
         }
 }
-
-// The gate's gradient: a thread eight columns of one gate row, over the rows that share it.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void gate_grad_kernel(NormArgs p) {
-    const int64_t D = p.width, c = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * 8;
-    if (c >= D) return;
-    const int64_t gates = (p.N + p.rows_per_gate - 1) / p.rows_per_gate;
-    for (int64_t k = blockIdx.x; k < gates; k += gridDim.x) {
-        const int64_t r0 = k * p.rows_per_gate, r1 = r0 + p.rows_per_gate < p.N ? r0 + p.rows_per_gate : p.N;
-        float v[8] = {};
-        for (int64_t row = r0; row < r1; ++row) {
-            Terms t;
-            terms8<T>(p, row, c, p.gu ? p.rstd_y[row] : 0.0f, p.rstd_h[row], p.partial[row], t);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (t.f[j] != 0.0f) v[j] += t.gx[j] * t.s[j] * t.f[j] * (t.nh[j] * t.w[j]);
-        }
-        store8((T*)p.ggate + k * D, c, D, v);
-    }
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void norm_sum_kernel(NormArgs p, int64_t chunks) {
-    const int64_t D = p.width, c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (c >= D) return;
-    void* to[3] = {p.gw, p.gscale, p.gwn};
-    for (int j = 0; j < 3; ++j) {
-        if (!to[j]) continue;
-        float v = 0.0f;
-        for (int64_t i = 0; i < chunks; ++i) v += p.partial[2 * p.N + (i * 3 + j) * D + c];
-        ((T*)to[j])[c] = (T)v;
-    }
-}
-
-// How the backward pass divides the rows: worker k takes `rows` of them from first(k) on, all of one gate row where
-// parts > 1 (that gate row's gradient is then the sum of `parts` workers'), else of whole gate rows.
-struct Rows { int64_t rows, parts, workers; };
 
 // One pass over the rows: gx, gh, the gate's gradient, and each work-group's column sums (of w, scale, w_next).
 // With q = scale gate drop w n_h, the two means of a row need three sums and no second pass:
@@ -475,11 +482,12 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_backward_rows(NormArgs p, 
             }
         }
     };
-    if (r0 < r1) fetch(r0);
+    constexpr bool kLean = TPR == 1024;
+    if (!kLean && r0 < r1) fetch(r0);
 #pragma unroll
     for (int i = 0; i < I; ++i) {
         const int c = (t + i * TPR) * 8;
-        wn[i] = ones8<T, TAIL>(p.wn, c, D);
+        if constexpr (!kLean) wn[i] = ones8<T, TAIL>(p.wn, c, D);
         if constexpr (H) {
             w[i] = ones8<T, TAIL>(p.w, c, D);
             sc[i] = ones8<T, TAIL>(p.scale, c, D);
@@ -487,6 +495,7 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_backward_rows(NormArgs p, 
     }
     int turn = 0;
     for (int64_t row = r0; row < r1; ++row, turn ^= 1) {
+        if constexpr (kLean) fetch(row);
         // per value: a = gy + r_y gu w_next, n_y, and for the block's side n_h and the dropout's factor
         const float ry = ryr, rh = rhr;
         float a[I][8], ny[I][8], nh[B][8], f[B][8];
@@ -495,6 +504,7 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_backward_rows(NormArgs p, 
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int c = (t + i * TPR) * 8;
+            if constexpr (kLean) wn[i] = ones8<T, TAIL>(p.wn, c, D);
             if constexpr (H) {
                 g[i] = gr[i];
                 drop8(p.drop, row, c, f[i]);
@@ -518,7 +528,7 @@ __global__ __launch_bounds__(group_of(TPR)) void norm_backward_rows(NormArgs p, 
         const int64_t gate_at = gate_row;
         if (row + 1 < r1) {
             if (row + 1 == gate_end) { ++gate_row; gate_end += p.rows_per_gate; }
-            fetch(row + 1);
+            if constexpr (!kLean) fetch(row + 1);
         }
         if constexpr (H) {
             worker_sum<TPR, 3>(sum, s, turn);
@@ -664,8 +674,12 @@ inline Shape shape_of(int64_t width, Pass pass) {
     return {0, 0};
 }
 
-inline Rows rows_of(const Shape& sh, int64_t N, int64_t rows_per_gate) {
-    const int64_t want = 512 * 256 / sh.tpr;   // eight waves a compute unit
+// Workers of the column kernel: about four work-groups a compute unit over all columns.
+inline int64_t column_blocks(int64_t width) { return (width + 8 * kThreads - 1) / (8 * kThreads); }
+
+inline Rows rows_of(const Shape& sh, int64_t width, int64_t N, int64_t rows_per_gate) {
+    // eight waves a compute unit
+    const int64_t wide = 1024 / column_blocks(width), want = sh.tpr ? 512 * 256 / sh.tpr : wide > 1 ? wide : 1;
     int64_t r = (N + want - 1) / want;
     if (r < 4) r = 4;
     Rows out;
@@ -682,7 +696,7 @@ inline Rows rows_of(const Shape& sh, int64_t N, int64_t rows_per_gate) {
 }
 
 inline int64_t groups_for(const Rows& r, const Shape& sh) {
-    const int64_t per = group_of(sh.tpr) / sh.tpr;
+    const int64_t per = sh.tpr ? group_of(sh.tpr) / sh.tpr : 1;
     return (r.workers + per - 1) / per;
 }
 
@@ -745,23 +759,12 @@ template <typename T> int forward(const NormArgs& a, hipStream_t s) {
 template <typename T> int backward(const NormArgs& a, hipStream_t s) {
     const bool block = a.h != nullptr, tail = a.width % 8 != 0;
     const Shape sh = shape_of(a.width, block ? kBackwardBlock : kBackward);
-    if (sh.tpr == 0) {
-        const int64_t chunks = (a.N + kChunk - 1) / kChunk;
-        const unsigned cols = (unsigned)((a.width + 8 * kThreads - 1) / (8 * kThreads));
-        if (a.N > 0) {
-            norm_means_kernel<T><<<dim3(row_groups(a.N)), kThreads, 0, s>>>(a);
-            if (a.ggate) {
-                const int64_t gates = (a.N + a.rows_per_gate - 1) / a.rows_per_gate;
-                gate_grad_kernel<T><<<dim3(row_groups(gates), cols), kThreads, 0, s>>>(a);
-            }
-            norm_grad_kernel<T><<<dim3((unsigned)chunks, cols), kThreads, 0, s>>>(a);
-        }
-        norm_sum_kernel<T><<<dim3((unsigned)((a.width + kThreads - 1) / kThreads)), kThreads, 0, s>>>(a, chunks);
-        return (int)hipGetLastError();
-    }
-    const Rows rw = rows_of(sh, a.N, block ? a.rows_per_gate : 1);
+    const Rows rw = rows_of(sh, a.width, a.N, block ? a.rows_per_gate : 1);
     const int64_t groups = groups_for(rw, sh);
-    if (groups > 0 && block) {
+    if (sh.tpr == 0 && groups > 0) {
+        norm_means_kernel<T><<<dim3(row_groups(a.N)), kThreads, 0, s>>>(a, rw);
+        norm_columns_kernel<T><<<dim3((unsigned)groups, (unsigned)column_blocks(a.width)), kThreads, 0, s>>>(a, rw);
+    } else if (groups > 0 && block) {
 #define FFN_BLOCK(TPR)                                                                                              \
     if (tail) norm_backward_rows<T, TPR, 1, true, true><<<dim3((unsigned)groups), group_of(TPR), 0, s>>>(a, rw);    \
     else norm_backward_rows<T, TPR, 1, false, true><<<dim3((unsigned)groups), group_of(TPR), 0, s>>>(a, rw)
@@ -800,9 +803,8 @@ template <typename T> int drop(const void* x, int64_t ldx, void* y, int64_t ldy,
 
 inline int64_t workspace_floats(int64_t width, int64_t N, int64_t rows_per_gate, bool residual) {
     const Shape sh = shape_of(width, residual ? kBackwardBlock : kBackward);
-    if (sh.tpr == 0) return 2 * N + (N + kChunk - 1) / kChunk * 3 * width;
-    const Rows rw = rows_of(sh, N, residual ? rows_per_gate : 1);
-    return (residual && rw.parts > 1 ? rw.workers * width : 0) + groups_for(rw, sh) * (residual ? 3 : 1) * width;
+    const Rows rw = rows_of(sh, width, N, residual ? rows_per_gate : 1);
+    return (residual && rw.parts > 1 ? rw.workers * width : 0) + groups_for(rw, sh) * (residual ? 3 : 1) * width + (sh.tpr ? 0 : 2 * N);
 }
 
 }  // namespace

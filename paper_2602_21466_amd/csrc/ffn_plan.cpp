@@ -100,7 +100,7 @@ struct Cut { int32_t tile, splits; };
 // The shortest by this count, in steps of a 256-wide tile (64 k; 1.6 us): a compute unit takes one such work-group, or
 // two of the 128-wide, whose steps take 0.66 of it when both run (measured on large bf16 products: 1.33 PFLOP/s with
 // 256-wide tiles, 1.0 with 128-wide); four steps stand for a tile's start and end.  Parts of k cost a launch (three
-// microseconds) and their sums, written and read once at 4 TB/s.
+// microseconds, and a tenth of one a part) and their sums, written and read once at 4 TB/s.
 Cut choose(int64_t M, int64_t N, int64_t steps) {
     Cut best = {256, 1};
     double least = 1e300;
@@ -108,7 +108,7 @@ Cut choose(int64_t M, int64_t N, int64_t steps) {
         const int64_t groups = tiles(M, tile) * tiles(N, tile), slots = tile == 256 ? 256 : 512;
         for (int32_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); ++s) {
             const double t = (double)tiles(groups * s, slots) * ((double)tiles(steps, s) + 4) * (tile == 256 ? 1.6 : 1.06) +
-                             (s > 1 ? 3.0 + (double)(M * N * s) * 8.0 / 4e6 : 0.0);
+                             (s > 1 ? 3.0 + 0.1 * s + (double)(M * N * s) * 8.0 / 4e6 : 0.0);
             if (t < least) { least = t; best = {tile, s}; }
         }
     }
