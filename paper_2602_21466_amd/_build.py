@@ -11,7 +11,7 @@ SOURCES = [os.path.join(HERE, "csrc", f) for f in
            ("cgtp_plan.cpp", "cgtp_kernels.hip", "cgtp_kernels_channels.hip", "cgtp_backward.hip", "cgtp_direct.hip", "cgtp_direct_backward.hip", "cgtp_kernels_real.hip", "istp_plan.cpp", "istp_kernels.hip", "istp_kernels_real.hip",
             "istp_kernels_channels.hip", "istp_kernels_tensor.hip", "istp_kernels_channels_tensor.hip",
             "istp_real.hip", "ffn_plan.cpp", "ffn_gemm.hip",
-            "ffn_tile_bf16.hip", "ffn_tile_fp16.hip", "ffn_tile_fp32.hip", "ffn_few_bf16.hip", "ffn_few_fp16.hip", "ffn_few_fp32.hip",
+            "ffn_tile_bf16.hip", "ffn_tile_fp16.hip", "ffn_tile_fp32.hip", "ffn_few_bf16.hip", "ffn_few_fp16.hip", "ffn_few_fp32.hip", "ffn_few_grad.hip",
             "ffn_norm_bf16.hip", "ffn_norm_fp16.hip", "ffn_norm_fp32.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -138,7 +138,13 @@ __global__ __launch_bounds__(512) void few_kernel(FewArgs p) {
     for (int f = 0; f < F; ++f)
 #pragma unroll
         for (int m = 0; m < MT; ++m)
-            few_sums[(wave * F * MT + f * MT + m) * 64 + lane] = HB == 1 || lane < 32 ? acc[f][m][0] : acc[f][m][HB - 1];
+            {
+            const f32x4 lo = acc[f][m][0], hi = acc[f][m][HB - 1];
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = lane < 32 ? lo[e] : hi[e];
+            few_sums[(wave * F * MT + f * MT + m) * 64 + lane] = HB == 1 ? lo : v;
+            }
     __syncthreads();
     constexpr int kLanes = 64 / HB;
     for (int i = threadIdx.x; i < RT * MT * kLanes; i += blockDim.x) {

@@ -52,6 +52,17 @@ int launch_few_bf16(const FewArgs& p, int32_t epilogue, int32_t nr, int32_t wave
 int launch_few_fp16(const FewArgs& p, int32_t epilogue, int32_t nr, int32_t waves, void* stream);
 int launch_few_fp32(const FewArgs& p, int32_t epilogue, int32_t nr, int32_t waves, void* stream);
 
+// Partial sums of C = A W, W [K, N] of 32-bit values with row stride ldw, for M <= kFewRows and N >= 4: floats
+// [splits, M, ldc].  plane: 0, or the distance of A's three planes.  See ffn_few_grad.hip.
+struct FewGradArgs {
+    const void *x, *w;
+    int64_t ldx, ldw, plane, M, N, K;
+    float* c;
+    int64_t ldc;
+    int32_t splits, waves;
+};
+int launch_few_grad(const FewGradArgs& p, void* stream);
+
 // out[i, j] = sum over splits of partial[s, i, j] (rows of ld floats), N columns, out contiguous.
 int launch_join(const float* partial, int64_t ld, int32_t splits, int64_t M, int64_t N, void* out, int32_t dtype, void* stream);
 

@@ -172,6 +172,31 @@ int few_product(const ffn::FewArgs& p, int32_t epilogue, int32_t dtype, void* st
     }
 }
 
+// Gradients' products for few rows of 32-bit arrays: about two work-groups a compute unit by parts of k.
+bool few_grad(int64_t M, int64_t N, int32_t dtype) { return dtype == FFN_FP32 && M <= ffn::kFewRows && N >= 4; }
+struct FewCut { int32_t splits, waves; };
+FewCut few_cut(int64_t M, int64_t N, int64_t K) {
+    const int32_t waves = M <= 32 ? 8 : 4;
+    const int64_t blocks = tiles(N, 64), most = tiles(K, 32 * waves), want = tiles(512, blocks);
+    return {(int32_t)(want < most ? want : most), waves};
+}
+int64_t few_grad_bytes(int64_t M, int64_t N, int64_t K) { return aligned(few_cut(M, N, K).splits * M * ((N + 3) & ~3LL) * 4); }
+
+// t describes the product and its results as for product(): t.a the rows (t.plane_a: 0, or planes), t.b [K, N] floats.
+int few_grad_product(ffn::TileArgs t, int32_t epilogue, void* partial, void* stream) {
+    const FewCut c = few_cut(t.M, t.N, t.K);
+    ffn::FewGradArgs f = {};
+    f.x = t.a; f.ldx = t.lda; f.plane = t.plane_a; f.w = t.b; f.ldw = t.ldb;
+    f.M = t.M; f.N = t.N; f.K = t.K;
+    f.c = (float*)partial; f.ldc = (t.N + 3) & ~3LL;
+    f.splits = c.splits; f.waves = c.waves;
+    const int rc = status(ffn::launch_few_grad(f, stream));
+    if (rc != CGTP_OK) return rc;
+    t.splits = c.splits;
+    if (epilogue == ffn::kGateGrad) return status(ffn::launch_join_gate(t, epilogue, f.c, f.ldc, FFN_FP32, stream));
+    return status(ffn::launch_join(f.c, f.ldc, c.splits, t.M, t.N, t.c, FFN_FP32, stream));
+}
+
 // A matrix as the products read it: 16-bit values (or three planes of them) on 16 bytes.
 struct Operand { const void* p; int64_t ld, plane; };
 
@@ -211,8 +236,8 @@ Layout layout(const ffn_plan_s* p, int64_t N, bool backward) {
     if (backward) {
         l.dgu = take(packed_bytes(N, 2 * df, t));
         l.gy = take(packed_bytes(N, d_o, t));
-        also(partial_bytes(N, df, d_o, t));
-        also(partial_bytes(N, di, 2 * df, t));
+        also(few_grad(N, df, t) ? few_grad_bytes(N, df, d_o) : partial_bytes(N, df, d_o, t));
+        also(few_grad(N, di, t) ? few_grad_bytes(N, di, 2 * df) : partial_bytes(N, di, 2 * df, t));
         also(partial_bytes(2 * df, di, N, t));
         also(partial_bytes(d_o, df, N, t));
     } else {
@@ -360,29 +385,42 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
         return rc;
     }
     char* ws = (char*)workspace;
+    const int32_t dt = plan->dtype;
+    const bool few_h = few_grad(N, df, dt), few_x = few_grad(N, di, dt);   // their products read the weights as they are
     ffn::PackJobs jobs = {};
-    const Operand Gy = operand(grad_y, ldg, N, d_o, plan->dtype, ws + l.gy, &jobs), Wo = operand(w_out, df, d_o, df, plan->dtype, ws + l.w_out, &jobs);
-    Operand X = {}, Wi = {};
-    if (grad_x) Wi = operand(w_in, di, 2 * df, di, plan->dtype, ws + l.w_in, &jobs);
-    if (grad_w_in) X = operand(x, ldx, N, di, plan->dtype, ws + l.x, &jobs);
-    rc = status(ffn::launch_pack(jobs, plan->dtype, hip_stream));
+    Operand X = {}, Wi = {}, Wo = {}, Gy = {};
+    if (!few_h || grad_w_out) Gy = operand(grad_y, ldg, N, d_o, dt, ws + l.gy, &jobs);
+    if (!few_h) Wo = operand(w_out, df, d_o, df, dt, ws + l.w_out, &jobs);
+    if (grad_x && !few_x) Wi = operand(w_in, di, 2 * df, di, dt, ws + l.w_in, &jobs);
+    if (grad_w_in) X = operand(x, ldx, N, di, dt, ws + l.x, &jobs);
+    rc = status(ffn::launch_pack(jobs, dt, hip_stream));
     if (rc != CGTP_OK) return rc;
     const Operand H = {ws + l.h, up8(df), packed(N, df)}, D = {ws + l.dgu, up8(2 * df), packed(N, 2 * df)};
     ffn::TileArgs g = {};
-    g.a = Gy.p; g.lda = Gy.ld; g.plane_a = Gy.plane;
-    g.b = Wo.p; g.ldb = Wo.ld; g.plane_b = Wo.plane;
+    if (few_h) {
+        g.a = grad_y; g.lda = ldg; g.b = w_out; g.ldb = df;
+    } else {
+        g.a = Gy.p; g.lda = Gy.ld; g.plane_a = Gy.plane;
+        g.b = Wo.p; g.ldb = Wo.ld; g.plane_b = Wo.plane;
+    }
     g.M = N; g.N = df; g.K = d_o;
     g.c = ws + l.dgu; g.ldc = D.ld; g.plane_c = D.plane;
     g.h = ws + l.h; g.ldh = H.ld; g.plane_h = H.plane;
     g.act = plan->act; g.saved = (float*)const_cast<void*>(saved);
-    rc = product(g, ffn::kGateGrad, false, true, plan->dtype, ws + l.partial, hip_stream);
+    rc = few_h ? few_grad_product(g, ffn::kGateGrad, ws + l.partial, hip_stream)
+               : product(g, ffn::kGateGrad, false, true, dt, ws + l.partial, hip_stream);
     if (rc == CGTP_OK && grad_x) {
         ffn::TileArgs t = {};
         t.a = D.p; t.lda = D.ld; t.plane_a = D.plane;
-        t.b = Wi.p; t.ldb = Wi.ld; t.plane_b = Wi.plane;
         t.M = N; t.N = di; t.K = 2 * df;
         t.c = grad_x; t.ldc = di;
-        rc = product(t, ffn::kStore, false, true, plan->dtype, ws + l.partial, hip_stream);
+        if (few_x) {
+            t.b = w_in; t.ldb = di;
+            rc = few_grad_product(t, ffn::kStore, ws + l.partial, hip_stream);
+        } else {
+            t.b = Wi.p; t.ldb = Wi.ld; t.plane_b = Wi.plane;
+            rc = product(t, ffn::kStore, false, true, dt, ws + l.partial, hip_stream);
+        }
     }
     if (rc == CGTP_OK && grad_w_in) {
         ffn::TileArgs t = {};

@@ -378,8 +378,9 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
                 *(f32x4*)(turn + (x * 16 + (lane & 15)) * kRow + j * 16 + (lane >> 4) * 4) = acc[i + x][j];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        // (kGateGrad: G and U of kAhead turns are asked for together)
-        constexpr int kTurns = 32 / kTake, kAhead = EPI == kGateGrad ? 4 : 1;
+        // (kGateGrad: G and U of kAhead turns are asked for together; with the planes of 32-bit arrays so much code would
+        // not be unrolled, and the sums would leave the registers)
+        constexpr int kTurns = 32 / kTake, kAhead = EPI == kGateGrad && sizeof(Out) == 2 ? 4 : 1;
 #pragma unroll 1
         for (int k0 = 0; k0 < kTurns; k0 += kAhead) {
         f32x4 gs[kAhead], us[kAhead];
