@@ -154,17 +154,19 @@ int product(ffn::TileArgs t, int32_t epilogue, bool ac, bool bc, int32_t dtype, 
     return status(ffn::launch_join_gate(t, epilogue, (const float*)partial, s.ldc, dtype, stream));
 }
 
-// A product for few rows: weight rows a work-group, and waves (parts of k).  Measured, bf16: below one work-group of
-// 16 a compute unit 8 rows are faster for up to 16 rows of x (2048 x 8192, one row: 10.3 against 12.5 us); 32 where
-// x's rows are read as often as the weights and two work-groups a unit are left (16384 x 4096 gated, 24 rows: 55
-// against 61 us).
+// A product for few rows: weight rows a work-group, and waves (parts of k).  Measured, bf16: up to 16 rows of x, 8 a
+// work-group (2048 x 8192, one row: 9.7 us against 12.6 with 16; 16384 x 4096 gated: 48.7 against 49.6), which the
+// 32-bit instruction, at an eighth of the rate, does not follow; with more rows of x 16 (4096 x 16384, 24 rows: 45
+// against 62), and 32 where two work-groups a compute unit are left (16384 x 4096 gated, 24 rows: 57 against 61).  8
+// always where 16 would leave a quarter of the compute units idle (2048 x 2048 gated, 40 rows: 10.3 against 11.7).
 int few_product(const ffn::FewArgs& p, int32_t epilogue, int32_t dtype, void* stream) {
     const bool gate = epilogue == ffn::kGate;
-    const int32_t nr = p.N < 16 * 256 && p.M <= 16 ? 8 : gate && p.M > 16 && p.N >= 32 * 512 ? 32 : 16;
+    const int32_t nr = (p.M <= 16 && dtype != FFN_FP32) || p.N < 16 * 192 ? 8 : gate && p.M > 16 && p.N >= 32 * 512 ? 32 : 16;
     const int32_t mt = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4, per = (nr > 16 ? 2 : 1) * (gate ? 2 : 1) * mt;
-    int32_t waves = nr == 8 ? 4 : 8;
-    const int64_t blocks = tiles(p.K, dtype == FFN_FP32 ? 32 : 64);
-    while (waves > 1 && (waves * per > 64 || waves > blocks)) waves /= 2;
+    int32_t waves = 8;
+    // blocks of k: one a wave or more, and where there are waves enough, four (8192 x 2048 gated: 13.5 us, with two 14.4)
+    const int64_t blocks = tiles(p.K, dtype == FFN_FP32 ? 64 : 128), groups = tiles(p.N, nr);
+    while (waves > 1 && (waves * per > 64 || waves > 2 * blocks || (waves * 4 > blocks && groups * waves > 4096))) waves /= 2;
     switch (dtype) {
         case FFN_FP32: return status(ffn::launch_few_fp32(p, epilogue, nr, waves, stream));
         case FFN_BF16: return status(ffn::launch_few_bf16(p, epilogue, nr, waves, stream));

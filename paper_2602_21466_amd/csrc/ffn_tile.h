@@ -238,6 +238,12 @@ template <int R, bool COLS> struct Fragments {
 __device__ __forceinline__ void place(int id, int tm, int tn, int splits, int& m, int& n, int& split) {
     const int tiles = tm * tn, total = tiles * splits, die = id & 7, per = total >> 3, more = total & 7;
     int t = die * per + (die < more ? die : more) + (id >> 3);
+    if (tm == 1) {   // nothing shared but x: a tile's parts side by side read its rows of B through (24 rows, 4096 x 16384: 29 us against 32)
+        split = t % splits;
+        m = 0;
+        n = t / splits;
+        return;
+    }
     split = t / tiles;
     t -= split * tiles;
     constexpr int kGroup = 8;
