@@ -30,22 +30,7 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(PackJobs jobs) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = c + e < j.width ? f[e] : (T)0.0f;
         }
-        uint16_t* t = (uint16_t*)j.to + row * j.to_ld + c;
-        if constexpr (sizeof(T) == 4) {
-            s16x8 o[3];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                uint16_t q[3];
-                planes_of(v[e], q);
-                o[0][e] = (short)q[0];
-                o[1][e] = (short)q[1];
-                o[2][e] = (short)q[2];
-            }
-#pragma unroll
-            for (int e = 0; e < 3; ++e) *(s16x8*)(t + e * j.plane) = o[e];
-        } else {
-            *(s16x8*)t = __builtin_bit_cast(s16x8, v);
-        }
+        *(V*)((T*)j.to + row * j.to_ld + c) = v;
         row += dr;
         at += da;
         if (at >= chunks) { at -= chunks; ++row; }
@@ -67,7 +52,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float* partial, in
 
 // The joining of split sums with the gate's epilogues; the same arithmetic as the tiles' own.  kGate: the sums hold
 // [G U] (2 N columns); kGateGrad: dH.
-template <typename T, typename Out, int EPI>
+template <typename T, int EPI>
 __global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const float* partial, int64_t ld) {
     const int64_t quads = (p.N + 3) >> 2, total = p.M * quads;
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
@@ -87,7 +72,7 @@ __global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const f
                 activate(p.act, v[e], a, da);
                 h[e] = a * u[e];
             }
-            store_mid<T, Out>(p.c, m, p.ldc, p.plane_c, n, p.N, p.ldc, h);
+            store4<T>((T*)p.c + m * p.ldc, n, p.N, p.ldc, h);
             if (p.saved) {
                 store4<float>(p.saved + m * 2 * p.N, n, p.N, 0, v);
                 store4<float>(p.saved + m * 2 * p.N + p.N, n, p.N, 0, u);
@@ -104,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const f
                 du[e] = v[e] * a;
                 h[e] = a * u[e];
             }
-            store_gate_grad<T, Out>(p, m, n, dg, du, h);
+            store_gate_grad<T>(p, m, n, dg, du, h);
         }
     }
 }
@@ -137,12 +122,12 @@ int launch_pack(PackJobs jobs, int32_t dtype, void* stream) {
 int launch_join_gate(const TileArgs& p, int32_t epilogue, const float* partial, int64_t ld, int32_t dtype, void* stream) {
     hipStream_t s = (hipStream_t)stream;
     const unsigned g = groups(p.M * ((p.N + 3) >> 2));
-#define FFN_JOIN(T, OUT)                                                                                       \
-    if (epilogue == kGate) join_gate_kernel<T, OUT, kGate><<<g, kThreads, 0, s>>>(p, partial, ld);             \
-    else join_gate_kernel<T, OUT, kGateGrad><<<g, kThreads, 0, s>>>(p, partial, ld)
-    if (dtype == FFN_FP32) { FFN_JOIN(bf16, float); }
-    else if (dtype == FFN_BF16) { FFN_JOIN(bf16, bf16); }
-    else { FFN_JOIN(fp16, fp16); }
+#define FFN_JOIN(T)                                                                                       \
+    if (epilogue == kGate) join_gate_kernel<T, kGate><<<g, kThreads, 0, s>>>(p, partial, ld);             \
+    else join_gate_kernel<T, kGateGrad><<<g, kThreads, 0, s>>>(p, partial, ld)
+    if (dtype == FFN_FP32) { FFN_JOIN(float); }
+    else if (dtype == FFN_BF16) { FFN_JOIN(bf16); }
+    else { FFN_JOIN(fp16); }
 #undef FFN_JOIN
     return (int)hipGetLastError();
 }

@@ -9,7 +9,7 @@
 namespace ffn {
 
 // ---------------------------------------------------------------- matrix products
-// C(m, n) = sum_k A(m, k) B(n, k) of 16-bit operands; see ffn_tile.h.
+// C(m, n) = sum_k A(m, k) B(n, k); see ffn_tile.h.
 enum Epilogue : int32_t {
     kStore = 0,      // C
     kGate = 1,       // B holds the gate's N rows, then the up projection's: H = act(G) * U; G, U kept in `saved`
@@ -18,19 +18,18 @@ enum Epilogue : int32_t {
 };
 
 // Operands and results of one launch.  Strides in elements; operands start on 16 bytes, with strides that are
-// multiples of 8, and, along k, zeros up to the next multiple of 8.
+// multiples of 16 bytes, and, along k, zeros up to the next multiple.
 struct TileArgs {
     const void *a, *b;
-    int64_t lda, ldb, plane_a, plane_b;   // plane: elements from one plane of a 32-bit array to the next
+    int64_t lda, ldb;
     int64_t M, N, K;
-    int32_t planes;                       // 1, or 3 for 32-bit arrays
     int32_t act;
     int32_t tiles_m, tiles_n, splits;
     void* c;                              // kStore: C; kPartial: floats [splits, M, ldc]; kGate: H; kGateGrad: [dG dU]
-    int64_t ldc, plane_c;
+    int64_t ldc;
     float* saved;                         // [M, 2 N]
     void* h;                              // kGateGrad: H
-    int64_t ldh, plane_h;
+    int64_t ldh;
 };
 
 int launch_tile_bf16(const TileArgs& p, int32_t epilogue, bool a_cols, bool b_cols, int32_t tile, void* stream);
@@ -53,10 +52,10 @@ int launch_few_fp16(const FewArgs& p, int32_t epilogue, int32_t nr, int32_t wave
 int launch_few_fp32(const FewArgs& p, int32_t epilogue, int32_t nr, int32_t waves, void* stream);
 
 // Partial sums of C = A W, W [K, N] of 32-bit values with row stride ldw, for M <= kFewRows and N >= 4: floats
-// [splits, M, ldc].  plane: 0, or the distance of A's three planes.  See ffn_few_grad.hip.
+// [splits, M, ldc].  See ffn_few_grad.hip.
 struct FewGradArgs {
     const void *x, *w;
-    int64_t ldx, ldw, plane, M, N, K;
+    int64_t ldx, ldw, M, N, K;
     float* c;
     int64_t ldc;
     int32_t splits, waves;
@@ -71,12 +70,12 @@ int launch_zero(void* p, int64_t bytes, void* stream);
 // The same for the gate's epilogues (p as for the tile launch: p.c is H or [dG dU], p.splits the parts).
 int launch_join_gate(const TileArgs& p, int32_t epilogue, const float* partial, int64_t ld, int32_t dtype, void* stream);
 
-// [rows, width] of `dtype` with row stride ld -> 16-bit operand with row stride `to_ld` (zeros from width on): a copy,
-// or three planes, `plane` elements apart, of 32-bit values.  Up to four matrices a launch.
+// [rows, width] with row stride ld -> the same with row stride `to_ld`, a multiple of 8 (zeros from width on).  Up to
+// four matrices a launch.
 struct PackJob {
     const void* from;
     void* to;
-    int64_t ld, rows, width, to_ld, plane;
+    int64_t ld, rows, width, to_ld;
     int32_t end;                          // work-groups up to here; set by the launcher
 };
 struct PackJobs {

@@ -97,17 +97,19 @@ int64_t tiles(int64_t n, int64_t t) { return (n + t - 1) / t; }
 // How a product is cut up: work-groups of `tile` x `tile` outputs, k in `splits` parts.
 struct Cut { int32_t tile, splits; };
 
-// The shortest by this count, in steps of a 256-wide tile (64 k; 1.6 us): a compute unit takes one such work-group, or
-// two of the 128-wide, whose steps take 0.66 of it when both run (measured on large bf16 products: 1.33 PFLOP/s with
-// 256-wide tiles, 1.0 with 128-wide); four steps stand for a tile's start and end.  Parts of k cost a launch (three
+// The shortest by this count, in microseconds.  A compute unit takes a 256-wide tile's step (64 k of 16 bits) in 1.6, or
+// two 128-wide tiles' in 1.06 (measured on large bf16 products: 1.33 and 1.0 PFLOP/s); a step of 32-bit arrays (32 k,
+// six products) is three of those.  Four steps stand for a tile's start and end.  Parts of k cost a launch (three
 // microseconds, and a tenth of one a part) and their sums, written and read once at 4 TB/s.
-Cut choose(int64_t M, int64_t N, int64_t steps) {
+Cut choose(int64_t M, int64_t N, int64_t K, int32_t dtype) {
+    const int64_t steps = tiles(K, dtype == FFN_FP32 ? 32 : 64);
+    const double unit = dtype == FFN_FP32 ? 3.0 : 1.0, ends = dtype == FFN_FP32 ? 2.0 : 4.0;
     Cut best = {256, 1};
     double least = 1e300;
     for (int32_t tile : {256, 128}) {
         const int64_t groups = tiles(M, tile) * tiles(N, tile), slots = tile == 256 ? 256 : 512;
         for (int32_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); ++s) {
-            const double t = (double)tiles(groups * s, slots) * ((double)tiles(steps, s) + 4) * (tile == 256 ? 1.6 : 1.06) +
+            const double t = (double)tiles(groups * s, slots) * ((double)tiles(steps, s) + ends) * (tile == 256 ? 1.6 : 1.06) * unit +
                              (s > 1 ? 3.0 + 0.1 * s + (double)(M * N * s) * 8.0 / 4e6 : 0.0);
             if (t < least) { least = t; best = {tile, s}; }
         }
@@ -115,11 +117,9 @@ Cut choose(int64_t M, int64_t N, int64_t steps) {
     return best;
 }
 
-int64_t steps_of(int64_t K, int32_t dtype) { return tiles(K, 64) * (dtype == FFN_FP32 ? 6 : 1); }
-
 // Bytes of the partial sums of an [M, N] product.
 int64_t partial_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype) {
-    const Cut c = choose(M, N, steps_of(K, dtype));
+    const Cut c = choose(M, N, K, dtype);
     return c.splits > 1 ? aligned(c.splits * M * ((N + 3) & ~3LL) * 4) : 0;
 }
 
@@ -134,9 +134,8 @@ int launch_tile(const ffn::TileArgs& t, int32_t epilogue, bool ac, bool bc, int3
 // Runs the product whose operands, sizes and results `t` describes; `partial` is scratch of partial_bytes() (for kGate,
 // of 2 N columns).
 int product(ffn::TileArgs t, int32_t epilogue, bool ac, bool bc, int32_t dtype, void* partial, void* stream) {
-    t.planes = dtype == FFN_FP32 ? 3 : 1;
     const int64_t columns = epilogue == ffn::kGate ? 2 * t.N : t.N;
-    const Cut c = choose(t.M, columns, steps_of(t.K, dtype));
+    const Cut c = choose(t.M, columns, t.K, dtype);
     const int64_t tm = tiles(t.M, c.tile), tn = tiles(columns, c.tile);
     if (tm * tn * c.splits > 0x7FFFFFFF / 512) return CGTP_EUNSUP;   // threads of a launch
     t.tiles_m = (int32_t)tm;
@@ -184,11 +183,11 @@ FewCut few_cut(int64_t M, int64_t N, int64_t K) {
 }
 int64_t few_grad_bytes(int64_t M, int64_t N, int64_t K) { return aligned(few_cut(M, N, K).splits * M * ((N + 3) & ~3LL) * 4); }
 
-// t describes the product and its results as for product(): t.a the rows (t.plane_a: 0, or planes), t.b [K, N] floats.
+// t describes the product and its results as for product(): t.a the rows, t.b [K, N].
 int few_grad_product(ffn::TileArgs t, int32_t epilogue, void* partial, void* stream) {
     const FewCut c = few_cut(t.M, t.N, t.K);
     ffn::FewGradArgs f = {};
-    f.x = t.a; f.ldx = t.lda; f.plane = t.plane_a; f.w = t.b; f.ldw = t.ldb;
+    f.x = t.a; f.ldx = t.lda; f.w = t.b; f.ldw = t.ldb;
     f.M = t.M; f.N = t.N; f.K = t.K;
     f.c = (float*)partial; f.ldc = (t.N + 3) & ~3LL;
     f.splits = c.splits; f.waves = c.waves;
@@ -199,25 +198,24 @@ int few_grad_product(ffn::TileArgs t, int32_t epilogue, void* partial, void* str
     return status(ffn::launch_join(f.c, f.ldc, c.splits, t.M, t.N, t.c, FFN_FP32, stream));
 }
 
-// A matrix as the products read it: 16-bit values (or three planes of them) on 16 bytes.
-struct Operand { const void* p; int64_t ld, plane; };
+// A matrix as the products read it.
+struct Operand { const void* p; int64_t ld; };
 
-// Elements of 16 bits of a packed [rows, width] matrix (one plane).
-int64_t packed(int64_t rows, int64_t width) { return rows * up8(width); }
-int64_t packed_bytes(int64_t rows, int64_t width, int32_t dtype) {
-    return aligned(packed(rows, width) * 2 * (dtype == FFN_FP32 ? 3 : 1));
-}
+int64_t packed_bytes(int64_t rows, int64_t width, int32_t dtype) { return aligned(rows * up8(width) * size_of(dtype)); }
 
-// 16-bit matrices whose rows start on 16 bytes and hold whole chunks of 16 are read where they are.
+// Values a 16-byte chunk holds.
+int64_t chunk(int32_t dtype) { return 16 / size_of(dtype); }
+
+// Matrices whose rows start on 16 bytes and hold whole chunks of 16 are read where they are, others packed.
 bool as_is(const void* p, int64_t ld, int64_t rows, int64_t width, int32_t dtype) {
-    return dtype != FFN_FP32 && ((uintptr_t)p & 15) == 0 && width % 8 == 0 && (ld % 8 == 0 || rows == 1);
+    const int64_t c = chunk(dtype);
+    return ((uintptr_t)p & 15) == 0 && width % c == 0 && (ld % c == 0 || rows == 1);
 }
 
 Operand operand(const void* p, int64_t ld, int64_t rows, int64_t width, int32_t dtype, void* scratch, ffn::PackJobs* jobs) {
-    if (as_is(p, ld, rows, width, dtype)) return {p, ld % 8 == 0 ? ld : up8(width), 0};
-    const Operand o = {scratch, up8(width), packed(rows, width)};
-    jobs->job[jobs->n++] = {p, scratch, ld, rows, width, o.ld, o.plane, 0};
-    return o;
+    if (as_is(p, ld, rows, width, dtype)) return {p, ld % chunk(dtype) == 0 ? ld : up8(width)};
+    jobs->job[jobs->n++] = {p, scratch, ld, rows, width, up8(width), 0};
+    return {scratch, up8(width)};
 }
 
 // Byte offsets in the block's workspace: intermediates, operands to be packed, partial sums.
@@ -231,8 +229,8 @@ Layout layout(const ffn_plan_s* p, int64_t N, bool backward) {
     // weights are contiguous and start on 16 bytes: they need packing by their width alone
     l.h = take(packed_bytes(N, df, t));
     l.x = take(packed_bytes(N, di, t));
-    l.w_in = take(t == FFN_FP32 || di % 8 ? packed_bytes(2 * df, di, t) : 0);
-    l.w_out = take(t == FFN_FP32 || df % 8 ? packed_bytes(d_o, df, t) : 0);
+    l.w_in = take(di % chunk(t) ? packed_bytes(2 * df, di, t) : 0);
+    l.w_out = take(df % chunk(t) ? packed_bytes(d_o, df, t) : 0);
     int64_t partial = 0;
     auto also = [&](int64_t bytes) { partial = bytes > partial ? bytes : partial; };
     if (backward) {
@@ -271,8 +269,8 @@ int dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t N, int64_t
 // Y = H Wo^T by tiles.
 int down(const ffn_plan_s* plan, const void* h, const Operand& w, void* y, int64_t N, void* partial, void* stream) {
     ffn::TileArgs o = {};
-    o.a = h; o.lda = up8(plan->d_ff); o.plane_a = packed(N, plan->d_ff);
-    o.b = w.p; o.ldb = w.ld; o.plane_b = w.plane;
+    o.a = h; o.lda = up8(plan->d_ff);
+    o.b = w.p; o.ldb = w.ld;
     o.M = N; o.N = plan->d_out; o.K = plan->d_ff;
     o.c = y; o.ldc = plan->d_out;
     return product(o, ffn::kStore, false, false, plan->dtype, partial, stream);
@@ -338,7 +336,7 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
         if (rc != CGTP_OK) return rc;
         // from here on the weights alone are many: 16-bit ones that need no packing go through LDS in 128-wide tiles with
         // k in parts, which passes 16 rows of x (4096 x 16384, 24 rows: 38 us with the joining, against 44)
-        if (N > 16 && as_is(w_out, df, d_o, df, plan->dtype)) return down(plan, ws + l.h, {w_out, df, 0}, y, N, ws + l.partial, hip_stream);
+        if (N > 16 && plan->dtype != FFN_FP32 && as_is(w_out, df, d_o, df, plan->dtype)) return down(plan, ws + l.h, {w_out, df}, y, N, ws + l.partial, hip_stream);
         ffn::FewArgs o = {};
         o.x = ws + l.h; o.ldx = up8(df); o.w = w_out; o.ldw = df;
         o.M = N; o.N = d_o; o.K = df;
@@ -351,10 +349,10 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
     rc = status(ffn::launch_pack(jobs, plan->dtype, hip_stream));
     if (rc != CGTP_OK) return rc;
     ffn::TileArgs g = {};
-    g.a = X.p; g.lda = X.ld; g.plane_a = X.plane;
-    g.b = Wi.p; g.ldb = Wi.ld; g.plane_b = Wi.plane;
+    g.a = X.p; g.lda = X.ld;
+    g.b = Wi.p; g.ldb = Wi.ld;
     g.M = N; g.N = df; g.K = di;
-    g.c = ws + l.h; g.ldc = up8(df); g.plane_c = packed(N, df);
+    g.c = ws + l.h; g.ldc = up8(df);
     g.act = plan->act; g.saved = (float*)saved;
     rc = product(g, ffn::kGate, false, false, plan->dtype, ws + l.partial, hip_stream);
     if (rc != CGTP_OK) return rc;
@@ -397,45 +395,45 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
     if (grad_w_in) X = operand(x, ldx, N, di, dt, ws + l.x, &jobs);
     rc = status(ffn::launch_pack(jobs, dt, hip_stream));
     if (rc != CGTP_OK) return rc;
-    const Operand H = {ws + l.h, up8(df), packed(N, df)}, D = {ws + l.dgu, up8(2 * df), packed(N, 2 * df)};
+    const Operand H = {ws + l.h, up8(df)}, D = {ws + l.dgu, up8(2 * df)};
     ffn::TileArgs g = {};
     if (few_h) {
         g.a = grad_y; g.lda = ldg; g.b = w_out; g.ldb = df;
     } else {
-        g.a = Gy.p; g.lda = Gy.ld; g.plane_a = Gy.plane;
-        g.b = Wo.p; g.ldb = Wo.ld; g.plane_b = Wo.plane;
+        g.a = Gy.p; g.lda = Gy.ld;
+        g.b = Wo.p; g.ldb = Wo.ld;
     }
     g.M = N; g.N = df; g.K = d_o;
-    g.c = ws + l.dgu; g.ldc = D.ld; g.plane_c = D.plane;
-    g.h = ws + l.h; g.ldh = H.ld; g.plane_h = H.plane;
+    g.c = ws + l.dgu; g.ldc = D.ld;
+    g.h = ws + l.h; g.ldh = H.ld;
     g.act = plan->act; g.saved = (float*)const_cast<void*>(saved);
     rc = few_h ? few_grad_product(g, ffn::kGateGrad, ws + l.partial, hip_stream)
                : product(g, ffn::kGateGrad, false, true, dt, ws + l.partial, hip_stream);
     if (rc == CGTP_OK && grad_x) {
         ffn::TileArgs t = {};
-        t.a = D.p; t.lda = D.ld; t.plane_a = D.plane;
+        t.a = D.p; t.lda = D.ld;
         t.M = N; t.N = di; t.K = 2 * df;
         t.c = grad_x; t.ldc = di;
         if (few_x) {
             t.b = w_in; t.ldb = di;
             rc = few_grad_product(t, ffn::kStore, ws + l.partial, hip_stream);
         } else {
-            t.b = Wi.p; t.ldb = Wi.ld; t.plane_b = Wi.plane;
+            t.b = Wi.p; t.ldb = Wi.ld;
             rc = product(t, ffn::kStore, false, true, dt, ws + l.partial, hip_stream);
         }
     }
     if (rc == CGTP_OK && grad_w_in) {
         ffn::TileArgs t = {};
-        t.a = D.p; t.lda = D.ld; t.plane_a = D.plane;
-        t.b = X.p; t.ldb = X.ld; t.plane_b = X.plane;
+        t.a = D.p; t.lda = D.ld;
+        t.b = X.p; t.ldb = X.ld;
         t.M = 2 * df; t.N = di; t.K = N;
         t.c = grad_w_in; t.ldc = di;
         rc = product(t, ffn::kStore, true, true, plan->dtype, ws + l.partial, hip_stream);
     }
     if (rc == CGTP_OK && grad_w_out) {
         ffn::TileArgs t = {};
-        t.a = Gy.p; t.lda = Gy.ld; t.plane_a = Gy.plane;
-        t.b = H.p; t.ldb = H.ld; t.plane_b = H.plane;
+        t.a = Gy.p; t.lda = Gy.ld;
+        t.b = H.p; t.ldb = H.ld;
         t.M = d_o; t.N = df; t.K = N;
         t.c = grad_w_out; t.ldc = df;
         rc = product(t, ffn::kStore, true, true, plan->dtype, ws + l.partial, hip_stream);

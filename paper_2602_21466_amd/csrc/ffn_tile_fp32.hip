@@ -3,6 +3,6 @@
 
 namespace ffn {
 int launch_tile_fp32(const TileArgs& p, int32_t epilogue, bool a_cols, bool b_cols, int32_t tile, void* stream) {
-    return dev::run_product<dev::bf16, float>(p, epilogue, a_cols, b_cols, tile, (hipStream_t)stream);
+    return dev::run_product<float>(p, epilogue, a_cols, b_cols, tile, (hipStream_t)stream);
 }
 }  // namespace ffn
