@@ -668,6 +668,7 @@ inline Shape shape_of(int64_t width, Pass pass) {
         return {0, 0};
     }
     if (chunks <= 128) return {64, 2};
+    if (pass == kForward && chunks <= 192) return {192, 1};   // (the backward pass: 54 us a pass of 4001 x 1089, 38 with 256)
     if (chunks <= 256) return {256, 1};
     for (int t : {256, 512, 1024})
         if (chunks <= 2 * t) return {t, 2};
@@ -730,6 +731,7 @@ inline unsigned row_groups(int64_t N) { return (unsigned)(N < (1 << 20) ? N : 1 
         case 32 * 8 + 1: RUN(32, 1); break;              \
         case 64 * 8 + 1: RUN(64, 1); break;              \
         case 64 * 8 + 2: RUN(64, 2); break;              \
+        case 192 * 8 + 1: RUN(192, 1); break;            \
         case 256 * 8 + 1: RUN(256, 1); break;            \
         case 256 * 8 + 2: RUN(256, 2); break;            \
         case 512 * 8 + 2: RUN(512, 2); break;            \

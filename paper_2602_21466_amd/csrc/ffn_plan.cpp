@@ -123,6 +123,12 @@ int64_t partial_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype) {
     return c.splits > 1 ? aligned(c.splits * M * ((N + 3) & ~3LL) * 4) : 0;
 }
 
+// Whether an [M, N] product's work-groups are within one launch.
+bool fits(int64_t M, int64_t N, int64_t K, int32_t dtype) {
+    const Cut c = choose(M, N, K, dtype);
+    return tiles(M, c.tile) * tiles(N, c.tile) * c.splits <= 0x7FFFFFFF / 512;
+}
+
 int launch_tile(const ffn::TileArgs& t, int32_t epilogue, bool ac, bool bc, int32_t dtype, int32_t tile, void* stream) {
     switch (dtype) {
         case FFN_FP32: return ffn::launch_tile_fp32(t, epilogue, ac, bc, tile, stream);
@@ -137,7 +143,6 @@ int product(ffn::TileArgs t, int32_t epilogue, bool ac, bool bc, int32_t dtype, 
     const int64_t columns = epilogue == ffn::kGate ? 2 * t.N : t.N;
     const Cut c = choose(t.M, columns, t.K, dtype);
     const int64_t tm = tiles(t.M, c.tile), tn = tiles(columns, c.tile);
-    if (tm * tn * c.splits > 0x7FFFFFFF / 512) return CGTP_EUNSUP;   // threads of a launch
     t.tiles_m = (int32_t)tm;
     t.tiles_n = (int32_t)tn;
     t.splits = c.splits;
@@ -317,6 +322,7 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
     if (N > FFN_MAX_ROWS || ldx > kMaxStride) return CGTP_EUNSUP;
     const int64_t e = size_of(plan->dtype), di = plan->d_in, df = plan->d_ff, d_o = plan->d_out;
     if (misaligned({x}, e) || misaligned({w_in, w_out, y, saved}, 16)) return CGTP_EINVAL;
+    if (!fits(N, 2 * df, di, plan->dtype) || !fits(N, d_o, df, plan->dtype)) return CGTP_EUNSUP;
     const Layout l = layout(plan, N, false);
     int rc = workspace_ok(workspace, workspace_bytes, l.total);
     if (rc != CGTP_OK) return rc;
@@ -367,6 +373,8 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
     if (N > 0 && (!x || !w_in || !w_out || !saved || !grad_y || ldx < di || ldg < d_o)) return CGTP_EINVAL;
     if (N > FFN_MAX_ROWS || ldx > kMaxStride || ldg > kMaxStride) return CGTP_EUNSUP;
     if (misaligned({x, grad_y}, e) || misaligned({w_in, w_out, saved, grad_x, grad_w_in, grad_w_out}, 16)) return CGTP_EINVAL;
+    if (!fits(N, df, d_o, plan->dtype) || !fits(N, di, 2 * df, plan->dtype) || !fits(2 * df, di, N, plan->dtype) || !fits(d_o, df, N, plan->dtype))
+        return CGTP_EUNSUP;
     const Layout l = layout(plan, N, true);
     int rc = workspace_ok(workspace, workspace_bytes, l.total);
     if (rc != CGTP_OK) return rc;
