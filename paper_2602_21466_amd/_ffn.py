@@ -192,6 +192,14 @@ def _new(shape, dtype, dev, other):
         return _t.empty(shape, dtype=dtype, device=_t.devices[dev])
 
 
+def _like(t, other):
+    """A new tensor like t, which is contiguous."""
+    if other is None:
+        return _t.empty_like(t)
+    with _t.on_stream(other):
+        return _t.empty_like(t)
+
+
 def _workspace(workspace, need, dev, other):
     if workspace is None:
         return _new((max(need, 1),), _t.uint8, dev, other)
@@ -244,8 +252,8 @@ class FfnPlan:
             return None, None, None
         sp, other = _stream(stream, dev)
         gx = _new((N, di), tdt, dev, other) if need_x else None
-        gwi = _new((2 * df, di), tdt, dev, other) if need_w_in else None
-        gwo = _new((do, df), tdt, dev, other) if need_w_out else None
+        gwi = _like(w_in, other) if need_w_in else None
+        gwo = _like(w_out, other) if need_w_out else None
         ws = _workspace(workspace, ffn_backward_workspace_bytes(self._h, N), dev, other)
         ptr = lambda t: t.data_ptr() if t is not None else None
         ffn_backward(self._h, x.data_ptr(), ldx, wi, wo, sv, grad_out.data_ptr(), ldg, ptr(gx), ptr(gwi), ptr(gwo), N,
@@ -342,8 +350,8 @@ class NormPlan:
         gp, np_ = _whole(gate, tdt, (self._gates(N), D), "gate", dev), _whole(w_next, tdt, (D,), "w_next", dev)
         sp, other = _stream(stream, dev)
         if out is None:
-            out = _new((N, D), tdt, dev, other)
-        u = _new((N, D), tdt, dev, other) if next_norm else None
+            out = _like(h, other)
+        u = _like(h, other) if next_norm else None
         stats = _new((2, N), _t.float32, dev, other)
         _call("ffn_residual_forward", self._norm(seed, offset), xp, hp, wp, gp, sc, np_, _whole(out, tdt, (N, D), "out", dev),
                              u.data_ptr() if next_norm else None, stats.data_ptr(), N, sp)
@@ -366,9 +374,8 @@ class NormPlan:
         st = _whole(stats, _t.float32, (2, N), "stats", dev)
         gyp, gup = _whole(grad_y, tdt, (N, D), "grad_y", dev), _whole(grad_u, tdt, (N, D), "grad_u", dev)
         sp, other = _stream(stream, dev)
-        gx, gh = _new((N, D), tdt, dev, other), _new((N, D), tdt, dev, other)
-        gw, gs, gn = (None if t is None else _new((D,), tdt, dev, other) for t in (w, scale, w_next))
-        gg = None if gate is None else _new(tuple(gate.shape), tdt, dev, other)
+        gx, gh = _like(h, other), _like(h, other)
+        gw, gs, gn, gg = (None if t is None else _like(t, other) for t in (w, scale, w_next, gate))
         norm = self._norm(seed, offset)
         ws = _workspace(workspace, ffn_norm_workspace_bytes(norm, N, 1), dev, other)
         ptr = lambda t: t.data_ptr() if t is not None else None
@@ -395,7 +402,7 @@ def dropout(x, p: float, seed: int, offset: int = 0, out=None, stream=None):
         raise ValueError("x must be contiguous, or [N, width] with strided rows")
     sp, other = _stream(stream, dev)
     if out is None:
-        out, ldy = _new(x.shape, x.dtype, dev, other), width
+        out, ldy = _like(x, other) if ldx == width else _new(x.shape, x.dtype, dev, other), width
     elif out.shape != x.shape or out.get_device() != dev or out.dtype != x.dtype:
         raise ValueError("out must have the shape, type and device of x")
     elif out.is_contiguous():
