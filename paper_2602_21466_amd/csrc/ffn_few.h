@@ -164,7 +164,7 @@ __global__ __launch_bounds__(512) void few_kernel(FewArgs p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float a, da;
-                activate(p.act, v[e], a, da);
+                activate<T>(p.act, v[e], a, da);
                 h[e] = a * u[e];
             }
             store4<T>((T*)p.c + r * p.ldc, n, p.N, p.ldc, h);

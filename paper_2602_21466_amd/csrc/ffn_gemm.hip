@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const f
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float a, da;
-                activate(p.act, v[e], a, da);
+                activate<T>(p.act, v[e], a, da);
                 h[e] = a * u[e];
             }
             store4<T>((T*)p.c + m * p.ldc, n, p.N, p.ldc, h);
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const f
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float a, da;
-                activate(p.act, g[e], a, da);
+                activate<T>(p.act, g[e], a, da);
                 dg[e] = v[e] * u[e] * da;
                 du[e] = v[e] * a;
                 h[e] = a * u[e];

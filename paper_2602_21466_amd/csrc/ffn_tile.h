@@ -434,7 +434,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float a, da;
-                    activate(p.act, v[e], a, da);
+                    activate<T>(p.act, v[e], a, da);
                     h[e] = a * u[e];
                 }
                 store4<T>((T*)p.c + m * p.ldc, n, p.N, p.ldc, h);
@@ -452,7 +452,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float a, da;
-                    activate(p.act, g[e], a, da);
+                    activate<T>(p.act, g[e], a, da);
                     dg[e] = v[e] * u[e] * da;
                     du[e] = v[e] * a;
                     h[e] = a * u[e];
