@@ -94,38 +94,41 @@ int check_norm(const ffn_norm* n, int64_t N, ffn::NormArgs* a) {
 int64_t up8(int64_t n) { return (n + 7) & ~7LL; }
 int64_t tiles(int64_t n, int64_t t) { return (n + t - 1) / t; }
 
-// How a product is cut up: work-groups of `tile` x `tile` outputs, k in `splits` parts.
-struct Cut { int32_t tile, splits; };
+// How a product is cut up: work-groups of `tile` x `tile` outputs, k in `splits` parts; joined: the parts' sums (also of
+// one part) go to memory and a second kernel finishes them.
+struct Cut { int32_t tile, splits; bool joined; };
 
 // The shortest by this count, in microseconds.  A compute unit takes a 256-wide tile's step (64 k of 16 bits) in 1.6, or
 // two 128-wide tiles' in 1.06 (measured on large bf16 products: 1.33 and 1.0 PFLOP/s); a step of 32-bit arrays (32 k,
 // six products) is three of those.  Four steps stand for a tile's start and end.  Parts of k cost a launch (three
-// microseconds, and a tenth of one a part) and their sums, written and read once at 4 TB/s.
-Cut choose(int64_t M, int64_t N, int64_t K, int32_t dtype) {
+// microseconds, and a tenth of one a part) and their sums, written and read once at 4 TB/s; the gate's gradient in the
+// tiles' own epilogue costs ten where they are few (4004 rows, 144 x 348: 26 us, against 15 with the joining kernel).
+Cut choose(int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t epilogue) {
     const int64_t steps = tiles(K, dtype == FFN_FP32 ? 32 : 64);
     const double unit = dtype == FFN_FP32 ? 3.0 : 1.0, ends = dtype == FFN_FP32 ? 2.0 : 4.0;
-    Cut best = {256, 1};
+    Cut best = {256, 1, false};
     double least = 1e300;
     for (int32_t tile : {256, 128}) {
         const int64_t groups = tiles(M, tile) * tiles(N, tile), slots = tile == 256 ? 256 : 512;
         for (int32_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); ++s) {
-            const double t = (double)tiles(groups * s, slots) * ((double)tiles(steps, s) + ends) * (tile == 256 ? 1.6 : 1.06) * unit +
-                             (s > 1 ? 3.0 + 0.1 * s + (double)(M * N * s) * 8.0 / 4e6 : 0.0);
-            if (t < least) { least = t; best = {tile, s}; }
+            const double t = (double)tiles(groups * s, slots) * ((double)tiles(steps, s) + ends) * (tile == 256 ? 1.6 : 1.06) * unit;
+            const double join = 3.0 + 0.1 * s + (double)(M * N * s) * 8.0 / 4e6, own = epilogue == ffn::kGateGrad ? 10.0 : 0.0;
+            const bool joined = s > 1 || own > join;
+            if (t + (joined ? join : own) < least) { least = t + (joined ? join : own); best = {tile, s, joined}; }
         }
     }
     return best;
 }
 
 // Bytes of the partial sums of an [M, N] product.
-int64_t partial_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype) {
-    const Cut c = choose(M, N, K, dtype);
-    return c.splits > 1 ? aligned(c.splits * M * ((N + 3) & ~3LL) * 4) : 0;
+int64_t partial_bytes(int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t epilogue = ffn::kStore) {
+    const Cut c = choose(M, N, K, dtype, epilogue);
+    return c.joined ? aligned(c.splits * M * ((N + 3) & ~3LL) * 4) : 0;
 }
 
 // Whether an [M, N] product's work-groups are within one launch.
-bool fits(int64_t M, int64_t N, int64_t K, int32_t dtype) {
-    const Cut c = choose(M, N, K, dtype);
+bool fits(int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t epilogue = ffn::kStore) {
+    const Cut c = choose(M, N, K, dtype, epilogue);
     return tiles(M, c.tile) * tiles(N, c.tile) * c.splits <= 0x7FFFFFFF / 512;
 }
 
@@ -141,12 +144,12 @@ int launch_tile(const ffn::TileArgs& t, int32_t epilogue, bool ac, bool bc, int3
 // of 2 N columns).
 int product(ffn::TileArgs t, int32_t epilogue, bool ac, bool bc, int32_t dtype, void* partial, void* stream) {
     const int64_t columns = epilogue == ffn::kGate ? 2 * t.N : t.N;
-    const Cut c = choose(t.M, columns, t.K, dtype);
+    const Cut c = choose(t.M, columns, t.K, dtype, epilogue);
     const int64_t tm = tiles(t.M, c.tile), tn = tiles(columns, c.tile);
     t.tiles_m = (int32_t)tm;
     t.tiles_n = (int32_t)tn;
     t.splits = c.splits;
-    if (c.splits == 1) return status(launch_tile(t, epilogue, ac, bc, dtype, c.tile, stream));
+    if (!c.joined) return status(launch_tile(t, epilogue, ac, bc, dtype, c.tile, stream));
     ffn::TileArgs s = t;
     s.c = partial;
     s.N = columns;
@@ -241,7 +244,7 @@ Layout layout(const ffn_plan_s* p, int64_t N, bool backward) {
     if (backward) {
         l.dgu = take(packed_bytes(N, 2 * df, t));
         l.gy = take(packed_bytes(N, d_o, t));
-        also(few_grad(N, df, t) ? few_grad_bytes(N, df, d_o) : partial_bytes(N, df, d_o, t));
+        also(few_grad(N, df, t) ? few_grad_bytes(N, df, d_o) : partial_bytes(N, df, d_o, t, ffn::kGateGrad));
         also(few_grad(N, di, t) ? few_grad_bytes(N, di, 2 * df) : partial_bytes(N, di, 2 * df, t));
         also(partial_bytes(2 * df, di, N, t));
         also(partial_bytes(d_o, df, N, t));
@@ -373,7 +376,7 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
     if (N > 0 && (!x || !w_in || !w_out || !saved || !grad_y || ldx < di || ldg < d_o)) return CGTP_EINVAL;
     if (N > FFN_MAX_ROWS || ldx > kMaxStride || ldg > kMaxStride) return CGTP_EUNSUP;
     if (misaligned({x, grad_y}, e) || misaligned({w_in, w_out, saved, grad_x, grad_w_in, grad_w_out}, 16)) return CGTP_EINVAL;
-    if (!fits(N, df, d_o, plan->dtype) || !fits(N, di, 2 * df, plan->dtype) || !fits(2 * df, di, N, plan->dtype) || !fits(d_o, df, N, plan->dtype))
+    if (!fits(N, df, d_o, plan->dtype, ffn::kGateGrad) || !fits(N, di, 2 * df, plan->dtype) || !fits(2 * df, di, N, plan->dtype) || !fits(d_o, df, N, plan->dtype))
         return CGTP_EUNSUP;
     const Layout l = layout(plan, N, true);
     int rc = workspace_ok(workspace, workspace_bytes, l.total);
