@@ -11,7 +11,9 @@
 // LDS layouts, chosen so that the direct loads write whole 1 KB runs and the
 // reads meet no bank twice:
 //   rows:    [row][128 bytes of k], 16-byte chunk c of row r kept at chunk
-//            c ^ (r & 7); fragments by 16-byte reads
+//            c ^ (r & 7), with 32 bits the even chunks before the odd ones
+//            (c / 2 + 4 (c % 2) in place of c); fragments by 16-byte reads, in
+//            both types of q ^ (r & 7) and that ^ 4 by lanes 16 q .. + 15
 //   columns, 16 bits: [k][BM or BN], 32-byte unit u of row k kept at u ^ s(k),
 //            s(k) = (k & 3) | ((k >> 3) & 1) << 2; fragments by the transposing
 //            8-byte read (16 lanes give four k-rows of 16 values and get back one
@@ -130,7 +132,7 @@ template <int ES, int R, int NW, bool COLS, int GATE> struct Loader {
 
     __device__ __forceinline__ void init(const void* p, int64_t ld, int64_t r0, int64_t rows, int64_t half, int wave, int lane) {
         if constexpr (!COLS) {
-            const int sub = lane >> 3, c = (lane & 7) ^ sub;
+            const int sub = lane >> 3, at = (lane & 7) ^ sub, c = ES == 4 ? (at & 3) * 2 + (at >> 2) : at;
             kpos = c * kPer;
             step = 128;
             base[0] = (const char*)p + r0 * ld * ES;
@@ -187,7 +189,7 @@ template <int ES, int R, int NW, bool COLS, int GATE> struct Loader {
 template <int ES, int R, bool COLS> struct Fragments {
     static __device__ __forceinline__ int base(int r0, int lane) {
         const int q = lane >> 4, i = lane & 15;
-        if constexpr (!COLS) return (r0 + i) * 128 + (((ES == 4 ? 2 * q : q) ^ (i & 7)) << 4);
+        if constexpr (!COLS) return (r0 + i) * 128 + ((q ^ (i & 7)) << 4);
         if constexpr (ES == 4) return 8 * q * R * 4 + (((r0 >> 4) ^ q) << 6) + i * 4;
         const int k = q * 8 + (i >> 2);
         return k * R * 2 + (((r0 >> 4) ^ Loader<2, R, 1, true, 0>::swizzle(k)) << 5) + (i & 3) * 8;
@@ -202,7 +204,7 @@ template <int ES, int R, bool COLS> struct Fragments {
     static __device__ __forceinline__ void get32(const char* lds, int base, int i, f32x4 (&v)[2]) {
         if constexpr (!COLS) {
             v[0] = *(const f32x4*)(lds + base + i * 2048);
-            v[1] = *(const f32x4*)(lds + (base ^ 16) + i * 2048);
+            v[1] = *(const f32x4*)(lds + (base ^ 64) + i * 2048);
         } else {
             const char* at = lds + (base ^ (i << 6));
 #pragma unroll
