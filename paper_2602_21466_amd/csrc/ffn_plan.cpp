@@ -98,20 +98,25 @@ int64_t tiles(int64_t n, int64_t t) { return (n + t - 1) / t; }
 // one part) go to memory and a second kernel finishes them.
 struct Cut { int32_t tile, splits; bool joined; };
 
-// The shortest by this count, in microseconds.  A compute unit takes a 256-wide tile's step (64 k of 16 bits) in 1.6, or
-// two 128-wide tiles' in 1.06 (measured on large bf16 products: 1.33 and 1.0 PFLOP/s); a step of 32-bit arrays (32 k,
-// six products) is three of those.  Four steps stand for a tile's start and end.  Parts of k cost a launch (three
-// microseconds, and a tenth of one a part) and their sums, written and read once at 4 TB/s; the gate's gradient in the
-// tiles' own epilogue costs ten where they are few (4004 rows, 144 x 348: 26 us, against 15 with the joining kernel).
+// The shortest by this count, in microseconds.  A compute unit takes a 256-wide tile's step (64 k of 16 bits, 32 of 32
+// bits) in 1.6 (4.5), or two 128-wide tiles' in 1.06 (2.6), one alone in about three quarters of that (measured on large products:
+// bf16 1.33 and 1.0 PFLOP/s, fp32 237 and 205 TFLOP/s).  Four (two) steps stand for a tile's start and end.  Parts of k cost
+// a launch (three microseconds, and a tenth of one a part) and their sums, written and read once at 4 TB/s; the gate's
+// gradient in the tiles' own epilogue costs ten where they are few (4004 rows, 144 x 348: 26 us, against 17 with the
+// joining kernel).
 Cut choose(int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t epilogue) {
-    const int64_t steps = tiles(K, dtype == FFN_FP32 ? 32 : 64);
-    const double unit = dtype == FFN_FP32 ? 3.0 : 1.0, ends = dtype == FFN_FP32 ? 2.0 : 4.0;
+    const bool wide = dtype == FFN_FP32;
+    const int64_t steps = tiles(K, wide ? 32 : 64);
+    const double ends = wide ? 2.0 : 4.0;
     Cut best = {256, 1, false};
     double least = 1e300;
     for (int32_t tile : {256, 128}) {
         const int64_t groups = tiles(M, tile) * tiles(N, tile), slots = tile == 256 ? 256 : 512;
+        const double step = tile == 256 ? (wide ? 4.5 : 1.6) : (wide ? 2.6 : 1.06);
         for (int32_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); ++s) {
-            const double t = (double)tiles(groups * s, slots) * ((double)tiles(steps, s) + ends) * (tile == 256 ? 1.6 : 1.06) * unit;
+            const int64_t whole = groups * s / slots, rest = groups * s - whole * slots;
+            const double rounds = (double)whole + (rest == 0 ? 0.0 : tile == 128 && rest <= 256 ? 0.75 : 1.0);
+            const double t = rounds * ((double)tiles(steps, s) + ends) * step;
             const double join = 3.0 + 0.1 * s + (double)(M * N * s) * 8.0 / 4e6, own = epilogue == ffn::kGateGrad ? 10.0 : 0.0;
             const bool joined = s > 1 || own > join;
             if (t + (joined ? join : own) < least) { least = t + (joined ? join : own); best = {tile, s, joined}; }
