@@ -108,7 +108,7 @@ struct NormArgs {
     float* partial;       // workspace
 };
 
-int64_t norm_workspace_floats(int64_t width, int64_t N, int64_t rows_per_gate, bool residual);
+int64_t norm_workspace_floats(int64_t width, int64_t N, int64_t rows_per_gate, bool residual, int bytes);
 
 #define FFN_NORM_LAUNCHERS(TYPE)                                                                                     \
     int launch_norm_forward_##TYPE(const NormArgs& a, void* stream);                                                 \

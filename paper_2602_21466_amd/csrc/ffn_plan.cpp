@@ -480,7 +480,7 @@ int ffn_norm_forward(const ffn_norm* norm, const void* x, int64_t ldx, const voi
 int64_t ffn_norm_workspace_bytes(const ffn_norm* norm, int64_t N, int32_t residual) {
     ffn::NormArgs a;
     if ((residual & ~1) || check_norm(norm, N, &a) != CGTP_OK) return -1;
-    return aligned(ffn::norm_workspace_floats(a.width, N, a.rows_per_gate, residual != 0) * 4);
+    return aligned(ffn::norm_workspace_floats(a.width, N, a.rows_per_gate, residual != 0, (int)size_of(norm->dtype)) * 4);
 }
 
 int ffn_norm_backward(const ffn_norm* norm, const void* x, int64_t ldx, const void* w, const float* rstd,

@@ -45,6 +45,15 @@ def test_norm_descriptions(kw):
     assert lib.ffn_norm_workspace_bytes(n, 4, 0) == -1
 
 
+@pytest.mark.parametrize("width", [1, 7, 64, 300, 1401, 5001, 20001, 1 << 20])
+@pytest.mark.parametrize("rows_per_gate", [1, 3, 1000, 1 << 30])
+def test_norm_workspace_of_any_rows(width, rows_per_gate):
+    for dtype in (0, 2, 3):
+        n = lib.ffn_norm(width, rows_per_gate, dtype, 1e-6, 0.0, 0, 0)
+        for rows in (0, 1, 5, 255, 256, 4097, 100000, 1 << 30):
+            assert all(lib.ffn_norm_workspace_bytes(n, rows, r) >= 0 for r in (0, 1))
+
+
 def test_norm_workspace_and_dtype():
     n = lib.ffn_norm(64, 1, 2, 1e-6, 0.0, 0, 0)
     assert lib.ffn_norm_workspace_bytes(n, 0, 0) >= 0

@@ -134,6 +134,36 @@ def test_dropout_of_more_than_32_bits_of_values():
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("N,D,rpg", [(700, 5001, 100), (4500, 1401, 1), (1100, 1029, 64), (300, 2500, 1000), (6000, 77, 7)])
+def test_residual_with_dropout(N, D, rpg, dtype):
+    """Widths whose last eight columns two threads share, rows divided within and over gate rows: against the same
+    formula in 64 bits with the mask that `dropout` gives, and in place of x."""
+    torch, lib = _setup()
+    g = torch.Generator(device="cuda").manual_seed(N + D)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=torch.float64).to(_dt(torch, dtype))
+    x, h, gy, gu, gate, w, scale, wn = r(N, D), r(N, D), r(N, D), r(N, D), r(-(-N // rpg), D), r(D), r(D), r(D)
+    plan = lib.NormPlan(D, dtype=dtype, rows_per_gate=rpg, eps=1e-4, dropout=0.25)
+    kw = {"gate": gate, "scale": scale, "w_next": wn, "seed": 77, "offset": 5}
+    y, u, stats = plan.residual(x, h, w, **kw)
+    grads = plan.residual_backward(h, y, w, stats, gy, gu, **kw)
+    keep = (lib.dropout(torch.ones(N, D, device="cuda"), 0.25, seed=77, offset=5) != 0).double() / 0.75
+    leaves = [t.double().requires_grad_(True) for t in (x, h, w, gate, scale, wn)]
+    xr, hr, wr, gr, sr, nr = leaves
+    norm = lambda v, f: v / (v.square().mean(1, keepdim=True) + 1e-4).sqrt() * f
+    yr = xr + sr * gr[torch.arange(N, device="cuda") // rpg] * keep * norm(hr, wr)
+    ur = norm(yr, nr)
+    want = torch.autograd.grad((yr * gy.double()).sum() + (ur * gu.double()).sum(), leaves)
+    assert _rel(y, yr.detach()) <= _tol(dtype, 1) and _rel(u, ur.detach()) <= _tol(dtype, 1)
+    for got, wt in zip(grads, want):
+        assert _rel(got, wt) <= _tol(dtype, 3)          # y is read back rounded
+    into = x.clone()
+    y2, u2, _ = plan.residual(into, h, w, out=into, **kw)
+    assert y2.data_ptr() == into.data_ptr() and torch.equal(y, y2) and torch.equal(u, u2)
+    for a, b in zip(grads, plan.residual_backward(h, y, w, stats, gy, gu, **kw)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 def test_example(dtype):
     """The operators together as a network uses them: the loss falls and the weighted products are finite."""
     torch, _ = _setup()
