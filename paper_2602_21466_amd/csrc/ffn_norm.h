@@ -15,55 +15,6 @@ template <typename T> __device__ __forceinline__ float load(const void* p, int64
     return p ? to_f32(((const T*)p)[i]) : missing;
 }
 
-// Dropout factor of (row, column).
-__device__ __forceinline__ float factor(const DropArgs& d, int64_t row, int64_t c) {
-    if (d.threshold == 0) return 1.0f;
-    const Words q = philox((uint32_t)(c >> 3), (uint32_t)row, d.offset, d.seed);
-    return kept(q, (int)(c & 7), d.threshold) ? d.scale : 0.0f;
-}
-
-// One row a work-group: y = x + scale * gate * drop(N(h; w)) where h is given, then u = N(y; wn).
-template <typename T>
-__global__ __launch_bounds__(kThreads) void norm_forward_kernel(NormArgs p) {
-    __shared__ float s[kThreads / 64];
-    const int64_t D = p.width;
-    for (int64_t row = blockIdx.x; row < p.N; row += gridDim.x) {
-    const T* x = (const T*)p.x + row * p.ldx;
-    const T* h = p.h ? (const T*)p.h + row * D : nullptr;
-    float rh = 0.0f;
-    if (h) {
-        float sum = 0.0f;
-        for (int64_t c = threadIdx.x; c < D; c += kThreads) sum += to_f32(h[c]) * to_f32(h[c]);
-        rh = 1.0f / sqrtf(group_sum(sum, s) / (float)D + p.eps);
-        if (p.rstd_h && threadIdx.x == 0) p.rstd_h[row] = rh;
-    }
-    const int64_t gate = row / p.rows_per_gate * D;
-    auto joined = [&](int64_t c) {
-        float v = to_f32(x[c]);
-        if (h) {
-            const float f = factor(p.drop, row, c);
-            const float n = to_f32(h[c]) * rh * load<T>(p.w, c, 1.0f);
-            const float b = f == 0.0f ? 0.0f : n * f;
-            v += load<T>(p.scale, c, 1.0f) * load<T>(p.gate, gate + c, 1.0f) * b;
-        }
-        return v;
-    };
-    if (p.u) {
-        float sum = 0.0f;
-        for (int64_t c = threadIdx.x; c < D; c += kThreads) { const float v = joined(c); sum += v * v; }
-        const float ry = 1.0f / sqrtf(group_sum(sum, s) / (float)D + p.eps);
-        if (p.rstd_y && threadIdx.x == 0) p.rstd_y[row] = ry;
-        for (int64_t c = threadIdx.x; c < D; c += kThreads) {
-            const float v = joined(c);
-            if (p.y) ((T*)p.y)[row * D + c] = (T)v;
-            ((T*)p.u)[row * p.ldu + c] = (T)(v * ry * load<T>(p.wn, c, 1.0f));
-        }
-    } else {
-        for (int64_t c = threadIdx.x; c < D; c += kThreads) ((T*)p.y)[row * D + c] = (T)joined(c);
-    }
-    }
-}
-
 // ---------------------------------------------------------------- rows held in registers
 //
 // A worker of TPR threads takes a row, eight adjacent values (one block of the generator) a thread and turn, I turns:
@@ -115,6 +66,65 @@ __device__ __forceinline__ void drop8(const DropArgs& d, int64_t row, int64_t c,
     const Words q = philox((uint32_t)(c >> 3), (uint32_t)row, d.offset, d.seed);
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = kept(q, j, d.threshold) ? d.scale : 0.0f;
+}
+
+// One row a work-group, eight columns a thread and turn: rows too narrow or too wide for registers.  y = x + scale * gate *
+// drop(N(h; w)) where h is given, then u = N(y; wn).  A row is read again for each sum, from the caches while it fits them
+// (1000 x 40000 in bf16: 55 us, 151 with the block's side;
+// by single values 184 and 643).
+template <typename T>
+__global__ __launch_bounds__(kThreads) void norm_forward_kernel(NormArgs p) {
+    __shared__ float s[kThreads / 64];
+    const int64_t D = p.width;
+    for (int64_t row = blockIdx.x; row < p.N; row += gridDim.x) {
+        const T* x = (const T*)p.x + row * p.ldx;
+        const T* h = p.h ? (const T*)p.h + row * D : nullptr;
+        const T* gate = p.h && p.gate ? (const T*)p.gate + row / p.rows_per_gate * D : nullptr;
+        float rh = 0.0f;
+        if (h) {
+            float sum = 0.0f;
+            for (int64_t c = threadIdx.x * 8; c < D; c += kThreads * 8) {
+                float v[8];
+                factors8<T>(h, c, D, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum += v[j] * v[j];   // (zeros beyond the row)
+            }
+            rh = 1.0f / sqrtf(group_sum(sum, s) / (float)D + p.eps);
+            if (p.rstd_h && threadIdx.x == 0) p.rstd_h[row] = rh;
+        }
+        auto joined = [&](int64_t c, float (&v)[8]) {
+            factors8<T>(x, c, D, v);
+            if (!h) return;
+            float n[8], w[8], sc[8], g[8], f[8];
+            factors8<T>(h, c, D, n);
+            factors8<T>(p.w, c, D, w);
+            factors8<T>(p.scale, c, D, sc);
+            factors8<T>(gate, c, D, g);
+            drop8(p.drop, row, c, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += sc[j] * g[j] * (f[j] == 0.0f ? 0.0f : n[j] * rh * w[j] * f[j]);
+        };
+        float sum = 0.0f;
+        for (int64_t c = threadIdx.x * 8; c < D; c += kThreads * 8) {
+            float v[8];
+            joined(c, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += c + j < D ? v[j] * v[j] : 0.0f;
+            if (!p.u) store8((T*)p.y + row * D, c, D, v);
+        }
+        if (!p.u) continue;
+        const float ry = 1.0f / sqrtf(group_sum(sum, s) / (float)D + p.eps);
+        if (p.rstd_y && threadIdx.x == 0) p.rstd_y[row] = ry;
+        for (int64_t c = threadIdx.x * 8; c < D; c += kThreads * 8) {
+            float v[8], wn[8];
+            joined(c, v);
+            if (p.y) store8((T*)p.y + row * D, c, D, v);
+            factors8<T>(p.wn, c, D, wn);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= ry * wn[j];
+            store8((T*)p.u + row * p.ldu, c, D, v);
+        }
+    }
 }
 
 // The kept of the generator's block of eight columns, bit j for column j; and of a row's columns c .. c + 7.
@@ -408,7 +418,9 @@ struct Walk {
     }
 };
 
-// The means of (gu w_next) n_y and of (d/dN(h)) w n_h.
+// The means of (gu w_next) n_y and of (d/dN(h)) w n_h, a row a work-group: all arrays are read here and again by the
+// columns' kernel (4000 x 12000 in bf16: 136 us and 254, 3.5 and 3.2 TB/s; rows of fewer than eight columns leave most of
+// a work-group idle, 100000 x 4 in fp32: 175 us and 180).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_means_kernel(NormArgs p, Rows rw) {
     __shared__ float s[kThreads / 64];
@@ -686,7 +698,8 @@ __global__ __launch_bounds__(group_of(TPR), backward_waves(sizeof(T), TPR, I, H)
 }
 
 // The work-groups' column sums added up, 64 columns a work-group, sixteen strands of rows; then, by the work-groups
-// after those, the parts of each gate row.  Every sum is taken in a fixed order.
+// after those, the parts of each gate row.  Every sum is taken in a fixed order.  (16384 x 4096 with 32 gate rows in 16
+// parts: 10 us for 26 MB, of which a launch is 3.)
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs p, Rows rw, int64_t groups, int sums) {
     const int64_t D = p.width, blocks = (D + 63) / 64, c = (int64_t)(blockIdx.x % blocks) * 64 + (threadIdx.x & 63);
@@ -790,7 +803,7 @@ inline int64_t groups_for(const Rows& r, const Shape& sh) {
 }
 
 // A thread a block of eight columns (one call of the generator) and turn; the row and block of its next turn follow
-// from the last one's without a division.
+// from the last one's without a division.  Bound by HBM: 5.2 TB/s at 8192 x 16384 in bf16 (103 us); 6 us at 8192 x 289 in fp32.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(const T* x, int64_t ldx, T* y, int64_t ldy, int64_t N, int64_t width,
                                                            DropArgs d, int64_t step_rows, int64_t step_blocks) {
