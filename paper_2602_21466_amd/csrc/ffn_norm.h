@@ -697,54 +697,56 @@ __global__ __launch_bounds__(group_of(TPR), backward_waves(sizeof(T), TPR, I, H)
     }
 }
 
-// The work-groups' column sums added up, 64 columns a work-group, sixteen strands of rows; then, by the work-groups
-// after those, the parts of each gate row.  Every sum is taken in a fixed order.  (16384 x 4096 with 32 gate rows in 16
-// parts: 10 us for 26 MB, of which a launch is 3.)
+// The work-groups' column sums added up, then, by the work-groups after those, the parts of each gate row: a work-group
+// takes 1024 / strands columns by so many strands of rows.  Every sum is taken in a fixed order.  (1001 sets of 2 x 1089
+// sums: 7.4 us, 7.8 with half the strands; beside them 32 gate rows of 4096 in 16 parts: 7.1 us with a strand for these, 11.2
+// with sixteen, which a gate row of 1000 columns in a thousand parts needs.)
+struct Join { int sums, strands, gate_strands; };   // strands: as powers of two
 template <typename T>
-__global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs p, Rows rw, int64_t groups, int sums) {
-    const int64_t D = p.width, blocks = (D + 63) / 64, c = (int64_t)(blockIdx.x % blocks) * 64 + (threadIdx.x & 63);
-    const int strand = threadIdx.x >> 6;
-    const int64_t job = blockIdx.x / blocks;
-    const bool gates = job >= sums;
+__global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs p, Rows rw, int64_t groups, Join jn) {
+    const int64_t D = p.width, sum_blocks = (D + (1024 >> jn.strands) - 1) >> (10 - jn.strands);
+    const bool gates = blockIdx.x >= sum_blocks * jn.sums;
+    const int shift = 10 - (gates ? jn.gate_strands : jn.strands), columns = 1 << shift, strands = 1024 >> shift;
+    const uint32_t blocks = (uint32_t)((D + columns - 1) >> shift), id = gates ? blockIdx.x - (uint32_t)sum_blocks * jn.sums : blockIdx.x;
+    const int64_t job = id / blocks;
+    const int strand = threadIdx.x >> shift;
+    const int64_t c = ((int64_t)(id % blocks) << shift) + (threadIdx.x & (columns - 1));
     const float* from;
     int64_t n;
-    const bool split = sums == 2 && rw.parts > 1;
+    const bool split = jn.sums == 2 && rw.parts > 1;
     if (gates) {
-        const int64_t gate = job - sums;
-        from = p.partial + gate * rw.parts * D + c;
+        from = p.partial + job * rw.parts * D + c;
         // the last gate row may have fewer rows: the workers beyond them wrote nothing
-        const int64_t left = p.N - gate * p.rows_per_gate;
+        const int64_t left = p.N - job * p.rows_per_gate;
         n = left < rw.parts ? left : rw.parts;
     } else {
         from = p.partial + (split ? rw.workers * D : 0) + job * D + c;
         n = groups;
     }
-    const int64_t step = gates ? D : sums * D;
+    const int64_t step = gates ? D : jn.sums * D;
     float v = 0.0f, u[8] = {};
     if (c < D) {
         int64_t i = strand;
-        for (; i + 112 < n; i += 128)   // eight loads in flight
+        for (; i + 7 * strands < n; i += 8 * strands)   // eight loads in flight
 #pragma unroll
-            for (int k = 0; k < 8; ++k) u[k] += from[(i + 16 * k) * step];
-        for (; i < n; i += 16) v += from[i * step];
+            for (int k = 0; k < 8; ++k) u[k] += from[(i + strands * k) * step];
+        for (; i < n; i += strands) v += from[i * step];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v += u[k];
     }
-    __shared__ float s[16][64];
-    s[strand][threadIdx.x & 63] = v;
+    __shared__ float s[1024];
+    s[threadIdx.x] = v;
     __syncthreads();
     if (strand || c >= D) return;
-#pragma unroll
-    for (int k = 1; k < 16; ++k) v += s[k][threadIdx.x];
+#pragma unroll 8
+    for (int k = 1; k < strands; ++k) v += s[(k << shift) + threadIdx.x];
     if (gates) {
-        ((T*)p.ggate)[(job - sums) * D + c] = (T)v;
+        ((T*)p.ggate)[job * D + c] = (T)v;
+    } else if (job == jn.sums - 1) {
+        if (p.gwn) ((T*)p.gwn)[c] = (T)v;
     } else {
-        if (job == sums - 1) {
-            if (p.gwn) ((T*)p.gwn)[c] = (T)v;
-        } else {
-            if (p.gw) ((T*)p.gw)[c] = (T)(v * load<T>(p.scale, c, 1.0f));
-            if (p.gscale) ((T*)p.gscale)[c] = (T)(v * load<T>(p.w, c, 1.0f));
-        }
+        if (p.gw) ((T*)p.gw)[c] = (T)(v * load<T>(p.scale, c, 1.0f));
+        if (p.gscale) ((T*)p.gscale)[c] = (T)(v * load<T>(p.w, c, 1.0f));
     }
 }
 
@@ -896,9 +898,11 @@ template <typename T> int backward(const NormArgs& a, hipStream_t s) {
 #undef FFN_BACKWARD
     }
     if (a.gw || a.gscale || a.gwn || (a.ggate && rw.parts > 1)) {
-        const int sums = block ? 2 : 1;
-        const int64_t jobs = sums + (a.ggate && rw.parts > 1 ? (a.N + a.rows_per_gate - 1) / a.rows_per_gate : 0);
-        norm_join_kernel<T><<<dim3((unsigned)(jobs * ((a.width + 63) / 64))), 1024, 0, s>>>(a, rw, groups, sums);
+        // one strand where a gate row has few parts
+        const Join jn = {block ? 2 : 1, 5, rw.parts > 64 ? 4 : 0};
+        auto blocks = [&](int strands) { return (a.width + (1024 >> strands) - 1) >> (10 - strands); };
+        const int64_t gates = a.ggate && rw.parts > 1 ? (a.N + a.rows_per_gate - 1) / a.rows_per_gate : 0;
+        norm_join_kernel<T><<<dim3((unsigned)(jn.sums * blocks(jn.strands) + gates * blocks(jn.gate_strands))), 1024, 0, s>>>(a, rw, groups, jn);
     }
     return (int)hipGetLastError();
 }
