@@ -14,15 +14,17 @@
  * Row strides (ldx, ...) count elements and must be >= the row's width; the
  * elements of a row are adjacent.  Arrays that have a row stride, and those of
  * the norms and of dropout, need the alignment of their element; the weights
- * and results of ffn_forward and ffn_backward start on 16 bytes (CGTP_EINVAL).  No output may overlap an input, the workspace or another
+ * and results of ffn_forward and ffn_backward start on 16 bytes
+ * (CGTP_EINVAL).  No output may overlap an input, the workspace or another
  * output (CGTP_EINVAL), except where a call says so.
  *
- * Every call runs asynchronously on hip_stream (NULL: the default stream),
- * allocates nothing, and may be captured in a HIP graph; scratch memory is the
- * caller's workspace, 256-byte aligned, of the size that the matching query
- * gives, whose contents need not be kept between calls.  N == 0 returns
- * CGTP_OK; gradients that sum over rows are then zero.  Status codes are those
- * of cgtp.h, and cgtp_strerror / cgtp_last_hip_error apply.
+ * Every call runs asynchronously on hip_stream (NULL: the default stream) of
+ * the current device, which must be the arrays' own, allocates nothing, and may
+ * be captured in a HIP graph; scratch memory is the caller's workspace,
+ * 256-byte aligned, of the size that the matching query gives, whose contents
+ * need not be kept between calls.  N == 0 returns CGTP_OK; gradients that sum
+ * over rows are then zero.  Status codes are those of cgtp.h, and
+ * cgtp_strerror / cgtp_last_hip_error apply.
  */
 #ifndef FFN_H
 #define FFN_H

@@ -145,6 +145,7 @@ class _Torch:
         import torch
         self.empty, self.empty_like, self.float32, self.uint8 = torch.empty, torch.empty_like, torch.float32, torch.uint8
         self.raw_stream, self.on_stream = torch._C._cuda_getCurrentRawStream, torch.cuda.stream
+        self.current_device = torch._C._cuda_getDevice
         self.dtypes = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
         self.codes = {t: _DTYPES[name] for name, t in self.dtypes.items()}
         self.devices = [torch.device("cuda", i) for i in range(max(torch.cuda.device_count(), 1))]
@@ -178,9 +179,14 @@ def _whole(t, tdt, shape, what, dev):
 
 
 def _stream(stream, dev):
-    """The HIP stream's handle, and the torch stream where it is not the current one."""
+    """The HIP stream's handle, and the torch stream where it is not the current one.  Kernels start on the current
+    device, which must be the tensors'."""
+    if _t.current_device() != dev:
+        raise ValueError("the tensors are on GPU %d, which is not the current device" % dev)
     if stream is None:
         return _t.raw_stream(dev), None
+    if stream.device_index != dev:
+        raise ValueError("the stream is not one of GPU %d" % dev)
     return stream.cuda_stream, stream
 
 

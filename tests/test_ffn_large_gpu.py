@@ -173,3 +173,21 @@ def test_example(dtype):
     losses, weights, z = mod.main(pairs=300, steps=20, L=3, channels=2, dtype=dtype)
     assert losses[-1] < 0.9 * losses[0] and weights.isfinite().all() and z.isfinite().all()
     assert z.shape == (300, 2, 256)
+
+
+def test_current_device_is_the_tensors(monkeypatch):
+    """Kernels start on the current device: tensors of another one are refused."""
+    torch, lib = _setup()
+    from paper_2602_21466_amd import _ffn
+    x = torch.ones(2, 8, device="cuda")
+    plan = lib.NormPlan(8)
+    _, rstd = plan.forward(x)
+    block, w_in, w_out = lib.FfnPlan(8, 8, 8), torch.ones(16, 8, device="cuda"), torch.ones(8, 8, device="cuda")
+    calls = (lambda: plan.forward(x), lambda: plan.residual(x, x), lambda: lib.dropout(x, 0.5, seed=1),
+             lambda: plan.backward(x, None, rstd, x), lambda: block.forward(x, w_in, w_out))
+    for call in calls:
+        call()
+    monkeypatch.setattr(_ffn._t, "current_device", lambda: 1)
+    for call in calls:
+        with pytest.raises(ValueError, match="current device"):
+            call()
