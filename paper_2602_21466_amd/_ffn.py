@@ -143,12 +143,11 @@ class _Torch:
 
     def __getattr__(self, name):
         import torch
-        self.empty, self.empty_like, self.float32, self.uint8 = torch.empty, torch.empty_like, torch.float32, torch.uint8
+        self.empty_like, self.float32, self.uint8 = torch.empty_like, torch.float32, torch.uint8
         self.raw_stream, self.on_stream = torch._C._cuda_getCurrentRawStream, torch.cuda.stream
         self.current_device = torch._C._cuda_getDevice
         self.dtypes = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
         self.codes = {t: _DTYPES[name] for name, t in self.dtypes.items()}
-        self.devices = [torch.device("cuda", i) for i in range(max(torch.cuda.device_count(), 1))]
         return self.__dict__[name]
 
 
@@ -173,7 +172,7 @@ def _whole(t, tdt, shape, what, dev):
     """Pointer of t, a contiguous tensor of this shape on GPU `dev` (None where t is None)."""
     if t is None:
         return None
-    if t.get_device() != dev or t.dtype != tdt or t.shape != shape or not t.is_contiguous():
+    if t.dtype != tdt or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor %s on GPU %d" % (what, tdt, list(shape), dev))
     return t.data_ptr()
 
@@ -190,12 +189,23 @@ def _stream(stream, dev):
     return stream.cuda_stream, stream
 
 
-def _new(shape, dtype, dev, other):
-    """A new tensor of the stream `other` (None: the current one), so that its memory is reused in that stream's order."""
+def _new(t, shape, other):
+    """A new tensor of t's type and device, of the stream `other` (None: the current one), so that its memory is reused
+    in that stream's order."""
     if other is None:
-        return _t.empty(shape, dtype=dtype, device=_t.devices[dev])
+        return t.new_empty(shape)
     with _t.on_stream(other):
-        return _t.empty(shape, dtype=dtype, device=_t.devices[dev])
+        return t.new_empty(shape)
+
+
+def _new32(t, shape, other):
+    """The same, of 32-bit floats."""
+    if t.dtype == _t.float32:
+        return _new(t, shape, other)
+    if other is None:
+        return t.new_empty(shape, dtype=_t.float32)
+    with _t.on_stream(other):
+        return t.new_empty(shape, dtype=_t.float32)
 
 
 def _like(t, other):
@@ -206,9 +216,11 @@ def _like(t, other):
         return _t.empty_like(t)
 
 
-def _workspace(workspace, need, dev, other):
+def _workspace(workspace, need, t, other):
+    """The caller's workspace, or a new one on t's device (of t's type, whose creation costs the least)."""
     if workspace is None:
-        return _new((max(need, 1),), _t.uint8, dev, other)
+        return _new(t, (need // t.element_size() + 1,), other)
+    dev = t.get_device()
     if workspace.dtype != _t.uint8 or workspace.get_device() != dev or not workspace.is_contiguous() or \
             workspace.numel() < need:
         raise ValueError("workspace must be a contiguous uint8 tensor of at least %d bytes on GPU %d" % (need, dev))
@@ -236,12 +248,13 @@ class FfnPlan:
         wi, wo = _whole(w_in, tdt, (2 * df, di), "w_in", dev), _whole(w_out, tdt, (do, df), "w_out", dev)
         sp, other = _stream(stream, dev)
         if out is None:
-            out = _new((N, do), tdt, dev, other)
+            out = _new(x, (N, do), other)
         if save and saved is None:
-            saved = _new((N, 2 * df), _t.float32, dev, other)
-        ws = _workspace(workspace, ffn_workspace_bytes(self._h, N), dev, other)
-        ffn_forward(self._h, x.data_ptr(), ldx, wi, wo, _whole(out, tdt, (N, do), "out", dev),
-                    _whole(saved, _t.float32, (N, 2 * df), "saved", dev), N, ws.data_ptr(), ws.numel(), sp)
+            saved = _new32(x, (N, 2 * df), other)
+        need = ffn_workspace_bytes(self._h, N)
+        ws = _workspace(workspace, need, x, other)
+        _call("ffn_forward", self._h, x.data_ptr(), ldx, wi, wo, _whole(out, tdt, (N, do), "out", dev),
+              _whole(saved, _t.float32, (N, 2 * df), "saved", dev), N, ws.data_ptr(), need, sp)
         return out if saved is None else (out, saved)
 
     def backward(self, x, w_in, w_out, saved, grad_out, need_x=True, need_w_in=True, need_w_out=True, workspace=None,
@@ -257,13 +270,14 @@ class FfnPlan:
         if not (need_x or need_w_in or need_w_out):
             return None, None, None
         sp, other = _stream(stream, dev)
-        gx = _new((N, di), tdt, dev, other) if need_x else None
+        gx = _new(x, (N, di), other) if need_x else None
         gwi = _like(w_in, other) if need_w_in else None
         gwo = _like(w_out, other) if need_w_out else None
-        ws = _workspace(workspace, ffn_backward_workspace_bytes(self._h, N), dev, other)
+        need = ffn_backward_workspace_bytes(self._h, N)
+        ws = _workspace(workspace, need, x, other)
         ptr = lambda t: t.data_ptr() if t is not None else None
-        ffn_backward(self._h, x.data_ptr(), ldx, wi, wo, sv, grad_out.data_ptr(), ldg, ptr(gx), ptr(gwi), ptr(gwo), N,
-                     ws.data_ptr(), ws.numel(), sp)
+        _call("ffn_backward", self._h, x.data_ptr(), ldx, wi, wo, sv, grad_out.data_ptr(), ldg, ptr(gx), ptr(gwi), ptr(gwo),
+              N, ws.data_ptr(), need, sp)
         return gx, gwi, gwo
 
     def close(self):
@@ -311,11 +325,13 @@ class NormPlan:
         wp = _whole(w, tdt, (D,), "w", dev)
         sp, other = _stream(stream, dev)
         if out is None:
-            out = _new((N, D), tdt, dev, other)
+            out, ldu = _new(x, (N, D), other), D
+        else:
+            ldu = _rows(out, tdt, N, D, "out", dev)
         if rstd is None:
-            rstd = _new((N,), _t.float32, dev, other)
-        _call("ffn_norm_forward", self._plain, x.data_ptr(), ldx, wp, out.data_ptr(), _rows(out, tdt, N, D, "out", dev),
-                         _whole(rstd, _t.float32, (N,), "rstd", dev), N, sp)
+            rstd = _new32(x, (N,), other)
+        _call("ffn_norm_forward", self._plain, x.data_ptr(), ldx, wp, out.data_ptr(), ldu,
+              _whole(rstd, _t.float32, (N,), "rstd", dev), N, sp)
         return out, rstd
 
     def backward(self, x, w, rstd, grad_out, need_x=True, need_w=True, workspace=None, stream=None):
@@ -329,12 +345,12 @@ class NormPlan:
             return None, None
         sp, other = _stream(stream, dev)
         norm = self._plain
-        gx = _new((N, D), tdt, dev, other) if need_x else None
-        gw = _new((D,), tdt, dev, other) if need_w else None
-        ws = _workspace(workspace, ffn_norm_workspace_bytes(norm, N, 0), dev, other)
-        ffn_norm_backward(norm, x.data_ptr(), ldx, wp, rp, grad_out.data_ptr(), ldg,
-                          gx.data_ptr() if need_x else None, gw.data_ptr() if need_w else None, N, ws.data_ptr(),
-                          ws.numel(), sp)
+        gx = _new(x, (N, D), other) if need_x else None
+        gw = _new(x, (D,), other) if need_w else None
+        need = ffn_norm_workspace_bytes(norm, N, 0)
+        ws = _workspace(workspace, need, x, other)
+        _call("ffn_norm_backward", norm, x.data_ptr(), ldx, wp, rp, grad_out.data_ptr(), ldg,
+              gx.data_ptr() if need_x else None, gw.data_ptr() if need_w else None, N, ws.data_ptr(), need, sp)
         return gx, gw
 
     def _gates(self, N):
@@ -358,7 +374,7 @@ class NormPlan:
         if out is None:
             out = _like(h, other)
         u = _like(h, other) if next_norm else None
-        stats = _new((2, N), _t.float32, dev, other)
+        stats = _new32(x, (2, N), other)
         _call("ffn_residual_forward", self._norm(seed, offset), xp, hp, wp, gp, sc, np_, _whole(out, tdt, (N, D), "out", dev),
                              u.data_ptr() if next_norm else None, stats.data_ptr(), N, sp)
         return out, u, stats
@@ -383,10 +399,11 @@ class NormPlan:
         gx, gh = _like(h, other), _like(h, other)
         gw, gs, gn, gg = (None if t is None else _like(t, other) for t in (w, scale, w_next, gate))
         norm = self._norm(seed, offset)
-        ws = _workspace(workspace, ffn_norm_workspace_bytes(norm, N, 1), dev, other)
+        need = ffn_norm_workspace_bytes(norm, N, 1)
+        ws = _workspace(workspace, need, h, other)
         ptr = lambda t: t.data_ptr() if t is not None else None
-        ffn_residual_backward(norm, hp, yp, wp, gp, sc, np_, st, gyp, gup, gx.data_ptr(), gh.data_ptr(), ptr(gw), ptr(gg),
-                              ptr(gs), ptr(gn), N, ws.data_ptr(), ws.numel(), sp)
+        _call("ffn_residual_backward", norm, hp, yp, wp, gp, sc, np_, st, gyp, gup, gx.data_ptr(), gh.data_ptr(), ptr(gw),
+              ptr(gg), ptr(gs), ptr(gn), N, ws.data_ptr(), need, sp)
         return gx, gh, gw, gg, gs, gn
 
 
@@ -408,7 +425,7 @@ def dropout(x, p: float, seed: int, offset: int = 0, out=None, stream=None):
         raise ValueError("x must be contiguous, or [N, width] with strided rows")
     sp, other = _stream(stream, dev)
     if out is None:
-        out, ldy = _like(x, other) if ldx == width else _new(x.shape, x.dtype, dev, other), width
+        out, ldy = _like(x, other) if ldx == width else _new(x, x.shape, other), width
     elif out.shape != x.shape or out.get_device() != dev or out.dtype != x.dtype:
         raise ValueError("out must have the shape, type and device of x")
     elif out.is_contiguous():
