@@ -41,7 +41,7 @@ template <typename T> __device__ __forceinline__ void activate(int act, float g,
         v = g * c;
         dv = c + g * 0.39894228040143267794f * e;
     } else {
-        v = g > 0.0f ? g : 0.0f;
+        v = g <= 0.0f ? 0.0f : g;   // (NaN stays)
         dv = g > 0.0f ? 1.0f : 0.0f;
     }
 }

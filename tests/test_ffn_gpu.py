@@ -155,6 +155,24 @@ def test_ffn_rows_do_not_mix():
         assert not got[7].isfinite().any() and got[21].isnan().all()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+def test_ffn_gate_that_is_nan_reaches_the_output(act, dtype):
+    """One row of the gate's weights is NaN, with every U finite: each Y is NaN, with few rows and with many, and so
+    are the gradients of w_out and of the up projection that its activation enters, and no others of the two."""
+    torch, lib = _setup()
+    for N in (5, 150):
+        x, wi, wo, gy = (t.cuda() for t in _ffn_case(torch, N, 64, 96, 64, dtype))
+        wi[11] = float("nan")
+        plan = lib.FfnPlan(64, 96, 64, dtype=dtype, activation=act)
+        y, saved = plan.forward(x, wi, wo, save=True)
+        assert y.isnan().all() and bool(saved[:, 11].isnan().all()) and bool(saved[:, 96:].isfinite().all())
+        gwi, gwo = plan.backward(x, wi, wo, saved, gy)[1:]
+        assert gwo[:, 11].isnan().all() and gwi[96 + 11].isnan().all()
+        other = [j for j in range(96) if j != 11]
+        assert gwo[:, other].isfinite().all() and gwi[96:][other].isfinite().all()
+
+
 def test_ffn_gradients_against_differences():
     """Central differences of sum(grad * Y) along random directions, in fp32 arrays at a small size: the step 2^-6
     leaves a third-order term of about 2^-12 relative and rounding of about 2^-24 * 2^6 relative to |Y|."""
