@@ -502,6 +502,7 @@ int ffn_norm_backward(const ffn_norm* norm, const void* x, int64_t ldx, const vo
     if (any_overlap(outs, ins)) return CGTP_EINVAL;
     a.y = const_cast<void*>(x); a.ldx = ldx; a.wn = w; a.rstd_y = const_cast<float*>(rstd);
     a.gu = grad_u; a.ldg = ldg; a.gx = grad_x; a.gwn = grad_w;
+    a.rows_per_gate = 1;   // there is no gate: its rows divide nothing (as the workspace's size has it)
     a.partial = (float*)workspace;
     return status(norm_backward(a, norm->dtype, hip_stream));
 }
