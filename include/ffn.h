@@ -89,8 +89,10 @@ int64_t ffn_backward_workspace_bytes(ffn_plan_t plan, int64_t N);
  * H is held in the arrays' type between the two products (as dG, dU and H are
  * in ffn_backward): in fp16 its values above 65504 become infinite.  32-bit
  * products of more than 64 rows, and the weights' gradients, run as six products
- * of bf16 parts of the operands, as exact as 32-bit sums of 32-bit products;
- * there a value that is not finite gives NaN in every sum that it enters.
+ * of bf16 parts of the operands, added in 32 bits: beside the rounding of the
+ * sum, each product x w is off by at most 2^-22 |x w|, of either sign (2^-25.5 in
+ * the root mean square; a 32-bit product is off by up to 2^-24); there a value
+ * that is not finite gives NaN in every sum that it enters.
  */
 int ffn_forward(ffn_plan_t plan, const void *x, int64_t ldx, const void *w_in, const void *w_out, void *y,
                 void *saved, int64_t N, void *workspace, int64_t workspace_bytes, void *hip_stream);

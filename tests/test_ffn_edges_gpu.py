@@ -1,6 +1,7 @@
 """The feed-forward sublayer where single values, views and the division of rows tell: bounds that hold for every value
 and not in the mean of many, arrays that lie in one another's gaps or in place of one another, and plans that differ in
 what a call does not read."""
+import numpy as np
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -40,3 +41,58 @@ def test_norm_before_does_not_depend_on_the_gate_rows(N, D, dtype):
         u2, rstd2 = other.forward(x, w)
         assert torch.equal(u, u2) and torch.equal(rstd, rstd2)
         assert all(torch.equal(a, b) for a, b in zip(want, other.backward(x, w, rstd, gu))), rpg
+
+
+# ---------------------------------------------------------------- 32-bit products, value by value
+
+# Significands of which cutting or rounding at 8 and at 16 bits leaves the most, and random ones of one sign: what a
+# product leaves out adds up instead of averaging out.
+ONE_STEP = 2.0 ** -22 + 2.0 ** -23 * 17 / 16
+
+
+@pytest.mark.parametrize("N,di,df", [(96, 8, 24), (300, 5, 130), (1030, 30, 516)])
+@pytest.mark.parametrize("bits", [0x3F80FFFF, 0x3F80FF80, 0x3F80FE80, 0x3F80FE7F, 0x3F808001, 0x3FFFFFFF, None])
+def test_products_of_one_sign_in_32_bits(N, di, df, bits):
+    """G and U of at most 32 terms, one step of the products: 2^-22 of |x| |w| left out, one rounding of the sum with the
+    last and largest of the six products, 2^-23 if it is by cutting, and a sixteenth of that for the roundings before,
+    of sums of at most 2^-6 of its size."""
+    torch, lib = _setup()
+    if bits is None:
+        g = torch.Generator(device="cuda").manual_seed(N)
+        draw = lambda *s: 1.0 + torch.rand(s, generator=g, device="cuda")
+    else:
+        draw = lambda *s: torch.full(s, np.uint32(bits).view(np.float32).item(), device="cuda")
+    x, wi, wo = draw(N, di), draw(2 * df, di), draw(8, df)
+    _, saved = lib.FfnPlan(di, df, 8, activation="relu").forward(x, wi, wo, save=True)
+    want = x.double() @ wi.double().T
+    assert float(((saved.double() - want).abs() / want).max()) <= ONE_STEP
+
+
+@pytest.mark.parametrize("bits", [0x3F80FFFF, 0x3F80FF80, 0x3F80FE80])
+def test_gradient_products_of_one_sign_in_32_bits(bits):
+    """grad_w_out = grad_y^T H with H = U (ReLU, G = 1), one step of 31 rows; both arrays are read by columns."""
+    torch, lib = _setup()
+    N, di, df, do = 31, 8, 64, 40
+    v = np.uint32(bits).view(np.float32).item()
+    one = lambda *s: torch.full(s, v, device="cuda")
+    saved = one(N, 2 * df)
+    saved[:, :df] = 1.0
+    plan = lib.FfnPlan(di, df, do, activation="relu")
+    gwo = plan.backward(one(N, di), one(2 * df, di), one(do, df), saved, one(N, do))[2]
+    want = N * v * v
+    assert float((gwo.double() - want).abs().max()) / want <= ONE_STEP
+
+
+def test_products_of_the_largest_values_in_32_bits():
+    """Values up to the largest of the type times small ones: finite, and as exact as others."""
+    torch, lib = _setup()
+    top = torch.finfo(torch.float32).max
+    for s in (1.0, -1.0):
+        x = torch.full((100, 8), s * top, device="cuda")
+        x[1::2] *= 0.997
+        x[2::3] *= 1.0 - 2.0 ** -9
+        wi, wo = torch.full((16, 8), 1.1e-38, device="cuda"), torch.ones(8, 8, device="cuda")
+        wi[3:9] *= 0.75
+        _, saved = lib.FfnPlan(8, 8, 8, activation="relu").forward(x, wi * 2.0 ** 20, wo, save=True)
+        want = x.double() @ (wi * 2.0 ** 20).double().T
+        assert float(((saved.double() - want).abs() / want.abs()).max()) <= ONE_STEP
