@@ -18,9 +18,13 @@ typedef _Float16 fp16;
 template <typename T> __device__ __forceinline__ float to_f32(T v) { return (float)v; }
 
 // act(g) and act'(g).  T: the arrays' type; for 16-bit ones the exponential and the reciprocal are the hardware's (within
-// 2^-20 for |g| < 16) and the error function is the polynomial of Abramowitz and Stegun, 7.1.26, whose exponential is the
-// derivative's own: erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2), t = 1 / (1 + p x), within 1.5e-7, a thousandth of those
-// types' rounding.  (A 128 x 128 tile's epilogue with erff and expf took as long as 16 steps of its products.)
+// 2^-20 for |g| < 16), and the error function takes the form of Abramowitz and Stegun, 7.1.26, whose exponential is the
+// derivative's own: erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2), t = 1 / (1 + p x), x >= 0.  The table's coefficients are for
+// the absolute error; those here are fitted to the relative one (least squares, weights after Lawson until the largest
+// errors are equal, for x up to 9.5), which decides gelu where the gate has nearly closed: 6.4e-7, and with the 32-bit
+// arithmetic 3e-6 for g >= -6 and 4e-5 down to -13.4, below which bf16 has no values: a 150th of fp16's unit roundoff and a
+// hundredth of bf16's.  (A 128 x 128 tile's epilogue with erff and expf took as long as 16 steps of its products.)  32-bit
+// arrays have the error function beside 1, as the plain form does: its rounding, 2^-24, is what is left of gelu's value there.
 template <typename T> __device__ __forceinline__ void activate(int act, float g, float& v, float& dv) {
     constexpr bool kFast = sizeof(T) == 2;
     if (act == FFN_SILU) {
@@ -31,8 +35,8 @@ template <typename T> __device__ __forceinline__ void activate(int act, float g,
         float c, e;
         if (kFast) {
             e = __builtin_amdgcn_exp2f(-0.72134752f * g * g);       // exp(-g^2 / 2)
-            const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * 0.70710678f * fabsf(g));
-            const float half = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+            const float t = __builtin_amdgcn_rcpf(1.0f + 0.375f * 0.70710678f * fabsf(g));
+            const float half = 0.5f * e * t * (0.21133945f + t * (0.215689163f + t * (0.166664659f + t * (0.283061293f + t * (-0.129596948f + t * (0.387937573f - t * 0.135095828f))))));
             c = g < 0.0f ? half : 1.0f - half;
         } else {
             e = expf(-0.5f * g * g);

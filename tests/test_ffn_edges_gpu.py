@@ -96,3 +96,43 @@ def test_products_of_the_largest_values_in_32_bits():
         _, saved = lib.FfnPlan(8, 8, 8, activation="relu").forward(x, wi * 2.0 ** 20, wo, save=True)
         want = x.double() @ (wi * 2.0 ** 20).double().T
         assert float(((saved.double() - want).abs() / want.abs()).max()) <= ONE_STEP
+
+
+# ---------------------------------------------------------------- activations, value by value
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("N", [9, 400])
+def test_activations_value_by_value(N, act, dtype):
+    """H = act(G) U and dG = U act'(G) with G given and U a power of two, through weights of ones: each is the
+    definition's value rounded once, to within a sixteenth of a rounding, also where the gate has nearly closed.  In 32
+    bits 2^-18 for the elementary functions, and for GELU 2^-23 of G for the error function's rounding beside 1."""
+    torch, lib = _setup()
+    tdt = _dt(torch, dtype)
+    low = -5.75 if dtype == "fp16" else -12.0            # (act(G) U stays a normal number of its type)
+    g = torch.linspace(low, 4.0, N, dtype=torch.float64, device="cuda").to(tdt)
+    size = 8192.0
+    x = torch.stack([g, torch.ones_like(g)], 1)
+    wi = torch.zeros(16, 2, dtype=tdt, device="cuda")
+    wi[:8, 0], wi[8:, 1] = 1.0, size
+    eye = torch.eye(8, dtype=tdt, device="cuda")
+    plan = lib.FfnPlan(2, 8, 8, dtype=dtype, activation=act)
+    y, saved = plan.forward(x, wi, eye, save=True)
+    assert torch.equal(saved[:, 0], g.float()) and bool((saved[:, 8:] == size).all())
+    gy = torch.zeros(N, 8, dtype=tdt, device="cuda")
+    gy[:, 0] = 1.0
+    gx = plan.backward(x, wi, eye, saved, gy, True, False, False)[0]
+    v = g.double()
+    if act == "silu":
+        s = torch.sigmoid(v)
+        a, da = v * s, s * (1.0 + v * (1.0 - s))
+    else:
+        cdf = 0.5 * torch.special.erfc(-v * 0.5 ** 0.5)     # (ndtr cancels beside 1 here)
+        a, da = v * cdf, cdf + v * torch.exp(-0.5 * v * v) / (2.0 * np.pi) ** 0.5
+    tol = {"fp32": 2.0 ** -18, "bf16": 2.0 ** -8 * 17 / 16, "fp16": 2.0 ** -11 * 17 / 16}[dtype]
+    slack = 2.0 ** -23 if dtype == "fp32" and act == "gelu" else 0.0
+    assert bool(((y.double() / size - a[:, None]).abs() <= tol * a[:, None].abs() + slack * v[:, None].abs()).all())
+    # (the derivative passes zero about G = -0.75 or -1.28, where its two terms, of 0.2 or more, cancel)
+    crossing = (v > -1.6) & (v < -0.5)
+    part = torch.where(crossing, da.abs().clamp_min(0.01), da.abs())
+    assert bool(((gx[:, 0].double() / size - da).abs() <= tol * part + slack).all())
