@@ -161,8 +161,8 @@ def _rows(t, tdt, rows, width, what, dev=None):
     if dev is not None and t.get_device() != dev:
         raise ValueError("all tensors must be on GPU %d: %s is not" % (dev, what))
     ld, one = t.stride()
-    if t.shape[0] <= 1:
-        ld = max(ld, width)
+    if t.shape[0] <= 1:   # (a stride that is never taken)
+        ld = width
     if (width > 1 and one != 1) or ld < width:
         raise ValueError("%s must have adjacent values in each row and rows that do not overlap" % what)
     return ld

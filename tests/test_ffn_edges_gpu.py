@@ -136,3 +136,24 @@ def test_activations_value_by_value(N, act, dtype):
     crossing = (v > -1.6) & (v < -0.5)
     part = torch.where(crossing, da.abs().clamp_min(0.01), da.abs())
     assert bool(((gx[:, 0].double() / size - da).abs() <= tol * part + slack).all())
+
+
+# ---------------------------------------------------------------- views and arrays in place of others
+
+def test_one_row_of_a_wide_array():
+    """The stride of a single row is never used: a row of an array of any width is taken."""
+    torch, lib = _setup()
+    big = torch.zeros(3, (1 << 21) + 64, dtype=torch.bfloat16, device="cuda")
+    x = big[1:2, 5:69]
+    x.copy_(_randn(torch, 1, (1, 64), "bf16"))
+    packed = x.clone()
+    wi, wo = _randn(torch, 2, (96, 64), "bf16"), _randn(torch, 3, (64, 48), "bf16")
+    plan, norm = lib.FfnPlan(64, 48, 64, dtype="bf16"), lib.NormPlan(64, dtype="bf16")
+    y, saved = plan.forward(x, wi, wo, save=True)
+    assert torch.equal(y, plan.forward(packed, wi, wo))
+    for a, b in zip(plan.backward(x, wi, wo, saved, x), plan.backward(packed, wi, wo, saved, packed)):
+        assert torch.equal(a, b)
+    u, rstd = norm.forward(x)
+    assert torch.equal(u, norm.forward(packed)[0])
+    assert torch.equal(norm.backward(x, None, rstd, x)[0], norm.backward(packed, None, rstd, packed)[0])
+    assert torch.equal(lib.dropout(x, 0.5, seed=1), lib.dropout(packed, 0.5, seed=1))
