@@ -16,7 +16,8 @@
  * the norms and of dropout, need the alignment of their element; the weights
  * and results of ffn_forward and ffn_backward start on 16 bytes
  * (CGTP_EINVAL).  No output may overlap an input, the workspace or another
- * output (CGTP_EINVAL), except where a call says so.
+ * output (CGTP_EINVAL), except where a call says so; neighbouring columns of one
+ * array (rows of one stride that share no element) do not overlap.
  *
  * Every call runs asynchronously on hip_stream (NULL: the default stream) of
  * the current device, which must be the arrays' own, allocates nothing, and may

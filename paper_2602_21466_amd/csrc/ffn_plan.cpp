@@ -18,12 +18,19 @@ namespace {
 
 constexpr int64_t kMaxStride = 1LL << 21;   // byte offsets within a tile of 256 rows stay below 2^31
 
-struct Range { const void* p; int64_t bytes; };
+// An array's bytes, from the first to the last; for rows with a stride, that and the row's own bytes (else 0).
+struct Range { const void* p; int64_t bytes, ld, width; };
 
+// Rows of one stride, or a block beside them, may lie in one another's gaps, as neighbouring columns of one array do.
 bool overlaps(const Range& a, const Range& b) {
     if (!a.p || !b.p || a.bytes <= 0 || b.bytes <= 0) return false;
-    const char *pa = (const char*)a.p, *pb = (const char*)b.p;
-    return pa < pb + b.bytes && pb < pa + a.bytes;
+    const int64_t apart = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
+    if (apart >= a.bytes || -apart >= b.bytes) return false;
+    const int64_t ld = a.ld ? a.ld : b.ld;
+    if (ld == 0 || (b.ld && b.ld != ld)) return true;
+    int64_t at = apart % ld;   // of b's rows in a's
+    if (at < 0) at += ld;
+    return at < (a.ld ? a.width : a.bytes) || at + (b.ld ? b.width : b.bytes) > ld;
 }
 
 // Whether any of the outputs meets an input or a later output.
@@ -40,8 +47,10 @@ template <size_t A, size_t B> bool any_overlap(const Range (&outs)[A], const Ran
 int64_t size_of(int32_t dtype) { return dtype == FFN_FP32 ? 4 : 2; }
 bool known(int32_t dtype) { return dtype == FFN_FP32 || dtype == FFN_BF16 || dtype == FFN_FP16; }
 int64_t aligned(int64_t bytes) { return (bytes + 255) & ~255LL; }
-// bytes from the first to the last value of N rows
-int64_t span(int64_t N, int64_t ld, int64_t width, int64_t e) { return N > 0 ? ((N - 1) * ld + width) * e : 0; }
+// N rows of `width` values, `ld` apart
+Range rows(const void* p, int64_t N, int64_t ld, int64_t width, int64_t e) {
+    return {p, N > 0 ? ((N - 1) * ld + width) * e : 0, ld * e, width * e};
+}
 
 bool misaligned(std::initializer_list<const void*> ps, int64_t e) {
     uintptr_t all = 0;
@@ -334,7 +343,7 @@ int ffn_forward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, c
     const Layout l = layout(plan, N, false);
     int rc = workspace_ok(workspace, workspace_bytes, l.total);
     if (rc != CGTP_OK) return rc;
-    const Range ins[] = {{x, span(N, ldx, di, e)}, {w_in, 2 * df * di * e}, {w_out, d_o * df * e}};
+    const Range ins[] = {rows(x, N, ldx, di, e), {w_in, 2 * df * di * e}, {w_out, d_o * df * e}};
     const Range outs[] = {{y, N * d_o * e}, {saved, N * 2 * df * 4}, {workspace, l.total}};
     if (any_overlap(outs, ins)) return CGTP_EINVAL;
     rc = current_device_is(plan->device);
@@ -386,8 +395,8 @@ int ffn_backward(ffn_plan_t plan, const void* x, int64_t ldx, const void* w_in, 
     const Layout l = layout(plan, N, true);
     int rc = workspace_ok(workspace, workspace_bytes, l.total);
     if (rc != CGTP_OK) return rc;
-    const Range ins[] = {{x, span(N, ldx, di, e)}, {w_in, 2 * df * di * e}, {w_out, d_o * df * e},
-                         {saved, N * 2 * df * 4}, {grad_y, span(N, ldg, d_o, e)}};
+    const Range ins[] = {rows(x, N, ldx, di, e), {w_in, 2 * df * di * e}, {w_out, d_o * df * e},
+                         {saved, N * 2 * df * 4}, rows(grad_y, N, ldg, d_o, e)};
     const Range outs[] = {{grad_x, N * di * e}, {grad_w_in, 2 * df * di * e}, {grad_w_out, d_o * df * e},
                           {workspace, l.total}};
     if (any_overlap(outs, ins)) return CGTP_EINVAL;
@@ -467,9 +476,9 @@ int ffn_norm_forward(const ffn_norm* norm, const void* x, int64_t ldx, const voi
     if (ldx > kMaxStride || ldu > kMaxStride) return CGTP_EUNSUP;
     const int64_t e = size_of(norm->dtype);
     if (misaligned({x, w, u}, e) || misaligned({rstd}, 4)) return CGTP_EINVAL;
-    const Range in_x[] = {{u == x && ldu == ldx ? nullptr : x, span(N, ldx, a.width, e)}, {w, a.width * e}};
-    const Range outs[] = {{u, span(N, ldu, a.width, e)}, {rstd, N * 4}};
-    const Range also[] = {{x, span(N, ldx, a.width, e)}};
+    const Range in_x[] = {rows(u == x && ldu == ldx ? nullptr : x, N, ldx, a.width, e), {w, a.width * e}};
+    const Range outs[] = {rows(u, N, ldu, a.width, e), {rstd, N * 4}};
+    const Range also[] = {rows(x, N, ldx, a.width, e)};
     const Range stat[] = {{rstd, N * 4}};
     if (any_overlap(outs, in_x) || any_overlap(stat, also)) return CGTP_EINVAL;
     a.x = x; a.ldx = ldx;
@@ -497,7 +506,7 @@ int ffn_norm_backward(const ffn_norm* norm, const void* x, int64_t ldx, const vo
     const int64_t need = ffn_norm_workspace_bytes(norm, N, 0);
     rc = workspace_ok(workspace, workspace_bytes, need);
     if (rc != CGTP_OK) return rc;
-    const Range ins[] = {{x, span(N, ldx, a.width, e)}, {w, a.width * e}, {rstd, N * 4}, {grad_u, span(N, ldg, a.width, e)}};
+    const Range ins[] = {rows(x, N, ldx, a.width, e), {w, a.width * e}, {rstd, N * 4}, rows(grad_u, N, ldg, a.width, e)};
     const Range outs[] = {{grad_x, N * a.width * e}, {grad_w, a.width * e}, {workspace, need}};
     if (any_overlap(outs, ins)) return CGTP_EINVAL;
     a.y = const_cast<void*>(x); a.ldx = ldx; a.wn = w; a.rstd_y = const_cast<float*>(rstd);
@@ -576,8 +585,8 @@ int ffn_dropout(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t N, int
     if (N > FFN_MAX_ROWS || width > (1LL << 34) || ldx > (1LL << 34) || ldy > (1LL << 34) ||
         N > (1LL << 60) / ((ldx > ldy ? ldx : ldy) * e))
         return CGTP_EUNSUP;
-    const Range ins[] = {{y == x && ldy == ldx ? nullptr : x, span(N, ldx, width, e)}};
-    const Range outs[] = {{y, span(N, ldy, width, e)}};
+    const Range ins[] = {rows(y == x && ldy == ldx ? nullptr : x, N, ldx, width, e)};
+    const Range outs[] = {rows(y, N, ldy, width, e)};
     if (any_overlap(outs, ins)) return CGTP_EINVAL;
     return status(dropout(x, ldx, y, ldy, N, width, dtype, d, hip_stream));
 }

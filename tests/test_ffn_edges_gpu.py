@@ -157,3 +157,33 @@ def test_one_row_of_a_wide_array():
     assert torch.equal(u, norm.forward(packed)[0])
     assert torch.equal(norm.backward(x, None, rstd, x)[0], norm.backward(packed, None, rstd, packed)[0])
     assert torch.equal(lib.dropout(x, 0.5, seed=1), lib.dropout(packed, 0.5, seed=1))
+
+
+def test_columns_of_one_array_side_by_side():
+    """An input and an output that are neighbouring columns of one array do not overlap; columns that meet do."""
+    torch, lib = _setup()
+    N, D = 37, 45
+    for width, at in ((2 * D, D), (2 * D + 9, D + 4), (3 * D, 2 * D)):
+        buf = torch.full((N, width), 7.0, device="cuda")
+        x, out = buf[:, :D], buf[:, at:at + D]
+        x.copy_(_randn(torch, width, (N, D), "fp32"))
+        packed = x.clone()
+        rest = torch.ones(width, dtype=torch.bool)
+        rest[:D] = rest[at:at + D] = False
+        norm = lib.NormPlan(D)
+        for call in (lambda a, **k: norm.forward(a, **k)[0], lambda a, **k: lib.dropout(a, 0.25, seed=5, **k)):
+            for a, b in ((x, out), (out, x)):
+                a.copy_(packed)
+                assert torch.equal(call(a, out=b), call(packed)) and torch.equal(a, packed)
+                assert bool((buf[:, rest] == 7.0).all())
+        for bad in (buf[:, at - 1:at - 1 + D] if at == D else buf[:, D - 1:2 * D - 1], buf[:, 1:D + 1]):
+            with pytest.raises(lib.CgtpError):
+                norm.forward(x, out=bad)
+            with pytest.raises(lib.CgtpError):
+                lib.dropout(x, 0.25, seed=5, out=bad)
+    # the output's rows begin inside the input's, and end in the row after
+    buf = torch.zeros(N + 1, 2 * D, device="cuda").reshape(-1)
+    x = torch.as_strided(buf, (N, D), (2 * D, 1), 0)
+    late = torch.as_strided(buf, (N, D), (2 * D, 1), D + 1)
+    with pytest.raises(lib.CgtpError):
+        lib.NormPlan(D).forward(x, out=late)
