@@ -184,10 +184,25 @@ template <typename T, int MT, int EPI> int run_few(const FewArgs& p, int nr, int
     const int tiles = (nr > 16 ? 2 : 1) * (EPI == kGate ? 2 : 1) * MT;
     const int lds = waves * tiles * 1024;
     if (lds > 64 * 1024) return (int)hipErrorInvalidValue;
-    if (nr == 8) few_kernel<T, MT, 8, EPI><<<grid, waves * 64, lds, s>>>(p);
-    else if (nr == 16) few_kernel<T, MT, 16, EPI><<<grid, waves * 64, lds, s>>>(p);
-    else few_kernel<T, MT, 32, EPI><<<grid, waves * 64, lds, s>>>(p);
-    return (int)hipGetLastError();
+    // (those that few_product() asks for)
+    constexpr bool k16 = MT > 1 || sizeof(T) == 4, k32 = MT > 1 && EPI == kGate;
+    if (nr == 8) {
+        few_kernel<T, MT, 8, EPI><<<grid, waves * 64, lds, s>>>(p);
+        return (int)hipGetLastError();
+    }
+    if constexpr (k16) {
+        if (nr == 16) {
+            few_kernel<T, MT, 16, EPI><<<grid, waves * 64, lds, s>>>(p);
+            return (int)hipGetLastError();
+        }
+    }
+    if constexpr (k32) {
+        if (nr == 32) {
+            few_kernel<T, MT, 32, EPI><<<grid, waves * 64, lds, s>>>(p);
+            return (int)hipGetLastError();
+        }
+    }
+    return (int)hipErrorInvalidValue;
 }
 
 template <typename T> int few(const FewArgs& p, int32_t epilogue, int nr, int waves, hipStream_t s) {

@@ -138,6 +138,24 @@ def test_activations_value_by_value(N, act, dtype):
     assert bool(((gx[:, 0].double() / size - da).abs() <= tol * part + slack).all())
 
 
+# ---------------------------------------------------------------- few rows
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("N", [3, 24, 40])
+@pytest.mark.parametrize("di,df,do", [(40, 70, 3100), (70, 3100, 40), (40, 16420, 24)])
+def test_few_rows_by_every_number_of_weight_rows(N, di, df, do, dtype):
+    """8, 16 and 32 weight rows a work-group, in both products: against 64 bits, H and the output rounded once each."""
+    torch, lib = _setup()
+    x, wi, wo = _randn(torch, N, (N, di), dtype), _randn(torch, 2, (2 * df, di), dtype), _randn(torch, 3, (do, df), dtype)
+    wi, wo = wi * di ** -0.5, wo * df ** -0.5
+    y, saved = lib.FfnPlan(di, df, do, dtype=dtype).forward(x, wi, wo, save=True)
+    z = x.double() @ wi.double().T
+    want = (torch.nn.functional.silu(z[:, :df]) * z[:, df:]) @ wo.double().T
+    unit = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "fp16": 2.0 ** -11}[dtype]
+    assert float((saved.double() - z).norm() / z.norm()) <= 4e-6
+    assert float((y.double() - want).norm() / want.norm()) <= 2 * unit + 4e-6
+
+
 # ---------------------------------------------------------------- views and arrays in place of others
 
 def test_one_row_of_a_wide_array():
