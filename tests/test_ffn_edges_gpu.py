@@ -205,3 +205,33 @@ def test_columns_of_one_array_side_by_side():
     late = torch.as_strided(buf, (N, D), (2 * D, 1), D + 1)
     with pytest.raises(lib.CgtpError):
         lib.NormPlan(D).forward(x, out=late)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("N,D", [(300, 40), (700, 1029), (400, 1401), (130, 5001), (90, 9001), (20, 5)])
+def test_results_in_place_of_inputs(N, D, dtype):
+    """u in place of x, and (by the C entry) grad_x in place of grad_y, also where two threads share columns: the same
+    bits as elsewhere."""
+    torch, lib = _setup()
+    x, h, gy, gu, gate = (_randn(torch, k, (N, D), dtype) for k in range(5))
+    w, scale, wn = (_randn(torch, 9 + k, (D,), dtype) for k in range(3))
+    plan = lib.NormPlan(D, dtype=dtype, dropout=0.25)
+    want, rstd = plan.forward(x, w)
+    into = x.clone()
+    got, rstd2 = plan.forward(into, w, out=into)
+    assert got is into and torch.equal(want, into) and torch.equal(rstd, rstd2)
+    kw = {"gate": gate, "scale": scale, "w_next": wn, "seed": 3, "offset": 8}
+    y, u, stats = plan.residual(x, h, w, **kw)
+    norm = lib.ffn_norm(D, 1, {"fp32": lib.FFN_FP32, "bf16": lib.FFN_BF16, "fp16": lib.FFN_FP16}[dtype], 1e-6, 0.25, 3, 8)
+    need = lib.ffn_norm_workspace_bytes(norm, N, 1)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    p = lambda t: None if t is None else t.data_ptr()
+    stream = torch.cuda.current_stream().cuda_stream
+    for last in (gu, None):
+        want = plan.residual_backward(h, y, w, stats, gy, last, **kw)
+        gx = gy.clone()
+        rest = [torch.empty_like(t) for t in (h, w, gate, scale, wn)]
+        lib.ffn_residual_backward(norm, p(h), p(y), p(w), p(gate), p(scale), p(wn), p(stats), p(gx), p(last), p(gx),
+                                  p(rest[0]), p(rest[1]), p(rest[2]), p(rest[3]), p(rest[4]), N, p(ws), need, stream)
+        for a, b in zip(want, [gx] + rest):
+            assert torch.equal(a, b)
