@@ -55,8 +55,10 @@ enum { FFN_SILU = 0, FFN_GELU = 1, FFN_RELU = 2 };
  *   w_in  [2 d_ff, d_in]: the d_ff rows of Wg, then the d_ff rows of Wu
  *   w_out [d_out, d_ff] = Wo
  *   Y     [N, d_out]
- * Both projections, the activation and the product are one kernel: G and U
- * are written only where `saved` asks for them (training).
+ * Both projections are one product, with the activation and the product with U
+ * in its epilogue: G and U are written only where `saved` asks for them
+ * (training).  Where that product is cut along d_in, having few tiles, its parts'
+ * 32-bit sums pass through the workspace and a second kernel finishes them.
  */
 typedef struct ffn_plan_s *ffn_plan_t;
 
