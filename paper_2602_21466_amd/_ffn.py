@@ -9,6 +9,7 @@ not give are allocated here, for the stream that uses them.
 from __future__ import annotations
 
 import ctypes
+import operator
 
 FFN_FP32, FFN_BF16, FFN_FP16 = 0, 2, 3
 FFN_SILU, FFN_GELU, FFN_RELU = 0, 1, 2
@@ -135,7 +136,9 @@ def ffn_dropout(x_ptr, ldx, y_ptr, ldy, N, width, dtype, p, seed, offset, stream
 
 # ---------------------------------------------------------------- convenience
 
-_U64 = (1 << 64) - 1
+def _word(n):
+    """A whole number of any kind (those of numpy among them) modulo 2^64."""
+    return operator.index(n) & 0xFFFFFFFFFFFFFFFF
 
 
 class _Torch:
@@ -315,7 +318,7 @@ class NormPlan:
         return self._describe(seed, offset)
 
     def _describe(self, seed, offset):
-        return ffn_norm(self.width, self.rows_per_gate, self._code, self.eps, self.dropout, seed & _U64, offset & _U64)
+        return ffn_norm(self.width, self.rows_per_gate, self._code, self.eps, self.dropout, _word(seed), _word(offset))
 
     def forward(self, x, w=None, out=None, rstd=None, stream=None):
         """(u, rstd): u = N(x; w) for x [N, width], rows may be strided, and the rows' 1 / sqrt(mean + eps)."""
@@ -434,5 +437,5 @@ def dropout(x, p: float, seed: int, offset: int = 0, out=None, stream=None):
         ldy = _rows(out, x.dtype, N, width, "out", dev)
     else:
         raise ValueError("out must be contiguous, or [N, width] with strided rows")
-    _call("ffn_dropout", x.data_ptr(), ldx, out.data_ptr(), ldy, N, width, code, float(p), seed & _U64, offset & _U64, sp)
+    _call("ffn_dropout", x.data_ptr(), ldx, out.data_ptr(), ldy, N, width, code, float(p), _word(seed), _word(offset), sp)
     return out
