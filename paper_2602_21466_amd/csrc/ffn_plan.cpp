@@ -109,7 +109,7 @@ struct Cut { int32_t tile, splits; bool joined; };
 
 // The shortest by this count, in microseconds.  A compute unit takes a 256-wide tile's step (64 k of 16 bits, 32 of 32
 // bits) in 1.6 (4.5), or two 128-wide tiles' in 1.06 (2.6), one alone in about three quarters of that (measured on large products:
-// bf16 1.33 and 1.0 PFLOP/s, fp32 237 and 205 TFLOP/s).  Four (two) steps stand for a tile's start and end.  Parts of k cost
+// bf16 1.33 and 1.0 PFLOP/s, fp32 238 and 209 TFLOP/s).  Four (two) steps stand for a tile's start and end.  Parts of k cost
 // a launch (three microseconds, and a tenth of one a part) and their sums, written and read once at 4 TB/s; the gate's
 // gradient in the tiles' own epilogue costs ten where they are few (4004 rows, 144 x 348: 26 us, against 17 with the
 // joining kernel).
