@@ -182,6 +182,36 @@ int ffn_residual_backward(const ffn_norm *norm, const void *h, const void *y, co
 /* Workspace bytes of ffn_norm_backward (residual = 0) or ffn_residual_backward (residual = 1); -1 if invalid. */
 int64_t ffn_norm_workspace_bytes(const ffn_norm *norm, int64_t N, int32_t residual);
 
+/* ------------------------------------------------------------------ layer norm
+ *
+ *   L(x; w, b) = (x - m) r * w + b,  m = mean(x),  r = 1 / sqrt(mean((x - m)^2) + eps)
+ * over the `width` values of a row, for scalar features that carry an offset.
+ * Of the description, width, dtype and eps are read (the rest has to be valid).
+ */
+
+/*
+ * u = L(x; w, b) of N rows; x and u have row strides ldx and ldu.  w NULL: all
+ * ones; b NULL: zeros.  stats: NULL, or [2, N] floats to receive m and then r of
+ * the rows.  u == x with ldu == ldx is allowed.  Statuses as ffn_norm_forward.
+ */
+int ffn_layer_forward(const ffn_norm *norm, const void *x, int64_t ldx, const void *w, const void *b, void *u,
+                      int64_t ldu, float *stats, int64_t N, void *hip_stream);
+
+/*
+ * Gradients of sum(grad_u * L(x; w, b)): with n = (x - m) r and a = grad_u w,
+ *   grad_x [N, width] = r (a - mean(a) - n mean(a n)),
+ *   grad_w [width] = sum over rows of grad_u n,  grad_b [width] = that of grad_u;
+ * any of them may be NULL, not all.  stats is what ffn_layer_forward wrote; m is
+ * corrected for its rounding.  grad_u has row stride ldg.  Workspace:
+ * ffn_layer_workspace_bytes(norm, N).
+ */
+int ffn_layer_backward(const ffn_norm *norm, const void *x, int64_t ldx, const void *w, const float *stats,
+                       const void *grad_u, int64_t ldg, void *grad_x, void *grad_w, void *grad_b, int64_t N,
+                       void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/* Workspace bytes of ffn_layer_backward; -1 if invalid. */
+int64_t ffn_layer_workspace_bytes(const ffn_norm *norm, int64_t N);
+
 /* ------------------------------------------------------------------ dropout
  *
  * y[r, c] = x[r, c] * 65536 / (65536 - t) where draw(r, c) >= t, else 0, with

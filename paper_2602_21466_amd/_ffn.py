@@ -1,9 +1,9 @@
 """Binding of include/ffn.h: the gated feed-forward block, the norms around it
-with gate and residual scale, and counter-based dropout.
+with gate and residual scale, the layer norm, and counter-based dropout.
 
 As in the package itself: the functions carry the C names and take device
-pointers and a HIP stream; ``FfnPlan``, ``NormPlan`` and ``dropout`` take and
-return CUDA (HIP) torch tensors.  Outputs and workspaces that the caller does
+pointers and a HIP stream; ``FfnPlan``, ``NormPlan``, ``LayerNormPlan`` and
+``dropout`` take and return CUDA (HIP) torch tensors.  Outputs and workspaces that the caller does
 not give are allocated here, for the stream that uses them.
 """
 from __future__ import annotations
@@ -17,7 +17,8 @@ FFN_MAX_WIDTH, FFN_MAX_ROWS = 1 << 20, 1 << 30
 __all__ = ["FFN_FP32", "FFN_BF16", "FFN_FP16", "FFN_SILU", "FFN_GELU", "FFN_RELU", "FFN_MAX_WIDTH", "FFN_MAX_ROWS",
            "ffn_norm", "ffn_plan", "ffn_destroy", "ffn_workspace_bytes", "ffn_backward_workspace_bytes", "ffn_forward",
            "ffn_backward", "ffn_norm_forward", "ffn_norm_backward", "ffn_norm_workspace_bytes", "ffn_residual_forward",
-           "ffn_residual_backward", "ffn_dropout", "FfnPlan", "NormPlan", "dropout"]
+           "ffn_residual_backward", "ffn_layer_forward", "ffn_layer_backward", "ffn_layer_workspace_bytes", "ffn_dropout",
+           "FfnPlan", "NormPlan", "LayerNormPlan", "dropout"]
 _DTYPES = {"fp32": FFN_FP32, "bf16": FFN_BF16, "fp16": FFN_FP16}
 _ACTIVATIONS = {"silu": FFN_SILU, "gelu": FFN_GELU, "relu": FFN_RELU}
 
@@ -42,6 +43,9 @@ SIGNATURES = {
     "ffn_residual_forward": (_int, [_np] + [_vp] * 9 + [_i64, _vp]),
     "ffn_residual_backward": (_int, [_np] + [_vp] * 15 + [_i64, _vp, _i64, _vp]),
     "ffn_norm_workspace_bytes": (_i64, [_np, _i64, _i32]),
+    "ffn_layer_forward": (_int, [_np, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "ffn_layer_backward": (_int, [_np, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "ffn_layer_workspace_bytes": (_i64, [_np, _i64]),
     "ffn_dropout": (_int, [_vp, _i64, _vp, _i64, _i64, _i64, _i32, ctypes.c_double, _u64, _u64, _vp]),
 }
 
@@ -130,6 +134,20 @@ def ffn_residual_backward(norm, h_ptr, y_ptr, w_ptr, gate_ptr, scale_ptr, w_next
           gu_ptr, gx_ptr, gh_ptr, gw_ptr, ggate_ptr, gscale_ptr, gw_next_ptr, N, ws_ptr, ws_bytes, stream_ptr)
 
 
+def ffn_layer_forward(norm, x_ptr, ldx, w_ptr, b_ptr, u_ptr, ldu, stats_ptr, N, stream_ptr=None) -> None:
+    _call("ffn_layer_forward", norm, x_ptr, ldx, w_ptr, b_ptr, u_ptr, ldu, stats_ptr, N, stream_ptr)
+
+
+def ffn_layer_backward(norm, x_ptr, ldx, w_ptr, stats_ptr, gu_ptr, ldg, gx_ptr, gw_ptr, gb_ptr, N, ws_ptr, ws_bytes,
+                       stream_ptr=None) -> None:
+    _call("ffn_layer_backward", norm, x_ptr, ldx, w_ptr, stats_ptr, gu_ptr, ldg, gx_ptr, gw_ptr, gb_ptr, N, ws_ptr,
+          ws_bytes, stream_ptr)
+
+
+def ffn_layer_workspace_bytes(norm, N: int) -> int:
+    return _entry("ffn_layer_workspace_bytes")(norm, N)
+
+
 def ffn_dropout(x_ptr, ldx, y_ptr, ldy, N, width, dtype, p, seed, offset, stream_ptr=None) -> None:
     _call("ffn_dropout", x_ptr, ldx, y_ptr, ldy, N, width, _code(_DTYPES, dtype, "dtype"), p, seed, offset, stream_ptr)
 
@@ -147,6 +165,7 @@ class _Torch:
     def __getattr__(self, name):
         import torch
         self.empty_like, self.float32, self.uint8 = torch.empty_like, torch.float32, torch.uint8
+        self.int32, self.int64 = torch.int32, torch.int64
         self.raw_stream, self.on_stream = torch._C._cuda_getCurrentRawStream, torch.cuda.stream
         self.current_device = torch._C._cuda_getDevice
         self.dtypes = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
@@ -408,6 +427,56 @@ class NormPlan:
         _call("ffn_residual_backward", norm, hp, yp, wp, gp, sc, np_, st, gyp, gup, gx.data_ptr(), gh.data_ptr(), ptr(gw),
               ptr(gg), ptr(gs), ptr(gn), N, ws.data_ptr(), need, sp)
         return gx, gh, gw, gg, gs, gn
+
+
+class LayerNormPlan:
+    """The layer norm: L(x; w, b) = (x - mean) / sqrt(mean((x - mean)^2) + eps) * w + b over rows of `width` values."""
+
+    def __init__(self, width: int, dtype: str = "fp32", eps: float = 1e-5):
+        self.width, self.dtype, self.eps = int(width), dtype, float(eps)
+        code = _code(_DTYPES, dtype, "dtype")
+        self._tdt = _t.dtypes[dtype]
+        self._norm = ffn_norm(self.width, 1, code, self.eps, 0.0, 0, 0)
+        if ffn_layer_workspace_bytes(self._norm, 0) < 0:
+            raise ValueError("width must be 1 .. %d and eps positive" % FFN_MAX_WIDTH)
+
+    def forward(self, x, w=None, b=None, out=None, stats=None, stream=None):
+        """(u, stats): u = L(x; w, b) for x [N, width], rows may be strided; w None: ones, b None: zeros.  stats [2, N]
+        holds the rows' means and 1 / sqrt(mean((x - mean)^2) + eps).  out may be x."""
+        tdt, D = self._tdt, self.width
+        ldx = _rows(x, tdt, None, D, "x")
+        N, dev = x.shape[0], x.get_device()
+        wp, bp = _whole(w, tdt, (D,), "w", dev), _whole(b, tdt, (D,), "b", dev)
+        sp, other = _stream(stream, dev)
+        if out is None:
+            out, ldu = _new(x, (N, D), other), D
+        else:
+            ldu = _rows(out, tdt, N, D, "out", dev)
+        if stats is None:
+            stats = _new32(x, (2, N), other)
+        _call("ffn_layer_forward", self._norm, x.data_ptr(), ldx, wp, bp, out.data_ptr(), ldu,
+              _whole(stats, _t.float32, (2, N), "stats", dev), N, sp)
+        return out, stats
+
+    def backward(self, x, w, stats, grad_out, need_x=True, need_w=True, need_b=True, workspace=None, stream=None):
+        """(grad_x, grad_w, grad_b) of sum(grad_out * L(x; w, b)); one not asked for is None."""
+        tdt, D = self._tdt, self.width
+        ldx = _rows(x, tdt, None, D, "x")
+        N, dev = x.shape[0], x.get_device()
+        ldg = _rows(grad_out, tdt, N, D, "grad_out", dev)
+        wp, st = _whole(w, tdt, (D,), "w", dev), _whole(stats, _t.float32, (2, N), "stats", dev)
+        if not (need_x or need_w or need_b):
+            return None, None, None
+        sp, other = _stream(stream, dev)
+        gx = _new(x, (N, D), other) if need_x else None
+        gw = _new(x, (D,), other) if need_w else None
+        gb = _new(x, (D,), other) if need_b else None
+        need = ffn_layer_workspace_bytes(self._norm, N)
+        ws = _workspace(workspace, need, x, other)
+        ptr = lambda t: t.data_ptr() if t is not None else None
+        _call("ffn_layer_backward", self._norm, x.data_ptr(), ldx, wp, st, grad_out.data_ptr(), ldg, ptr(gx), ptr(gw),
+              ptr(gb), N, ws.data_ptr(), need, sp)
+        return gx, gw, gb
 
 
 def dropout(x, p: float, seed: int, offset: int = 0, out=None, stream=None):

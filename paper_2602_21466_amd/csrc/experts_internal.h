@@ -1,0 +1,64 @@
+// Launch descriptions shared by the C entries of the layer norm, the sorting of rows by expert and the experts' blocks
+// (ffn_layer.cpp, experts_plan.cpp) and their kernels.  Internal.
+#pragma once
+
+#include <cstdint>
+
+#include "experts.h"
+#include "ffn_internal.h"
+
+namespace ffn {
+
+// ---------------------------------------------------------------- layer norm
+
+struct LayerArgs {
+    int64_t width, N;
+    float eps;
+    const void *x, *w, *b;
+    int64_t ldx;
+    void* u;                              // forward
+    int64_t ldu;
+    float* stats;                         // [2, N]: written forward, read backward
+    const void* gu;                       // backward
+    int64_t ldg;
+    void *gx, *gw, *gb;
+    float* partial;                       // workspace
+};
+int64_t layer_workspace_floats(int64_t width, int64_t N, int bytes);
+
+#define FFN_LAYER_LAUNCHERS(TYPE)                                    \
+    int launch_layer_forward_##TYPE(const LayerArgs& a, void* stream); \
+    int launch_layer_backward_##TYPE(const LayerArgs& a, void* stream);
+FFN_LAYER_LAUNCHERS(fp32)
+FFN_LAYER_LAUNCHERS(bf16)
+FFN_LAYER_LAUNCHERS(fp16)
+#undef FFN_LAYER_LAUNCHERS
+
+// ---------------------------------------------------------------- rows sorted by expert
+
+struct SortArgs {
+    const void* index;
+    int32_t index_bytes, experts;
+    int64_t slots, chunk;                 // slots a work-group
+    int32_t groups;
+    int32_t *place, *source, *offsets;
+    int32_t* counts;                      // workspace [groups, experts]
+};
+int launch_sort(const SortArgs& a, void* stream);
+
+struct RouteArgs {
+    int64_t N, width, per_row, slots;
+    const int32_t *place, *offsets;       // offsets: NULL where no rows behind the last are written
+    int32_t experts;
+    const float* weights;                 // NULL: ones
+    const void *rows, *sorted;            // inputs [N, width] (stride ld) and [slots, width]
+    int64_t ld;
+    void *out_rows, *out_sorted;          // outputs; out_rows has stride ld_out, out_sorted ld_sorted (zeros behind width)
+    int64_t ld_out, ld_sorted;
+    float* grad_weights;
+};
+int launch_gather(const RouteArgs& a, int32_t dtype, void* stream);            // rows -> out_sorted
+int launch_combine(const RouteArgs& a, int32_t dtype, void* stream);           // sorted -> out_rows
+int launch_combine_backward(const RouteArgs& a, int32_t dtype, void* stream);  // rows (, sorted) -> out_sorted, grad_weights
+
+}  // namespace ffn
