@@ -239,32 +239,46 @@ __device__ __forceinline__ void place(int id, int tm, int tn, int splits, int& m
     n = r / rows;
 }
 
+// The work-group meets with every wave's direct loads in LDS.  (A barrier alone orders the waves' own LDS accesses; the
+// direct loads of the others are in flight as far as it goes, and whether the compiler waits for them before it depends on
+// what it can tell of the buffers.)
+__device__ __forceinline__ void landed() {
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    __syncthreads();
+}
+
+// What one work-group multiplies: rows m0 .. m_end - 1 of A, of which it takes BM, by B's rows from tile tn on, over K, of
+// which it takes part `split`; row m of the result is row out_row + m of out_rows in memory.
+struct Work {
+    const void *a, *b;
+    int64_t m0, m_end, K, out_row, out_rows;
+    int tn, split;
+};
+
 template <typename T, int BM, int BN, int WM, int WN, bool AC, bool BC, int EPI>
-__global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
+__device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w) {
 #ifdef __HIP_DEVICE_COMPILE__   // (the host's pass needs the launch stub alone)
     constexpr int NW = WM * WN, MT = BM / WM / 16, CW = BN / WN, NT = CW / 16, ES = (int)sizeof(T), kStep = 128 / ES;
     __shared__ __align__(1024) char sa0[BM * 128], sb0[BN * 128];
     __shared__ __align__(1024) char sa1[BM * 128], sb1[BN * 128];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * CW;
-    int tm, tn, split;
-    place(blockIdx.x, p.tiles_m, p.tiles_n, p.splits, tm, tn, split);
     constexpr int kCols = EPI == kGate ? BN / 2 : BN;      // columns of C a tile covers
-    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * kCols;
+    const int64_t m0 = w.m0, n0 = (int64_t)w.tn * kCols;
 
     Loader<ES, BM, NW, AC, 0> la;
     Loader<ES, BN, NW, BC, EPI == kGate ? CW : 0> lb;
-    la.init(p.a, p.lda, m0, p.M, 0, wave, lane);
-    lb.init(p.b, p.ldb, n0, p.N, p.N, wave, lane);
+    la.init(w.a, p.lda, m0, w.m_end, 0, wave, lane);
+    lb.init(w.b, p.ldb, n0, p.N, p.N, wave, lane);
 
     // this part's steps
-    const int steps = (int)((p.K + kStep - 1) / kStep);
-    const int s0 = (int)((int64_t)steps * split / p.splits), s1 = (int)((int64_t)steps * (split + 1) / p.splits), n = s1 - s0;
+    const int steps = (int)((w.K + kStep - 1) / kStep);
+    const int s0 = (int)((int64_t)steps * w.split / p.splits), s1 = (int)((int64_t)steps * (w.split + 1) / p.splits), n = s1 - s0;
     int ks = s0;
     auto issue = [&](char* a, char* b) {
         la.seek(ks * la.step);
         lb.seek(ks * lb.step);
-        const int64_t left = p.K - (int64_t)ks * kStep;
+        const int64_t left = w.K - (int64_t)ks * kStep;
         la.issue(a, wave, left < kStep ? (int)left : kStep);
         lb.issue(b, wave, left < kStep ? (int)left : kStep);
         ++ks;
@@ -308,10 +322,10 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            __syncthreads();
+            landed();
         };
         if (n > 0) issue(sa0, sb0);
-        __syncthreads();
+        landed();
         int s = 0;
         for (; s + 1 < n; s += 2) {
             step(sa0, sb0, sa1, sb1, true);
@@ -360,7 +374,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
                 meet();
             };
             if (n > 0) issue(sa0, sb0);
-            __syncthreads();
+            landed();
             if (wave >= 4) meet();
             int s = 0;
             for (; s + 1 < n; s += 2) {
@@ -376,14 +390,14 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
             auto step = [&](char* a, char* b, char* an, char* bn, bool more) {
                 read(a, b, 1);
                 multiply(0);
-                __syncthreads();
+                landed();
                 if (more) issue(a, b);
                 read(an, bn, 0);
                 multiply(1);
             };
             if (n > 0) issue(sa0, sb0);
             if (n > 1) issue(sa1, sb1);
-            __syncthreads();
+            landed();
             read(sa0, sb0, 0);
             int s = 0;
             for (; s + 1 < n; s += 2) {
@@ -423,7 +437,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
             for (int k = 0; k < kAhead; ++k) {
                 const int64_t m = mb + lane / kLanes + (k0 + k) * kTake;
                 gs[k] = us[k] = f32x4{};
-                if (m < p.M) {
+                if (m < w.m_end) {
                     gs[k] = load4(p.saved + m * 2 * p.N, n, p.N);
                     us[k] = load4(p.saved + m * 2 * p.N + p.N, n, p.N);
                 }
@@ -433,7 +447,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
         for (int k = 0; k < kAhead; ++k) {
             const int r = lane / kLanes + (k0 + k) * kTake;
             const int64_t m = mb + r;
-            if (m >= p.M) continue;
+            if (m >= w.m_end) continue;
             const f32x4 v = *(const f32x4*)(turn + r * kRow + tc);
             if constexpr (EPI == kGate) {
                 const f32x4 u = *(const f32x4*)(turn + r * kRow + CW / 2 + tc);
@@ -450,9 +464,9 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
                     store4<float>(p.saved + m * 2 * p.N + p.N, n, p.N, 0, u);
                 }
             } else if constexpr (EPI == kStore) {
-                store4<T>((T*)p.c + m * p.ldc, n, p.N, 0, v);
+                store4<T>((T*)p.c + (w.out_row + m) * p.ldc, n, p.N, 0, v);
             } else if constexpr (EPI == kPartial) {
-                store4<float>((float*)p.c + ((int64_t)split * p.M + m) * p.ldc, n, p.N, 0, v);
+                store4<float>((float*)p.c + ((int64_t)w.split * w.out_rows + w.out_row + m) * p.ldc, n, p.N, 0, v);
             } else {
                 const f32x4 g = gs[k], u = us[k];
                 f32x4 dg, du, h;
@@ -472,6 +486,13 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
         __builtin_amdgcn_wave_barrier();
     }
 #endif
+}
+
+template <typename T, int BM, int BN, int WM, int WN, bool AC, bool BC, int EPI>
+__global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
+    int tm, tn, split;
+    place(blockIdx.x, p.tiles_m, p.tiles_n, p.splits, tm, tn, split);
+    tile_body<T, BM, BN, WM, WN, AC, BC, EPI>(p, Work{p.a, p.b, (int64_t)tm * BM, p.M, p.K, 0, p.M, tn, split});
 }
 
 template <typename T, int BM, bool AC, bool BC, int EPI> int run_tile(const TileArgs& p, hipStream_t s) {
