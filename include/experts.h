@@ -76,6 +76,53 @@ int ffn_route_combine_backward(const void *ys, const int32_t *place, const int32
                                const void *grad_y, int64_t ldg, void *grad_ys, float *grad_weights, int64_t N,
                                int32_t per_row, int32_t experts, int64_t width, int32_t dtype, void *hip_stream);
 
+/* ------------------------------------------------------------------ the experts' gated blocks
+ *
+ * For the sorted rows p of expert e, X_p being row source[p] / per_row of x:
+ *   G = X Wg_e^T,  U = X Wu_e^T,  H = act(G) * U,  Y = H Wo_e^T
+ *   w_in  [experts, 2 d_ff, d_in]: of each expert, the d_ff rows of Wg, then those of Wu
+ *   w_out [experts, d_out, d_ff]
+ * How many rows an expert has is known on the device alone: nothing is copied to the host.
+ */
+typedef struct ffn_experts_s *ffn_experts_t;
+
+/*
+ * A plan on the current HIP device, as ffn_plan makes one for a single block; it
+ * owns no device memory.  CGTP_EUNSUP also for experts above FFN_MAX_EXPERTS, or
+ * weights of more than 2^30 rows (experts * 2 d_ff, experts * d_out).
+ */
+int ffn_experts_plan(int32_t experts, int64_t d_in, int64_t d_ff, int64_t d_out, int32_t activation, int32_t dtype,
+                     ffn_experts_t *plan_out);
+
+/* Frees the plan.  NULL is a no-op. */
+int ffn_experts_destroy(ffn_experts_t plan);
+
+/* Workspace bytes ffn_experts_forward (ffn_experts_backward) needs; -1 for a NULL plan, N or per_row out of range. */
+int64_t ffn_experts_workspace_bytes(ffn_experts_t plan, int64_t N, int32_t per_row);
+int64_t ffn_experts_backward_workspace_bytes(ffn_experts_t plan, int64_t N, int32_t per_row);
+
+/*
+ * y [S, d_out] of the sorted rows; rows from offsets[experts] on are left as they
+ * were.  x: [N, d_in], row stride ldx.  saved: NULL, or [S, 2 d_ff] 32-bit floats
+ * to receive G and U of the sorted rows for ffn_experts_backward.  Roundings and
+ * statuses as ffn_forward.
+ */
+int ffn_experts_forward(ffn_experts_t plan, const void *x, int64_t ldx, const int32_t *place, const int32_t *source,
+                        const int32_t *offsets, const void *w_in, const void *w_out, void *y, void *saved, int64_t N,
+                        int32_t per_row, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Gradients of sum(grad_y * y), grad_y [S, d_out] in the sorted order (rows from
+ * offsets[experts] on are not read):
+ *   grad_x [N, d_in]: of each row the sum over its choices, added in 32 bits (zeros where it has none)
+ *   grad_w_in, grad_w_out like the weights (zeros for an expert without rows)
+ * Any may be NULL, not all.  saved is what ffn_experts_forward wrote.
+ */
+int ffn_experts_backward(ffn_experts_t plan, const void *x, int64_t ldx, const int32_t *place, const int32_t *source,
+                         const int32_t *offsets, const void *w_in, const void *w_out, const void *saved,
+                         const void *grad_y, void *grad_x, void *grad_w_in, void *grad_w_out, int64_t N,
+                         int32_t per_row, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

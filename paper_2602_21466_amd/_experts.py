@@ -2,19 +2,20 @@
 weights, and the experts' gated feed-forward blocks.
 
 As in the package itself: the functions carry the C names and take device
-pointers and a HIP stream; ``Routes`` takes and returns CUDA (HIP) torch tensors.
-Outputs and workspaces that the caller does not give are allocated here, for the
+pointers and a HIP stream; ``Routes`` and ``ExpertsPlan`` take and return CUDA (HIP)
+torch tensors.  Outputs and workspaces that the caller does not give are allocated here, for the
 stream that uses them.
 """
 from __future__ import annotations
 
 import ctypes
 
-from ._ffn import _call, _code, _DTYPES, _entry, _new, _new32, _rows, _stream, _t, _whole
+from ._ffn import _ACTIVATIONS, _call, _code, _DTYPES, _entry, _like, _new, _new32, _rows, _stream, _t, _whole, _workspace
 
 FFN_MAX_EXPERTS = 1024
 __all__ = ["FFN_MAX_EXPERTS", "ffn_route", "ffn_route_workspace_bytes", "ffn_route_gather", "ffn_route_combine",
-           "ffn_route_combine_backward", "Routes"]
+           "ffn_route_combine_backward", "ffn_experts_plan", "ffn_experts_destroy", "ffn_experts_workspace_bytes",
+           "ffn_experts_backward_workspace_bytes", "ffn_experts_forward", "ffn_experts_backward", "Routes", "ExpertsPlan"]
 
 _i32, _i64, _vp, _int = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int
 SIGNATURES = {
@@ -23,6 +24,12 @@ SIGNATURES = {
     "ffn_route_gather": (_int, [_vp, _i64, _vp, _vp, _vp, _i64, _i32, _i32, _i64, _i32, _vp]),
     "ffn_route_combine": (_int, [_vp, _vp, _vp, _vp, _i64, _i64, _i32, _i64, _i32, _vp]),
     "ffn_route_combine_backward": (_int, [_vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _i32, _i32, _i64, _i32, _vp]),
+    "ffn_experts_plan": (_int, [_i32, _i64, _i64, _i64, _i32, _i32, ctypes.POINTER(_vp)]),
+    "ffn_experts_destroy": (_int, [_vp]),
+    "ffn_experts_workspace_bytes": (_i64, [_vp, _i64, _i32]),
+    "ffn_experts_backward_workspace_bytes": (_i64, [_vp, _i64, _i32]),
+    "ffn_experts_forward": (_int, [_vp, _vp, _i64] + [_vp] * 7 + [_i64, _i32, _vp, _i64, _vp]),
+    "ffn_experts_backward": (_int, [_vp, _vp, _i64] + [_vp] * 10 + [_i64, _i32, _vp, _i64, _vp]),
 }
 
 
@@ -53,6 +60,37 @@ def ffn_route_combine_backward(ys_ptr, place_ptr, offsets_ptr, weights_ptr, gy_p
                                experts, width, dtype, stream_ptr=None) -> None:
     _call("ffn_route_combine_backward", ys_ptr, place_ptr, offsets_ptr, weights_ptr, gy_ptr, ldg, gys_ptr, gw_ptr, N,
           per_row, experts, width, _code(_DTYPES, dtype, "dtype"), stream_ptr)
+
+
+def ffn_experts_plan(experts: int, d_in: int, d_ff: int, d_out: int, activation="silu", dtype="fp32") -> ctypes.c_void_p:
+    h = ctypes.c_void_p()
+    _call("ffn_experts_plan", int(experts), int(d_in), int(d_ff), int(d_out), _code(_ACTIVATIONS, activation, "activation"),
+          _code(_DTYPES, dtype, "dtype"), ctypes.byref(h))
+    return h
+
+
+def ffn_experts_destroy(plan) -> None:
+    _call("ffn_experts_destroy", plan)
+
+
+def ffn_experts_workspace_bytes(plan, N: int, per_row: int) -> int:
+    return _entry("ffn_experts_workspace_bytes")(plan, N, per_row)
+
+
+def ffn_experts_backward_workspace_bytes(plan, N: int, per_row: int) -> int:
+    return _entry("ffn_experts_backward_workspace_bytes")(plan, N, per_row)
+
+
+def ffn_experts_forward(plan, x_ptr, ldx, place_ptr, source_ptr, offsets_ptr, w_in_ptr, w_out_ptr, y_ptr, saved_ptr, N,
+                        per_row, ws_ptr, ws_bytes, stream_ptr=None) -> None:
+    _call("ffn_experts_forward", plan, x_ptr, ldx, place_ptr, source_ptr, offsets_ptr, w_in_ptr, w_out_ptr, y_ptr,
+          saved_ptr, N, per_row, ws_ptr, ws_bytes, stream_ptr)
+
+
+def ffn_experts_backward(plan, x_ptr, ldx, place_ptr, source_ptr, offsets_ptr, w_in_ptr, w_out_ptr, saved_ptr, gy_ptr,
+                         gx_ptr, gw_in_ptr, gw_out_ptr, N, per_row, ws_ptr, ws_bytes, stream_ptr=None) -> None:
+    _call("ffn_experts_backward", plan, x_ptr, ldx, place_ptr, source_ptr, offsets_ptr, w_in_ptr, w_out_ptr, saved_ptr,
+          gy_ptr, gx_ptr, gw_in_ptr, gw_out_ptr, N, per_row, ws_ptr, ws_bytes, stream_ptr)
 
 
 # ---------------------------------------------------------------- convenience
@@ -153,6 +191,81 @@ class Routes:
               gys.data_ptr() if need_ys else None, gw.data_ptr() if need_weights else None, self.rows, self.per_row,
               self.experts, D, code, sp)
         return gys, gw
+
+
+class ExpertsPlan:
+    """Owns a plan of `experts` gated blocks of one shape: Y_p = (act(X_p Wg_e^T) * (X_p Wu_e^T)) Wo_e^T for the sorted
+    rows p of each expert e, in the order that a Routes of as many experts holds."""
+
+    def __init__(self, experts: int, d_in: int, d_ff: int, d_out: int | None = None, dtype: str = "fp32",
+                 activation: str = "silu"):
+        self.experts, self.d_in, self.d_ff = int(experts), int(d_in), int(d_ff)
+        self.d_out = self.d_in if d_out is None else int(d_out)
+        self.dtype, self.activation = dtype, activation
+        _code(_DTYPES, dtype, "dtype")
+        self._h = ffn_experts_plan(self.experts, self.d_in, self.d_ff, self.d_out, activation, dtype)
+        self._tdt = _t.dtypes[dtype]
+
+    def _args(self, x, routes, w_in, w_out):
+        if not isinstance(routes, Routes) or routes.experts != self.experts:
+            raise ValueError("routes must be a Routes of %d experts" % self.experts)
+        dev = routes.device
+        ldx = _rows(x, self._tdt, routes.rows, self.d_in, "x", dev)
+        return dev, ldx, _whole(w_in, self._tdt, (self.experts, 2 * self.d_ff, self.d_in), "w_in", dev), \
+            _whole(w_out, self._tdt, (self.experts, self.d_out, self.d_ff), "w_out", dev)
+
+    def forward(self, x, routes, w_in, w_out, save=False, out=None, saved=None, workspace=None, stream=None):
+        """x: [N, d_in], rows may be strided, N and the choices as in routes; w_in: [experts, 2 d_ff, d_in], of each
+        expert the gate's rows, then the up projection's; w_out: [experts, d_out, d_ff].  Returns [S, d_out] in the
+        sorted order, for Routes.combine(); rows from routes.offsets[experts] on are not written.  With save=True (or
+        `saved`, a [S, 2 d_ff] fp32 tensor to write) also the values that backward() reads."""
+        dev, ldx, wi, wo = self._args(x, routes, w_in, w_out)
+        S, df, do = routes.source.shape[0], self.d_ff, self.d_out
+        sp, other = _stream(stream, dev)
+        if out is None:
+            out = _new(x, (S, do), other)
+        if save and saved is None:
+            saved = _new32(x, (S, 2 * df), other)
+        need = ffn_experts_workspace_bytes(self._h, routes.rows, routes.per_row)
+        ws = _workspace(workspace, need, x, other)
+        _call("ffn_experts_forward", self._h, x.data_ptr(), ldx, routes.place.data_ptr(), routes.source.data_ptr(),
+              routes.offsets.data_ptr(), wi, wo, _whole(out, self._tdt, (S, do), "out", dev),
+              _whole(saved, _t.float32, (S, 2 * df), "saved", dev), routes.rows, routes.per_row, ws.data_ptr(), need, sp)
+        return out if saved is None else (out, saved)
+
+    def backward(self, x, routes, w_in, w_out, saved, grad_out, need_x=True, need_w_in=True, need_w_out=True,
+                 workspace=None, stream=None):
+        """(grad_x, grad_w_in, grad_w_out) of sum(grad_out * forward(x, ...)) over the sorted rows of an expert, grad_out
+        [S, d_out] (as Routes.combine_backward() gives it): grad_x [N, d_in] is the sum over a row's choices; one not
+        asked for is None.  saved: what forward() returned beside Y."""
+        dev, ldx, wi, wo = self._args(x, routes, w_in, w_out)
+        S = routes.source.shape[0]
+        gy = _whole(grad_out, self._tdt, (S, self.d_out), "grad_out", dev)
+        sv = _whole(saved, _t.float32, (S, 2 * self.d_ff), "saved", dev)
+        if not (need_x or need_w_in or need_w_out):
+            return None, None, None
+        sp, other = _stream(stream, dev)
+        gx = _new(x, (routes.rows, self.d_in), other) if need_x else None
+        gwi = _like(w_in, other) if need_w_in else None
+        gwo = _like(w_out, other) if need_w_out else None
+        need = ffn_experts_backward_workspace_bytes(self._h, routes.rows, routes.per_row)
+        ws = _workspace(workspace, need, x, other)
+        ptr = lambda t: t.data_ptr() if t is not None else None
+        _call("ffn_experts_backward", self._h, x.data_ptr(), ldx, routes.place.data_ptr(), routes.source.data_ptr(),
+              routes.offsets.data_ptr(), wi, wo, sv, gy, ptr(gx), ptr(gwi), ptr(gwo), routes.rows, routes.per_row,
+              ws.data_ptr(), need, sp)
+        return gx, gwi, gwo
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            ffn_experts_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def _new_int(t, shape, other):

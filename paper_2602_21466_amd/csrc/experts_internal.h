@@ -61,4 +61,32 @@ int launch_gather(const RouteArgs& a, int32_t dtype, void* stream);            /
 int launch_combine(const RouteArgs& a, int32_t dtype, void* stream);           // sorted -> out_rows
 int launch_combine_backward(const RouteArgs& a, int32_t dtype, void* stream);  // rows (, sorted) -> out_sorted, grad_weights
 
+// out_rows[n] = sum over k and over `splits` parts of the sorted rows place[n, k], floats [splits, slots, ld] in `sorted`.
+int launch_combine_parts(const RouteArgs& a, int32_t splits, int32_t dtype, void* stream);
+
+// ---------------------------------------------------------------- the experts' products
+
+// The runs of sorted rows that a launch's products are about.
+struct Groups {
+    const int32_t* offsets;
+    int32_t experts;
+    int64_t rows;                         // sorted rows there may be
+    int64_t b_step;                       // bytes from one expert's B to the next's
+};
+// C = A B^T for the rows of every expert with its own B: t.M is groups.rows, t.tiles_m as many tiles of rows as there can
+// be (rows / tile + experts with a row).
+int launch_expert_rows_bf16(const TileArgs& t, const Groups& g, int32_t epilogue, bool b_cols, int32_t tile, void* stream);
+int launch_expert_rows_fp16(const TileArgs& t, const Groups& g, int32_t epilogue, bool b_cols, int32_t tile, void* stream);
+int launch_expert_rows_fp32(const TileArgs& t, const Groups& g, int32_t epilogue, bool b_cols, int32_t tile, void* stream);
+// C_e = A_e^T B_e, the sum over the rows of expert e, for every expert: C [experts, t.M, t.N], kStore or kPartial.
+int launch_expert_sums_bf16(const TileArgs& t, const Groups& g, int32_t epilogue, int32_t tile, void* stream);
+int launch_expert_sums_fp16(const TileArgs& t, const Groups& g, int32_t epilogue, int32_t tile, void* stream);
+int launch_expert_sums_fp32(const TileArgs& t, const Groups& g, int32_t epilogue, int32_t tile, void* stream);
+
+// launch_join and launch_join_gate for as many of the rows as *limit says (NULL: all).
+int launch_join_rows(const float* partial, int64_t ld, int32_t splits, int64_t M, int64_t N, void* out, int32_t dtype,
+                     const int32_t* limit, void* stream);
+int launch_join_gate_rows(const TileArgs& p, int32_t epilogue, const float* partial, int64_t ld, int32_t dtype,
+                          const int32_t* limit, void* stream);
+
 }  // namespace ffn

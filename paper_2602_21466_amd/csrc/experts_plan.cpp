@@ -6,6 +6,11 @@
 #include "experts_internal.h"
 #include "ffn_checks.h"
 
+struct ffn_experts_s {
+    int64_t d_in, d_ff, d_out;
+    int32_t experts, act, dtype, device;
+};
+
 namespace {
 
 // Slots a work-group of the sorting kernels, and work-groups.  One alone up to 8192 slots; at most 128, each of which reads
@@ -30,6 +35,168 @@ int check_rows(int64_t N, int64_t per_row, int64_t experts, int64_t width, int32
     if (rc == CGTP_EINVAL) return rc;
     if (!known(dtype)) return CGTP_EDTYPE;
     return width > FFN_MAX_WIDTH ? CGTP_EUNSUP : rc;
+}
+
+// ---------------------------------------------------------------- the experts' products
+
+// How products are cut: work-groups of `tile` x `tile` outputs, k in `splits` parts; joined: the parts' sums (also of one
+// part) go to memory and a second kernel finishes them.
+struct Cut { int32_t tile, splits; bool joined; };
+
+// The shortest by a count in microseconds, as a single block's products are cut (ffn_plan.cpp), with what the host knows:
+// `groups(tile)` work-groups by the mean, of `steps` steps of k each.
+template <typename Groups> Cut shortest(Groups groups, int64_t steps, double outputs, bool wide, bool gate_grad) {
+    const double ends = wide ? 2.0 : 4.0;
+    Cut best = {128, 1, false};
+    double least = 1e300;
+    for (int32_t tile : {256, 128}) {
+        const double all = groups(tile), slots = tile == 256 ? 256.0 : 512.0;
+        const double step = tile == 256 ? (wide ? 4.5 : 1.6) : (wide ? 2.6 : 1.06);
+        for (int32_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); ++s) {
+            const double n = all * s / slots;
+            const double rounds = n > 1.0 ? n + 0.5 : tile == 128 && n <= 0.5 ? 0.75 : 1.0;
+            const double t = rounds * ((double)tiles(steps, s) + ends) * step;
+            const double join = 3.0 + 0.1 * s + outputs * s * 8.0 / 4e6, own = gate_grad ? 10.0 : 0.0;
+            const bool joined = s > 1 || own > join;
+            if (t + (joined ? join : own) < least) { least = t + (joined ? join : own); best = {tile, s, joined}; }
+        }
+    }
+    return best;
+}
+
+// One product: R rows over the plan's experts, N columns, K values.
+struct Shape { int64_t R, E, N, K; };
+
+// Tiles of rows there may be.
+int64_t most_tiles(const Shape& s, int32_t tile) { return s.R / tile + (s.E < s.R ? s.E : s.R); }
+
+// [R, N], B by expert.  A run of rows ends in half a tile by the mean.
+Cut cut_rows(const Shape& s, int32_t dtype, int32_t epilogue) {
+    const bool wide = dtype == FFN_FP32;
+    auto groups = [&](int32_t tile) { return ((double)s.R / tile + 0.5 * (double)(s.E < s.R ? s.E : s.R)) * (double)tiles(s.N, tile); };
+    Cut c = shortest(groups, tiles(s.K, wide ? 32 : 64), (double)s.R * s.N, wide, epilogue == ffn::kGateGrad);
+    c.joined = c.joined || epilogue == ffn::kPartial;
+    return c;
+}
+
+// [experts, M, N], sums over each expert's rows (R / experts of them by the mean).
+Cut cut_sums(int64_t M, const Shape& s, int32_t dtype) {
+    const bool wide = dtype == FFN_FP32;
+    auto groups = [&](int32_t tile) { return (double)(s.E * tiles(M, tile) * tiles(s.N, tile)); };
+    return shortest(groups, tiles(tiles(s.R, s.E), wide ? 32 : 64), (double)(s.E * M) * s.N, wide, false);
+}
+
+int64_t up4(int64_t n) { return (n + 3) & ~3LL; }
+int64_t rows_partial(const Shape& s, int32_t dtype, int32_t epilogue) {
+    const Cut c = cut_rows(s, dtype, epilogue);
+    return c.joined ? aligned(c.splits * s.R * up4(s.N) * 4) : 0;
+}
+int64_t sums_partial(int64_t M, const Shape& s, int32_t dtype) {
+    const Cut c = cut_sums(M, s, dtype);
+    return c.joined ? aligned(c.splits * s.E * M * up4(s.N) * 4) : 0;
+}
+
+constexpr int64_t kMostGroups = 0x7FFFFFFF / 512;
+bool rows_fit(const Shape& s, int32_t dtype, int32_t epilogue) {
+    const Cut c = cut_rows(s, dtype, epilogue);
+    return most_tiles(s, c.tile) * tiles(s.N, c.tile) * c.splits <= kMostGroups;
+}
+bool sums_fit(int64_t M, const Shape& s, int32_t dtype) {
+    const Cut c = cut_sums(M, s, dtype);
+    return (tiles(M, c.tile) * tiles(s.N, c.tile) * c.splits + 8) * s.E <= kMostGroups;
+}
+
+int launch_rows(const ffn::TileArgs& t, const ffn::Groups& g, int32_t epilogue, bool bc, int32_t dtype, int32_t tile, void* stream) {
+    switch (dtype) {
+        case FFN_FP32: return ffn::launch_expert_rows_fp32(t, g, epilogue, bc, tile, stream);
+        case FFN_BF16: return ffn::launch_expert_rows_bf16(t, g, epilogue, bc, tile, stream);
+        default: return ffn::launch_expert_rows_fp16(t, g, epilogue, bc, tile, stream);
+    }
+}
+int launch_sums(const ffn::TileArgs& t, const ffn::Groups& g, int32_t epilogue, int32_t dtype, int32_t tile, void* stream) {
+    switch (dtype) {
+        case FFN_FP32: return ffn::launch_expert_sums_fp32(t, g, epilogue, tile, stream);
+        case FFN_BF16: return ffn::launch_expert_sums_bf16(t, g, epilogue, tile, stream);
+        default: return ffn::launch_expert_sums_fp16(t, g, epilogue, tile, stream);
+    }
+}
+
+// Runs the product of rows whose operands, sizes (t.M: the sorted rows) and results t describes; `partial` is scratch of
+// rows_partial() (kGate: of 2 N columns).  kPartial: the sums stay there, in *splits parts.
+int rows_product(ffn::TileArgs t, const ffn::Groups& g, int32_t epilogue, bool bc, int32_t dtype, void* partial, int32_t* splits, void* stream) {
+    const int64_t columns = epilogue == ffn::kGate ? 2 * t.N : t.N;
+    const Shape s = {t.M, g.experts, columns, t.K};
+    const Cut c = cut_rows(s, dtype, epilogue);
+    t.tiles_m = (int32_t)most_tiles(s, c.tile);
+    t.tiles_n = (int32_t)tiles(columns, c.tile);
+    t.splits = c.splits;
+    if (!c.joined) return status(launch_rows(t, g, epilogue, bc, dtype, c.tile, stream));
+    ffn::TileArgs p = t;
+    p.c = partial;
+    p.N = columns;
+    p.ldc = up4(columns);
+    const int rc = status(launch_rows(p, g, ffn::kPartial, bc, dtype, c.tile, stream));
+    if (splits) *splits = c.splits;
+    if (rc != CGTP_OK || epilogue == ffn::kPartial) return rc;
+    const int32_t* limit = g.offsets + g.experts;
+    if (epilogue == ffn::kStore)
+        return status(ffn::launch_join_rows((const float*)partial, p.ldc, c.splits, t.M, t.N, t.c, dtype, limit, stream));
+    return status(ffn::launch_join_gate_rows(t, epilogue, (const float*)partial, p.ldc, dtype, limit, stream));
+}
+
+// The sums over each expert's rows: t.M x t.N results an expert, contiguous.
+int sums_product(ffn::TileArgs t, const ffn::Groups& g, int32_t dtype, void* partial, void* stream) {
+    const Cut c = cut_sums(t.M, {g.rows, g.experts, t.N, 0}, dtype);
+    t.tiles_m = (int32_t)tiles(t.M, c.tile);
+    t.tiles_n = (int32_t)tiles(t.N, c.tile);
+    t.splits = c.splits;
+    t.ldc = t.N;
+    if (!c.joined) return status(launch_sums(t, g, ffn::kStore, dtype, c.tile, stream));
+    ffn::TileArgs p = t;
+    p.c = partial;
+    p.ldc = up4(t.N);
+    const int rc = status(launch_sums(p, g, ffn::kPartial, dtype, c.tile, stream));
+    if (rc != CGTP_OK) return rc;
+    return status(ffn::launch_join((const float*)partial, p.ldc, c.splits, g.experts * t.M, t.N, t.c, dtype, stream));
+}
+
+// Byte offsets in the workspace: x's rows in the sorted order, intermediates, operands to be packed, partial sums.
+struct Layout { int64_t x, h, dgu, gy, w_in, w_out, partial, total; };
+Layout layout(const ffn_experts_s* p, int64_t R, bool backward) {
+    const int64_t di = p->d_in, df = p->d_ff, d_o = p->d_out, E = p->experts;
+    const int32_t t = p->dtype;
+    Layout l = {};
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) { const int64_t o = at; at += bytes; return o; };
+    l.x = take(packed_bytes(R, di, t));
+    l.h = take(packed_bytes(R, df, t));
+    l.w_in = take(di % chunk(t) ? packed_bytes(E * 2 * df, di, t) : 0);
+    l.w_out = take(df % chunk(t) ? packed_bytes(E * d_o, df, t) : 0);
+    int64_t partial = 0;
+    auto also = [&](int64_t bytes) { partial = bytes > partial ? bytes : partial; };
+    if (backward) {
+        l.dgu = take(packed_bytes(R, 2 * df, t));
+        l.gy = take(packed_bytes(R, d_o, t));
+        also(rows_partial({R, E, df, d_o}, t, ffn::kGateGrad));
+        also(rows_partial({R, E, di, 2 * df}, t, ffn::kPartial));
+        also(sums_partial(2 * df, {R, E, di, 0}, t));
+        also(sums_partial(d_o, {R, E, df, 0}, t));
+    } else {
+        also(rows_partial({R, E, 2 * df, di}, t, ffn::kGate));
+        also(rows_partial({R, E, d_o, df}, t, ffn::kStore));
+    }
+    l.partial = take(partial);
+    l.total = at;
+    return l;
+}
+
+// x's rows in the sorted order, of up8(d_in) values.
+int gather(const ffn_experts_s* plan, const void* x, int64_t ldx, const int32_t* place, void* to, int64_t N, int64_t per_row, void* stream) {
+    ffn::RouteArgs a = {};
+    a.N = N; a.width = plan->d_in; a.per_row = per_row; a.slots = N * per_row;
+    a.place = place; a.rows = x; a.ld = ldx;
+    a.out_sorted = to; a.ld_sorted = up8(plan->d_in);
+    return status(ffn::launch_gather(a, plan->dtype, stream));
 }
 
 }  // namespace
@@ -124,6 +291,167 @@ int ffn_route_combine_backward(const void* ys, const int32_t* place, const int32
     a.rows = grad_y; a.ld = ldg; a.sorted = ys;
     a.out_sorted = grad_ys; a.ld_sorted = width; a.grad_weights = grad_weights;
     return status(ffn::launch_combine_backward(a, dtype, hip_stream));
+}
+
+int ffn_experts_plan(int32_t experts, int64_t d_in, int64_t d_ff, int64_t d_out, int32_t activation, int32_t dtype,
+                     ffn_experts_t* plan_out) {
+    if (!plan_out || experts < 1 || d_in < 1 || d_ff < 1 || d_out < 1) return CGTP_EINVAL;
+    if (activation < FFN_SILU || activation > FFN_RELU) return CGTP_EINVAL;
+    if (!known(dtype)) return CGTP_EDTYPE;
+    if (experts > FFN_MAX_EXPERTS || d_in > FFN_MAX_WIDTH || d_ff > FFN_MAX_WIDTH || d_out > FFN_MAX_WIDTH) return CGTP_EUNSUP;
+    if (experts * 2 * d_ff > FFN_MAX_ROWS || experts * d_out > FFN_MAX_ROWS) return CGTP_EUNSUP;
+    int dev = -1;
+    const hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return status((int)e);
+    ffn_experts_s* p = new (std::nothrow) ffn_experts_s{d_in, d_ff, d_out, experts, activation, dtype, dev};
+    if (!p) return CGTP_ENOMEM;
+    *plan_out = p;
+    return CGTP_OK;
+}
+
+int ffn_experts_destroy(ffn_experts_t plan) {
+    delete plan;
+    return CGTP_OK;
+}
+
+int64_t ffn_experts_workspace_bytes(ffn_experts_t plan, int64_t N, int32_t per_row) {
+    if (!plan || check_slots(N, per_row, 1) != CGTP_OK) return -1;
+    return layout(plan, N * per_row, false).total;
+}
+
+int64_t ffn_experts_backward_workspace_bytes(ffn_experts_t plan, int64_t N, int32_t per_row) {
+    if (!plan || check_slots(N, per_row, 1) != CGTP_OK) return -1;
+    return layout(plan, N * per_row, true).total;
+}
+
+int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const int32_t* place, const int32_t* source,
+                        const int32_t* offsets, const void* w_in, const void* w_out, void* y, void* saved, int64_t N,
+                        int32_t per_row, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    if (!plan) return CGTP_EINVAL;
+    int rc = check_slots(N, per_row, 1);
+    if (rc != CGTP_OK) return rc;
+    if (N == 0) return CGTP_OK;
+    const int64_t e = size_of(plan->dtype), di = plan->d_in, df = plan->d_ff, d_o = plan->d_out, E = plan->experts, R = N * per_row;
+    const int32_t dt = plan->dtype;
+    if (!x || !place || !source || !offsets || !w_in || !w_out || !y || ldx < di) return CGTP_EINVAL;
+    if (ldx > kMaxStride) return CGTP_EUNSUP;
+    if (misaligned({x}, e) || misaligned({place, source, offsets}, 4) || misaligned({w_in, w_out, y, saved}, 16)) return CGTP_EINVAL;
+    if (!rows_fit({R, E, 2 * df, di}, dt, ffn::kGate) || !rows_fit({R, E, d_o, df}, dt, ffn::kStore)) return CGTP_EUNSUP;
+    const Layout l = layout(plan, R, false);
+    rc = workspace_ok(workspace, workspace_bytes, l.total);
+    if (rc != CGTP_OK) return rc;
+    const Range ins[] = {rows(x, N, ldx, di, e), {place, R * 4}, {source, R * 4}, {offsets, (E + 1) * 4}, {w_in, E * 2 * df * di * e}, {w_out, E * d_o * df * e}};
+    const Range outs[] = {{y, R * d_o * e}, {saved, R * 2 * df * 4}, {workspace, l.total}};
+    if (any_overlap(outs, ins)) return CGTP_EINVAL;
+    rc = current_device_is(plan->device);
+    if (rc != CGTP_OK) return rc;
+    char* ws = (char*)workspace;
+    ffn::PackJobs jobs = {};
+    const Operand Wi = operand(w_in, di, E * 2 * df, di, dt, ws + l.w_in, &jobs), Wo = operand(w_out, df, E * d_o, df, dt, ws + l.w_out, &jobs);
+    rc = status(ffn::launch_pack(jobs, dt, hip_stream));
+    if (rc == CGTP_OK) rc = gather(plan, x, ldx, place, ws + l.x, N, per_row, hip_stream);
+    if (rc != CGTP_OK) return rc;
+    ffn::TileArgs t = {};
+    t.a = ws + l.x; t.lda = up8(di);
+    t.b = Wi.p; t.ldb = Wi.ld;
+    t.M = R; t.N = df; t.K = di;
+    t.c = ws + l.h; t.ldc = up8(df);
+    t.act = plan->act; t.saved = (float*)saved;
+    ffn::Groups g = {offsets, plan->experts, R, 2 * df * Wi.ld * e};
+    rc = rows_product(t, g, ffn::kGate, false, dt, ws + l.partial, nullptr, hip_stream);
+    if (rc != CGTP_OK) return rc;
+    ffn::TileArgs o = {};
+    o.a = ws + l.h; o.lda = up8(df);
+    o.b = Wo.p; o.ldb = Wo.ld;
+    o.M = R; o.N = d_o; o.K = df;
+    o.c = y; o.ldc = d_o;
+    g.b_step = d_o * Wo.ld * e;
+    return rows_product(o, g, ffn::kStore, false, dt, ws + l.partial, nullptr, hip_stream);
+}
+
+int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const int32_t* place, const int32_t* source,
+                         const int32_t* offsets, const void* w_in, const void* w_out, const void* saved,
+                         const void* grad_y, void* grad_x, void* grad_w_in, void* grad_w_out, int64_t N,
+                         int32_t per_row, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    if (!plan) return CGTP_EINVAL;
+    int rc = check_slots(N, per_row, 1);
+    if (rc != CGTP_OK) return rc;
+    if (N == 0 && !grad_w_in && !grad_w_out) return CGTP_OK;   // (an empty grad_x may be NULL)
+    if (!grad_x && !grad_w_in && !grad_w_out) return CGTP_EINVAL;
+    const int64_t e = size_of(plan->dtype), di = plan->d_in, df = plan->d_ff, d_o = plan->d_out, E = plan->experts, R = N * per_row;
+    const int32_t dt = plan->dtype;
+    if (N > 0 && (!x || !place || !source || !offsets || !w_in || !w_out || !saved || !grad_y || ldx < di)) return CGTP_EINVAL;
+    if (ldx > kMaxStride) return CGTP_EUNSUP;
+    if (misaligned({x, grad_y}, e) || misaligned({place, source, offsets}, 4) ||
+        misaligned({w_in, w_out, saved, grad_x, grad_w_in, grad_w_out}, 16))
+        return CGTP_EINVAL;
+    if (!rows_fit({R, E, df, d_o}, dt, ffn::kGateGrad) || !rows_fit({R, E, di, 2 * df}, dt, ffn::kPartial) ||
+        !sums_fit(2 * df, {R, E, di, 0}, dt) || !sums_fit(d_o, {R, E, df, 0}, dt))
+        return CGTP_EUNSUP;
+    const Layout l = layout(plan, R, true);
+    rc = workspace_ok(workspace, workspace_bytes, l.total);
+    if (rc != CGTP_OK) return rc;
+    const Range ins[] = {rows(x, N, ldx, di, e), {place, R * 4}, {source, R * 4}, {offsets, (E + 1) * 4}, {w_in, E * 2 * df * di * e}, {w_out, E * d_o * df * e},
+                         {saved, R * 2 * df * 4}, {grad_y, R * d_o * e}};
+    const Range outs[] = {{grad_x, N * di * e}, {grad_w_in, E * 2 * df * di * e}, {grad_w_out, E * d_o * df * e}, {workspace, l.total}};
+    if (any_overlap(outs, ins)) return CGTP_EINVAL;
+    rc = current_device_is(plan->device);
+    if (rc != CGTP_OK) return rc;
+    if (N == 0) {
+        // sums over no rows
+        if (grad_w_in) rc = status(ffn::launch_zero(grad_w_in, E * 2 * df * di * e, hip_stream));
+        if (rc == CGTP_OK && grad_w_out) rc = status(ffn::launch_zero(grad_w_out, E * d_o * df * e, hip_stream));
+        return rc;
+    }
+    char* ws = (char*)workspace;
+    ffn::PackJobs jobs = {};
+    const Operand Gy = operand(grad_y, d_o, R, d_o, dt, ws + l.gy, &jobs), Wo = operand(w_out, df, E * d_o, df, dt, ws + l.w_out, &jobs);
+    Operand Wi = {};
+    if (grad_x) Wi = operand(w_in, di, E * 2 * df, di, dt, ws + l.w_in, &jobs);
+    rc = status(ffn::launch_pack(jobs, dt, hip_stream));
+    if (rc == CGTP_OK && grad_w_in) rc = gather(plan, x, ldx, place, ws + l.x, N, per_row, hip_stream);
+    if (rc != CGTP_OK) return rc;
+    const Operand H = {ws + l.h, up8(df)}, D = {ws + l.dgu, up8(2 * df)};
+    ffn::Groups g = {offsets, plan->experts, R, d_o * Wo.ld * e};
+    ffn::TileArgs t = {};
+    t.a = Gy.p; t.lda = Gy.ld;
+    t.b = Wo.p; t.ldb = Wo.ld;
+    t.M = R; t.N = df; t.K = d_o;
+    t.c = ws + l.dgu; t.ldc = D.ld;
+    t.h = ws + l.h; t.ldh = H.ld;
+    t.act = plan->act; t.saved = (float*)const_cast<void*>(saved);
+    rc = rows_product(t, g, ffn::kGateGrad, true, dt, ws + l.partial, nullptr, hip_stream);
+    if (rc == CGTP_OK && grad_x) {
+        // its sums stay in 32 bits until a row's choices are added
+        ffn::TileArgs d = {};
+        d.a = D.p; d.lda = D.ld;
+        d.b = Wi.p; d.ldb = Wi.ld;
+        d.M = R; d.N = di; d.K = 2 * df;
+        g.b_step = 2 * df * Wi.ld * e;
+        int32_t splits = 1;
+        rc = rows_product(d, g, ffn::kPartial, true, dt, ws + l.partial, &splits, hip_stream);
+        ffn::RouteArgs a = {};
+        a.N = N; a.width = di; a.per_row = per_row; a.slots = R;
+        a.place = place; a.sorted = ws + l.partial; a.out_rows = grad_x; a.ld_out = di;
+        if (rc == CGTP_OK) rc = status(ffn::launch_combine_parts(a, splits, dt, hip_stream));
+    }
+    if (rc == CGTP_OK && grad_w_in) {
+        ffn::TileArgs w = {};
+        w.a = D.p; w.lda = D.ld;
+        w.b = ws + l.x; w.ldb = up8(di);
+        w.M = 2 * df; w.N = di;
+        w.c = grad_w_in;
+        rc = sums_product(w, g, dt, ws + l.partial, hip_stream);
+    }
+    if (rc == CGTP_OK && grad_w_out) {
+        ffn::TileArgs w = {};
+        w.a = Gy.p; w.lda = Gy.ld;
+        w.b = H.p; w.ldb = H.ld;
+        w.M = d_o; w.N = df;
+        w.c = grad_w_out;
+        rc = sums_product(w, g, dt, ws + l.partial, hip_stream);
+    }
+    return rc;
 }
 
 }  // extern "C"

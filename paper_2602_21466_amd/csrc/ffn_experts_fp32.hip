@@ -1,0 +1,11 @@
+// The experts' tiled products of fp32 arrays.
+#include "ffn_experts.h"
+
+namespace ffn {
+int launch_expert_rows_fp32(const TileArgs& t, const Groups& g, int32_t epilogue, bool b_cols, int32_t tile, void* stream) {
+    return dev::expert_rows<float>(t, g, epilogue, b_cols, tile, (hipStream_t)stream);
+}
+int launch_expert_sums_fp32(const TileArgs& t, const Groups& g, int32_t epilogue, int32_t tile, void* stream) {
+    return dev::expert_sums<float>(t, g, epilogue, tile, (hipStream_t)stream);
+}
+}  // namespace ffn

@@ -1,4 +1,5 @@
 // Packing of operands for the tiled products, and the joining of their split sums.
+#include "experts_internal.h"
 #include "ffn_tile.h"
 
 namespace ffn {
@@ -38,10 +39,17 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(PackJobs jobs) {
     }
 }
 
+// Of M rows those that are finished: all, or as many as the device knows of (sorted by expert).
+__device__ __forceinline__ int64_t rows_of(int64_t M, const int32_t* limit) {
+    if (!limit) return M;
+    const int64_t n = *limit;
+    return n < 0 ? 0 : n < M ? n : M;
+}
+
 // Splits are added in order: the result does not depend on when they were done.  (3281 x 512 in 9 parts, fp32: 11 us.)
 template <typename Out>
-__global__ __launch_bounds__(kThreads) void join_kernel(const float* partial, int64_t ld, int splits, int64_t M, int64_t N, Out* out) {
-    const int64_t quads = (N + 3) >> 2, total = M * quads;
+__global__ __launch_bounds__(kThreads) void join_kernel(const float* partial, int64_t ld, int splits, int64_t M, int64_t N, Out* out, const int32_t* limit) {
+    const int64_t quads = (N + 3) >> 2, total = rows_of(M, limit) * quads;
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
         const int64_t row = i / quads, c = (i - row * quads) * 4;
         f32x4 v = {};
@@ -54,8 +62,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float* partial, in
 // The joining of split sums with the gate's epilogues; the same arithmetic as the tiles' own.  kGate: the sums hold
 // [G U] (2 N columns); kGateGrad: dH.  (8192 x 512, fp32: 23 us, 5.0 TB/s.)
 template <typename T, int EPI>
-__global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const float* partial, int64_t ld) {
-    const int64_t quads = (p.N + 3) >> 2, total = p.M * quads;
+__global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const float* partial, int64_t ld, const int32_t* limit) {
+    const int64_t quads = (p.N + 3) >> 2, total = rows_of(p.M, limit) * quads;
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
         const int64_t m = i / quads, n = (i - m * quads) * 4;
         f32x4 v = {}, u = {};
@@ -121,11 +129,15 @@ int launch_pack(PackJobs jobs, int32_t dtype, void* stream) {
 }
 
 int launch_join_gate(const TileArgs& p, int32_t epilogue, const float* partial, int64_t ld, int32_t dtype, void* stream) {
+    return launch_join_gate_rows(p, epilogue, partial, ld, dtype, nullptr, stream);
+}
+
+int launch_join_gate_rows(const TileArgs& p, int32_t epilogue, const float* partial, int64_t ld, int32_t dtype, const int32_t* limit, void* stream) {
     hipStream_t s = (hipStream_t)stream;
     const unsigned g = groups(p.M * ((p.N + 3) >> 2));
 #define FFN_JOIN(T)                                                                                       \
-    if (epilogue == kGate) join_gate_kernel<T, kGate><<<g, kThreads, 0, s>>>(p, partial, ld);             \
-    else join_gate_kernel<T, kGateGrad><<<g, kThreads, 0, s>>>(p, partial, ld)
+    if (epilogue == kGate) join_gate_kernel<T, kGate><<<g, kThreads, 0, s>>>(p, partial, ld, limit);      \
+    else join_gate_kernel<T, kGateGrad><<<g, kThreads, 0, s>>>(p, partial, ld, limit)
     if (dtype == FFN_FP32) { FFN_JOIN(float); }
     else if (dtype == FFN_BF16) { FFN_JOIN(bf16); }
     else { FFN_JOIN(fp16); }
@@ -139,11 +151,15 @@ int launch_zero(void* p, int64_t bytes, void* stream) {
 }
 
 int launch_join(const float* partial, int64_t ld, int32_t splits, int64_t M, int64_t N, void* out, int32_t dtype, void* stream) {
+    return launch_join_rows(partial, ld, splits, M, N, out, dtype, nullptr, stream);
+}
+
+int launch_join_rows(const float* partial, int64_t ld, int32_t splits, int64_t M, int64_t N, void* out, int32_t dtype, const int32_t* limit, void* stream) {
     hipStream_t s = (hipStream_t)stream;
     const unsigned g = groups(M * ((N + 3) >> 2));
-    if (dtype == FFN_FP32) join_kernel<float><<<g, kThreads, 0, s>>>(partial, ld, splits, M, N, (float*)out);
-    else if (dtype == FFN_BF16) join_kernel<bf16><<<g, kThreads, 0, s>>>(partial, ld, splits, M, N, (bf16*)out);
-    else join_kernel<fp16><<<g, kThreads, 0, s>>>(partial, ld, splits, M, N, (fp16*)out);
+    if (dtype == FFN_FP32) join_kernel<float><<<g, kThreads, 0, s>>>(partial, ld, splits, M, N, (float*)out, limit);
+    else if (dtype == FFN_BF16) join_kernel<bf16><<<g, kThreads, 0, s>>>(partial, ld, splits, M, N, (bf16*)out, limit);
+    else join_kernel<fp16><<<g, kThreads, 0, s>>>(partial, ld, splits, M, N, (fp16*)out, limit);
     return (int)hipGetLastError();
 }
 

@@ -214,6 +214,24 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(RouteArgs p) {
     }
 }
 
+// The same of 32-bit sums in parts, four columns a thread.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void combine_parts_kernel(RouteArgs p, int splits) {
+    const int64_t ld = (p.width + 3) & ~3LL;
+    for (Chunks k(p.N, ld >> 2); k.more(); k.next()) {
+        const int32_t* place = p.place + k.row * p.per_row;
+        f32x4 sum = {};
+        for (int j = 0; j < p.per_row; ++j) {
+            const uint32_t from = (uint32_t)place[j];
+            if (from >= (uint64_t)p.slots) continue;
+            f32x4 v = {};
+            for (int s = 0; s < splits; ++s) v += *(const f32x4*)((const float*)p.sorted + ((int64_t)s * p.slots + from) * ld + k.at * 4);
+            sum += v;
+        }
+        store4<T>((T*)p.out_rows + k.row * p.ld_out, k.at * 4, p.width, 0, sum);
+    }
+}
+
 // TPR threads a row: they read grad_y's row once for four of its choices, and add up the products with those rows.
 template <typename T, int TPR>
 __global__ __launch_bounds__(kThreads) void combine_backward_kernel(RouteArgs p) {
@@ -309,6 +327,14 @@ int launch_gather(const RouteArgs& a, int32_t dtype, void* stream) {
 int launch_combine(const RouteArgs& a, int32_t dtype, void* stream) {
     const dim3 grid(chunk_groups(a.N, a.width));
 #define FFN_RUN(T) combine_kernel<T><<<grid, kThreads, 0, (hipStream_t)stream>>>(a)
+    FFN_BY_TYPE(FFN_RUN)
+#undef FFN_RUN
+    return (int)hipGetLastError();
+}
+
+int launch_combine_parts(const RouteArgs& a, int32_t splits, int32_t dtype, void* stream) {
+    const dim3 grid(chunk_groups(a.N, 2 * a.width));
+#define FFN_RUN(T) combine_parts_kernel<T><<<grid, kThreads, 0, (hipStream_t)stream>>>(a, splits)
     FFN_BY_TYPE(FFN_RUN)
 #undef FFN_RUN
     return (int)hipGetLastError();

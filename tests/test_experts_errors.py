@@ -89,3 +89,19 @@ def test_row_refusals(p):
     assert b(ys=None) == E and b(gys=None, gw=None) == E and b(gy=None) == E and b(ldg=7) == E and b(off=None) == E
     assert b(gys=p) == E and b(gw=p + 16384) == E and b(gw=p + 4608) == E and b(gw=p + 32769) == E and b(dtype=1) == D
     assert b(N=0) == lib.CGTP_OK
+
+
+@pytest.mark.parametrize("args,rc", [((0, 4, 4, 4, 0, 2), E), ((4, 0, 4, 4, 0, 2), E), ((4, 4, 0, 4, 0, 2), E), ((4, 4, 4, -1, 0, 2), E),
+                                     ((4, 4, 4, 4, 3, 2), E), ((4, 4, 4, 4, 0, 1), D), ((1025, 4, 4, 4, 0, 2), U),
+                                     ((4, (1 << 20) + 1, 4, 4, 0, 2), U), ((1024, 4, 1 << 20, 4, 0, 2), U)])
+def test_experts_plan_refusals(args, rc):
+    h = ctypes.c_void_p()
+    assert lib._load().ffn_experts_plan(*args, ctypes.byref(h)) == rc and h.value is None
+
+
+def test_experts_null_arguments():
+    f = lib._load()
+    assert f.ffn_experts_plan(2, 4, 4, 4, 0, 0, None) == E and f.ffn_experts_destroy(None) == lib.CGTP_OK
+    assert f.ffn_experts_workspace_bytes(None, 4, 1) == -1 and f.ffn_experts_backward_workspace_bytes(None, 4, 1) == -1
+    assert f.ffn_experts_forward(None, None, 0, *[None] * 7, 1, 1, None, 0, None) == E
+    assert f.ffn_experts_backward(None, None, 0, *[None] * 10, 1, 1, None, 0, None) == E
