@@ -132,21 +132,238 @@ __global__ __launch_bounds__(kThreads) void layer_columns_kernel(LayerArgs p, in
         }
 }
 
-inline int64_t layer_workers(int64_t width, int64_t N) {
-    const int64_t most = 1024 / column_blocks(width), least = N >= 256 ? N / 2 : N;
-    return N == 0 ? 0 : most < 1 ? 1 : most < least ? most : least;
+// A worker of TPR threads holds a row in registers, eight adjacent columns a thread and turn (as the norms of ffn_norm.h),
+// with the next row's loads in flight: x is read and u written once.
+template <typename T, int TPR, int I, bool TAIL>
+__global__ __launch_bounds__(group_of(TPR), forward_waves(sizeof(T), TPR, I, false)) void layer_forward_rows(LayerArgs p) {
+    __shared__ float s[4 * (TPR > 64 ? TPR / 64 : 1)];
+    constexpr int kWorkers = group_of(TPR) / TPR;
+    typedef Eight<T> V;
+    const int D = (int)p.width, t = threadIdx.x % TPR;
+    const int64_t step = (int64_t)gridDim.x * kWorkers;
+    const int sub = kWorkers == 1 ? 0 : TPR < 64 ? threadIdx.x / TPR : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    int64_t row = (int64_t)blockIdx.x * kWorkers + sub;
+    if (row >= p.N) return;
+    V w[I], b[I], xr[I];
+    Place at8[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) at8[i] = place8<TAIL>((t + i * TPR) * 8, D);
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) xr[i] = row8<T>((const T*)p.x + r * p.ldx, at8[i]);
+    };
+    auto factors = [&](int i) {
+        w[i] = ones8<T>(p.w, at8[i]);
+        b[i] = p.b ? row8<T>((const T*)p.b, at8[i]) : V{};
+    };
+    constexpr bool kLean = TPR == 1024;   // (128 registers a thread: neither the next row nor the factors are held)
+    if constexpr (!kLean) {
+        fetch(row);
+#pragma unroll
+        for (int i = 0; i < I; ++i) factors(i);
+    }
+    for (; row < p.N; row += step) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) {   // neither lanes' addresses nor converted factors are held over the rows
+            if constexpr (!kLean) {
+                asm volatile("" : "+v"(at8[i].c));
+                keep(w[i]);
+                keep(b[i]);
+            }
+        }
+        if constexpr (kLean) fetch(row);
+        float v[I][8], one[1] = {0.0f}, two[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            if constexpr (TAIL) keep(xr[i]);   // here before another thread may write u over it
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[i][j] = at(xr[i], j);
+                one[0] += (TAIL ? j >= at8[i].skip : at8[i].skip == 0) ? v[i][j] : 0.0f;
+            }
+        }
+        if (!kLean && row + step < p.N) fetch(row + step);
+        worker_sum<TPR, 1>(one, s, 0);
+        const float m = one[0] / (float)D;
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[i][j] -= m;
+                const float c = (TAIL ? j >= at8[i].skip : at8[i].skip == 0) ? v[i][j] : 0.0f;
+                two[0] += c;
+                two[1] += c * c;
+            }
+        worker_sum<TPR, 2>(two, s, 1);
+        const float d = two[0] / (float)D, r = 1.0f / sqrtf(fmaxf(two[1] / (float)D - d * d, 0.0f) + p.eps);
+        if (p.stats && t == 0) {
+            p.stats[row] = m + d;
+            p.stats[p.N + row] = r;
+        }
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            float o[8];
+            if constexpr (kLean) factors(i);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = (v[i][j] - d) * r * at(w[i], j) + at(b[i], j);
+            if (at8[i].skip < 8) put8<T>((T*)p.u + row * p.ldu, at8[i], o);
+        }
+    }
+}
+
+// Waves a SIMD that the backward rows' registers are bounded for: two column sums a value live through the rows.
+constexpr int layer_backward_waves(int bytes, int tpr, int turns) { return turns == 1 || tpr == 1024 || bytes == 2 ? 4 : 3; }
+
+// One pass over the rows: gx, and each work-group's column sums.
+template <typename T, int TPR, int I, bool TAIL>
+__global__ __launch_bounds__(group_of(TPR), layer_backward_waves(sizeof(T), TPR, I)) void layer_backward_rows(LayerArgs p, int64_t workers) {
+    constexpr int kGroup = group_of(TPR), kWorkers = kGroup / TPR;
+    __shared__ float s[2 * 3 * (TPR > 64 ? TPR / 64 : 1)];
+    __shared__ float cols[kWorkers > 1 ? kWorkers * TPR * I * 8 : 1];
+    typedef Eight<T> V;
+    const int D = (int)p.width, t = threadIdx.x % TPR;
+    const int sub = kWorkers == 1 ? 0 : TPR < 64 ? threadIdx.x / TPR : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    const int64_t worker = (int64_t)blockIdx.x * kWorkers + sub;
+    int64_t row = worker < workers ? worker : p.N;
+    float sw[I][8] = {}, sb[I][8] = {}, mr = 0.0f, rr = 0.0f;
+    V xr[I], gr[I], w[I];
+    Place at8[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) at8[i] = place8<TAIL>((t + i * TPR) * 8, D);
+    auto fetch = [&](int64_t r) {
+        mr = p.stats[r];
+        rr = p.stats[p.N + r];
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            xr[i] = row8<T>((const T*)p.x + r * p.ldx, at8[i]);
+            gr[i] = row8<T>((const T*)p.gu + r * p.ldg, at8[i]);
+        }
+    };
+    constexpr bool kLean = TPR == 1024;
+    if constexpr (!kLean) {
+        if (row < p.N) fetch(row);
+#pragma unroll
+        for (int i = 0; i < I; ++i) w[i] = ones8<T>(p.w, at8[i]);
+    }
+    for (int turn = 0; row < p.N; turn ^= 1) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) asm volatile("" : "+v"(at8[i].c), "+v"(at8[i].skip));
+        if constexpr (kLean) fetch(row);
+        const float m = mr, r = rr;
+        V x[I], g[I];
+        float sum[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            if constexpr (kLean) w[i] = ones8<T>(p.w, at8[i]);
+            x[i] = xr[i];
+            g[i] = gr[i];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool own = TAIL ? j >= at8[i].skip : at8[i].skip == 0;
+                const float a = own ? at(g[i], j) * at(w[i], j) : 0.0f, c = own ? at(x[i], j) - m : 0.0f;
+                sum[0] += a;
+                sum[1] += c;
+                sum[2] += a * c;
+            }
+            keep(x[i]);   // the next half starts from the loaded values
+            keep(g[i]);
+            keep(w[i]);
+        }
+        const int64_t at_row = row;
+        row += workers;
+        if (!kLean && row < p.N) fetch(row);
+        worker_sum<TPR, 3>(sum, s, turn);
+        const float ma = sum[0] / (float)D, d = sum[1] / (float)D, man = r * (sum[2] / (float)D - d * ma);
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            if (at8[i].skip == 8) continue;
+            float gx[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float gu = at(g[i], j), n = (at(x[i], j) - m - d) * r;
+                sw[i][j] += gu * n;
+                sb[i][j] += gu;
+                gx[j] = r * (gu * at(w[i], j) - ma - n * man);
+            }
+            if (p.gx) put8<T>((T*)p.gx + at_row * D, at8[i], gx);
+        }
+    }
+
+    // column sums of the work-group
+    float* out = p.partial + (int64_t)blockIdx.x * 2 * D;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if constexpr (kWorkers > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (at8[i].skip < 8) cols[sub * (TPR * I * 8) + at8[i].c + j] = k ? sb[i][j] : sw[i][j];
+            __syncthreads();
+            for (int c = threadIdx.x; c < D; c += kGroup) {
+                float v = 0.0f;
+#pragma unroll
+                for (int q = 0; q < kWorkers; ++q) v += cols[q * (TPR * I * 8) + c];
+                out[(int64_t)k * D + c] = v;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                if (at8[i].skip == 8) continue;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) out[(int64_t)k * D + at8[i].c + j] = k ? sb[i][j] : sw[i][j];
+            }
+        }
+    }
+}
+
+// Workers of the backward pass: as many as the compute units hold at once, with two or four rows each where there are many
+// (the joining kernel reads a set of sums for each work-group).
+inline int64_t layer_workers(const Shape& sh, int64_t N, int64_t width, int bytes) {
+    const int64_t least = N >= 4096 ? 4 : N >= 256 ? 2 : 1, some = (N + least - 1) / least;
+    int64_t most = 1024 / column_blocks(width);
+    if (sh.tpr) most = 256 * (256 * layer_backward_waves(bytes, sh.tpr, sh.turns) / group_of(sh.tpr)) * (group_of(sh.tpr) / sh.tpr);
+    if (most < 1) most = 1;
+    return some < most ? some : most;
+}
+inline int64_t layer_groups(const Shape& sh, int64_t workers) {
+    const int64_t per = sh.tpr ? group_of(sh.tpr) / sh.tpr : 1;
+    return (workers + per - 1) / per;
 }
 
 template <typename T> int layer_forward(const LayerArgs& a, hipStream_t s) {
-    layer_forward_kernel<T><<<dim3(row_groups(a.N)), kThreads, 0, s>>>(a);
+    const Shape sh = shape_of(a.width, kForward, (int)sizeof(T));
+    if (sh.tpr == 0) {
+        layer_forward_kernel<T><<<dim3(row_groups(a.N)), kThreads, 0, s>>>(a);
+        return (int)hipGetLastError();
+    }
+    const bool tail = a.width % 8 != 0;
+    const int64_t per = group_of(sh.tpr) / sh.tpr, all = (a.N + per - 1) / per;
+    const int64_t most = 256 * (256 * forward_waves(sizeof(T), sh.tpr, sh.turns, false) / group_of(sh.tpr));
+    const dim3 grid((unsigned)(all < most ? all : most));
+#define FFN_RUN(TPR, I)                                                                  \
+    if (tail) layer_forward_rows<T, TPR, I, true><<<grid, group_of(TPR), 0, s>>>(a);     \
+    else layer_forward_rows<T, TPR, I, false><<<grid, group_of(TPR), 0, s>>>(a)
+    FFN_SHAPES(FFN_RUN)
+#undef FFN_RUN
     return (int)hipGetLastError();
 }
 
 template <typename T> int layer_backward(const LayerArgs& a, hipStream_t s) {
-    const int64_t groups = layer_workers(a.width, a.N);
-    if (groups > 0) {
+    const Shape sh = shape_of(a.width, kBackward, (int)sizeof(T));
+    const int64_t workers = layer_workers(sh, a.N, a.width, (int)sizeof(T)), groups = layer_groups(sh, workers);
+    if (groups > 0 && sh.tpr == 0) {
         layer_means_kernel<T><<<dim3(row_groups(a.N)), kThreads, 0, s>>>(a, groups);
         layer_columns_kernel<T><<<dim3((unsigned)groups, (unsigned)column_blocks(a.width)), kThreads, 0, s>>>(a, groups);
+    } else if (groups > 0) {
+        const bool tail = a.width % 8 != 0;
+        const dim3 grid((unsigned)groups);
+#define FFN_RUN(TPR, I)                                                                           \
+    if (tail) layer_backward_rows<T, TPR, I, true><<<grid, group_of(TPR), 0, s>>>(a, workers);    \
+    else layer_backward_rows<T, TPR, I, false><<<grid, group_of(TPR), 0, s>>>(a, workers)
+        FFN_SHAPES(FFN_RUN)
+#undef FFN_RUN
     }
     if (a.gw || a.gb) {
         // the work-groups' sums added by the norms' joining kernel
@@ -161,7 +378,10 @@ template <typename T> int layer_backward(const LayerArgs& a, hipStream_t s) {
     return (int)hipGetLastError();
 }
 
-inline int64_t layer_floats(int64_t width, int64_t N, int bytes) { (void)bytes; return layer_workers(width, N) * 2 * width + 3 * N; }
+inline int64_t layer_floats(int64_t width, int64_t N, int bytes) {
+    const Shape sh = shape_of(width, kBackward, bytes);
+    return layer_groups(sh, layer_workers(sh, N, width, bytes)) * 2 * width + (sh.tpr ? 0 : 3 * N);
+}
 
 }  // namespace
 }  // namespace ffn
