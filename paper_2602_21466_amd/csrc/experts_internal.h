@@ -72,7 +72,11 @@ struct Groups {
     int32_t experts;
     int64_t rows;                         // sorted rows there may be
     int64_t b_step;                       // bytes from one expert's B to the next's
+    const void *a_end, *b_end;            // behind the last bytes that may be read of either operand
+    const int32_t* source;                // rows of A are those of slots source[..] / per_row; NULL: they are in their order
+    int32_t per_row;
 };
+// Operands lie in memory as they are: rows start on any element, with anything behind them.
 // C = A B^T for the rows of every expert with its own B: t.M is groups.rows, t.tiles_m as many tiles of rows as there can
 // be (rows / tile + experts with a row).
 int launch_expert_rows_bf16(const TileArgs& t, const Groups& g, int32_t epilogue, bool b_cols, int32_t tile, void* stream);

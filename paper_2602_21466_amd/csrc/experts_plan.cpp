@@ -160,23 +160,43 @@ int sums_product(ffn::TileArgs t, const ffn::Groups& g, int32_t dtype, void* par
     return status(ffn::launch_join((const float*)partial, p.ldc, c.splits, g.experts * t.M, t.N, t.c, dtype, stream));
 }
 
-// Byte offsets in the workspace: x's rows in the sorted order, intermediates, operands to be packed, partial sums.
+// A matrix as a product reads it: where it is, and behind its last byte that may be read.
+struct Matrix { const void* p; int64_t ld; const void* end; };
+
+// Direct loads take four bytes at a time: of 16-bit arrays two bytes more than the last value, which are in the array's own
+// four where its rows start on four bytes, and else on its page of memory unless the array ends with a page.
+bool direct(const void* p, int64_t rows, int64_t ld, int64_t width, int64_t e) {
+    return e == 4 || (((uintptr_t)p & 3) == 0 && (ld % 2 == 0 || rows == 1)) || (((uintptr_t)p + ((rows - 1) * ld + width) * e) & 4095) != 0;
+}
+Matrix matrix(const void* p, int64_t rows, int64_t ld, int64_t width, int64_t e) {
+    return {p, ld, (const char*)p + ((rows - 1) * ld + width) * e + (e == 2 ? 2 : 0)};
+}
+// It, or a copy of it in `scratch`.
+Matrix readable(const void* p, int64_t rows, int64_t width, int32_t dtype, void* scratch, ffn::PackJobs* jobs) {
+    const int64_t e = size_of(dtype);
+    if (direct(p, rows, width, width, e)) return matrix(p, rows, width, width, e);
+    jobs->job[jobs->n++] = {p, scratch, width, rows, width, up8(width), 0};
+    return matrix(scratch, rows, up8(width), width, e);
+}
+
+// Byte offsets in the workspace: x's rows in the sorted order, intermediates, copies of operands, partial sums.
 struct Layout { int64_t x, h, dgu, gy, w_in, w_out, partial, total; };
 Layout layout(const ffn_experts_s* p, int64_t R, bool backward) {
     const int64_t di = p->d_in, df = p->d_ff, d_o = p->d_out, E = p->experts;
     const int32_t t = p->dtype;
+    const bool narrow = t != FFN_FP32;
     Layout l = {};
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t o = at; at += bytes; return o; };
     l.x = take(packed_bytes(R, di, t));
     l.h = take(packed_bytes(R, df, t));
-    l.w_in = take(di % chunk(t) ? packed_bytes(E * 2 * df, di, t) : 0);
-    l.w_out = take(df % chunk(t) ? packed_bytes(E * d_o, df, t) : 0);
+    l.w_in = take(narrow && di % 2 ? packed_bytes(E * 2 * df, di, t) : 0);
+    l.w_out = take(narrow && df % 2 ? packed_bytes(E * d_o, df, t) : 0);
     int64_t partial = 0;
     auto also = [&](int64_t bytes) { partial = bytes > partial ? bytes : partial; };
     if (backward) {
         l.dgu = take(packed_bytes(R, 2 * df, t));
-        l.gy = take(packed_bytes(R, d_o, t));
+        l.gy = take(narrow ? packed_bytes(R, d_o, t) : 0);
         also(rows_partial({R, E, df, d_o}, t, ffn::kGateGrad));
         also(rows_partial({R, E, di, 2 * df}, t, ffn::kPartial));
         also(sums_partial(2 * df, {R, E, di, 0}, t));
@@ -347,25 +367,28 @@ int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const in
     if (rc != CGTP_OK) return rc;
     char* ws = (char*)workspace;
     ffn::PackJobs jobs = {};
-    const Operand Wi = operand(w_in, di, E * 2 * df, di, dt, ws + l.w_in, &jobs), Wo = operand(w_out, df, E * d_o, df, dt, ws + l.w_out, &jobs);
+    const Matrix Wi = readable(w_in, E * 2 * df, di, dt, ws + l.w_in, &jobs), Wo = readable(w_out, E * d_o, df, dt, ws + l.w_out, &jobs);
     rc = status(ffn::launch_pack(jobs, dt, hip_stream));
-    if (rc == CGTP_OK) rc = gather(plan, x, ldx, place, ws + l.x, N, per_row, hip_stream);
+    // x's rows where they are, by 32-bit offsets, or copied in the sorted order
+    const bool there = direct(x, N, ldx, di, e) && ((N - 1) * ldx + di) * e < (1LL << 31) - 256;
+    if (rc == CGTP_OK && !there) rc = gather(plan, x, ldx, place, ws + l.x, N, per_row, hip_stream);
     if (rc != CGTP_OK) return rc;
+    const Matrix X = there ? matrix(x, N, ldx, di, e) : matrix(ws + l.x, R, up8(di), di, e), H = matrix(ws + l.h, R, up8(df), df, e);
     ffn::TileArgs t = {};
-    t.a = ws + l.x; t.lda = up8(di);
+    t.a = X.p; t.lda = X.ld;
     t.b = Wi.p; t.ldb = Wi.ld;
     t.M = R; t.N = df; t.K = di;
-    t.c = ws + l.h; t.ldc = up8(df);
+    t.c = ws + l.h; t.ldc = H.ld;
     t.act = plan->act; t.saved = (float*)saved;
-    ffn::Groups g = {offsets, plan->experts, R, 2 * df * Wi.ld * e};
+    ffn::Groups g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, X.end, Wi.end, there ? source : nullptr, per_row};
     rc = rows_product(t, g, ffn::kGate, false, dt, ws + l.partial, nullptr, hip_stream);
     if (rc != CGTP_OK) return rc;
     ffn::TileArgs o = {};
-    o.a = ws + l.h; o.lda = up8(df);
+    o.a = H.p; o.lda = H.ld;
     o.b = Wo.p; o.ldb = Wo.ld;
     o.M = R; o.N = d_o; o.K = df;
     o.c = y; o.ldc = d_o;
-    g.b_step = d_o * Wo.ld * e;
+    g = {offsets, plan->experts, R, d_o * Wo.ld * e, H.end, Wo.end, nullptr, 1};
     return rows_product(o, g, ffn::kStore, false, dt, ws + l.partial, nullptr, hip_stream);
 }
 
@@ -405,14 +428,14 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
     }
     char* ws = (char*)workspace;
     ffn::PackJobs jobs = {};
-    const Operand Gy = operand(grad_y, d_o, R, d_o, dt, ws + l.gy, &jobs), Wo = operand(w_out, df, E * d_o, df, dt, ws + l.w_out, &jobs);
-    Operand Wi = {};
-    if (grad_x) Wi = operand(w_in, di, E * 2 * df, di, dt, ws + l.w_in, &jobs);
+    const Matrix Gy = readable(grad_y, R, d_o, dt, ws + l.gy, &jobs), Wo = readable(w_out, E * d_o, df, dt, ws + l.w_out, &jobs);
+    Matrix Wi = {};
+    if (grad_x) Wi = readable(w_in, E * 2 * df, di, dt, ws + l.w_in, &jobs);
     rc = status(ffn::launch_pack(jobs, dt, hip_stream));
     if (rc == CGTP_OK && grad_w_in) rc = gather(plan, x, ldx, place, ws + l.x, N, per_row, hip_stream);
     if (rc != CGTP_OK) return rc;
-    const Operand H = {ws + l.h, up8(df)}, D = {ws + l.dgu, up8(2 * df)};
-    ffn::Groups g = {offsets, plan->experts, R, d_o * Wo.ld * e};
+    const Matrix H = matrix(ws + l.h, R, up8(df), df, e), D = matrix(ws + l.dgu, R, up8(2 * df), 2 * df, e), X = matrix(ws + l.x, R, up8(di), di, e);
+    ffn::Groups g = {offsets, plan->experts, R, d_o * Wo.ld * e, Gy.end, Wo.end, nullptr, 1};
     ffn::TileArgs t = {};
     t.a = Gy.p; t.lda = Gy.ld;
     t.b = Wo.p; t.ldb = Wo.ld;
@@ -427,7 +450,7 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
         d.a = D.p; d.lda = D.ld;
         d.b = Wi.p; d.ldb = Wi.ld;
         d.M = R; d.N = di; d.K = 2 * df;
-        g.b_step = 2 * df * Wi.ld * e;
+        g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, D.end, Wi.end, nullptr, 1};
         int32_t splits = 1;
         rc = rows_product(d, g, ffn::kPartial, true, dt, ws + l.partial, &splits, hip_stream);
         ffn::RouteArgs a = {};
@@ -438,9 +461,10 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
     if (rc == CGTP_OK && grad_w_in) {
         ffn::TileArgs w = {};
         w.a = D.p; w.lda = D.ld;
-        w.b = ws + l.x; w.ldb = up8(di);
+        w.b = X.p; w.ldb = X.ld;
         w.M = 2 * df; w.N = di;
         w.c = grad_w_in;
+        g = {offsets, plan->experts, R, 0, D.end, X.end, nullptr, 1};
         rc = sums_product(w, g, dt, ws + l.partial, hip_stream);
     }
     if (rc == CGTP_OK && grad_w_out) {
@@ -449,6 +473,7 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
         w.b = H.p; w.ldb = H.ld;
         w.M = d_o; w.N = df;
         w.c = grad_w_out;
+        g = {offsets, plan->experts, R, 0, Gy.end, H.end, nullptr, 1};
         rc = sums_product(w, g, dt, ws + l.partial, hip_stream);
     }
     return rc;

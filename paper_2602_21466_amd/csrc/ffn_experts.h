@@ -74,7 +74,9 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_rows_kernel(TileArgs p, G
     int tm, tn, split;
     place(blockIdx.x, total, p.tiles_n, p.splits, tm, tn, split);
     const Run r = find_tile(g, lane, BM, first, tm);
-    tile_body<T, BM, BM, WM, WN, false, BC, EPI>(p, Work{p.a, (const char*)p.b + r.expert * g.b_step, (int64_t)r.begin + (int64_t)r.tile * BM, r.end, p.K, 0, p.M, tn, split});
+    const Exact xa = {(const char*)g.a_end, g.source, (uint32_t)g.per_row, (uint32_t)g.rows}, xb = {(const char*)g.b_end, nullptr, 1, 0};
+    tile_body<T, BM, BM, WM, WN, false, BC, EPI, true>(p, Work{p.a, (const char*)p.b + r.expert * g.b_step, (int64_t)r.begin + (int64_t)r.tile * BM, r.end, p.K, 0, p.M,
+                                                              tn, split, xa, xb});
 }
 
 // Each expert's tiles go round the eight dies, as its rows may be many more than another's.
@@ -88,8 +90,9 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_sums_kernel(TileArgs p, G
     end = end < begin ? begin : end < R ? end : R;
     place(id, p.tiles_m, p.tiles_n, p.splits, tm, tn, split);
     constexpr int64_t ES = (int64_t)sizeof(T);
-    tile_body<T, BM, BM, WM, WN, true, true, EPI>(p, Work{(const char*)p.a + begin * p.lda * ES, (const char*)p.b + begin * p.ldb * ES, (int64_t)tm * BM, p.M, end - begin,
-                                                          (int64_t)e * p.M, g.experts * p.M, tn, split});
+    const Exact xa = {(const char*)g.a_end, nullptr, 1, 0}, xb = {(const char*)g.b_end, nullptr, 1, 0};
+    tile_body<T, BM, BM, WM, WN, true, true, EPI, true>(p, Work{(const char*)p.a + begin * p.lda * ES, (const char*)p.b + begin * p.ldb * ES, (int64_t)tm * BM, p.M, end - begin,
+                                                                (int64_t)e * p.M, g.experts * p.M, tn, split, xa, xb});
 }
 
 template <typename T, int BM, bool BC, int EPI> int run_rows(const TileArgs& p, const Groups& g, hipStream_t s) {

@@ -225,6 +225,7 @@ __global__ __launch_bounds__(kThreads) void combine_parts_kernel(RouteArgs p, in
             const uint32_t from = (uint32_t)place[j];
             if (from >= (uint64_t)p.slots) continue;
             f32x4 v = {};
+#pragma unroll 8
             for (int s = 0; s < splits; ++s) v += *(const f32x4*)((const float*)p.sorted + ((int64_t)s * p.slots + from) * ld + k.at * 4);
             sum += v;
         }

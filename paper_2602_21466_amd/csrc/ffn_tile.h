@@ -119,9 +119,19 @@ __device__ __forceinline__ f32x4 load4(const float* p, int64_t n, int64_t N) {
 
 constexpr uint32_t kOut = 0x80000000u;    // beyond every buffer: a direct load from there writes zeros
 
+// An operand that is read as it lies in memory: `end` is behind its last byte that may be read, and rows of a (COLS not)
+// are rows index[..] / per of it, slots of `slots`, where index is given.
+struct Exact {
+    const char* end;
+    const int32_t* index;
+    uint32_t per, slots;
+};
+
 // The direct loads of one operand: `R` rows of C's index a tile, a step of k, by NW waves, values of ES bytes.  GATE: in
-// blocks of GATE tile rows, half of the gate's rows, then the same half of the up projection's.
-template <int ES, int R, int NW, bool COLS, int GATE> struct Loader {
+// blocks of GATE tile rows, half of the gate's rows, then the same half of the up projection's.  EXACT: rows start on any
+// element and hold no zeros behind them (a direct load takes 16 bytes from any address that its values have, and zeros for
+// each four bytes that are not wholly inside the buffer's range).
+template <int ES, int R, int NW, bool COLS, int GATE, bool EXACT = false> struct Loader {
     static constexpr int kLoads = R * 128 / 1024 / NW, kPer = 16 / ES, kStep = 128 / ES;   // values a chunk, k a step
     static constexpr int kRows = R * ES <= 1024 ? 1024 / (R * ES) : 1, kChunks = 64 / kRows;   // columns: k rows a load, chunks of one
     __amdgpu_buffer_rsrc_t rsrc[GATE ? 2 : 1];
@@ -129,25 +139,33 @@ template <int ES, int R, int NW, bool COLS, int GATE> struct Loader {
     uint32_t voff[kLoads];
     uint32_t kpos;       // first k of this lane's chunk (rows) or k row of its first load (columns)
     int64_t step;
+    const char* end;     // EXACT
 
     static __device__ __forceinline__ int swizzle(int k) {
         if constexpr (ES == 4) return k >> 3;
         return (k & 3) | ((k >> 3) & 1) << 2;
     }
 
-    __device__ __forceinline__ void init(const void* p, int64_t ld, int64_t r0, int64_t rows, int64_t half, int wave, int lane) {
+    __device__ __forceinline__ void init(const void* p, int64_t ld, int64_t r0, int64_t rows, int64_t half, int wave, int lane, const Exact& x = {}) {
+        end = x.end;
         if constexpr (!COLS) {
             const int sub = lane >> 3, at = (lane & 7) ^ sub, c = ES == 4 ? (at & 3) * 2 + (at >> 2) : at;
             kpos = c * kPer;
             step = 128;
             base[0] = (const char*)p + r0 * ld * ES;
             if constexpr (GATE != 0) base[1] = base[0] + half * ld * ES;
+            const bool indexed = EXACT && x.index;
+            if (indexed) base[0] = (const char*)p;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int t = (i * NW + wave) * 8 + sub;
                 int64_t r = t;
                 if constexpr (GATE != 0) r = t / GATE * (GATE / 2) + t % (GATE / 2);
                 if (r0 + r >= rows) r = rows - 1 - r0;
+                if (indexed) {
+                    const uint32_t slot = (uint32_t)x.index[r0 + r];
+                    r = slot < x.slots ? slot / x.per : 0;
+                }
                 voff[i] = (uint32_t)(r * ld * ES + c * 16);
             }
         } else {
@@ -165,10 +183,15 @@ template <int ES, int R, int NW, bool COLS, int GATE> struct Loader {
         }
     }
 
+    __device__ __forceinline__ int range(const char* from) const {
+        if constexpr (!EXACT) return 0x7FFFFFFF;
+        const int64_t left = end - from;
+        return left < 0 ? 0 : left < 0x7FFFFFFF ? (int)left : 0x7FFFFFFF;
+    }
     __device__ __forceinline__ void seek(int64_t bytes) {
 #pragma unroll
         for (int g = 0; g < (GATE ? 2 : 1); ++g)
-            rsrc[g] = __builtin_amdgcn_make_buffer_rsrc((void*)(base[g] + bytes), 0, (int)0x7FFFFFFF, 0x00020000);
+            rsrc[g] = __builtin_amdgcn_make_buffer_rsrc((void*)(base[g] + bytes), 0, range(base[g] + bytes), 0x00020000);
     }
 
     // left: k from this step's first on, or more
@@ -253,9 +276,12 @@ struct Work {
     const void *a, *b;
     int64_t m0, m_end, K, out_row, out_rows;
     int tn, split;
+    Exact xa, xb;                         // EXACT
 };
 
-template <typename T, int BM, int BN, int WM, int WN, bool AC, bool BC, int EPI>
+// EXACT: operands as they lie in memory (see Loader).  Where rows end inside a chunk of 16 bytes, what follows them is set to
+// zero in the registers, on both sides, in the last step.
+template <typename T, int BM, int BN, int WM, int WN, bool AC, bool BC, int EPI, bool EXACT = false>
 __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w) {
 #ifdef __HIP_DEVICE_COMPILE__   // (the host's pass needs the launch stub alone)
     constexpr int NW = WM * WN, MT = BM / WM / 16, CW = BN / WN, NT = CW / 16, ES = (int)sizeof(T), kStep = 128 / ES;
@@ -266,14 +292,17 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w) {
     constexpr int kCols = EPI == kGate ? BN / 2 : BN;      // columns of C a tile covers
     const int64_t m0 = w.m0, n0 = (int64_t)w.tn * kCols;
 
-    Loader<ES, BM, NW, AC, 0> la;
-    Loader<ES, BN, NW, BC, EPI == kGate ? CW : 0> lb;
-    la.init(w.a, p.lda, m0, w.m_end, 0, wave, lane);
-    lb.init(w.b, p.ldb, n0, p.N, p.N, wave, lane);
+    Loader<ES, BM, NW, AC, 0, EXACT> la;
+    Loader<ES, BN, NW, BC, EPI == kGate ? CW : 0, EXACT> lb;
+    la.init(w.a, p.lda, m0, w.m_end, 0, wave, lane, w.xa);
+    lb.init(w.b, p.ldb, n0, p.N, p.N, wave, lane, w.xb);
 
     // this part's steps
     const int steps = (int)((w.K + kStep - 1) / kStep);
     const int s0 = (int)((int64_t)steps * w.split / p.splits), s1 = (int)((int64_t)steps * (w.split + 1) / p.splits), n = s1 - s0;
+    const int last = steps - 1 - s0;                       // of the product, counted from this part's first
+    const int rest = (int)(w.K - (int64_t)(steps - 1) * kStep);   // k in it
+    const int clean = EXACT && (!AC || !BC) && rest % (16 / ES) != 0 ? last : -1;
     int ks = s0;
     auto issue = [&](char* a, char* b) {
         la.seek(ks * la.step);
@@ -289,25 +318,38 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w) {
     if constexpr (ES == 4) {
         // One step out of (a, b) while the next goes to (an, bn).  The planes of A's fragment i + 1 are cut, and fragment
         // i + 2 is read, behind the 6 NT matrix instructions of fragment i.
-        auto step = [&](const char* a, const char* b, char* an, char* bn, bool more) {
+        auto step = [&](const char* a, const char* b, char* an, char* bn, int s, bool more) {
             if (more) issue(an, bn);
+            auto cut = [&](f32x4 (&v)[2]) {
+                if constexpr (EXACT)
+                    if (s == clean) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e >> 2][e & 3] = 8 * (lane >> 4) + e < rest ? v[e >> 2][e & 3] : 0.0f;
+                    }
+            };
             int oa = base_a, ob = base_b;   // (made anew at every step: kept over the loop their sums would not fit the registers)
             asm volatile("" : "+v"(oa), "+v"(ob));
             Planes fb[NT], fa[2];
             f32x4 raw[2][2];
             Fragments<4, BM, AC>::get32(a, oa, 0, raw[0]);
+            if constexpr (!AC) cut(raw[0]);
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 f32x4 v[2];
                 Fragments<4, BN, BC>::get32(b, ob, j, v);
+                if constexpr (!BC) cut(v);
                 fb[j] = planes_of(v);
             }
             fa[0] = planes_of(raw[0]);
             Fragments<4, BM, AC>::get32(a, oa, 1, raw[1]);
+            if constexpr (!AC) cut(raw[1]);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                if (i + 2 < MT) Fragments<4, BM, AC>::get32(a, oa, i + 2, raw[i & 1]);
+                if (i + 2 < MT) {
+                    Fragments<4, BM, AC>::get32(a, oa, i + 2, raw[i & 1]);
+                    if constexpr (!AC) cut(raw[i & 1]);
+                }
                 if (i + 1 < MT) fa[(i + 1) & 1] = planes_of(raw[(i + 1) & 1]);
                 // planes (0, 2), (2, 0), (1, 1), (0, 1), (1, 0), (0, 0): the smallest first
 #pragma unroll
@@ -328,19 +370,31 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w) {
         landed();
         int s = 0;
         for (; s + 1 < n; s += 2) {
-            step(sa0, sb0, sa1, sb1, true);
-            step(sa1, sb1, sa0, sb0, s + 2 < n);
+            step(sa0, sb0, sa1, sb1, s, true);
+            step(sa1, sb1, sa0, sb0, s + 1, s + 2 < n);
         }
-        if (s < n) step(sa0, sb0, sa1, sb1, false);
+        if (s < n) step(sa0, sb0, sa1, sb1, s, false);
     } else {
         s16x8 fa[2][MT], fb[2][NT];
-        auto read = [&](const char* a, const char* b, int kk) {
+        auto read = [&](const char* a, const char* b, int kk, int s) {
             int oa = base_a, ob = base_b;   // (as above)
             asm volatile("" : "+v"(oa), "+v"(ob));
 #pragma unroll
             for (int j = 0; j < NT; ++j) fb[kk][j] = Fragments<2, BN, BC>::get(b, ob, j, kk);
 #pragma unroll
             for (int i = 0; i < MT; ++i) fa[kk][i] = Fragments<2, BM, AC>::get(a, oa, i, kk);
+            if constexpr (EXACT && (!AC || !BC))
+                if (s == clean) {
+                    s16x8 keep;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) keep[e] = 32 * kk + 8 * (lane >> 4) + e < rest ? -1 : 0;
+                    if constexpr (!BC)
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) fb[kk][j] &= keep;
+                    if constexpr (!AC)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) fa[kk][i] &= keep;
+                }
         };
         auto multiply = [&](int kk) {
 #pragma unroll
@@ -356,16 +410,16 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w) {
                 __builtin_amdgcn_s_barrier();
                 __builtin_amdgcn_sched_barrier(0);
             };
-            auto phases = [&](char* a, char* b, char* an, char* bn, bool more) {
+            auto phases = [&](char* a, char* b, char* an, char* bn, int s, bool more) {
                 if (more) issue(an, bn);
-                read(a, b, 0);
+                read(a, b, 0, s);
                 __builtin_amdgcn_s_waitcnt(0xC07F);     // own LDS reads done
                 meet();
                 __builtin_amdgcn_s_setprio(1);
                 multiply(0);
                 __builtin_amdgcn_s_setprio(0);
                 meet();
-                read(a, b, 1);
+                read(a, b, 1, s);
                 __builtin_amdgcn_s_waitcnt(0x0070);     // own LDS reads done, own direct loads landed
                 meet();
                 __builtin_amdgcn_s_setprio(1);
@@ -378,33 +432,33 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w) {
             if (wave >= 4) meet();
             int s = 0;
             for (; s + 1 < n; s += 2) {
-                phases(sa0, sb0, sa1, sb1, true);
-                phases(sa1, sb1, sa0, sb0, s + 2 < n);
+                phases(sa0, sb0, sa1, sb1, s, true);
+                phases(sa1, sb1, sa0, sb0, s + 1, s + 2 < n);
             }
-            if (s < n) phases(sa0, sb0, sa1, sb1, false);
+            if (s < n) phases(sa0, sb0, sa1, sb1, s, false);
             if (wave < 4) meet();
         } else {
             // While the matrix instructions of one half of a step run, the fragments of the next half are read.  Between
             // the halves all waves meet: by then each has read the last of this step's buffer, which takes the step after
             // next from memory, and the next step's data, asked for a whole step earlier, is there.
-            auto step = [&](char* a, char* b, char* an, char* bn, bool more) {
-                read(a, b, 1);
+            auto step = [&](char* a, char* b, char* an, char* bn, int s, bool more) {
+                read(a, b, 1, s);
                 multiply(0);
                 landed();
                 if (more) issue(a, b);
-                read(an, bn, 0);
+                read(an, bn, 0, s + 1);
                 multiply(1);
             };
             if (n > 0) issue(sa0, sb0);
             if (n > 1) issue(sa1, sb1);
             landed();
-            read(sa0, sb0, 0);
+            read(sa0, sb0, 0, 0);
             int s = 0;
             for (; s + 1 < n; s += 2) {
-                step(sa0, sb0, sa1, sb1, s + 2 < n);
-                step(sa1, sb1, sa0, sb0, s + 3 < n);
+                step(sa0, sb0, sa1, sb1, s, s + 2 < n);
+                step(sa1, sb1, sa0, sb0, s + 1, s + 3 < n);
             }
-            if (s < n) step(sa0, sb0, sa1, sb1, false);
+            if (s < n) step(sa0, sb0, sa1, sb1, s, false);
         }
     }
 

@@ -170,9 +170,10 @@ def test_one_expert_takes_all_or_none(N, kind, dtype):
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("N", [1, 20, 150])
-def test_strided_rows_single_gradients_and_other_stream(N, dtype):
+@pytest.mark.parametrize("di,df,do", [(80, 64, 72), (77, 61, 35), (78, 66, 70)])
+def test_strided_rows_single_gradients_and_other_stream(N, di, df, do, dtype):
     torch, lib = _setup()
-    K, E, di, df, do = 2, 5, 80, 64, 72
+    K, E = 2, 5
     index, x, wi, wo, gy = _case(torch, N, K, E, di, df, do, dtype, "even")
     x, wi, wo, gy = (t.cuda() for t in (x, wi, wo, gy))
     routes = lib.Routes(torch.from_numpy(index).cuda(), E)
@@ -225,6 +226,69 @@ def test_rows_and_experts_do_not_mix(N):
         for e in range(4):
             for p, q in zip(g1[1:], g2[1:]):
                 assert q[e].isnan().any() if e == 2 else torch.equal(p[e], q[e])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("N", [9, 150, 700])
+@pytest.mark.parametrize("di,df,do", [(77, 61, 35), (66, 130, 6), (131, 257, 129)])
+def test_rows_that_end_inside_a_chunk_do_not_mix(N, di, df, do, dtype):
+    """What lies behind a row in memory, the next row, the next expert's or the array's end, adds nothing to it, though it
+    is infinite or NaN."""
+    torch, lib = _setup()
+    K, E = 2, 3
+    index, x, wi, wo, gy = (t.cuda() if torch.is_tensor(t) else t for t in _case(torch, N, K, E, di, df, do, dtype, "even"))
+    routes = lib.Routes(torch.from_numpy(index).cuda(), E)
+    plan = lib.ExpertsPlan(E, di, df, do, dtype=dtype)
+    y, saved = plan.forward(x, routes, wi, wo, save=True)
+    grads = plan.backward(x, routes, wi, wo, saved, gy)
+    a, b = routes.offsets[1:3].tolist()
+    for bad in (float("nan"), float("inf")):
+        # a row of the second expert's weights: its column of G (or U) alone, of the expert's rows alone
+        for row in (1, df, 2 * df - 1):
+            w = wi.clone()
+            w[1, row] = bad
+            got = plan.forward(x, routes, w, wo, save=True)[1]
+            hit = torch.zeros(saved.shape, dtype=torch.bool, device="cuda")
+            hit[a:b, row] = True
+            assert not got[hit].isfinite().any() and torch.equal(got[~hit], saved[~hit])
+        for row in (0, do - 1):
+            w = wo.clone()
+            w[1, row] = bad
+            got = plan.forward(x, routes, wi, w)
+            hit = torch.zeros(y.shape, dtype=torch.bool, device="cuda")
+            hit[a:b, row] = True
+            assert not got[hit].isfinite().any() and torch.equal(got[~hit], y[~hit])
+        # a row of grad_y: its own row's gradients
+        g = gy.clone()
+        g[a] = bad
+        token = int(routes.source[a]) // K
+        gx = plan.backward(x, routes, wi, wo, saved, g, True, False, False)[0]
+        keep = [n for n in range(N) if n != token]
+        assert not gx[token].isfinite().any() and torch.equal(gx[keep], grads[0][keep])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_weights_that_end_with_a_page(dtype):
+    """Odd rows, in arrays whose last byte is the last of a page of memory, and in others: the same bits."""
+    torch, lib = _setup()
+    E, di, df, do, N = 2, 3, 512, 512, 40
+    index, x, wi, wo, gy = _case(torch, N, 1, E, di, df, do, dtype, "even")
+    plan = lib.ExpertsPlan(E, di, df, do, dtype=dtype)
+    routes = lib.Routes(torch.from_numpy(index).cuda(), E)
+    outs = []
+    for shift in (0, 256):
+        def at_page(t):
+            raw = torch.zeros(t.numel() * t.element_size() + 16384, dtype=torch.uint8, device="cuda")
+            end = (raw.data_ptr() + t.numel() * t.element_size() + 4095) // 4096 * 4096 + 4096 - shift
+            first = end - t.numel() * t.element_size() - raw.data_ptr()
+            out = raw[first:first + t.numel() * t.element_size()].view(t.dtype).view(t.shape)
+            out.copy_(t)
+            return out
+        a = [at_page(t.cuda()) for t in (x, wi, wo, gy)]
+        assert all((t.data_ptr() + t.numel() * t.element_size()) % 4096 == (-shift) % 4096 for t in a)
+        y, saved = plan.forward(a[0], routes, a[1], a[2], save=True)
+        outs.append((y, saved) + plan.backward(a[0], routes, a[1], a[2], saved, a[3]))
+    assert all(torch.equal(p, q) for p, q in zip(*outs))
 
 
 def test_one_expert_is_the_single_block():
