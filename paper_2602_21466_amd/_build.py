@@ -14,7 +14,8 @@ SOURCES = [os.path.join(HERE, "csrc", f) for f in
             "ffn_tile_bf16.hip", "ffn_tile_fp16.hip", "ffn_tile_fp32.hip", "ffn_few_bf16.hip", "ffn_few_fp16.hip", "ffn_few_fp32.hip", "ffn_few_grad.hip",
             "ffn_norm_bf16.hip", "ffn_norm_fp16.hip", "ffn_norm_fp32.hip",
             "ffn_layer.cpp", "ffn_layer_bf16.hip", "ffn_layer_fp16.hip", "ffn_layer_fp32.hip",
-            "experts_plan.cpp", "ffn_route.hip", "ffn_experts_bf16.hip", "ffn_experts_fp16.hip", "ffn_experts_fp32.hip")]
+            "experts_plan.cpp", "ffn_route.hip", "ffn_experts_bf16.hip", "ffn_experts_fp16.hip", "ffn_experts_fp32.hip",
+            "ffn_experts_few_bf16.hip", "ffn_experts_few_fp16.hip", "ffn_experts_few_fp32.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # Packed FP32 instructions are switched off for all device code.

@@ -73,6 +73,7 @@ struct Groups {
     int64_t rows;                         // sorted rows there may be
     int64_t b_step;                       // bytes from one expert's B to the next's
     const void *a_end, *b_end;            // behind the last bytes that may be read of either operand
+    int32_t chunk;                        // sums: rows of a part; 0: an expert's rows are one part
     const int32_t* source;                // rows of A are those of slots source[..] / per_row; NULL: they are in their order
     int32_t per_row;
 };
@@ -82,10 +83,18 @@ struct Groups {
 int launch_expert_rows_bf16(const TileArgs& t, const Groups& g, int32_t epilogue, bool b_cols, int32_t tile, void* stream);
 int launch_expert_rows_fp16(const TileArgs& t, const Groups& g, int32_t epilogue, bool b_cols, int32_t tile, void* stream);
 int launch_expert_rows_fp32(const TileArgs& t, const Groups& g, int32_t epilogue, bool b_cols, int32_t tile, void* stream);
-// C_e = A_e^T B_e, the sum over the rows of expert e, for every expert: C [experts, t.M, t.N], kStore or kPartial.
-int launch_expert_sums_bf16(const TileArgs& t, const Groups& g, int32_t epilogue, int32_t tile, void* stream);
-int launch_expert_sums_fp16(const TileArgs& t, const Groups& g, int32_t epilogue, int32_t tile, void* stream);
-int launch_expert_sums_fp32(const TileArgs& t, const Groups& g, int32_t epilogue, int32_t tile, void* stream);
+// The forward products for few rows an expert, as launch_few_* for a single block: x's rows by g.source, results in the
+// sorted order; tiles of `rows` rows (16, 32 or 64), `most` of them at the most.
+int launch_expert_few_bf16(const FewArgs& p, const Groups& g, int32_t epilogue, int32_t rows, int32_t nr, int32_t waves, int64_t most, void* stream);
+int launch_expert_few_fp16(const FewArgs& p, const Groups& g, int32_t epilogue, int32_t rows, int32_t nr, int32_t waves, int64_t most, void* stream);
+int launch_expert_few_fp32(const FewArgs& p, const Groups& g, int32_t epilogue, int32_t rows, int32_t nr, int32_t waves, int64_t most, void* stream);
+// C_e = A_e^T B_e, the sum over the rows of expert e, for every expert: C [experts, t.M, t.N].  An expert of more than
+// g.chunk rows has as many parts; theirs go to `partial`, floats [parts, t.M, t.N up to a multiple of four], for
+// launch_join_sums.  t.splits: parts there may be.
+int launch_expert_sums_bf16(const TileArgs& t, const Groups& g, float* partial, int32_t tile, void* stream);
+int launch_expert_sums_fp16(const TileArgs& t, const Groups& g, float* partial, int32_t tile, void* stream);
+int launch_expert_sums_fp32(const TileArgs& t, const Groups& g, float* partial, int32_t tile, void* stream);
+int launch_join_sums(const TileArgs& t, const Groups& g, const float* partial, int32_t dtype, void* stream);
 
 // launch_join and launch_join_gate for as many of the rows as *limit says (NULL: all).
 int launch_join_rows(const float* partial, int64_t ld, int32_t splits, int64_t M, int64_t N, void* out, int32_t dtype,

@@ -79,12 +79,37 @@ Cut cut_rows(const Shape& s, int32_t dtype, int32_t epilogue) {
     return c;
 }
 
-// [experts, M, N], sums over each expert's rows (R / experts of them by the mean).
-Cut cut_sums(int64_t M, const Shape& s, int32_t dtype) {
+// [experts, M, N], sums over each expert's rows.  chunk: rows of a part, 0 where an expert's are one part.  Counted like
+// shortest(): all work-groups' steps over those that run at one time, then half of the longest one alone; a few experts may
+// have three times the mean.
+struct Sums { int32_t tile, chunk; };
+Sums cut_sums(int64_t M, const Shape& s, int32_t dtype) {
     const bool wide = dtype == FFN_FP32;
-    auto groups = [&](int32_t tile) { return (double)(s.E * tiles(M, tile) * tiles(s.N, tile)); };
-    return shortest(groups, tiles(tiles(s.R, s.E), wide ? 32 : 64), (double)(s.E * M) * s.N, wide, false);
+    const double k = wide ? 32.0 : 64.0, ends = wide ? 2.0 : 4.0, mean = (double)s.R / s.E;
+    Sums best = {256, 0};
+    double least = 1e300;
+    for (int32_t tile : {256, 128}) {
+        const double each = (double)(tiles(M, tile) * tiles(s.N, tile)), slots = tile == 256 ? 256.0 : 512.0;
+        const double step = tile == 256 ? (wide ? 4.5 : 1.6) : (wide ? 2.6 : 1.06);
+        auto time = [&](double parts, double rows) {
+            const double all = each * ((double)s.R / k + parts * ends) / slots, one = rows / k + ends;
+            return step * (each * parts <= slots ? (one > all ? one : all) : all + 0.5 * one);
+        };
+        const double longest = 3.0 * mean < (double)s.R ? 3.0 * mean : (double)s.R;
+        const double t = time((double)s.E, longest);
+        if (t < least) { least = t; best = {tile, 0}; }
+        for (int64_t chunk = tiles(s.R, 64) * 64; chunk >= 4 * (int64_t)k; chunk = (chunk / 2 + 63) & ~63LL) {
+            if ((double)chunk >= longest) continue;
+            const double parts = (double)s.R / chunk + 0.5 * s.E;
+            const double tc = time(parts, (double)chunk) + 4.0 + parts * (double)(M * s.N) * 8.0 / 4e6;
+            if (tc < least) { least = tc; best = {tile, (int32_t)chunk}; }
+            if (chunk <= 64) break;
+        }
+    }
+    return best;
 }
+// Parts there may be.
+int64_t most_parts(const Shape& s, const Sums& c) { return s.E + (c.chunk ? s.R / c.chunk : 0); }
 
 int64_t up4(int64_t n) { return (n + 3) & ~3LL; }
 int64_t rows_partial(const Shape& s, int32_t dtype, int32_t epilogue) {
@@ -92,8 +117,8 @@ int64_t rows_partial(const Shape& s, int32_t dtype, int32_t epilogue) {
     return c.joined ? aligned(c.splits * s.R * up4(s.N) * 4) : 0;
 }
 int64_t sums_partial(int64_t M, const Shape& s, int32_t dtype) {
-    const Cut c = cut_sums(M, s, dtype);
-    return c.joined ? aligned(c.splits * s.E * M * up4(s.N) * 4) : 0;
+    const Sums c = cut_sums(M, s, dtype);
+    return c.chunk ? aligned(most_parts(s, c) * M * up4(s.N) * 4) : 0;
 }
 
 constexpr int64_t kMostGroups = 0x7FFFFFFF / 512;
@@ -102,8 +127,8 @@ bool rows_fit(const Shape& s, int32_t dtype, int32_t epilogue) {
     return most_tiles(s, c.tile) * tiles(s.N, c.tile) * c.splits <= kMostGroups;
 }
 bool sums_fit(int64_t M, const Shape& s, int32_t dtype) {
-    const Cut c = cut_sums(M, s, dtype);
-    return (tiles(M, c.tile) * tiles(s.N, c.tile) * c.splits + 8) * s.E <= kMostGroups;
+    const Sums c = cut_sums(M, s, dtype);
+    return (tiles(M, c.tile) * tiles(s.N, c.tile) + 8) * most_parts(s, c) <= kMostGroups;
 }
 
 int launch_rows(const ffn::TileArgs& t, const ffn::Groups& g, int32_t epilogue, bool bc, int32_t dtype, int32_t tile, void* stream) {
@@ -113,11 +138,11 @@ int launch_rows(const ffn::TileArgs& t, const ffn::Groups& g, int32_t epilogue, 
         default: return ffn::launch_expert_rows_fp16(t, g, epilogue, bc, tile, stream);
     }
 }
-int launch_sums(const ffn::TileArgs& t, const ffn::Groups& g, int32_t epilogue, int32_t dtype, int32_t tile, void* stream) {
+int launch_sums(const ffn::TileArgs& t, const ffn::Groups& g, float* partial, int32_t dtype, int32_t tile, void* stream) {
     switch (dtype) {
-        case FFN_FP32: return ffn::launch_expert_sums_fp32(t, g, epilogue, tile, stream);
-        case FFN_BF16: return ffn::launch_expert_sums_bf16(t, g, epilogue, tile, stream);
-        default: return ffn::launch_expert_sums_fp16(t, g, epilogue, tile, stream);
+        case FFN_FP32: return ffn::launch_expert_sums_fp32(t, g, partial, tile, stream);
+        case FFN_BF16: return ffn::launch_expert_sums_bf16(t, g, partial, tile, stream);
+        default: return ffn::launch_expert_sums_fp16(t, g, partial, tile, stream);
     }
 }
 
@@ -145,19 +170,53 @@ int rows_product(ffn::TileArgs t, const ffn::Groups& g, int32_t epilogue, bool b
 }
 
 // The sums over each expert's rows: t.M x t.N results an expert, contiguous.
-int sums_product(ffn::TileArgs t, const ffn::Groups& g, int32_t dtype, void* partial, void* stream) {
-    const Cut c = cut_sums(t.M, {g.rows, g.experts, t.N, 0}, dtype);
+int sums_product(ffn::TileArgs t, ffn::Groups g, int32_t dtype, void* partial, void* stream) {
+    const Shape s = {g.rows, g.experts, t.N, 0};
+    const Sums c = cut_sums(t.M, s, dtype);
     t.tiles_m = (int32_t)tiles(t.M, c.tile);
     t.tiles_n = (int32_t)tiles(t.N, c.tile);
-    t.splits = c.splits;
+    t.splits = (int32_t)most_parts(s, c);
     t.ldc = t.N;
-    if (!c.joined) return status(launch_sums(t, g, ffn::kStore, dtype, c.tile, stream));
-    ffn::TileArgs p = t;
-    p.c = partial;
-    p.ldc = up4(t.N);
-    const int rc = status(launch_sums(p, g, ffn::kPartial, dtype, c.tile, stream));
-    if (rc != CGTP_OK) return rc;
-    return status(ffn::launch_join((const float*)partial, p.ldc, c.splits, g.experts * t.M, t.N, t.c, dtype, stream));
+    g.chunk = c.chunk;
+    const int rc = status(launch_sums(t, g, (float*)partial, dtype, c.tile, stream));
+    if (rc != CGTP_OK || c.chunk == 0) return rc;
+    return status(ffn::launch_join_sums(t, g, (const float*)partial, dtype, stream));
+}
+
+// The forward products for few rows an expert, where reading the weights is the time: tiles of 16, 32 or 64 rows, so that
+// most experts have one; weight rows a work-group and waves as for a single block (ffn_plan.cpp), the work-groups being
+// those of all experts with a row.
+struct Few { int32_t rows, nr, waves; };
+Few few_cut(const Shape& s, bool gate, int32_t dtype) {
+    const int64_t with = s.E < s.R ? s.E : s.R, mean = tiles(s.R, with), all = with * s.N;
+    Few c;
+    // 64 rows, two of 16 experts each, 2048 x 4096: bf16 168 us by tiles of 32 rows and 198 of 16; fp32 332 by 16, 399 by 32
+    c.rows = mean <= (dtype == FFN_FP32 ? 10 : 6) ? 16 : mean <= 24 ? 32 : 64;
+    c.nr = (c.rows == 16 && dtype != FFN_FP32) || all < 16 * 192 ? 8 : gate && c.rows > 16 && all >= 32 * 512 ? 32 : 16;
+    const int32_t per = (c.nr > 16 ? 2 : 1) * (gate ? 2 : 1) * (c.rows / 16);
+    const int64_t blocks = tiles(s.K, dtype == FFN_FP32 ? 64 : 128), groups = tiles(all, c.nr);
+    c.waves = 8;
+    while (c.waves > 1 && (c.waves * per > 64 || c.waves > 2 * blocks || (c.waves * 4 > blocks && groups * c.waves > 4096))) c.waves /= 2;
+    return c;
+}
+// Whether these kernels are the faster ones: against tiles, 16 experts of 2048 x 4096 in bf16 take 28 us for one row (47), 168
+// for 8 rows an expert (190), 198 for 16 (196); in fp32 473 for 16 (618) and 728 for 32 (617); small weights, which are read
+// from the caches, 19.6 for 32 rows an expert (27.5; 8 experts, 512 x 1024, bf16).
+bool few_rows(int64_t R, const ffn_experts_s* p) {
+    const int64_t with = p->experts < R ? p->experts : R, mean = tiles(R, with);
+    const int64_t bytes = with * p->d_ff * (2 * p->d_in + p->d_out) * size_of(p->dtype);
+    return mean <= (bytes <= (1 << 25) ? 40 : p->dtype == FFN_FP32 ? 24 : 16);
+}
+int few_product(ffn::FewArgs p, const ffn::Groups& g, int32_t epilogue, int32_t dtype, void* stream) {
+    const bool gate = epilogue == ffn::kGate;
+    const Shape s = {g.rows, g.experts, p.N, p.K};
+    const Few c = few_cut(s, gate, dtype);
+    const int64_t most = most_tiles(s, c.rows);
+    switch (dtype) {
+        case FFN_FP32: return status(ffn::launch_expert_few_fp32(p, g, epilogue, c.rows, c.nr, c.waves, most, stream));
+        case FFN_BF16: return status(ffn::launch_expert_few_bf16(p, g, epilogue, c.rows, c.nr, c.waves, most, stream));
+        default: return status(ffn::launch_expert_few_fp16(p, g, epilogue, c.rows, c.nr, c.waves, most, stream));
+    }
 }
 
 // A matrix as a product reads it: where it is, and behind its last byte that may be read.
@@ -366,6 +425,19 @@ int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const in
     rc = current_device_is(plan->device);
     if (rc != CGTP_OK) return rc;
     char* ws = (char*)workspace;
+    if (few_rows(R, plan)) {
+        ffn::FewArgs f = {};
+        f.x = x; f.ldx = ldx; f.w = w_in; f.ldw = di;
+        f.N = df; f.K = di;
+        f.c = ws + l.h; f.ldc = up8(df);
+        f.saved = (float*)saved; f.act = plan->act;
+        rc = few_product(f, {offsets, plan->experts, R, 2 * df * di * e, nullptr, nullptr, 0, source, per_row}, ffn::kGate, dt, hip_stream);
+        if (rc != CGTP_OK) return rc;
+        f.x = ws + l.h; f.ldx = up8(df); f.w = w_out; f.ldw = df;
+        f.N = d_o; f.K = df;
+        f.c = y; f.ldc = d_o; f.saved = nullptr;
+        return few_product(f, {offsets, plan->experts, R, d_o * df * e, nullptr, nullptr, 0, nullptr, 1}, ffn::kStore, dt, hip_stream);
+    }
     ffn::PackJobs jobs = {};
     const Matrix Wi = readable(w_in, E * 2 * df, di, dt, ws + l.w_in, &jobs), Wo = readable(w_out, E * d_o, df, dt, ws + l.w_out, &jobs);
     rc = status(ffn::launch_pack(jobs, dt, hip_stream));
@@ -380,7 +452,7 @@ int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const in
     t.M = R; t.N = df; t.K = di;
     t.c = ws + l.h; t.ldc = H.ld;
     t.act = plan->act; t.saved = (float*)saved;
-    ffn::Groups g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, X.end, Wi.end, there ? source : nullptr, per_row};
+    ffn::Groups g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, X.end, Wi.end, 0, there ? source : nullptr, per_row};
     rc = rows_product(t, g, ffn::kGate, false, dt, ws + l.partial, nullptr, hip_stream);
     if (rc != CGTP_OK) return rc;
     ffn::TileArgs o = {};
@@ -388,7 +460,7 @@ int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const in
     o.b = Wo.p; o.ldb = Wo.ld;
     o.M = R; o.N = d_o; o.K = df;
     o.c = y; o.ldc = d_o;
-    g = {offsets, plan->experts, R, d_o * Wo.ld * e, H.end, Wo.end, nullptr, 1};
+    g = {offsets, plan->experts, R, d_o * Wo.ld * e, H.end, Wo.end, 0, nullptr, 1};
     return rows_product(o, g, ffn::kStore, false, dt, ws + l.partial, nullptr, hip_stream);
 }
 
@@ -435,7 +507,7 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
     if (rc == CGTP_OK && grad_w_in) rc = gather(plan, x, ldx, place, ws + l.x, N, per_row, hip_stream);
     if (rc != CGTP_OK) return rc;
     const Matrix H = matrix(ws + l.h, R, up8(df), df, e), D = matrix(ws + l.dgu, R, up8(2 * df), 2 * df, e), X = matrix(ws + l.x, R, up8(di), di, e);
-    ffn::Groups g = {offsets, plan->experts, R, d_o * Wo.ld * e, Gy.end, Wo.end, nullptr, 1};
+    ffn::Groups g = {offsets, plan->experts, R, d_o * Wo.ld * e, Gy.end, Wo.end, 0, nullptr, 1};
     ffn::TileArgs t = {};
     t.a = Gy.p; t.lda = Gy.ld;
     t.b = Wo.p; t.ldb = Wo.ld;
@@ -450,7 +522,7 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
         d.a = D.p; d.lda = D.ld;
         d.b = Wi.p; d.ldb = Wi.ld;
         d.M = R; d.N = di; d.K = 2 * df;
-        g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, D.end, Wi.end, nullptr, 1};
+        g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, D.end, Wi.end, 0, nullptr, 1};
         int32_t splits = 1;
         rc = rows_product(d, g, ffn::kPartial, true, dt, ws + l.partial, &splits, hip_stream);
         ffn::RouteArgs a = {};
@@ -464,7 +536,7 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
         w.b = X.p; w.ldb = X.ld;
         w.M = 2 * df; w.N = di;
         w.c = grad_w_in;
-        g = {offsets, plan->experts, R, 0, D.end, X.end, nullptr, 1};
+        g = {offsets, plan->experts, R, 0, D.end, X.end, 0, nullptr, 1};
         rc = sums_product(w, g, dt, ws + l.partial, hip_stream);
     }
     if (rc == CGTP_OK && grad_w_out) {
@@ -473,7 +545,7 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
         w.b = H.p; w.ldb = H.ld;
         w.M = d_o; w.N = df;
         w.c = grad_w_out;
-        g = {offsets, plan->experts, R, 0, Gy.end, H.end, nullptr, 1};
+        g = {offsets, plan->experts, R, 0, Gy.end, H.end, 0, nullptr, 1};
         rc = sums_product(w, g, dt, ws + l.partial, hip_stream);
     }
     return rc;

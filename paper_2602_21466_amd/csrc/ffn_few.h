@@ -30,9 +30,18 @@ __device__ __forceinline__ f32x4 few_mfma(Few<float>::V a, Few<float>::V b, f32x
     return c;
 }
 
+// What one work-group multiplies: weight rows n0 .. of w, M rows from row0 on of x and of the results; where index is given,
+// x's rows are index[..] / per, slots of `slots`.
+struct FewWork {
+    const void* w;
+    int64_t M, n0, row0;
+    const int32_t* index;
+    uint32_t per, slots;
+};
+
 // MT: tiles of 16 rows of x.  EPI: kGate or kStore.
 template <typename T, int MT, int NR, int EPI>
-__global__ __launch_bounds__(512) void few_kernel(FewArgs p) {
+__device__ __forceinline__ void few_body(const FewArgs& p, const FewWork& work) {
 #ifdef __HIP_DEVICE_COMPILE__
     typedef typename Few<T>::V V;
     constexpr int kPer = Few<T>::kPer, kChunk = Few<T>::kChunk, HB = NR == 8 ? 2 : 1, kStep = HB * kChunk;
@@ -40,7 +49,7 @@ __global__ __launch_bounds__(512) void few_kernel(FewArgs p) {
     constexpr int kBlock = U * kStep;
     extern __shared__ f32x4 few_sums[];                  // [waves][tiles][64]
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-    const int64_t n0 = (int64_t)blockIdx.x * NR;
+    const int64_t n0 = work.n0;
     const int K = (int)p.K, q = (lane >> 4) * kPer, qw = q + (HB == 2 ? (lane >> 3 & 1) * kChunk : 0);
 
     const T *w[F], *x[MT];
@@ -48,12 +57,17 @@ __global__ __launch_bounds__(512) void few_kernel(FewArgs p) {
     for (int f = 0; f < F; ++f) {
         int64_t n = n0 + (f % RT) * kRows + (lane & (kRows - 1));
         if (n >= p.N) n = p.N - 1;
-        w[f] = (const T*)p.w + (n + (f / RT) * p.N) * p.ldw;
+        w[f] = (const T*)work.w + (n + (f / RT) * p.N) * p.ldw;
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         int64_t r = m * 16 + (lane & 15);
-        if (r >= p.M) r = p.M - 1;
+        if (r >= work.M) r = work.M - 1;
+        r += work.row0;
+        if (work.index) {
+            const uint32_t slot = (uint32_t)work.index[r];
+            r = slot < work.slots ? slot / work.per : 0;
+        }
         x[m] = (const T*)p.x + r * p.ldx;
     }
 
@@ -148,8 +162,8 @@ __global__ __launch_bounds__(512) void few_kernel(FewArgs p) {
     constexpr int kLanes = 64 / HB;
     for (int i = threadIdx.x; i < RT * MT * kLanes; i += blockDim.x) {
         const int l = i % kLanes, tile = i / kLanes, rt = tile / MT, mt = tile % MT;
-        const int64_t r = mt * 16 + (l & 15), n = n0 + rt * kRows + (l >> 4) * 4;
-        if (r >= p.M || n >= p.N) continue;
+        const int64_t at = mt * 16 + (l & 15), r = work.row0 + at, n = n0 + rt * kRows + (l >> 4) * 4;
+        if (at >= work.M || n >= p.N) continue;
         f32x4 v = {}, u = {};
         for (int s = 0; s < waves; ++s) {
             const f32x4* t = few_sums + (s * F * MT + tile) * 64 + l;
@@ -177,6 +191,11 @@ __global__ __launch_bounds__(512) void few_kernel(FewArgs p) {
         }
     }
 #endif
+}
+
+template <typename T, int MT, int NR, int EPI>
+__global__ __launch_bounds__(512) void few_kernel(FewArgs p) {
+    few_body<T, MT, NR, EPI>(p, FewWork{p.w, p.M, (int64_t)blockIdx.x * NR, 0, nullptr, 1, 0});
 }
 
 template <typename T, int MT, int EPI> int run_few(const FewArgs& p, int nr, int waves, hipStream_t s) {

@@ -1,5 +1,5 @@
 // Packing of operands for the tiled products, and the joining of their split sums.
-#include "experts_internal.h"
+#include "experts_device.h"
 #include "ffn_tile.h"
 
 namespace ffn {
@@ -103,6 +103,33 @@ __global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const f
     }
 }
 
+// The parts of the experts that have more than one, added in order.
+template <typename Out>
+__global__ __launch_bounds__(kThreads) void join_sums_kernel(TileArgs p, Groups g, const float* partial) {
+    const int e = blockIdx.y, lane = threadIdx.x & 63;
+    int first = 0, parts = 0;
+    for (int e0 = 0; e0 <= e; e0 += 64) {
+        Scan s;
+        s.read(g, e0, lane, g.chunk, 1);
+        const int rows = s.end - s.begin;
+        if (e - e0 >= 64) {
+            first += s.total();
+            continue;
+        }
+        parts = Scan::tiles_of(__builtin_amdgcn_readlane(rows, e - e0), g.chunk, 1);
+        first += __builtin_amdgcn_readlane(s.upto, e - e0) - parts;
+    }
+    if (parts == 1) return;
+    const int64_t ld = (p.N + 3) & ~3LL, quads = ld >> 2, total = p.M * quads, part = p.M * ld;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t row = i / quads, c = (i - row * quads) * 4;
+        f32x4 v = {};
+#pragma unroll 8
+        for (int s = 0; s < parts; ++s) v += *(const f32x4*)(partial + (first + s) * part + row * ld + c);
+        store4<Out>((Out*)p.c + (e * p.M + row) * p.N, c, p.N, 0, v);
+    }
+}
+
 // (a kernel, not a memset: it may be captured in a graph)
 __global__ __launch_bounds__(kThreads) void zero_kernel(uint16_t* p, int64_t n) {
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) p[i] = 0;
@@ -142,6 +169,16 @@ int launch_join_gate_rows(const TileArgs& p, int32_t epilogue, const float* part
     else if (dtype == FFN_BF16) { FFN_JOIN(bf16); }
     else { FFN_JOIN(fp16); }
 #undef FFN_JOIN
+    return (int)hipGetLastError();
+}
+
+int launch_join_sums(const TileArgs& t, const Groups& g, const float* partial, int32_t dtype, void* stream) {
+    hipStream_t s = (hipStream_t)stream;
+    const unsigned all = groups(t.M * ((t.N + 3) >> 2));
+    const dim3 grid(all < 1024 ? all : 1024, (unsigned)g.experts);
+    if (dtype == FFN_FP32) join_sums_kernel<float><<<grid, kThreads, 0, s>>>(t, g, partial);
+    else if (dtype == FFN_BF16) join_sums_kernel<bf16><<<grid, kThreads, 0, s>>>(t, g, partial);
+    else join_sums_kernel<fp16><<<grid, kThreads, 0, s>>>(t, g, partial);
     return (int)hipGetLastError();
 }
 

@@ -15,6 +15,7 @@ enum Epilogue : int32_t {
     kGate = 1,       // B holds the gate's N rows, then the up projection's: H = act(G) * U; G, U kept in `saved`
     kGateGrad = 2,   // the sum is dH: dG, dU into C [M, 2 N], H into `h`
     kPartial = 3,    // 32-bit partial sums of one split of k
+    kEither = 4,     // C, or the 32-bit sums of a part of an expert's rows
 };
 
 // Operands and results of one launch.  Strides in elements; operands start on 16 bytes, with strides that are

@@ -277,6 +277,7 @@ struct Work {
     int64_t m0, m_end, K, out_row, out_rows;
     int tn, split;
     Exact xa, xb;                         // EXACT
+    float* part;                          // kEither: where the sums go, in rows of N up to a multiple of four; NULL: C
 };
 
 // EXACT: operands as they lie in memory (see Loader).  Where rows end inside a chunk of 16 bytes, what follows them is set to
@@ -519,6 +520,9 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w) {
                 }
             } else if constexpr (EPI == kStore) {
                 store4<T>((T*)p.c + (w.out_row + m) * p.ldc, n, p.N, 0, v);
+            } else if constexpr (EPI == kEither) {
+                if (w.part) store4<float>(w.part + m * ((p.N + 3) & ~3LL), n, p.N, 0, v);
+                else store4<T>((T*)p.c + (w.out_row + m) * p.ldc, n, p.N, 0, v);
             } else if constexpr (EPI == kPartial) {
                 store4<float>((float*)p.c + ((int64_t)w.split * w.out_rows + w.out_row + m) * p.ldc, n, p.N, 0, v);
             } else {
