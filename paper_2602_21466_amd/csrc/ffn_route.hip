@@ -127,7 +127,8 @@ __global__ __launch_bounds__(kSort) void sort_place_kernel(SortArgs a) {
 
 // ---------------------------------------------------------------- rows
 //
-// A thread takes chunks of eight values of a row: every row is read once and written to, or gathered from, its places.
+// TPR threads take a row, two chunks of eight values a thread and turn: x's rows (grad_y's) are read once for all of their
+// choices, and the loads of two chunks of four choices are in flight together.
 
 template <typename T> struct Chunk { typedef T V __attribute__((ext_vector_type(8))); };
 template <typename T> __device__ __forceinline__ typename Chunk<T>::V load_chunk(const T* row, int64_t c, int64_t D) {
@@ -150,11 +151,21 @@ template <typename T> __device__ __forceinline__ void store_chunk(T* row, int64_
     }
 }
 
+// A result: past the caches where all of them are more than these hold, as what stays there is written to memory during
+// the next kernel (16384 x 4096 in bf16, two choices a row, gather and combine after each other and their gradients: 346 us;
+// 366 with all kept, 366 with gather's alone kept; rows of 4001 x 1089 in fp32 85 and 93).
+template <typename T> __device__ __forceinline__ void put_chunk(T* row, int64_t c, int64_t D, typename Chunk<T>::V v, bool past) {
+    typedef typename Chunk<T>::V U __attribute__((aligned(sizeof(T))));
+    if (past && c + 8 <= D) __builtin_nontemporal_store(v, (U*)(row + c));
+    else store_chunk(row, c, D, v);
+}
+template <typename T> __device__ __forceinline__ bool large(const RouteArgs& p) { return p.slots * p.width * (int64_t)sizeof(T) >= 16 << 20; }
+
 // Walks the chunks of `rows` rows, one a thread and turn, without a division a turn.
 struct Chunks {
     int64_t row, at, rows, chunks, dr, da;
-    __device__ Chunks(int64_t rows_, int64_t chunks_) : rows(rows_), chunks(chunks_) {
-        const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, stride = (int64_t)gridDim.x * blockDim.x;
+    __device__ Chunks(int64_t rows_, int64_t chunks_, int64_t block, int64_t blocks) : rows(rows_), chunks(chunks_) {
+        const int64_t i = block * blockDim.x + threadIdx.x, stride = blocks * blockDim.x;
         row = i / chunks;
         at = i - row * chunks;
         dr = stride / chunks;
@@ -168,49 +179,85 @@ struct Chunks {
     }
 };
 
-// Sorted rows from offsets[experts] on.
-__device__ __forceinline__ int64_t held_rows(const RouteArgs& p) {
-    const int64_t n = p.offsets[p.experts];
-    return n < 0 ? 0 : n < p.slots ? n : p.slots;
-}
+// Zeros in the sorted rows from offsets[experts] on, by the work-groups behind those of the rows.
+constexpr unsigned kZeroGroups = 64;
 template <typename T> __device__ __forceinline__ void zero_behind(const RouteArgs& p) {
-    if (!p.offsets) return;
-    const int64_t held = held_rows(p);
+    int64_t held = p.offsets[p.experts];
+    held = held < 0 ? 0 : held < p.slots ? held : p.slots;
     const typename Chunk<T>::V zero = {};
-    for (Chunks k(p.slots - held, (p.ld_sorted + 7) >> 3); k.more(); k.next())
+    for (Chunks k(p.slots - held, (p.ld_sorted + 7) >> 3, blockIdx.x - (gridDim.x - kZeroGroups), kZeroGroups); k.more(); k.next())
         store_chunk((T*)p.out_sorted + (held + k.row) * p.ld_sorted, k.at * 8, p.ld_sorted, zero);
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void gather_kernel(RouteArgs p) {
-    for (Chunks k(p.N, (p.width + 7) >> 3); k.more(); k.next()) {
-        const auto v = load_chunk((const T*)p.rows + k.row * p.ld, k.at * 8, p.width);
-        const int32_t* place = p.place + k.row * p.per_row;
-        for (int j = 0; j < p.per_row; ++j) {
-            const uint32_t to = (uint32_t)place[j];
-            if (to < (uint64_t)p.slots) store_chunk((T*)p.out_sorted + (int64_t)to * p.ld_sorted, k.at * 8, p.ld_sorted, v);
-        }
-    }
-    zero_behind<T>(p);
+// This thread's row, and its place among the row's threads.
+template <int TPR> __device__ __forceinline__ int64_t own_row(int& t) {
+    t = threadIdx.x % TPR;
+    const int sub = TPR >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : threadIdx.x / TPR;
+    return (int64_t)blockIdx.x * (kThreads / TPR) + sub;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void combine_kernel(RouteArgs p) {
-    for (Chunks k(p.N, (p.width + 7) >> 3); k.more(); k.next()) {
-        const int32_t* place = p.place + k.row * p.per_row;
-        float sum[8] = {};
+template <typename T, int TPR>
+__global__ __launch_bounds__(kThreads) void gather_kernel(RouteArgs p) {
+    if (p.offsets && blockIdx.x >= gridDim.x - kZeroGroups) return zero_behind<T>(p);
+    int t;
+    const int64_t n = own_row<TPR>(t), D = p.width;
+    if (n >= p.N) return;
+    const T* row = (const T*)p.rows + n * p.ld;
+    const bool past = large<T>(p);
+    const int32_t* place = p.place + n * p.per_row;
+    for (int64_t c = t * 8; c < D; c += TPR * 16) {
+        const int64_t c2 = c + TPR * 8;
+        const auto v = load_chunk(row, c, D), v2 = load_chunk(row, c2 < D ? c2 : c, D);
         for (int j = 0; j < p.per_row; ++j) {
-            const uint32_t from = (uint32_t)place[j];
-            if (from >= (uint64_t)p.slots) continue;
-            const float w = p.weights ? p.weights[k.row * p.per_row + j] : 1.0f;
-            const auto v = load_chunk((const T*)p.sorted + (int64_t)from * p.width, k.at * 8, p.width);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += w * to_f32(v[e]);
+            const uint32_t to = (uint32_t)place[j];
+            if (to >= (uint64_t)p.slots) continue;
+            T* out = (T*)p.out_sorted + (int64_t)to * p.ld_sorted;
+            put_chunk(out, c, p.ld_sorted, v, past);
+            if (c2 < D) put_chunk(out, c2, p.ld_sorted, v2, past);
         }
-        typename Chunk<T>::V o;
+    }
+}
+
+template <typename T, int TPR>
+__global__ __launch_bounds__(kThreads) void combine_kernel(RouteArgs p) {
+    int t;
+    const int64_t n = own_row<TPR>(t), D = p.width;
+    if (n >= p.N) return;
+    const int32_t* place = p.place + n * p.per_row;
+    const float* weights = p.weights ? p.weights + n * p.per_row : nullptr;
+    const bool past = large<T>(p);
+    for (int64_t c = t * 8; c < D; c += TPR * 16) {
+        const int64_t c2 = c + TPR * 8;
+        float sum[2][8] = {};
+        for (int k = 0; k < p.per_row; k += 4) {
+            typename Chunk<T>::V v[4][2] = {};
+            float w[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = (T)sum[e];
-        store_chunk((T*)p.out_rows + k.row * p.ld_out, k.at * 8, p.width, o);
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t from = k + j < p.per_row ? (uint32_t)place[k + j] : ~0u;
+                w[j] = 0.0f;
+                if (from >= (uint64_t)p.slots) continue;
+                w[j] = weights ? weights[k + j] : 1.0f;
+                const T* row = (const T*)p.sorted + (int64_t)from * D;
+                v[j][0] = load_chunk(row, c, D);
+                v[j][1] = load_chunk(row, c2 < D ? c2 : c, D);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    sum[0][e] += w[j] * to_f32(v[j][0][e]);
+                    sum[1][e] += w[j] * to_f32(v[j][1][e]);
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            typename Chunk<T>::V o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = (T)sum[i][e];
+            if (i && c2 >= D) continue;
+            put_chunk((T*)p.out_rows + n * p.ld_out, i ? c2 : c, D, o, past);
+        }
     }
 }
 
@@ -218,7 +265,7 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(RouteArgs p) {
 template <typename T>
 __global__ __launch_bounds__(kThreads) void combine_parts_kernel(RouteArgs p, int splits) {
     const int64_t ld = (p.width + 3) & ~3LL;
-    for (Chunks k(p.N, ld >> 2); k.more(); k.next()) {
+    for (Chunks k(p.N, ld >> 2, blockIdx.x, gridDim.x); k.more(); k.next()) {
         const int32_t* place = p.place + k.row * p.per_row;
         f32x4 sum = {};
         for (int j = 0; j < p.per_row; ++j) {
@@ -233,68 +280,71 @@ __global__ __launch_bounds__(kThreads) void combine_parts_kernel(RouteArgs p, in
     }
 }
 
-// TPR threads a row: they read grad_y's row once for four of its choices, and add up the products with those rows.
+// grad_y's row times the weights into its places, and its products with the rows there.
 template <typename T, int TPR>
 __global__ __launch_bounds__(kThreads) void combine_backward_kernel(RouteArgs p) {
+    if (p.out_sorted && blockIdx.x >= gridDim.x - kZeroGroups) return zero_behind<T>(p);
     __shared__ float s[4 * (kThreads / 64)];
-    constexpr int kRows = kThreads / TPR;
-    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-    const int64_t D = p.width;
-    for (int64_t n0 = (int64_t)blockIdx.x * kRows; n0 < p.N; n0 += (int64_t)gridDim.x * kRows) {
-        const int64_t n = n0 + sub < p.N ? n0 + sub : p.N - 1;
-        const bool mine = n0 + sub < p.N;
-        for (int k0 = 0; k0 < p.per_row; k0 += 4) {
-            uint32_t at[4];
-            float w[4], dot[4] = {};
+    int t;
+    const int64_t row = own_row<TPR>(t), n = row < p.N ? row : p.N - 1, D = p.width;
+    const bool mine = row < p.N;
+    const T* gy = (const T*)p.rows + n * p.ld;
+    const bool past = large<T>(p);
+    for (int k0 = 0; k0 < p.per_row; k0 += 4) {
+        uint32_t at[4];
+        float w[4], dot[4] = {};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                at[j] = k0 + j < p.per_row && mine ? (uint32_t)p.place[n * p.per_row + k0 + j] : ~0u;
-                w[j] = k0 + j < p.per_row && p.weights ? p.weights[n * p.per_row + k0 + j] : 1.0f;
-            }
-            for (int64_t c = t * 8; c < D; c += TPR * 8) {
-                const auto g = load_chunk((const T*)p.rows + n * p.ld, c, D);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (at[j] >= (uint64_t)p.slots) continue;
-                    if (p.grad_weights) {
-                        const auto v = load_chunk((const T*)p.sorted + (int64_t)at[j] * D, c, D);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) dot[j] += c + e < D ? to_f32(g[e]) * to_f32(v[e]) : 0.0f;
-                    }
-                    if (p.out_sorted) {
-                        typename Chunk<T>::V o;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) o[e] = (T)(w[j] * to_f32(g[e]));
-                        store_chunk((T*)p.out_sorted + (int64_t)at[j] * p.ld_sorted, c, p.ld_sorted, o);
-                    }
-                }
-            }
-            if (!p.grad_weights) continue;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-#pragma unroll
-                for (int o = TPR < 64 ? TPR / 2 : 32; o; o >>= 1) dot[j] += __shfl_xor(dot[j], o, 64);
-            }
-            if constexpr (TPR > 64) {
-                constexpr int W = TPR / 64;
-                __syncthreads();
-                if ((t & 63) == 0)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) s[(t >> 6) * 4 + j] = dot[j];
-                __syncthreads();
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    dot[j] = s[j];
-#pragma unroll
-                    for (int w2 = 1; w2 < W; ++w2) dot[j] += s[w2 * 4 + j];
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (t == j && mine && k0 + j < p.per_row) p.grad_weights[n * p.per_row + k0 + j] = dot[j];
+        for (int j = 0; j < 4; ++j) {
+            at[j] = k0 + j < p.per_row && mine ? (uint32_t)p.place[n * p.per_row + k0 + j] : ~0u;
+            w[j] = k0 + j < p.per_row && p.weights ? p.weights[n * p.per_row + k0 + j] : 1.0f;
         }
+        for (int64_t c = t * 8; c < D; c += TPR * 8) {
+            const auto g = load_chunk(gy, c, D);
+            typename Chunk<T>::V v[4] = {};
+            if (p.grad_weights) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (at[j] < (uint64_t)p.slots) v[j] = load_chunk((const T*)p.sorted + (int64_t)at[j] * D, c, D);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (at[j] >= (uint64_t)p.slots) continue;
+                if (p.grad_weights) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dot[j] += to_f32(g[e]) * to_f32(v[j][e]);   // (zeros beyond the rows)
+                }
+                if (p.out_sorted) {
+                    typename Chunk<T>::V o;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = (T)(w[j] * to_f32(g[e]));
+                    put_chunk((T*)p.out_sorted + (int64_t)at[j] * p.ld_sorted, c, p.ld_sorted, o, past);
+                }
+            }
+        }
+        if (!p.grad_weights) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int o = TPR < 64 ? TPR / 2 : 32; o; o >>= 1) dot[j] += __shfl_xor(dot[j], o, 64);
+        }
+        if constexpr (TPR > 64) {
+            constexpr int W = TPR / 64;
+            __syncthreads();
+            if ((t & 63) == 0)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[(t >> 6) * 4 + j] = dot[j];
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                dot[j] = s[j];
+#pragma unroll
+                for (int w2 = 1; w2 < W; ++w2) dot[j] += s[w2 * 4 + j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (t == j % TPR && mine && k0 + j < p.per_row) p.grad_weights[n * p.per_row + k0 + j] = dot[j];
     }
-    if (p.out_sorted) zero_behind<T>(p);
 }
 
 unsigned chunk_groups(int64_t rows, int64_t width) {
@@ -316,18 +366,39 @@ int launch_sort(const SortArgs& a, void* stream) {
     else if (dtype == FFN_BF16) { RUN(bf16); } \
     else { RUN(fp16); }
 
-int launch_gather(const RouteArgs& a, int32_t dtype, void* stream) {
-    const dim3 grid(chunk_groups(a.N, a.width));
-#define FFN_RUN(T) gather_kernel<T><<<grid, kThreads, 0, (hipStream_t)stream>>>(a)
-    if (dtype == FFN_FP32) FFN_RUN(float);
-    else FFN_RUN(bf16);   // bits alone
+// Threads a row: one for two chunks, in steps of four.
+#define FFN_BY_WIDTH(RUN, T)                   \
+    const int64_t chunks = (a.width + 7) / 8;  \
+    if (chunks <= 8) { RUN(T, 4); }            \
+    else if (chunks <= 32) { RUN(T, 16); }     \
+    else if (chunks <= 256) { RUN(T, 64); }    \
+    else { RUN(T, 256); }
+unsigned row_blocks(int64_t N, int tpr, bool zeros) { return (unsigned)((N * tpr + kThreads - 1) / kThreads) + (zeros ? kZeroGroups : 0); }
+
+template <typename T> void run_gather(const RouteArgs& a, hipStream_t s) {
+#define FFN_RUN(T, TPR) gather_kernel<T, TPR><<<dim3(row_blocks(a.N, TPR, a.offsets != nullptr)), kThreads, 0, s>>>(a)
+    FFN_BY_WIDTH(FFN_RUN, T)
 #undef FFN_RUN
+}
+template <typename T> void run_combine(const RouteArgs& a, hipStream_t s) {
+#define FFN_RUN(T, TPR) combine_kernel<T, TPR><<<dim3(row_blocks(a.N, TPR, false)), kThreads, 0, s>>>(a)
+    FFN_BY_WIDTH(FFN_RUN, T)
+#undef FFN_RUN
+}
+template <typename T> void run_combine_backward(const RouteArgs& a, hipStream_t s) {
+#define FFN_RUN(T, TPR) combine_backward_kernel<T, TPR><<<dim3(row_blocks(a.N, TPR, a.out_sorted != nullptr)), kThreads, 0, s>>>(a)
+    FFN_BY_WIDTH(FFN_RUN, T)
+#undef FFN_RUN
+}
+
+int launch_gather(const RouteArgs& a, int32_t dtype, void* stream) {
+    if (dtype == FFN_FP32) run_gather<float>(a, (hipStream_t)stream);
+    else run_gather<bf16>(a, (hipStream_t)stream);   // bits alone
     return (int)hipGetLastError();
 }
 
 int launch_combine(const RouteArgs& a, int32_t dtype, void* stream) {
-    const dim3 grid(chunk_groups(a.N, a.width));
-#define FFN_RUN(T) combine_kernel<T><<<grid, kThreads, 0, (hipStream_t)stream>>>(a)
+#define FFN_RUN(T) run_combine<T>(a, (hipStream_t)stream)
     FFN_BY_TYPE(FFN_RUN)
 #undef FFN_RUN
     return (int)hipGetLastError();
@@ -342,8 +413,7 @@ int launch_combine_parts(const RouteArgs& a, int32_t splits, int32_t dtype, void
 }
 
 int launch_combine_backward(const RouteArgs& a, int32_t dtype, void* stream) {
-    const dim3 grid((unsigned)(a.N < 4096 ? a.N : 4096));
-#define FFN_RUN(T) combine_backward_kernel<T, 256><<<grid, kThreads, 0, (hipStream_t)stream>>>(a)
+#define FFN_RUN(T) run_combine_backward<T>(a, (hipStream_t)stream)
     FFN_BY_TYPE(FFN_RUN)
 #undef FFN_RUN
     return (int)hipGetLastError();
