@@ -88,13 +88,21 @@ int launch_expert_rows_fp32(const TileArgs& t, const Groups& g, int32_t epilogue
 int launch_expert_few_bf16(const FewArgs& p, const Groups& g, int32_t epilogue, int32_t rows, int32_t nr, int32_t waves, int64_t most, void* stream);
 int launch_expert_few_fp16(const FewArgs& p, const Groups& g, int32_t epilogue, int32_t rows, int32_t nr, int32_t waves, int64_t most, void* stream);
 int launch_expert_few_fp32(const FewArgs& p, const Groups& g, int32_t epilogue, int32_t rows, int32_t nr, int32_t waves, int64_t most, void* stream);
-// C_e = A_e^T B_e, the sum over the rows of expert e, for every expert: C [experts, t.M, t.N].  An expert of more than
-// g.chunk rows has as many parts; theirs go to `partial`, floats [parts, t.M, t.N up to a multiple of four], for
-// launch_join_sums.  t.splits: parts there may be.
-int launch_expert_sums_bf16(const TileArgs& t, const Groups& g, float* partial, int32_t tile, void* stream);
-int launch_expert_sums_fp16(const TileArgs& t, const Groups& g, float* partial, int32_t tile, void* stream);
-int launch_expert_sums_fp32(const TileArgs& t, const Groups& g, float* partial, int32_t tile, void* stream);
-int launch_join_sums(const TileArgs& t, const Groups& g, const float* partial, int32_t dtype, void* stream);
+// The gradients' products, in one launch; those whose t.a is NULL are left out.
+//   0: C = A B^T for the rows of every expert as above (kPartial, B by columns)
+//   1, 2: C_e = A_e^T B_e, the sum over the rows of expert e, for every expert: C [experts, t.M, t.N].  An expert of more than
+//      g.chunk rows has as many parts; theirs go to partial[k - 1], floats [parts, t.M, t.N up to a multiple of four], for
+//      launch_join_sums.  t.splits: parts there may be.
+struct ExpertGrads {
+    TileArgs t[3];
+    Groups g[3];
+    float* partial[2];
+    int32_t end[3];                       // work-groups up to here; set by the launcher
+};
+int launch_expert_grads_bf16(const ExpertGrads& a, int32_t tile, void* stream);
+int launch_expert_grads_fp16(const ExpertGrads& a, int32_t tile, void* stream);
+int launch_expert_grads_fp32(const ExpertGrads& a, int32_t tile, void* stream);
+int launch_join_sums(const ExpertGrads& a, int32_t dtype, void* stream);
 
 // launch_join and launch_join_gate for as many of the rows as *limit says (NULL: all).
 int launch_join_rows(const float* partial, int64_t ld, int32_t splits, int64_t M, int64_t N, void* out, int32_t dtype,

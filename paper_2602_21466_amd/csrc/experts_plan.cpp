@@ -74,61 +74,57 @@ int64_t most_tiles(const Shape& s, int32_t tile) { return s.R / tile + (s.E < s.
 Cut cut_rows(const Shape& s, int32_t dtype, int32_t epilogue) {
     const bool wide = dtype == FFN_FP32;
     auto groups = [&](int32_t tile) { return ((double)s.R / tile + 0.5 * (double)(s.E < s.R ? s.E : s.R)) * (double)tiles(s.N, tile); };
-    Cut c = shortest(groups, tiles(s.K, wide ? 32 : 64), (double)s.R * s.N, wide, epilogue == ffn::kGateGrad);
-    c.joined = c.joined || epilogue == ffn::kPartial;
-    return c;
+    return shortest(groups, tiles(s.K, wide ? 32 : 64), (double)s.R * s.N, wide, epilogue == ffn::kGateGrad);
 }
 
-// [experts, M, N], sums over each expert's rows.  chunk: rows of a part, 0 where an expert's are one part.  Counted like
-// shortest(): all work-groups' steps over those that run at one time, then half of the longest one alone; a few experts may
-// have three times the mean.
-struct Sums { int32_t tile, chunk; };
-Sums cut_sums(int64_t M, const Shape& s, int32_t dtype) {
-    const bool wide = dtype == FFN_FP32;
-    const double k = wide ? 32.0 : 64.0, ends = wide ? 2.0 : 4.0, mean = (double)s.R / s.E;
-    Sums best = {256, 0};
+// The gradients' products of one launch: the rows' [R, d_in], whose k is in `splits` parts, and the weights', sums over each
+// expert's rows in parts of `chunk` of them (0: one part an expert).  Counted like shortest(): all work-groups' steps over
+// those that run at one time, then half of the longest one alone; a few experts may have three times the mean.
+struct GradCut { int32_t tile, splits, chunk; };
+GradCut cut_grads(const ffn_experts_s* p, int64_t R) {
+    const bool wide = p->dtype == FFN_FP32;
+    const int64_t di = p->d_in, df = p->d_ff, d_o = p->d_out, E = p->experts, kstep = wide ? 32 : 64, steps = tiles(2 * df, kstep);
+    const double k = (double)kstep, ends = wide ? 2.0 : 4.0, mean = (double)R / E, longest = 3.0 * mean < (double)R ? 3.0 * mean : (double)R;
+    const double outputs = (double)(2 * df * di) + (double)(d_o * df);
+    GradCut best = {128, 1, 0};
     double least = 1e300;
     for (int32_t tile : {256, 128}) {
-        const double each = (double)(tiles(M, tile) * tiles(s.N, tile)), slots = tile == 256 ? 256.0 : 512.0;
-        const double step = tile == 256 ? (wide ? 4.5 : 1.6) : (wide ? 2.6 : 1.06);
-        auto time = [&](double parts, double rows) {
-            const double all = each * ((double)s.R / k + parts * ends) / slots, one = rows / k + ends;
-            return step * (each * parts <= slots ? (one > all ? one : all) : all + 0.5 * one);
+        const double slots = tile == 256 ? 256.0 : 512.0, step = tile == 256 ? (wide ? 4.5 : 1.6) : (wide ? 2.6 : 1.06);
+        const double rows = ((double)R / tile + 0.5 * (double)(E < R ? E : R)) * (double)tiles(di, tile);
+        const double each = (double)(tiles(2 * df, tile) * tiles(di, tile) + tiles(d_o, tile) * tiles(df, tile));
+        auto consider = [&](int32_t chunk) {
+            const double parts = chunk ? (double)R / chunk + 0.5 * E : (double)E, sums = each * ((double)R / k + parts * ends);
+            const double one = (chunk ? (double)chunk : longest) / k + ends, join = chunk ? 4.0 + parts * outputs * 8.0 / 4e6 : 0.0;
+            for (int32_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); s += s < 4 ? 1 : s / 2) {
+                const double own = (double)tiles(steps, s) + ends, all = (rows * s * own + sums) / slots, last = own > one ? own : one;
+                const double t = step * (rows * s + each * parts <= slots ? (last > all ? last : all) : all + 0.5 * last) + join + 0.1 * s + (double)R * di * s * 8.0 / 4e6;
+                if (t < least) { least = t; best = {tile, s, chunk}; }
+            }
         };
-        const double longest = 3.0 * mean < (double)s.R ? 3.0 * mean : (double)s.R;
-        const double t = time((double)s.E, longest);
-        if (t < least) { least = t; best = {tile, 0}; }
-        for (int64_t chunk = tiles(s.R, 64) * 64; chunk >= 4 * (int64_t)k; chunk = (chunk / 2 + 63) & ~63LL) {
-            if ((double)chunk >= longest) continue;
-            const double parts = (double)s.R / chunk + 0.5 * s.E;
-            const double tc = time(parts, (double)chunk) + 4.0 + parts * (double)(M * s.N) * 8.0 / 4e6;
-            if (tc < least) { least = tc; best = {tile, (int32_t)chunk}; }
-            if (chunk <= 64) break;
-        }
+        consider(0);
+        for (int64_t chunk = tiles(R, 64) * 64; chunk >= 4 * kstep; chunk = (chunk / 2 + 63) & ~63LL)
+            if ((double)chunk < longest) consider((int32_t)chunk);
     }
     return best;
 }
-// Parts there may be.
-int64_t most_parts(const Shape& s, const Sums& c) { return s.E + (c.chunk ? s.R / c.chunk : 0); }
+// Parts of an expert's rows there may be.
+int64_t most_parts(int64_t R, int64_t E, const GradCut& c) { return E + (c.chunk ? R / c.chunk : 0); }
 
 int64_t up4(int64_t n) { return (n + 3) & ~3LL; }
 int64_t rows_partial(const Shape& s, int32_t dtype, int32_t epilogue) {
     const Cut c = cut_rows(s, dtype, epilogue);
     return c.joined ? aligned(c.splits * s.R * up4(s.N) * 4) : 0;
 }
-int64_t sums_partial(int64_t M, const Shape& s, int32_t dtype) {
-    const Sums c = cut_sums(M, s, dtype);
-    return c.chunk ? aligned(most_parts(s, c) * M * up4(s.N) * 4) : 0;
-}
-
 constexpr int64_t kMostGroups = 0x7FFFFFFF / 512;
 bool rows_fit(const Shape& s, int32_t dtype, int32_t epilogue) {
     const Cut c = cut_rows(s, dtype, epilogue);
     return most_tiles(s, c.tile) * tiles(s.N, c.tile) * c.splits <= kMostGroups;
 }
-bool sums_fit(int64_t M, const Shape& s, int32_t dtype) {
-    const Sums c = cut_sums(M, s, dtype);
-    return (tiles(M, c.tile) * tiles(s.N, c.tile) + 8) * most_parts(s, c) <= kMostGroups;
+bool grads_fit(const ffn_experts_s* p, int64_t R) {
+    const GradCut c = cut_grads(p, R);
+    const int64_t di = p->d_in, df = p->d_ff, d_o = p->d_out, E = p->experts, t = c.tile;
+    return most_tiles({R, E, di, 0}, c.tile) * tiles(di, t) * c.splits +
+               (tiles(2 * df, t) * tiles(di, t) + tiles(d_o, t) * tiles(df, t) + 16) * most_parts(R, E, c) <= kMostGroups;
 }
 
 int launch_rows(const ffn::TileArgs& t, const ffn::Groups& g, int32_t epilogue, bool bc, int32_t dtype, int32_t tile, void* stream) {
@@ -138,17 +134,9 @@ int launch_rows(const ffn::TileArgs& t, const ffn::Groups& g, int32_t epilogue, 
         default: return ffn::launch_expert_rows_fp16(t, g, epilogue, bc, tile, stream);
     }
 }
-int launch_sums(const ffn::TileArgs& t, const ffn::Groups& g, float* partial, int32_t dtype, int32_t tile, void* stream) {
-    switch (dtype) {
-        case FFN_FP32: return ffn::launch_expert_sums_fp32(t, g, partial, tile, stream);
-        case FFN_BF16: return ffn::launch_expert_sums_bf16(t, g, partial, tile, stream);
-        default: return ffn::launch_expert_sums_fp16(t, g, partial, tile, stream);
-    }
-}
-
 // Runs the product of rows whose operands, sizes (t.M: the sorted rows) and results t describes; `partial` is scratch of
-// rows_partial() (kGate: of 2 N columns).  kPartial: the sums stay there, in *splits parts.
-int rows_product(ffn::TileArgs t, const ffn::Groups& g, int32_t epilogue, bool bc, int32_t dtype, void* partial, int32_t* splits, void* stream) {
+// rows_partial() (kGate: of 2 N columns).
+int rows_product(ffn::TileArgs t, const ffn::Groups& g, int32_t epilogue, bool bc, int32_t dtype, void* partial, void* stream) {
     const int64_t columns = epilogue == ffn::kGate ? 2 * t.N : t.N;
     const Shape s = {t.M, g.experts, columns, t.K};
     const Cut c = cut_rows(s, dtype, epilogue);
@@ -161,26 +149,11 @@ int rows_product(ffn::TileArgs t, const ffn::Groups& g, int32_t epilogue, bool b
     p.N = columns;
     p.ldc = up4(columns);
     const int rc = status(launch_rows(p, g, ffn::kPartial, bc, dtype, c.tile, stream));
-    if (splits) *splits = c.splits;
-    if (rc != CGTP_OK || epilogue == ffn::kPartial) return rc;
+    if (rc != CGTP_OK) return rc;
     const int32_t* limit = g.offsets + g.experts;
     if (epilogue == ffn::kStore)
         return status(ffn::launch_join_rows((const float*)partial, p.ldc, c.splits, t.M, t.N, t.c, dtype, limit, stream));
     return status(ffn::launch_join_gate_rows(t, epilogue, (const float*)partial, p.ldc, dtype, limit, stream));
-}
-
-// The sums over each expert's rows: t.M x t.N results an expert, contiguous.
-int sums_product(ffn::TileArgs t, ffn::Groups g, int32_t dtype, void* partial, void* stream) {
-    const Shape s = {g.rows, g.experts, t.N, 0};
-    const Sums c = cut_sums(t.M, s, dtype);
-    t.tiles_m = (int32_t)tiles(t.M, c.tile);
-    t.tiles_n = (int32_t)tiles(t.N, c.tile);
-    t.splits = (int32_t)most_parts(s, c);
-    t.ldc = t.N;
-    g.chunk = c.chunk;
-    const int rc = status(launch_sums(t, g, (float*)partial, dtype, c.tile, stream));
-    if (rc != CGTP_OK || c.chunk == 0) return rc;
-    return status(ffn::launch_join_sums(t, g, (const float*)partial, dtype, stream));
 }
 
 // The forward products for few rows an expert, where reading the weights is the time: tiles of 16, 32 or 64 rows, so that
@@ -239,7 +212,7 @@ Matrix readable(const void* p, int64_t rows, int64_t width, int32_t dtype, void*
 }
 
 // Byte offsets in the workspace: x's rows in the sorted order, intermediates, copies of operands, partial sums.
-struct Layout { int64_t x, h, dgu, gy, w_in, w_out, partial, total; };
+struct Layout { int64_t x, h, dgu, gy, w_in, w_out, partial, part_in, part_out, total; };
 Layout layout(const ffn_experts_s* p, int64_t R, bool backward) {
     const int64_t di = p->d_in, df = p->d_ff, d_o = p->d_out, E = p->experts;
     const int32_t t = p->dtype;
@@ -257,9 +230,12 @@ Layout layout(const ffn_experts_s* p, int64_t R, bool backward) {
         l.dgu = take(packed_bytes(R, 2 * df, t));
         l.gy = take(narrow ? packed_bytes(R, d_o, t) : 0);
         also(rows_partial({R, E, df, d_o}, t, ffn::kGateGrad));
-        also(rows_partial({R, E, di, 2 * df}, t, ffn::kPartial));
-        also(sums_partial(2 * df, {R, E, di, 0}, t));
-        also(sums_partial(d_o, {R, E, df, 0}, t));
+        const GradCut c = cut_grads(p, R);
+        also(aligned(c.splits * R * up4(di) * 4));
+        if (c.chunk) {
+            l.part_in = take(aligned(most_parts(R, E, c) * 2 * df * up4(di) * 4));
+            l.part_out = take(aligned(most_parts(R, E, c) * d_o * up4(df) * 4));
+        }
     } else {
         also(rows_partial({R, E, 2 * df, di}, t, ffn::kGate));
         also(rows_partial({R, E, d_o, df}, t, ffn::kStore));
@@ -453,7 +429,7 @@ int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const in
     t.c = ws + l.h; t.ldc = H.ld;
     t.act = plan->act; t.saved = (float*)saved;
     ffn::Groups g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, X.end, Wi.end, 0, there ? source : nullptr, per_row};
-    rc = rows_product(t, g, ffn::kGate, false, dt, ws + l.partial, nullptr, hip_stream);
+    rc = rows_product(t, g, ffn::kGate, false, dt, ws + l.partial, hip_stream);
     if (rc != CGTP_OK) return rc;
     ffn::TileArgs o = {};
     o.a = H.p; o.lda = H.ld;
@@ -461,7 +437,7 @@ int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const in
     o.M = R; o.N = d_o; o.K = df;
     o.c = y; o.ldc = d_o;
     g = {offsets, plan->experts, R, d_o * Wo.ld * e, H.end, Wo.end, 0, nullptr, 1};
-    return rows_product(o, g, ffn::kStore, false, dt, ws + l.partial, nullptr, hip_stream);
+    return rows_product(o, g, ffn::kStore, false, dt, ws + l.partial, hip_stream);
 }
 
 int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const int32_t* place, const int32_t* source,
@@ -480,9 +456,7 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
     if (misaligned({x, grad_y}, e) || misaligned({place, source, offsets}, 4) ||
         misaligned({w_in, w_out, saved, grad_x, grad_w_in, grad_w_out}, 16))
         return CGTP_EINVAL;
-    if (!rows_fit({R, E, df, d_o}, dt, ffn::kGateGrad) || !rows_fit({R, E, di, 2 * df}, dt, ffn::kPartial) ||
-        !sums_fit(2 * df, {R, E, di, 0}, dt) || !sums_fit(d_o, {R, E, df, 0}, dt))
-        return CGTP_EUNSUP;
+    if (!rows_fit({R, E, df, d_o}, dt, ffn::kGateGrad) || !grads_fit(plan, R)) return CGTP_EUNSUP;
     const Layout l = layout(plan, R, true);
     rc = workspace_ok(workspace, workspace_bytes, l.total);
     if (rc != CGTP_OK) return rc;
@@ -515,39 +489,43 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
     t.c = ws + l.dgu; t.ldc = D.ld;
     t.h = ws + l.h; t.ldh = H.ld;
     t.act = plan->act; t.saved = (float*)const_cast<void*>(saved);
-    rc = rows_product(t, g, ffn::kGateGrad, true, dt, ws + l.partial, nullptr, hip_stream);
-    if (rc == CGTP_OK && grad_x) {
+    rc = rows_product(t, g, ffn::kGateGrad, true, dt, ws + l.partial, hip_stream);
+    if (rc != CGTP_OK || (!grad_x && !grad_w_in && !grad_w_out)) return rc;
+    const GradCut c = cut_grads(plan, R);
+    ffn::ExpertGrads a = {};
+    auto sums = [&](int k, const Matrix& A, const Matrix& B, int64_t M, int64_t columns, void* to, int64_t part) {
+        ffn::TileArgs& w = a.t[k];
+        w.a = A.p; w.lda = A.ld; w.b = B.p; w.ldb = B.ld;
+        w.M = M; w.N = columns; w.c = to; w.ldc = columns;
+        w.tiles_m = (int32_t)tiles(M, c.tile);
+        w.tiles_n = (int32_t)tiles(columns, c.tile);
+        w.splits = (int32_t)most_parts(R, E, c);
+        a.g[k] = {offsets, plan->experts, R, 0, A.end, B.end, c.chunk, nullptr, 1};
+        a.partial[k - 1] = (float*)(ws + part);
+    };
+    if (grad_x) {
         // its sums stay in 32 bits until a row's choices are added
-        ffn::TileArgs d = {};
-        d.a = D.p; d.lda = D.ld;
-        d.b = Wi.p; d.ldb = Wi.ld;
+        ffn::TileArgs& d = a.t[0];
+        d.a = D.p; d.lda = D.ld; d.b = Wi.p; d.ldb = Wi.ld;
         d.M = R; d.N = di; d.K = 2 * df;
-        g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, D.end, Wi.end, 0, nullptr, 1};
-        int32_t splits = 1;
-        rc = rows_product(d, g, ffn::kPartial, true, dt, ws + l.partial, &splits, hip_stream);
-        ffn::RouteArgs a = {};
-        a.N = N; a.width = di; a.per_row = per_row; a.slots = R;
-        a.place = place; a.sorted = ws + l.partial; a.out_rows = grad_x; a.ld_out = di;
-        if (rc == CGTP_OK) rc = status(ffn::launch_combine_parts(a, splits, dt, hip_stream));
+        d.c = ws + l.partial; d.ldc = up4(di);
+        d.tiles_m = (int32_t)most_tiles({R, E, di, 0}, c.tile);
+        d.tiles_n = (int32_t)tiles(di, c.tile);
+        d.splits = c.splits;
+        a.g[0] = {offsets, plan->experts, R, 2 * df * Wi.ld * e, D.end, Wi.end, 0, nullptr, 1};
     }
-    if (rc == CGTP_OK && grad_w_in) {
-        ffn::TileArgs w = {};
-        w.a = D.p; w.lda = D.ld;
-        w.b = X.p; w.ldb = X.ld;
-        w.M = 2 * df; w.N = di;
-        w.c = grad_w_in;
-        g = {offsets, plan->experts, R, 0, D.end, X.end, 0, nullptr, 1};
-        rc = sums_product(w, g, dt, ws + l.partial, hip_stream);
+    if (grad_w_in) sums(1, D, X, 2 * df, di, grad_w_in, l.part_in);
+    if (grad_w_out) sums(2, Gy, H, d_o, df, grad_w_out, l.part_out);
+    rc = status(dt == FFN_FP32   ? ffn::launch_expert_grads_fp32(a, c.tile, hip_stream)
+                : dt == FFN_BF16 ? ffn::launch_expert_grads_bf16(a, c.tile, hip_stream)
+                                 : ffn::launch_expert_grads_fp16(a, c.tile, hip_stream));
+    if (rc == CGTP_OK && grad_x) {
+        ffn::RouteArgs r = {};
+        r.N = N; r.width = di; r.per_row = per_row; r.slots = R;
+        r.place = place; r.sorted = ws + l.partial; r.out_rows = grad_x; r.ld_out = di;
+        rc = status(ffn::launch_combine_parts(r, c.splits, dt, hip_stream));
     }
-    if (rc == CGTP_OK && grad_w_out) {
-        ffn::TileArgs w = {};
-        w.a = Gy.p; w.lda = Gy.ld;
-        w.b = H.p; w.ldb = H.ld;
-        w.M = d_o; w.N = df;
-        w.c = grad_w_out;
-        g = {offsets, plan->experts, R, 0, Gy.end, H.end, 0, nullptr, 1};
-        rc = sums_product(w, g, dt, ws + l.partial, hip_stream);
-    }
+    if (rc == CGTP_OK && c.chunk && (grad_w_in || grad_w_out)) rc = status(ffn::launch_join_sums(a, dt, hip_stream));
     return rc;
 }
 

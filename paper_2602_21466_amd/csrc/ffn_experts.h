@@ -11,18 +11,25 @@
 namespace ffn {
 namespace dev {
 
-template <typename T, int BM, int WM, int WN, bool BC, int EPI>
-__global__ __launch_bounds__(64 * WM * WN) void expert_rows_kernel(TileArgs p, Groups g) {
+// Work-group `block` of C = A B^T by expert.
+template <typename T, int BM, bool BC, int EPI>
+__device__ __forceinline__ void rows_group(const TileArgs& p, const Groups& g, int block, char* sa0, char* sb0, char* sa1, char* sb1) {
+    constexpr int WM = 2, WN = BM == 256 ? 4 : 2;
     const int lane = threadIdx.x & 63;
     Scan first;
     const int total = count_tiles(g, lane, BM, 0, first);
-    if ((int64_t)blockIdx.x >= (int64_t)total * p.tiles_n * p.splits) return;
+    if ((int64_t)block >= (int64_t)total * p.tiles_n * p.splits) return;
     int tm, tn, split;
-    place(blockIdx.x, total, p.tiles_n, p.splits, tm, tn, split);
+    place(block, total, p.tiles_n, p.splits, tm, tn, split);
     const Run r = find_tile(g, lane, BM, 0, first, tm);
     const Exact xa = {(const char*)g.a_end, g.source, (uint32_t)g.per_row, (uint32_t)g.rows}, xb = {(const char*)g.b_end, nullptr, 1, 0};
     tile_body<T, BM, BM, WM, WN, false, BC, EPI, true>(p, Work{p.a, (const char*)p.b + r.expert * g.b_step, (int64_t)r.begin + (int64_t)r.tile * BM, r.end, p.K, 0, p.M,
-                                                              tn, split, xa, xb, nullptr});
+                                                              tn, split, xa, xb, nullptr}, sa0, sb0, sa1, sb1);
+}
+template <typename T, int BM, bool BC, int EPI>
+__global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_rows_kernel(TileArgs p, Groups g) {
+    FFN_TILE_LDS(BM, BM);
+    rows_group<T, BM, BC, EPI>(p, g, blockIdx.x, sa0, sb0, sa1, sb1);
 }
 
 constexpr int kManyTiles = 64;
@@ -32,10 +39,11 @@ __host__ __device__ __forceinline__ constexpr int64_t sums_step(int64_t tiles) {
 // does), each part's to all dies, as its rows may be many more than another's; where they are few, one after the other.  An
 // expert of many rows is cut into parts of them, so that no work-group has
 // many times another's steps (5 experts, the largest of 8192 rows' half, 3281 x 512 in fp32: 160 us, 294 without).
-template <typename T, int BM, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void expert_sums_kernel(TileArgs p, Groups g, float* partial) {
+template <typename T, int BM>
+__device__ __forceinline__ void sums_group(TileArgs p, const Groups& g, float* partial, int block, char* sa0, char* sb0, char* sa1, char* sb1) {
+    constexpr int WM = 2, WN = BM == 256 ? 4 : 2;
     const int lane = threadIdx.x & 63, tiles = p.tiles_m * p.tiles_n, step = (int)sums_step(tiles);
-    const int unit = blockIdx.x / step, id = blockIdx.x - unit * step;
+    const int unit = block / step, id = block - unit * step;
     if (id >= tiles) return;
     Run r = {unit, 0, 0, 0};
     bool whole = true;
@@ -59,18 +67,35 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_sums_kernel(TileArgs p, G
     p.splits = 1;
     tile_body<T, BM, BM, WM, WN, true, true, kEither, true>(p, Work{(const char*)p.a + r.begin * p.lda * ES, (const char*)p.b + r.begin * p.ldb * ES, (int64_t)tm * BM, p.M,
                                                                     r.end - r.begin, r.expert * p.M, 0, tn, 0, xa, xb,
-                                                                    whole ? nullptr : partial + (int64_t)unit * p.M * ((p.N + 3) & ~3LL)});
+                                                                    whole ? nullptr : partial + (int64_t)unit * p.M * ((p.N + 3) & ~3LL)}, sa0, sb0, sa1, sb1);
+}
+
+// The three products of the gradients that need dG, dU and H alone, in one launch: the rows' gradients first, whose sums are
+// long, and the weights' in the places that these leave.
+template <typename T, int BM>
+__global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_grads_kernel(ExpertGrads a) {
+    FFN_TILE_LDS(BM, BM);
+    const int block = blockIdx.x;
+    if (block < a.end[0]) {
+        rows_group<T, BM, true, kPartial>(a.t[0], a.g[0], block, sa0, sb0, sa1, sb1);
+    } else {
+        const int k = block < a.end[1] ? 1 : 2;
+        sums_group<T, BM>(a.t[k], a.g[k], a.partial[k - 1], block - a.end[k - 1], sa0, sb0, sa1, sb1);
+    }
 }
 
 template <typename T, int BM, bool BC, int EPI> int run_rows(const TileArgs& p, const Groups& g, hipStream_t s) {
-    constexpr int WM = 2, WN = BM == 256 ? 4 : 2;
-    expert_rows_kernel<T, BM, WM, WN, BC, EPI><<<dim3((unsigned)(p.tiles_m * p.tiles_n * p.splits)), 64 * WM * WN, 0, s>>>(p, g);
+    expert_rows_kernel<T, BM, BC, EPI><<<dim3((unsigned)(p.tiles_m * p.tiles_n * p.splits)), BM == 256 ? 512 : 256, 0, s>>>(p, g);
     return (int)hipGetLastError();
 }
-template <typename T, int BM> int run_sums(const TileArgs& p, const Groups& g, float* partial, hipStream_t s) {
-    constexpr int WM = 2, WN = BM == 256 ? 4 : 2;
-    const int64_t step = sums_step((int64_t)p.tiles_m * p.tiles_n);
-    expert_sums_kernel<T, BM, WM, WN><<<dim3((unsigned)(step * p.splits)), 64 * WM * WN, 0, s>>>(p, g, partial);
+template <typename T, int BM> int run_grads(ExpertGrads a, hipStream_t s) {
+    int64_t end = 0;
+    for (int k = 0; k < 3; ++k) {
+        const TileArgs& t = a.t[k];
+        if (t.a) end += (k == 0 ? (int64_t)t.tiles_m * t.tiles_n : sums_step((int64_t)t.tiles_m * t.tiles_n)) * t.splits;
+        a.end[k] = (int32_t)end;
+    }
+    expert_grads_kernel<T, BM><<<dim3((unsigned)end), BM == 256 ? 512 : 256, 0, s>>>(a);
     return (int)hipGetLastError();
 }
 
@@ -83,9 +108,7 @@ template <typename T> int expert_rows(const TileArgs& p, const Groups& g, int32_
 #undef FFN_RUN
     return (int)hipErrorInvalidValue;
 }
-template <typename T> int expert_sums(const TileArgs& p, const Groups& g, float* partial, int32_t tile, hipStream_t s) {
-    return tile == 256 ? run_sums<T, 256>(p, g, partial, s) : run_sums<T, 128>(p, g, partial, s);
-}
+template <typename T> int expert_grads(const ExpertGrads& a, int32_t tile, hipStream_t s) { return tile == 256 ? run_grads<T, 256>(a, s) : run_grads<T, 128>(a, s); }
 
 }  // namespace dev
 }  // namespace ffn

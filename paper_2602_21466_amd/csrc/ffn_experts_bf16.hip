@@ -5,7 +5,5 @@ namespace ffn {
 int launch_expert_rows_bf16(const TileArgs& t, const Groups& g, int32_t epilogue, bool b_cols, int32_t tile, void* stream) {
     return dev::expert_rows<dev::bf16>(t, g, epilogue, b_cols, tile, (hipStream_t)stream);
 }
-int launch_expert_sums_bf16(const TileArgs& t, const Groups& g, float* partial, int32_t tile, void* stream) {
-    return dev::expert_sums<dev::bf16>(t, g, partial, tile, (hipStream_t)stream);
-}
+int launch_expert_grads_bf16(const ExpertGrads& a, int32_t tile, void* stream) { return dev::expert_grads<dev::bf16>(a, tile, (hipStream_t)stream); }
 }  // namespace ffn

@@ -5,7 +5,5 @@ namespace ffn {
 int launch_expert_rows_fp32(const TileArgs& t, const Groups& g, int32_t epilogue, bool b_cols, int32_t tile, void* stream) {
     return dev::expert_rows<float>(t, g, epilogue, b_cols, tile, (hipStream_t)stream);
 }
-int launch_expert_sums_fp32(const TileArgs& t, const Groups& g, float* partial, int32_t tile, void* stream) {
-    return dev::expert_sums<float>(t, g, partial, tile, (hipStream_t)stream);
-}
+int launch_expert_grads_fp32(const ExpertGrads& a, int32_t tile, void* stream) { return dev::expert_grads<float>(a, tile, (hipStream_t)stream); }
 }  // namespace ffn

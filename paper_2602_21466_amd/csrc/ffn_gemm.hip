@@ -105,7 +105,11 @@ __global__ __launch_bounds__(kThreads) void join_gate_kernel(TileArgs p, const f
 
 // The parts of the experts that have more than one, added in order.
 template <typename Out>
-__global__ __launch_bounds__(kThreads) void join_sums_kernel(TileArgs p, Groups g, const float* partial) {
+__global__ __launch_bounds__(kThreads) void join_sums_kernel(ExpertGrads a) {
+    const TileArgs& p = a.t[1 + blockIdx.z];
+    const Groups& g = a.g[1 + blockIdx.z];
+    const float* partial = a.partial[blockIdx.z];
+    if (!p.a) return;
     const int e = blockIdx.y, lane = threadIdx.x & 63;
     int first = 0, parts = 0;
     for (int e0 = 0; e0 <= e; e0 += 64) {
@@ -172,13 +176,16 @@ int launch_join_gate_rows(const TileArgs& p, int32_t epilogue, const float* part
     return (int)hipGetLastError();
 }
 
-int launch_join_sums(const TileArgs& t, const Groups& g, const float* partial, int32_t dtype, void* stream) {
+int launch_join_sums(const ExpertGrads& a, int32_t dtype, void* stream) {
     hipStream_t s = (hipStream_t)stream;
-    const unsigned all = groups(t.M * ((t.N + 3) >> 2));
-    const dim3 grid(all < 1024 ? all : 1024, (unsigned)g.experts);
-    if (dtype == FFN_FP32) join_sums_kernel<float><<<grid, kThreads, 0, s>>>(t, g, partial);
-    else if (dtype == FFN_BF16) join_sums_kernel<bf16><<<grid, kThreads, 0, s>>>(t, g, partial);
-    else join_sums_kernel<fp16><<<grid, kThreads, 0, s>>>(t, g, partial);
+    int64_t most = 0;
+    for (int k : {1, 2})
+        if (a.t[k].a && a.t[k].M * ((a.t[k].N + 3) >> 2) > most) most = a.t[k].M * ((a.t[k].N + 3) >> 2);
+    const unsigned all = groups(most);
+    const dim3 grid(all < 1024 ? all : 1024, (unsigned)(a.t[1].a ? a.g[1] : a.g[2]).experts, 2);
+    if (dtype == FFN_FP32) join_sums_kernel<float><<<grid, kThreads, 0, s>>>(a);
+    else if (dtype == FFN_BF16) join_sums_kernel<bf16><<<grid, kThreads, 0, s>>>(a);
+    else join_sums_kernel<fp16><<<grid, kThreads, 0, s>>>(a);
     return (int)hipGetLastError();
 }
 

@@ -281,13 +281,15 @@ struct Work {
 };
 
 // EXACT: operands as they lie in memory (see Loader).  Where rows end inside a chunk of 16 bytes, what follows them is set to
-// zero in the registers, on both sides, in the last step.
+// zero in the registers, on both sides, in the last step.  sa0 .. sb1: LDS, of BM and BN rows of 128 bytes, the kernel's own
+// arrays by FFN_TILE_LDS (apart, so that the compiler can tell them apart).
+#define FFN_TILE_LDS(BM, BN)                                      \
+    __shared__ __align__(1024) char sa0[BM * 128], sb0[BN * 128]; \
+    __shared__ __align__(1024) char sa1[BM * 128], sb1[BN * 128]
 template <typename T, int BM, int BN, int WM, int WN, bool AC, bool BC, int EPI, bool EXACT = false>
-__device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w) {
+__device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, char* sa0, char* sb0, char* sa1, char* sb1) {
 #ifdef __HIP_DEVICE_COMPILE__   // (the host's pass needs the launch stub alone)
     constexpr int NW = WM * WN, MT = BM / WM / 16, CW = BN / WN, NT = CW / 16, ES = (int)sizeof(T), kStep = 128 / ES;
-    __shared__ __align__(1024) char sa0[BM * 128], sb0[BN * 128];
-    __shared__ __align__(1024) char sa1[BM * 128], sb1[BN * 128];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * CW;
     constexpr int kCols = EPI == kGate ? BN / 2 : BN;      // columns of C a tile covers
@@ -548,9 +550,10 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w) {
 
 template <typename T, int BM, int BN, int WM, int WN, bool AC, bool BC, int EPI>
 __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
+    FFN_TILE_LDS(BM, BN);
     int tm, tn, split;
     place(blockIdx.x, p.tiles_m, p.tiles_n, p.splits, tm, tn, split);
-    tile_body<T, BM, BN, WM, WN, AC, BC, EPI>(p, Work{p.a, p.b, (int64_t)tm * BM, p.M, p.K, 0, p.M, tn, split});
+    tile_body<T, BM, BN, WM, WN, AC, BC, EPI>(p, Work{p.a, p.b, (int64_t)tm * BM, p.M, p.K, 0, p.M, tn, split}, sa0, sb0, sa1, sb1);
 }
 
 template <typename T, int BM, bool AC, bool BC, int EPI> int run_tile(const TileArgs& p, hipStream_t s) {
