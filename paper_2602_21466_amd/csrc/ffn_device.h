@@ -50,6 +50,26 @@ template <typename T> __device__ __forceinline__ void activate(int act, float g,
     }
 }
 
+// The same of N values: one branch for all, so that their arithmetic overlaps.
+template <typename T, int N, typename V> __device__ __forceinline__ void activate_all(int act, const V& g, V& v, V& dv) {
+#define FFN_ALL(ACT)              \
+    _Pragma("unroll")             \
+    for (int e = 0; e < N; ++e) { \
+        float a, d;               \
+        activate<T>(ACT, g[e], a, d); \
+        v[e] = a;                 \
+        dv[e] = d;                \
+    }
+    if (act == FFN_SILU) {
+        FFN_ALL(FFN_SILU)
+    } else if (act == FFN_GELU) {
+        FFN_ALL(FFN_GELU)
+    } else {
+        FFN_ALL(FFN_RELU)
+    }
+#undef FFN_ALL
+}
+
 // Philox 4x32, 10 rounds (Salmon et al. 2011): two 32 x 32 -> 64 bit products a round
 // mix the four counter words; the key steps by fixed constants (the golden ratio, sqrt 3 - 1).
 struct Words { uint32_t w[4]; };

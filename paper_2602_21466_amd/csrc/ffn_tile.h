@@ -473,10 +473,15 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, char
     static_assert(kFit >= 1 && 4 * kFit >= NW, "a turn buffer for every wave");
     float* turn = (float*)((wave / kFit == 0 ? sa0 : wave / kFit == 1 ? sb0 : wave / kFit == 2 ? sa1 : sb1) + wave % kFit * kTurn);
     constexpr int kLanes = EPI == kGate ? CW / 8 : CW / 4, kTake = 64 / kLanes;      // lanes a row, rows a turn
-    const int tc = (lane % kLanes) * 4;
+    const int tr = lane / kLanes, tc = (lane % kLanes) * 4;
+    // this wave's first column, and whether it and the ones behind it are all inside, with nothing to be written behind the
+    // last (EXACT: whoever reads the rows cuts them)
+    const int64_t nb = n0 + (EPI == kGate ? wn / 2 : wn), past = nb + kLanes * 4;
+    const int64_t pad = EXACT ? 0 : EPI == kGate ? p.ldc : EPI == kGateGrad ? (p.ldc > 2 * p.N || p.ldh > p.N ? p.N + 1 : 0) : 0;
+    const bool whole = past < p.N || (past == p.N && pad <= p.N);
 #pragma unroll
     for (int i = 0; i < MT; i += 2) {
-        const int64_t mb = m0 + wm + i * 16, n = n0 + (EPI == kGate ? wn / 2 : wn) + tc;
+        const int64_t mb = m0 + wm + i * 16, n = nb + tc;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -485,62 +490,105 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, char
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         // (kGateGrad: G and U of kAhead turns are asked for together)
-        constexpr int kTurns = 32 / kTake, kAhead = EPI == kGateGrad ? 4 : 1;
+        constexpr int kTurns = 32 / kTake, kAhead = EPI == kGateGrad ? 4 : 2;
+        const float* from = turn + tr * kRow + tc;
+        if (whole && mb + 32 <= w.m_end) {
+            // All 32 rows inside: a wave's addresses are one scalar and 32-bit offsets of its lanes.  (Beside a short k the
+            // epilogue is what counts: 11712 rows of 408 values to 2 x 1339 gated columns in bf16: 67 us, 79 with the bounds
+            // and the activation's branch at every value.)
+            const int64_t row = w.out_row + mb;
+            const uint32_t ld = (uint32_t)p.ldc;
+            char *c = nullptr, *h = nullptr, *sv = nullptr;
+            if constexpr (EPI == kPartial) c = (char*)((float*)p.c + ((int64_t)w.split * w.out_rows + row) * p.ldc + nb);
+            else c = (char*)((T*)p.c + row * p.ldc + nb);
+            if constexpr (EPI == kGate || EPI == kGateGrad) sv = (char*)(p.saved + mb * 2 * p.N + nb);
+            if constexpr (EPI == kGateGrad) h = (char*)((T*)p.h + mb * p.ldh + nb);
+            auto put = [](char* base, uint32_t at, f32x4 v, auto zero) {
+                typedef decltype(zero) Out;
+                typedef Out Out4 __attribute__((ext_vector_type(4)));
+                Out4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = (Out)v[e];
+                __builtin_memcpy(base + at, &o, sizeof(o));
+            };
+            auto get = [](const char* base, uint32_t at) {
+                f32x4 v;
+                __builtin_memcpy(&v, base + at, sizeof(v));
+                return v;
+            };
+            const uint32_t two = (uint32_t)(8 * p.N), up = (uint32_t)(4 * p.N);   // bytes of a row of `saved`, of half of one
 #pragma unroll 1
-        for (int k0 = 0; k0 < kTurns; k0 += kAhead) {
-        f32x4 gs[kAhead], us[kAhead];
-        if constexpr (EPI == kGateGrad) {
+            for (int k0 = 0; k0 < kTurns; k0 += kAhead) {
+                f32x4 gs[kAhead], us[kAhead];
+                if constexpr (EPI == kGateGrad) {
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const int64_t m = mb + lane / kLanes + (k0 + k) * kTake;
-                gs[k] = us[k] = f32x4{};
-                if (m < w.m_end) {
-                    gs[k] = load4(p.saved + m * 2 * p.N, n, p.N);
-                    us[k] = load4(p.saved + m * 2 * p.N + p.N, n, p.N);
+                    for (int k = 0; k < kAhead; ++k) {
+                        const uint32_t at = (tr + (k0 + k) * kTake) * two + tc * 4;
+                        gs[k] = get(sv, at);
+                        us[k] = get(sv + up, at);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const int dr = (k0 + k) * kTake;
+                    const uint32_t at = (tr + dr) * ld + tc;
+                    const f32x4 v = *(const f32x4*)(from + dr * kRow);
+                    if constexpr (EPI == kGate) {
+                        const f32x4 u = *(const f32x4*)(from + dr * kRow + CW / 2);
+                        f32x4 a, da;
+                        activate_all<T, 4>(p.act, v, a, da);
+                        put(c, at * ES, a * u, T());
+                        if (p.saved) {
+                            const uint32_t as = (tr + dr) * two + tc * 4;
+                            put(sv, as, v, 0.0f);
+                            put(sv + up, as, u, 0.0f);
+                        }
+                    } else if constexpr (EPI == kStore) {
+                        put(c, at * ES, v, T());
+                    } else if constexpr (EPI == kPartial) {
+                        put(c, at * 4, v, 0.0f);
+                    } else if constexpr (EPI == kEither) {
+                        if (w.part) put((char*)(w.part + mb * ((p.N + 3) & ~3LL) + nb), ((tr + dr) * (uint32_t)((p.N + 3) & ~3LL) + tc) * 4, v, 0.0f);
+                        else put(c, at * ES, v, T());
+                    } else {
+                        f32x4 a, da;
+                        activate_all<T, 4>(p.act, gs[k], a, da);
+                        put(c, at * ES, v * us[k] * da, T());
+                        put(c + p.N * ES, at * ES, v * a, T());
+                        put(h, ((tr + dr) * (uint32_t)p.ldh + tc) * ES, a * us[k], T());
+                    }
                 }
             }
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int r = lane / kLanes + (k0 + k) * kTake;
-            const int64_t m = mb + r;
-            if (m >= w.m_end) continue;
-            const f32x4 v = *(const f32x4*)(turn + r * kRow + tc);
-            if constexpr (EPI == kGate) {
-                const f32x4 u = *(const f32x4*)(turn + r * kRow + CW / 2 + tc);
-                f32x4 h;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float a, da;
-                    activate<T>(p.act, v[e], a, da);
-                    h[e] = a * u[e];
+        } else {
+#pragma unroll 1
+            for (int k0 = 0; k0 < kTurns; ++k0) {
+                const int r = tr + k0 * kTake;
+                const int64_t m = mb + r;
+                if (m >= w.m_end) continue;
+                const f32x4 v = *(const f32x4*)(turn + r * kRow + tc);
+                if constexpr (EPI == kGate) {
+                    const f32x4 u = *(const f32x4*)(turn + r * kRow + CW / 2 + tc);
+                    f32x4 a, da;
+                    activate_all<T, 4>(p.act, v, a, da);
+                    store4<T>((T*)p.c + m * p.ldc, n, p.N, EXACT ? 0 : p.ldc, a * u);
+                    if (p.saved) {
+                        store4<float>(p.saved + m * 2 * p.N, n, p.N, 0, v);
+                        store4<float>(p.saved + m * 2 * p.N + p.N, n, p.N, 0, u);
+                    }
+                } else if constexpr (EPI == kStore) {
+                    store4<T>((T*)p.c + (w.out_row + m) * p.ldc, n, p.N, 0, v);
+                } else if constexpr (EPI == kEither) {
+                    if (w.part) store4<float>(w.part + m * ((p.N + 3) & ~3LL), n, p.N, 0, v);
+                    else store4<T>((T*)p.c + (w.out_row + m) * p.ldc, n, p.N, 0, v);
+                } else if constexpr (EPI == kPartial) {
+                    store4<float>((float*)p.c + ((int64_t)w.split * w.out_rows + w.out_row + m) * p.ldc, n, p.N, 0, v);
+                } else {
+                    const f32x4 g = load4(p.saved + m * 2 * p.N, n, p.N), u = load4(p.saved + m * 2 * p.N + p.N, n, p.N);
+                    f32x4 a, da;
+                    activate_all<T, 4>(p.act, g, a, da);
+                    store_gate_grad<T>(p, m, n, v * u * da, v * a, a * u);
                 }
-                store4<T>((T*)p.c + m * p.ldc, n, p.N, p.ldc, h);
-                if (p.saved) {
-                    store4<float>(p.saved + m * 2 * p.N, n, p.N, 0, v);
-                    store4<float>(p.saved + m * 2 * p.N + p.N, n, p.N, 0, u);
-                }
-            } else if constexpr (EPI == kStore) {
-                store4<T>((T*)p.c + (w.out_row + m) * p.ldc, n, p.N, 0, v);
-            } else if constexpr (EPI == kEither) {
-                if (w.part) store4<float>(w.part + m * ((p.N + 3) & ~3LL), n, p.N, 0, v);
-                else store4<T>((T*)p.c + (w.out_row + m) * p.ldc, n, p.N, 0, v);
-            } else if constexpr (EPI == kPartial) {
-                store4<float>((float*)p.c + ((int64_t)w.split * w.out_rows + w.out_row + m) * p.ldc, n, p.N, 0, v);
-            } else {
-                const f32x4 g = gs[k], u = us[k];
-                f32x4 dg, du, h;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float a, da;
-                    activate<T>(p.act, g[e], a, da);
-                    dg[e] = v[e] * u[e] * da;
-                    du[e] = v[e] * a;
-                    h[e] = a * u[e];
-                }
-                store_gate_grad<T>(p, m, n, dg, du, h);
             }
-        }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
