@@ -97,7 +97,8 @@ struct ExpertGrads {
     TileArgs t[3];
     Groups g[3];
     float* partial[2];
-    int32_t end[3];                       // work-groups up to here; set by the launcher
+    int32_t order[3];                     // which product comes first, second, third
+    int32_t end[3];                       // work-groups up to here, in that order; set by the launcher
 };
 int launch_expert_grads_bf16(const ExpertGrads& a, int32_t tile, void* stream);
 int launch_expert_grads_fp16(const ExpertGrads& a, int32_t tile, void* stream);

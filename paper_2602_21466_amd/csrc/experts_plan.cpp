@@ -43,19 +43,27 @@ int check_rows(int64_t N, int64_t per_row, int64_t experts, int64_t width, int32
 // part) go to memory and a second kernel finishes them.
 struct Cut { int32_t tile, splits; bool joined; };
 
-// The shortest by a count in microseconds, as a single block's products are cut (ffn_plan.cpp), with what the host knows:
-// `groups(tile)` work-groups by the mean, of `steps` steps of k each.
+// What a compute unit takes for a step of k (64 values of 16 bits, 32 of 32) of a 256-wide tile, or of two 128-wide ones, in
+// microseconds, and the steps that a tile's start and end stand for (16384 x 4096 outputs, k of 64 and 256: bf16 39 and 57.5
+// us by 256-wide tiles, 40 and 67.5 by 128-wide ones; fp32 96 and 215, 83 and 219).
+struct Cost { double step, ends; };
+Cost cost_of(int32_t tile, bool wide) { return wide ? (tile == 256 ? Cost{4.9, 2.8} : Cost{2.8, 1.8}) : tile == 256 ? Cost{1.6, 5.5} : Cost{1.12, 4.0}; }
+
+// The shortest by a count of those, as a single block's products are cut (ffn_plan.cpp), with what the host knows:
+// `groups(tile)` work-groups by the mean, of `steps` steps of k each.  256 of 256-wide tiles or 512 of 128-wide ones run at
+// one time, and one 128-wide tile alone takes three quarters of what two take.  Parts of k cost a launch, a tenth of a
+// microsecond a part and their sums, written and read once at 4 TB/s; the gate's gradient in the tiles' own epilogue costs
+// ten where they are few.
 template <typename Groups> Cut shortest(Groups groups, int64_t steps, double outputs, bool wide, bool gate_grad) {
-    const double ends = wide ? 2.0 : 4.0;
     Cut best = {128, 1, false};
     double least = 1e300;
     for (int32_t tile : {256, 128}) {
         const double all = groups(tile), slots = tile == 256 ? 256.0 : 512.0;
-        const double step = tile == 256 ? (wide ? 4.5 : 1.6) : (wide ? 2.6 : 1.06);
+        const Cost cost = cost_of(tile, wide);
         for (int32_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); ++s) {
-            const double n = all * s / slots;
-            const double rounds = n > 1.0 ? n + 0.5 : tile == 128 && n <= 0.5 ? 0.75 : 1.0;
-            const double t = rounds * ((double)tiles(steps, s) + ends) * step;
+            const double n = all * s / slots, full = std::floor(n), rest = n - full;
+            const double rounds = full + (rest == 0.0 ? 0.0 : tile == 128 && rest <= 0.5 ? 0.75 : 1.0);
+            const double t = rounds * ((double)tiles(steps, s) + cost.ends) * cost.step;
             const double join = 3.0 + 0.1 * s + outputs * s * 8.0 / 4e6, own = gate_grad ? 10.0 : 0.0;
             const bool joined = s > 1 || own > join;
             if (t + (joined ? join : own) < least) { least = t + (joined ? join : own); best = {tile, s, joined}; }
@@ -70,35 +78,43 @@ struct Shape { int64_t R, E, N, K; };
 // Tiles of rows there may be.
 int64_t most_tiles(const Shape& s, int32_t tile) { return s.R / tile + (s.E < s.R ? s.E : s.R); }
 
-// [R, N], B by expert.  A run of rows ends in half a tile by the mean.
+// By the mean, and a little more: a run of rows ends in half a tile, with a third of a tile as the standard deviation.
+double mean_tiles(const Shape& s, int32_t tile) {
+    const double with = (double)(s.E < s.R ? s.E : s.R);
+    return (double)s.R / tile + (s.E > 1 ? 0.5 * with + 0.3 * std::sqrt(with) : 0.0);
+}
+
+// [R, N], B by expert.
 Cut cut_rows(const Shape& s, int32_t dtype, int32_t epilogue) {
     const bool wide = dtype == FFN_FP32;
-    auto groups = [&](int32_t tile) { return ((double)s.R / tile + 0.5 * (double)(s.E < s.R ? s.E : s.R)) * (double)tiles(s.N, tile); };
+    auto groups = [&](int32_t tile) { return (s.E > 1 ? mean_tiles(s, tile) : (double)tiles(s.R, tile)) * (double)tiles(s.N, tile); };
     return shortest(groups, tiles(s.K, wide ? 32 : 64), (double)s.R * s.N, wide, epilogue == ffn::kGateGrad);
 }
 
 // The gradients' products of one launch: the rows' [R, d_in], whose k is in `splits` parts, and the weights', sums over each
 // expert's rows in parts of `chunk` of them (0: one part an expert).  Counted like shortest(): all work-groups' steps over
-// those that run at one time, then half of the longest one alone; a few experts may have three times the mean.
-struct GradCut { int32_t tile, splits, chunk; };
+// those that run at one time, then half of one that comes late, of the shorter kind; a few experts may have three times the
+// mean.
+struct GradCut { int32_t tile, splits, chunk; bool sums_first; };
 GradCut cut_grads(const ffn_experts_s* p, int64_t R) {
     const bool wide = p->dtype == FFN_FP32;
     const int64_t di = p->d_in, df = p->d_ff, d_o = p->d_out, E = p->experts, kstep = wide ? 32 : 64, steps = tiles(2 * df, kstep);
-    const double k = (double)kstep, ends = wide ? 2.0 : 4.0, mean = (double)R / E, longest = 3.0 * mean < (double)R ? 3.0 * mean : (double)R;
+    const double k = (double)kstep, mean = (double)R / E, longest = 3.0 * mean < (double)R ? 3.0 * mean : (double)R;
     const double outputs = (double)(2 * df * di) + (double)(d_o * df);
-    GradCut best = {128, 1, 0};
+    GradCut best = {128, 1, 0, false};
     double least = 1e300;
     for (int32_t tile : {256, 128}) {
-        const double slots = tile == 256 ? 256.0 : 512.0, step = tile == 256 ? (wide ? 4.5 : 1.6) : (wide ? 2.6 : 1.06);
-        const double rows = ((double)R / tile + 0.5 * (double)(E < R ? E : R)) * (double)tiles(di, tile);
+        const double slots = tile == 256 ? 256.0 : 512.0, step = cost_of(tile, wide).step, ends = cost_of(tile, wide).ends;
+        const double rows = mean_tiles({R, E, di, 0}, tile) * (double)tiles(di, tile);
         const double each = (double)(tiles(2 * df, tile) * tiles(di, tile) + tiles(d_o, tile) * tiles(df, tile));
         auto consider = [&](int32_t chunk) {
             const double parts = chunk ? (double)R / chunk + 0.5 * E : (double)E, sums = each * ((double)R / k + parts * ends);
             const double one = (chunk ? (double)chunk : longest) / k + ends, join = chunk ? 4.0 + parts * outputs * 8.0 / 4e6 : 0.0;
             for (int32_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); s += s < 4 ? 1 : s / 2) {
-                const double own = (double)tiles(steps, s) + ends, all = (rows * s * own + sums) / slots, last = own > one ? own : one;
-                const double t = step * (rows * s + each * parts <= slots ? (last > all ? last : all) : all + 0.5 * last) + join + 0.1 * s + (double)R * di * s * 8.0 / 4e6;
-                if (t < least) { least = t; best = {tile, s, chunk}; }
+                const double own = (double)tiles(steps, s) + ends, all = (rows * s * own + sums) / slots, late = rows * s + each * parts <= slots ? 0.0 : 0.5 * (own < one ? own : one);
+                const double longest_one = own > one ? own : one, run = all + late > longest_one ? all + late : longest_one;
+                const double t = step * run + join + 0.1 * s + (double)R * di * s * 8.0 / 4e6;
+                if (t < least) { least = t; best = {tile, s, chunk, one > own}; }
             }
         };
         consider(0);
@@ -178,7 +194,7 @@ Few few_cut(const Shape& s, bool gate, int32_t dtype) {
 bool few_rows(int64_t R, const ffn_experts_s* p) {
     const int64_t with = p->experts < R ? p->experts : R, mean = tiles(R, with);
     const int64_t bytes = with * p->d_ff * (2 * p->d_in + p->d_out) * size_of(p->dtype);
-    return mean <= (bytes <= (1 << 25) ? 40 : p->dtype == FFN_FP32 ? 24 : 16);
+    return mean <= (p->dtype == FFN_FP32 ? 24 : bytes <= (1 << 25) ? 30 : 16);
 }
 int few_product(ffn::FewArgs p, const ffn::Groups& g, int32_t epilogue, int32_t dtype, void* stream) {
     const bool gate = epilogue == ffn::kGate;
@@ -493,6 +509,7 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
     if (rc != CGTP_OK || (!grad_x && !grad_w_in && !grad_w_out)) return rc;
     const GradCut c = cut_grads(plan, R);
     ffn::ExpertGrads a = {};
+    for (int k = 0; k < 3; ++k) a.order[k] = c.sums_first ? (k + 1) % 3 : k;
     auto sums = [&](int k, const Matrix& A, const Matrix& B, int64_t M, int64_t columns, void* to, int64_t part) {
         ffn::TileArgs& w = a.t[k];
         w.a = A.p; w.lda = A.ld; w.b = B.p; w.ldb = B.ld;

@@ -70,18 +70,15 @@ __device__ __forceinline__ void sums_group(TileArgs p, const Groups& g, float* p
                                                                     whole ? nullptr : partial + (int64_t)unit * p.M * ((p.N + 3) & ~3LL)}, sa0, sb0, sa1, sb1);
 }
 
-// The three products of the gradients that need dG, dU and H alone, in one launch: the rows' gradients first, whose sums are
-// long, and the weights' in the places that these leave.
+// The three products of the gradients that need dG, dU and H alone, in one launch, those of the longest sums first: the
+// others take the places that these leave.
 template <typename T, int BM>
 __global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_grads_kernel(ExpertGrads a) {
     FFN_TILE_LDS(BM, BM);
-    const int block = blockIdx.x;
-    if (block < a.end[0]) {
-        rows_group<T, BM, true, kPartial>(a.t[0], a.g[0], block, sa0, sb0, sa1, sb1);
-    } else {
-        const int k = block < a.end[1] ? 1 : 2;
-        sums_group<T, BM>(a.t[k], a.g[k], a.partial[k - 1], block - a.end[k - 1], sa0, sb0, sa1, sb1);
-    }
+    const int at = (int)blockIdx.x < a.end[0] ? 0 : (int)blockIdx.x < a.end[1] ? 1 : 2, k = a.order[at];
+    const int block = at ? blockIdx.x - a.end[at - 1] : blockIdx.x;
+    if (k == 0) rows_group<T, BM, true, kPartial>(a.t[0], a.g[0], block, sa0, sb0, sa1, sb1);
+    else sums_group<T, BM>(a.t[k], a.g[k], a.partial[k - 1], block, sa0, sb0, sa1, sb1);
 }
 
 template <typename T, int BM, bool BC, int EPI> int run_rows(const TileArgs& p, const Groups& g, hipStream_t s) {
@@ -90,10 +87,11 @@ template <typename T, int BM, bool BC, int EPI> int run_rows(const TileArgs& p, 
 }
 template <typename T, int BM> int run_grads(ExpertGrads a, hipStream_t s) {
     int64_t end = 0;
-    for (int k = 0; k < 3; ++k) {
+    for (int at = 0; at < 3; ++at) {
+        const int k = a.order[at];
         const TileArgs& t = a.t[k];
         if (t.a) end += (k == 0 ? (int64_t)t.tiles_m * t.tiles_n : sums_step((int64_t)t.tiles_m * t.tiles_n)) * t.splits;
-        a.end[k] = (int32_t)end;
+        a.end[at] = (int32_t)end;
     }
     expert_grads_kernel<T, BM><<<dim3((unsigned)end), BM == 256 ? 512 : 256, 0, s>>>(a);
     return (int)hipGetLastError();
