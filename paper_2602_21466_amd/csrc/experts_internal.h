@@ -76,6 +76,7 @@ struct Groups {
     int32_t chunk;                        // sums: rows of a part; 0: an expert's rows are one part
     const int32_t* source;                // rows of A are those of slots source[..] / per_row; NULL: they are in their order
     int32_t per_row;
+    bool deep;                            // rows: no more tiles than compute units, by the mean (16-bit arrays, 128-wide tiles)
 };
 // Operands lie in memory as they are: rows start on any element, with anything behind them.
 // C = A B^T for the rows of every expert with its own B: t.M is groups.rows, t.tiles_m as many tiles of rows as there can

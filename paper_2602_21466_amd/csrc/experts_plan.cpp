@@ -78,16 +78,18 @@ struct Shape { int64_t R, E, N, K; };
 // Tiles of rows there may be.
 int64_t most_tiles(const Shape& s, int32_t tile) { return s.R / tile + (s.E < s.R ? s.E : s.R); }
 
-// By the mean, and a little more: a run of rows ends in half a tile, with a third of a tile as the standard deviation.
+// By the mean, and a little more: each expert with a row has a tile or more, and a run of rows ends in half a tile, with a
+// third of a tile as the standard deviation.
 double mean_tiles(const Shape& s, int32_t tile) {
-    const double with = (double)(s.E < s.R ? s.E : s.R);
-    return (double)s.R / tile + (s.E > 1 ? 0.5 * with + 0.3 * std::sqrt(with) : 0.0);
+    if (s.E == 1) return (double)tiles(s.R, tile);
+    const double with = (double)(s.E < s.R ? s.E : s.R), each = (double)s.R / (with * tile) + 0.5;
+    return each < 1.0 ? with : with * each + 0.3 * std::sqrt(with);
 }
 
 // [R, N], B by expert.
 Cut cut_rows(const Shape& s, int32_t dtype, int32_t epilogue) {
     const bool wide = dtype == FFN_FP32;
-    auto groups = [&](int32_t tile) { return (s.E > 1 ? mean_tiles(s, tile) : (double)tiles(s.R, tile)) * (double)tiles(s.N, tile); };
+    auto groups = [&](int32_t tile) { return mean_tiles(s, tile) * (double)tiles(s.N, tile); };
     return shortest(groups, tiles(s.K, wide ? 32 : 64), (double)s.R * s.N, wide, epilogue == ffn::kGateGrad);
 }
 
@@ -152,13 +154,14 @@ int launch_rows(const ffn::TileArgs& t, const ffn::Groups& g, int32_t epilogue, 
 }
 // Runs the product of rows whose operands, sizes (t.M: the sorted rows) and results t describes; `partial` is scratch of
 // rows_partial() (kGate: of 2 N columns).
-int rows_product(ffn::TileArgs t, const ffn::Groups& g, int32_t epilogue, bool bc, int32_t dtype, void* partial, void* stream) {
+int rows_product(ffn::TileArgs t, ffn::Groups g, int32_t epilogue, bool bc, int32_t dtype, void* partial, void* stream) {
     const int64_t columns = epilogue == ffn::kGate ? 2 * t.N : t.N;
     const Shape s = {t.M, g.experts, columns, t.K};
     const Cut c = cut_rows(s, dtype, epilogue);
     t.tiles_m = (int32_t)most_tiles(s, c.tile);
     t.tiles_n = (int32_t)tiles(columns, c.tile);
     t.splits = c.splits;
+    g.deep = dtype != FFN_FP32 && c.tile == 128 && mean_tiles(s, 128) * t.tiles_n * c.splits <= 256.0;
     if (!c.joined) return status(launch_rows(t, g, epilogue, bc, dtype, c.tile, stream));
     ffn::TileArgs p = t;
     p.c = partial;

@@ -12,8 +12,8 @@ namespace ffn {
 namespace dev {
 
 // Work-group `block` of C = A B^T by expert.
-template <typename T, int BM, bool BC, int EPI>
-__device__ __forceinline__ void rows_group(const TileArgs& p, const Groups& g, int block, char* sa0, char* sb0, char* sa1, char* sb1) {
+template <typename T, int BM, bool BC, int EPI, int NB>
+__device__ __forceinline__ void rows_group(const TileArgs& p, const Groups& g, int block, const TileLds<NB>& lds) {
     constexpr int WM = 2, WN = BM == 256 ? 4 : 2;
     const int lane = threadIdx.x & 63;
     Scan first;
@@ -23,13 +23,19 @@ __device__ __forceinline__ void rows_group(const TileArgs& p, const Groups& g, i
     place(block, total, p.tiles_n, p.splits, tm, tn, split);
     const Run r = find_tile(g, lane, BM, 0, first, tm);
     const Exact xa = {(const char*)g.a_end, g.source, (uint32_t)g.per_row, (uint32_t)g.rows}, xb = {(const char*)g.b_end, nullptr, 1, 0};
-    tile_body<T, BM, BM, WM, WN, false, BC, EPI, true>(p, Work{p.a, (const char*)p.b + r.expert * g.b_step, (int64_t)r.begin + (int64_t)r.tile * BM, r.end, p.K, 0, p.M,
-                                                              tn, split, xa, xb, nullptr}, sa0, sb0, sa1, sb1);
+    tile_body<T, BM, BM, WM, WN, false, BC, EPI, true, NB>(p, Work{p.a, (const char*)p.b + r.expert * g.b_step, (int64_t)r.begin + (int64_t)r.tile * BM, r.end, p.K, 0, p.M,
+                                                              tn, split, xa, xb, nullptr}, lds);
 }
 template <typename T, int BM, bool BC, int EPI>
 __global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_rows_kernel(TileArgs p, Groups g) {
     FFN_TILE_LDS(BM, BM);
-    rows_group<T, BM, BC, EPI>(p, g, blockIdx.x, sa0, sb0, sa1, sb1);
+    rows_group<T, BM, BC, EPI>(p, g, blockIdx.x, lds);
+}
+// The same for launches of no more tiles than compute units: what a step waits for is memory's latency, not its rate.
+template <typename T, bool BC, int EPI>
+__global__ __launch_bounds__(256) void expert_rows_deep_kernel(TileArgs p, Groups g) {
+    FFN_TILE_LDS4(128, 128);
+    rows_group<T, 128, BC, EPI>(p, g, blockIdx.x, lds);
 }
 
 constexpr int kManyTiles = 64;
@@ -39,8 +45,8 @@ __host__ __device__ __forceinline__ constexpr int64_t sums_step(int64_t tiles) {
 // does), each part's to all dies, as its rows may be many more than another's; where they are few, one after the other.  An
 // expert of many rows is cut into parts of them, so that no work-group has
 // many times another's steps (5 experts, the largest of 8192 rows' half, 3281 x 512 in fp32: 160 us, 294 without).
-template <typename T, int BM>
-__device__ __forceinline__ void sums_group(TileArgs p, const Groups& g, float* partial, int block, char* sa0, char* sb0, char* sa1, char* sb1) {
+template <typename T, int BM, int NB>
+__device__ __forceinline__ void sums_group(TileArgs p, const Groups& g, float* partial, int block, const TileLds<NB>& lds) {
     constexpr int WM = 2, WN = BM == 256 ? 4 : 2;
     const int lane = threadIdx.x & 63, tiles = p.tiles_m * p.tiles_n, step = (int)sums_step(tiles);
     const int unit = block / step, id = block - unit * step;
@@ -65,9 +71,9 @@ __device__ __forceinline__ void sums_group(TileArgs p, const Groups& g, float* p
     constexpr int64_t ES = (int64_t)sizeof(T);
     const Exact xa = {(const char*)g.a_end, nullptr, 1, 0}, xb = {(const char*)g.b_end, nullptr, 1, 0};
     p.splits = 1;
-    tile_body<T, BM, BM, WM, WN, true, true, kEither, true>(p, Work{(const char*)p.a + r.begin * p.lda * ES, (const char*)p.b + r.begin * p.ldb * ES, (int64_t)tm * BM, p.M,
+    tile_body<T, BM, BM, WM, WN, true, true, kEither, true, NB>(p, Work{(const char*)p.a + r.begin * p.lda * ES, (const char*)p.b + r.begin * p.ldb * ES, (int64_t)tm * BM, p.M,
                                                                     r.end - r.begin, r.expert * p.M, 0, tn, 0, xa, xb,
-                                                                    whole ? nullptr : partial + (int64_t)unit * p.M * ((p.N + 3) & ~3LL)}, sa0, sb0, sa1, sb1);
+                                                                    whole ? nullptr : partial + (int64_t)unit * p.M * ((p.N + 3) & ~3LL)}, lds);
 }
 
 // The three products of the gradients that need dG, dU and H alone, in one launch, those of the longest sums first: the
@@ -77,12 +83,18 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_grads_kernel(Exp
     FFN_TILE_LDS(BM, BM);
     const int at = (int)blockIdx.x < a.end[0] ? 0 : (int)blockIdx.x < a.end[1] ? 1 : 2, k = a.order[at];
     const int block = at ? blockIdx.x - a.end[at - 1] : blockIdx.x;
-    if (k == 0) rows_group<T, BM, true, kPartial>(a.t[0], a.g[0], block, sa0, sb0, sa1, sb1);
-    else sums_group<T, BM>(a.t[k], a.g[k], a.partial[k - 1], block, sa0, sb0, sa1, sb1);
+    if (k == 0) rows_group<T, BM, true, kPartial>(a.t[0], a.g[0], block, lds);
+    else sums_group<T, BM>(a.t[k], a.g[k], a.partial[k - 1], block, lds);
 }
 
 template <typename T, int BM, bool BC, int EPI> int run_rows(const TileArgs& p, const Groups& g, hipStream_t s) {
-    expert_rows_kernel<T, BM, BC, EPI><<<dim3((unsigned)(p.tiles_m * p.tiles_n * p.splits)), BM == 256 ? 512 : 256, 0, s>>>(p, g);
+    const dim3 grid((unsigned)(p.tiles_m * p.tiles_n * p.splits));
+    if constexpr (BM == 128 && sizeof(T) == 2)
+        if (g.deep) {
+            expert_rows_deep_kernel<T, BC, EPI><<<grid, 256, 0, s>>>(p, g);
+            return (int)hipGetLastError();
+        }
+    expert_rows_kernel<T, BM, BC, EPI><<<grid, BM == 256 ? 512 : 256, 0, s>>>(p, g);
     return (int)hipGetLastError();
 }
 template <typename T, int BM> int run_grads(ExpertGrads a, hipStream_t s) {

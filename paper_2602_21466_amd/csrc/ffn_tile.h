@@ -282,16 +282,28 @@ struct Work {
     float* part;                          // kEither: where the sums go, in rows of N up to a multiple of four; NULL: C
 };
 
+// A work-group's LDS: NB buffers of both operands, BM and BN rows of 128 bytes each, the kernel's own arrays (apart, so that
+// the compiler can tell them apart).
+template <int NB> struct TileLds { char *a[NB], *b[NB]; };
+#define FFN_TILE_LDS(BM, BN)                                       \
+    __shared__ __align__(1024) char sa0[BM * 128], sb0[BN * 128];  \
+    __shared__ __align__(1024) char sa1[BM * 128], sb1[BN * 128];  \
+    const TileLds<2> lds = {{sa0, sa1}, {sb0, sb1}}
+#define FFN_TILE_LDS4(BM, BN)                                      \
+    __shared__ __align__(1024) char sa0[BM * 128], sb0[BN * 128];  \
+    __shared__ __align__(1024) char sa1[BM * 128], sb1[BN * 128];  \
+    __shared__ __align__(1024) char sa2[BM * 128], sb2[BN * 128];  \
+    __shared__ __align__(1024) char sa3[BM * 128], sb3[BN * 128];  \
+    const TileLds<4> lds = {{sa0, sa1, sa2, sa3}, {sb0, sb1, sb2, sb3}}
+
 // EXACT: operands as they lie in memory (see Loader).  Where rows end inside a chunk of 16 bytes, what follows them is set to
-// zero in the registers, on both sides, in the last step.  sa0 .. sb1: LDS, of BM and BN rows of 128 bytes, the kernel's own
-// arrays by FFN_TILE_LDS (apart, so that the compiler can tell them apart).
-#define FFN_TILE_LDS(BM, BN)                                      \
-    __shared__ __align__(1024) char sa0[BM * 128], sb0[BN * 128]; \
-    __shared__ __align__(1024) char sa1[BM * 128], sb1[BN * 128]
-template <typename T, int BM, int BN, int WM, int WN, bool AC, bool BC, int EPI, bool EXACT = false>
-__device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, char* sa0, char* sb0, char* sa1, char* sb1) {
+// zero in the registers, on both sides, in the last step.
+// NB == 4 (four waves of 16-bit arrays): three steps are in flight where a work-group has a compute unit for itself.
+template <typename T, int BM, int BN, int WM, int WN, bool AC, bool BC, int EPI, bool EXACT = false, int NB = 2>
+__device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, const TileLds<NB>& lds) {
 #ifdef __HIP_DEVICE_COMPILE__   // (the host's pass needs the launch stub alone)
     constexpr int NW = WM * WN, MT = BM / WM / 16, CW = BN / WN, NT = CW / 16, ES = (int)sizeof(T), kStep = 128 / ES;
+    char *const sa0 = lds.a[0], *const sb0 = lds.b[0], *const sa1 = lds.a[1], *const sb1 = lds.b[1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * CW;
     constexpr int kCols = EPI == kGate ? BN / 2 : BN;      // columns of C a tile covers
@@ -448,26 +460,48 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, char
             if (wave < 4) meet();
         } else {
             // While the matrix instructions of one half of a step run, the fragments of the next half are read.  Between
-            // the halves all waves meet: by then each has read the last of this step's buffer, which takes the step after
-            // next from memory, and the next step's data, asked for a whole step earlier, is there.
-            auto step = [&](char* a, char* b, char* an, char* bn, int s, bool more) {
-                read(a, b, 1, s);
+            // the halves all waves meet: by then each has read the last of this step's buffer, which takes the step NB
+            // further on from memory, and the next step's data, asked for NB - 1 steps earlier, is there.
+            constexpr int kIssued = (BM + BN) * 128 / 1024 / NW;   // a wave's direct loads a step
+            static_assert(NB == 2 || (NB == 4 && kIssued == 8), "the waits below");
+            // All waves, with step s's data: own LDS reads are done, and of the direct loads those of later steps, of which
+            // `ahead` at the most have been asked for, may be in flight.
+            auto arrived = [&](int s, int ahead) {
+                if constexpr (NB == 2) {
+                    landed();
+                } else {
+                    const int later = n - 1 - s < ahead ? n - 1 - s : ahead;
+                    if (later >= 3) __builtin_amdgcn_s_waitcnt(0x4078);        // 24 loads
+                    else if (later == 2) __builtin_amdgcn_s_waitcnt(0x4070);   // 16
+                    else if (later == 1) __builtin_amdgcn_s_waitcnt(0x0078);   // 8
+                    else __builtin_amdgcn_s_waitcnt(0x0070);
+                    __builtin_amdgcn_sched_barrier(0);
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");   // (no read moves up)
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            auto step = [&](int at, int s) {
+                const int next = (at + 1) % NB;
+                read(lds.a[at], lds.b[at], 1, s);
                 multiply(0);
-                landed();
-                if (more) issue(a, b);
-                read(an, bn, 0, s + 1);
+                arrived(s + 1, NB - 2);
+                if (s + NB < n) issue(lds.a[at], lds.b[at]);
+                read(lds.a[next], lds.b[next], 0, s + 1);
                 multiply(1);
             };
-            if (n > 0) issue(sa0, sb0);
-            if (n > 1) issue(sa1, sb1);
-            landed();
+#pragma unroll
+            for (int k = 0; k < NB; ++k)
+                if (n > k) issue(lds.a[k], lds.b[k]);
+            arrived(0, NB - 1);
             read(sa0, sb0, 0, 0);
             int s = 0;
-            for (; s + 1 < n; s += 2) {
-                step(sa0, sb0, sa1, sb1, s, s + 2 < n);
-                step(sa1, sb1, sa0, sb0, s + 1, s + 3 < n);
-            }
-            if (s < n) step(sa0, sb0, sa1, sb1, s, false);
+            for (; s + NB <= n; s += NB)
+#pragma unroll
+                for (int k = 0; k < NB; ++k) step(k, s + k);
+#pragma unroll
+            for (int k = 0; k < NB - 1; ++k)
+                if (s + k < n) step(k, s + k);
         }
     }
 
@@ -607,7 +641,7 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(TileArgs p) {
     FFN_TILE_LDS(BM, BN);
     int tm, tn, split;
     place(blockIdx.x, p.tiles_m, p.tiles_n, p.splits, tm, tn, split);
-    tile_body<T, BM, BN, WM, WN, AC, BC, EPI>(p, Work{p.a, p.b, (int64_t)tm * BM, p.M, p.K, 0, p.M, tn, split}, sa0, sb0, sa1, sb1);
+    tile_body<T, BM, BN, WM, WN, AC, BC, EPI>(p, Work{p.a, p.b, (int64_t)tm * BM, p.M, p.K, 0, p.M, tn, split}, lds);
 }
 
 template <typename T, int BM, bool AC, bool BC, int EPI> int run_tile(const TileArgs& p, hipStream_t s) {
