@@ -189,31 +189,33 @@ template <typename T> __device__ __forceinline__ void zero_behind(const RouteArg
         store_chunk((T*)p.out_sorted + (held + k.row) * p.ld_sorted, k.at * 8, p.ld_sorted, zero);
 }
 
-// This thread's row, and its place among the row's threads.
+// This thread's first row, its place among the row's threads, and from a row to its next one (of `groups` work-groups).
 template <int TPR> __device__ __forceinline__ int64_t own_row(int& t) {
     t = threadIdx.x % TPR;
     const int sub = TPR >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : threadIdx.x / TPR;
     return (int64_t)blockIdx.x * (kThreads / TPR) + sub;
 }
+template <int TPR> __device__ __forceinline__ int64_t row_step(unsigned groups) { return (int64_t)groups * (kThreads / TPR); }
 
 template <typename T, int TPR>
 __global__ __launch_bounds__(kThreads) void gather_kernel(RouteArgs p) {
     if (p.offsets && blockIdx.x >= gridDim.x - kZeroGroups) return zero_behind<T>(p);
     int t;
-    const int64_t n = own_row<TPR>(t), D = p.width;
-    if (n >= p.N) return;
-    const T* row = (const T*)p.rows + n * p.ld;
+    const int64_t D = p.width;
     const bool past = large<T>(p);
-    const int32_t* place = p.place + n * p.per_row;
-    for (int64_t c = t * 8; c < D; c += TPR * 16) {
-        const int64_t c2 = c + TPR * 8;
-        const auto v = load_chunk(row, c, D), v2 = load_chunk(row, c2 < D ? c2 : c, D);
-        for (int j = 0; j < p.per_row; ++j) {
-            const uint32_t to = (uint32_t)place[j];
-            if (to >= (uint64_t)p.slots) continue;
-            T* out = (T*)p.out_sorted + (int64_t)to * p.ld_sorted;
-            put_chunk(out, c, p.ld_sorted, v, past);
-            if (c2 < D) put_chunk(out, c2, p.ld_sorted, v2, past);
+    for (int64_t n = own_row<TPR>(t); n < p.N; n += row_step<TPR>(gridDim.x - (p.offsets ? kZeroGroups : 0))) {
+        const T* row = (const T*)p.rows + n * p.ld;
+        const int32_t* place = p.place + n * p.per_row;
+        for (int64_t c = t * 8; c < D; c += TPR * 16) {
+            const int64_t c2 = c + TPR * 8;
+            const auto v = load_chunk(row, c, D), v2 = load_chunk(row, c2 < D ? c2 : c, D);
+            for (int j = 0; j < p.per_row; ++j) {
+                const uint32_t to = (uint32_t)place[j];
+                if (to >= (uint64_t)p.slots) continue;
+                T* out = (T*)p.out_sorted + (int64_t)to * p.ld_sorted;
+                put_chunk(out, c, p.ld_sorted, v, past);
+                if (c2 < D) put_chunk(out, c2, p.ld_sorted, v2, past);
+            }
         }
     }
 }
@@ -221,42 +223,43 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(RouteArgs p) {
 template <typename T, int TPR>
 __global__ __launch_bounds__(kThreads) void combine_kernel(RouteArgs p) {
     int t;
-    const int64_t n = own_row<TPR>(t), D = p.width;
-    if (n >= p.N) return;
-    const int32_t* place = p.place + n * p.per_row;
-    const float* weights = p.weights ? p.weights + n * p.per_row : nullptr;
+    const int64_t D = p.width;
     const bool past = large<T>(p);
-    for (int64_t c = t * 8; c < D; c += TPR * 16) {
-        const int64_t c2 = c + TPR * 8;
-        float sum[2][8] = {};
-        for (int k = 0; k < p.per_row; k += 4) {
-            typename Chunk<T>::V v[4][2] = {};
-            float w[4];
+    for (int64_t n = own_row<TPR>(t); n < p.N; n += row_step<TPR>(gridDim.x)) {
+        const int32_t* place = p.place + n * p.per_row;
+        const float* weights = p.weights ? p.weights + n * p.per_row : nullptr;
+        for (int64_t c = t * 8; c < D; c += TPR * 16) {
+            const int64_t c2 = c + TPR * 8;
+            float sum[2][8] = {};
+            for (int k = 0; k < p.per_row; k += 4) {
+                typename Chunk<T>::V v[4][2] = {};
+                float w[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t from = k + j < p.per_row ? (uint32_t)place[k + j] : ~0u;
-                w[j] = 0.0f;
-                if (from >= (uint64_t)p.slots) continue;
-                w[j] = weights ? weights[k + j] : 1.0f;
-                const T* row = (const T*)p.sorted + (int64_t)from * D;
-                v[j][0] = load_chunk(row, c, D);
-                v[j][1] = load_chunk(row, c2 < D ? c2 : c, D);
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t from = k + j < p.per_row ? (uint32_t)place[k + j] : ~0u;
+                    w[j] = 0.0f;
+                    if (from >= (uint64_t)p.slots) continue;
+                    w[j] = weights ? weights[k + j] : 1.0f;
+                    const T* row = (const T*)p.sorted + (int64_t)from * D;
+                    v[j][0] = load_chunk(row, c, D);
+                    v[j][1] = load_chunk(row, c2 < D ? c2 : c, D);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        sum[0][e] += w[j] * to_f32(v[j][0][e]);
+                        sum[1][e] += w[j] * to_f32(v[j][1][e]);
+                    }
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int i = 0; i < 2; ++i) {
+                typename Chunk<T>::V o;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    sum[0][e] += w[j] * to_f32(v[j][0][e]);
-                    sum[1][e] += w[j] * to_f32(v[j][1][e]);
-                }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            typename Chunk<T>::V o;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = (T)sum[i][e];
-            if (i && c2 >= D) continue;
-            put_chunk((T*)p.out_rows + n * p.ld_out, i ? c2 : c, D, o, past);
+                for (int e = 0; e < 8; ++e) o[e] = (T)sum[i][e];
+                if (i && c2 >= D) continue;
+                put_chunk((T*)p.out_rows + n * p.ld_out, i ? c2 : c, D, o, past);
+            }
         }
     }
 }
@@ -286,64 +289,67 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(RouteArgs p)
     if (p.out_sorted && blockIdx.x >= gridDim.x - kZeroGroups) return zero_behind<T>(p);
     __shared__ float s[4 * (kThreads / 64)];
     int t;
-    const int64_t row = own_row<TPR>(t), n = row < p.N ? row : p.N - 1, D = p.width;
-    const bool mine = row < p.N;
-    const T* gy = (const T*)p.rows + n * p.ld;
+    const int64_t D = p.width, first = own_row<TPR>(t), step = row_step<TPR>(gridDim.x - (p.out_sorted ? kZeroGroups : 0));
     const bool past = large<T>(p);
-    for (int k0 = 0; k0 < p.per_row; k0 += 4) {
-        uint32_t at[4];
-        float w[4], dot[4] = {};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            at[j] = k0 + j < p.per_row && mine ? (uint32_t)p.place[n * p.per_row + k0 + j] : ~0u;
-            w[j] = k0 + j < p.per_row && p.weights ? p.weights[n * p.per_row + k0 + j] : 1.0f;
-        }
-        for (int64_t c = t * 8; c < D; c += TPR * 8) {
-            const auto g = load_chunk(gy, c, D);
-            typename Chunk<T>::V v[4] = {};
-            if (p.grad_weights) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (at[j] < (uint64_t)p.slots) v[j] = load_chunk((const T*)p.sorted + (int64_t)at[j] * D, c, D);
-            }
+    for (int64_t start = (int64_t)blockIdx.x * (kThreads / TPR); start < p.N; start += step) {   // (the same turns for all threads)
+        const int64_t row = first + (start - (int64_t)blockIdx.x * (kThreads / TPR)), n = row < p.N ? row : p.N - 1;
+        const bool mine = row < p.N;
+        const T* gy = (const T*)p.rows + n * p.ld;
+        for (int k0 = 0; k0 < p.per_row; k0 += 4) {
+            uint32_t at[4];
+            float w[4], dot[4] = {};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (at[j] >= (uint64_t)p.slots) continue;
+                at[j] = k0 + j < p.per_row && mine ? (uint32_t)p.place[n * p.per_row + k0 + j] : ~0u;
+                w[j] = k0 + j < p.per_row && p.weights ? p.weights[n * p.per_row + k0 + j] : 1.0f;
+            }
+            for (int64_t c = t * 8; c < D; c += TPR * 8) {
+                const auto g = load_chunk(gy, c, D);
+                typename Chunk<T>::V v[4] = {};
                 if (p.grad_weights) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) dot[j] += to_f32(g[e]) * to_f32(v[j][e]);   // (zeros beyond the rows)
+                    for (int j = 0; j < 4; ++j)
+                        if (at[j] < (uint64_t)p.slots) v[j] = load_chunk((const T*)p.sorted + (int64_t)at[j] * D, c, D);
                 }
-                if (p.out_sorted) {
-                    typename Chunk<T>::V o;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = (T)(w[j] * to_f32(g[e]));
-                    put_chunk((T*)p.out_sorted + (int64_t)at[j] * p.ld_sorted, c, p.ld_sorted, o, past);
+                for (int j = 0; j < 4; ++j) {
+                    if (at[j] >= (uint64_t)p.slots) continue;
+                    if (p.grad_weights) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) dot[j] += to_f32(g[e]) * to_f32(v[j][e]);   // (zeros beyond the rows)
+                    }
+                    if (p.out_sorted) {
+                        typename Chunk<T>::V o;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) o[e] = (T)(w[j] * to_f32(g[e]));
+                        put_chunk((T*)p.out_sorted + (int64_t)at[j] * p.ld_sorted, c, p.ld_sorted, o, past);
+                    }
                 }
             }
-        }
-        if (!p.grad_weights) continue;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-#pragma unroll
-            for (int o = TPR < 64 ? TPR / 2 : 32; o; o >>= 1) dot[j] += __shfl_xor(dot[j], o, 64);
-        }
-        if constexpr (TPR > 64) {
-            constexpr int W = TPR / 64;
-            __syncthreads();
-            if ((t & 63) == 0)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[(t >> 6) * 4 + j] = dot[j];
-            __syncthreads();
+            if (!p.grad_weights) continue;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                dot[j] = s[j];
 #pragma unroll
-                for (int w2 = 1; w2 < W; ++w2) dot[j] += s[w2 * 4 + j];
+                for (int o = TPR < 64 ? TPR / 2 : 32; o; o >>= 1) dot[j] += __shfl_xor(dot[j], o, 64);
             }
-        }
+            if constexpr (TPR > 64) {
+                constexpr int W = TPR / 64;
+                __syncthreads();
+                if ((t & 63) == 0)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (t == j % TPR && mine && k0 + j < p.per_row) p.grad_weights[n * p.per_row + k0 + j] = dot[j];
+                    for (int j = 0; j < 4; ++j) s[(t >> 6) * 4 + j] = dot[j];
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    dot[j] = s[j];
+#pragma unroll
+                    for (int w2 = 1; w2 < W; ++w2) dot[j] += s[w2 * 4 + j];
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (t == j % TPR && mine && k0 + j < p.per_row) p.grad_weights[n * p.per_row + k0 + j] = dot[j];
+        }
     }
 }
 
@@ -373,7 +379,10 @@ int launch_sort(const SortArgs& a, void* stream) {
     else if (chunks <= 32) { RUN(T, 16); }     \
     else if (chunks <= 256) { RUN(T, 64); }    \
     else { RUN(T, 256); }
-unsigned row_blocks(int64_t N, int tpr, bool zeros) { return (unsigned)((N * tpr + kThreads - 1) / kThreads) + (zeros ? kZeroGroups : 0); }
+unsigned row_blocks(int64_t N, int tpr, bool zeros) {
+    const int64_t n = (N * tpr + kThreads - 1) / kThreads;
+    return (unsigned)(n < (1 << 22) ? n : 1 << 22) + (zeros ? kZeroGroups : 0);   // (a launch has fewer than 2^32 threads)
+}
 
 template <typename T> void run_gather(const RouteArgs& a, hipStream_t s) {
 #define FFN_RUN(T, TPR) gather_kernel<T, TPR><<<dim3(row_blocks(a.N, TPR, a.offsets != nullptr)), kThreads, 0, s>>>(a)
