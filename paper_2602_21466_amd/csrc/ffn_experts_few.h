@@ -45,10 +45,13 @@ template <typename T, int MT, int EPI> int run_expert_few(const FewArgs& p, cons
 }
 
 template <typename T> int expert_few(const FewArgs& p, const Groups& g, int32_t epilogue, int32_t rows, int nr, int waves, int64_t most, hipStream_t s) {
+    // (fp32 takes tiles of 64 rows by the other kernels)
+    constexpr int kMost = sizeof(T) == 4 ? 2 : 4;
+    if (rows > 16 * kMost) return (int)hipErrorInvalidValue;
 #define FFN_RUN(EPI)                                                       \
     (rows == 16   ? run_expert_few<T, 1, EPI>(p, g, nr, waves, most, s)    \
      : rows == 32 ? run_expert_few<T, 2, EPI>(p, g, nr, waves, most, s)    \
-                  : run_expert_few<T, 4, EPI>(p, g, nr, waves, most, s))
+                  : run_expert_few<T, kMost, EPI>(p, g, nr, waves, most, s))
     return epilogue == kGate ? FFN_RUN(kGate) : FFN_RUN(kStore);
 #undef FFN_RUN
 }
