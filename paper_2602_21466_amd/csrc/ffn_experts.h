@@ -19,9 +19,15 @@ __device__ __forceinline__ void rows_group(const TileArgs& p, const Groups& g, i
     Scan first;
     const int total = count_tiles(g, lane, BM, 0, first);
     if ((int64_t)block >= (int64_t)total * p.tiles_n * p.splits) return;
-    int tm, tn, split;
-    place(block, total, p.tiles_n, p.splits, tm, tn, split);
-    const Run r = find_tile(g, lane, BM, 0, first, tm);
+    // as place() does, but expert by expert, so that tiles side by side share an expert's B (16384 rows over 16 experts of 2048 x
+    // 4096, a training step in bf16: 2.87 ms, 2.91 by rows of tiles across experts)
+    int t = by_die(block, total * p.tiles_n * p.splits), tm, tn;
+    const int split = t / (total * p.tiles_n);
+    t -= split * total * p.tiles_n;
+    Run r = find_tile(g, lane, BM, 0, first, t / p.tiles_n);
+    const int its = Scan::tiles_of(r.end - r.begin, BM, 0), bands = (its + 7) >> 3;
+    walk(t % p.tiles_n + r.tile * p.tiles_n, its, p.tiles_n, (its + bands - 1) / bands, tm, tn);
+    r.tile = tm;
     const Exact xa = {(const char*)g.a_end, g.source, (uint32_t)g.per_row, (uint32_t)g.rows}, xb = {(const char*)g.b_end, nullptr, 1, 0};
     tile_body<T, BM, BM, WM, WN, false, BC, EPI, true, NB>(p, Work{p.a, (const char*)p.b + r.expert * g.b_step, (int64_t)r.begin + (int64_t)r.tile * BM, r.end, p.K, 0, p.M,
                                                               tn, split, xa, xb, nullptr}, lds);
@@ -31,9 +37,11 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_rows_kernel(Tile
     FFN_TILE_LDS(BM, BM);
     rows_group<T, BM, BC, EPI>(p, g, blockIdx.x, lds);
 }
-// The same for launches of no more tiles than compute units: what a step waits for is memory's latency, not its rate.
+// The same for launches of no more tiles than compute units, where a step waits for memory and for the steps of its own
+// work: deeper buffers, and two waves a SIMD (2002 rows of 1089 values over 6 experts to 2 x 725 gated columns and back to
+// 1089, fp16: 23.4 and 15.5 us; 27.2 and 18.4 with a wave a SIMD, which reads and multiplies in turn).
 template <typename T, bool BC, int EPI>
-__global__ __launch_bounds__(256) void expert_rows_deep_kernel(TileArgs p, Groups g) {
+__global__ __launch_bounds__(512) void expert_rows_deep_kernel(TileArgs p, Groups g) {
     FFN_TILE_LDS4(128, 128);
     rows_group<T, 128, BC, EPI>(p, g, blockIdx.x, lds);
 }
@@ -91,7 +99,7 @@ template <typename T, int BM, bool BC, int EPI> int run_rows(const TileArgs& p, 
     const dim3 grid((unsigned)(p.tiles_m * p.tiles_n * p.splits));
     if constexpr (BM == 128 && sizeof(T) == 2)
         if (g.deep) {
-            expert_rows_deep_kernel<T, BC, EPI><<<grid, 256, 0, s>>>(p, g);
+            expert_rows_deep_kernel<T, BC, EPI><<<grid, 512, 0, s>>>(p, g);
             return (int)hipGetLastError();
         }
     expert_rows_kernel<T, BM, BC, EPI><<<grid, BM == 256 ? 512 : 256, 0, s>>>(p, g);

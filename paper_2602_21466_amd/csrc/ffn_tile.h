@@ -241,12 +241,23 @@ template <int ES, int R, bool COLS> struct Fragments {
     }
 };
 
-// Which part of k and which tile a work-group takes.  Consecutive work-groups go to the eight dies in turn; each die gets
-// a run of consecutive tiles of one part, and a run walks down eight rows of tiles before it moves one column on, so
-// that a die's L2 holds what its tiles share (down projection, 8192 x 4096 x 16384: 1.28 against 0.99 PFLOP/s without).
+// Consecutive work-groups go to the eight dies in turn; each die gets a run of consecutive numbers of `total`.
+__device__ __forceinline__ int by_die(int id, int total) {
+    const int die = id & 7, per = total >> 3, more = total & 7;
+    return die * per + (die < more ? die : more) + (id >> 3);
+}
+// Tile t of tm x tn: down `group` rows of tiles before one column on, so that what consecutive tiles read is little.
+__device__ __forceinline__ void walk(int t, int tm, int tn, int group, int& m, int& n) {
+    const int band = t / (group * tn), r = t - band * group * tn;
+    const int rows = tm - band * group < group ? tm - band * group : group;
+    m = band * group + r % rows;
+    n = r / rows;
+}
+// Which part of k and which tile a work-group takes: each die a run of consecutive tiles of one part, down eight rows of
+// them at a time, so that a die's L2 holds what its tiles share (down projection, 8192 x 4096 x 16384: 1.28 against 0.99
+// PFLOP/s without).
 __device__ __forceinline__ void place(int id, int tm, int tn, int splits, int& m, int& n, int& split) {
-    const int tiles = tm * tn, total = tiles * splits, die = id & 7, per = total >> 3, more = total & 7;
-    int t = die * per + (die < more ? die : more) + (id >> 3);
+    const int tiles = tm * tn, t = by_die(id, tiles * splits);
     if (tm == 1) {   // nothing shared but x: a tile's parts side by side read its rows of B through (24 rows, 4096 x 16384: 29 us against 32)
         split = t % splits;
         m = 0;
@@ -254,12 +265,7 @@ __device__ __forceinline__ void place(int id, int tm, int tn, int splits, int& m
         return;
     }
     split = t / tiles;
-    t -= split * tiles;
-    constexpr int kGroup = 8;
-    const int band = t / (kGroup * tn), r = t - band * kGroup * tn;
-    const int rows = tm - band * kGroup < kGroup ? tm - band * kGroup : kGroup;
-    m = band * kGroup + r % rows;
-    n = r / rows;
+    walk(t - split * tiles, tm, tn, 8, m, n);
 }
 
 template <bool V> struct Flag { static constexpr bool value = V; };
@@ -298,14 +304,20 @@ template <int NB> struct TileLds { char *a[NB], *b[NB]; };
 
 // EXACT: operands as they lie in memory (see Loader).  Where rows end inside a chunk of 16 bytes, what follows them is set to
 // zero in the registers, on both sides, in the last step.
-// NB == 4 (four waves of 16-bit arrays): three steps are in flight where a work-group has a compute unit for itself.
+// NB == 4 (128-wide tiles of 16-bit arrays): three steps are in flight where a work-group has a compute unit for itself, and
+// each block of outputs has two waves, one for each half of a step, whose sums are added at the end.
 template <typename T, int BM, int BN, int WM, int WN, bool AC, bool BC, int EPI, bool EXACT = false, int NB = 2>
 __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, const TileLds<NB>& lds) {
 #ifdef __HIP_DEVICE_COMPILE__   // (the host's pass needs the launch stub alone)
-    constexpr int NW = WM * WN, MT = BM / WM / 16, CW = BN / WN, NT = CW / 16, ES = (int)sizeof(T), kStep = 128 / ES;
+    constexpr int KS = NB == 4 ? 2 : 1, NW = WM * WN * KS, MT = BM / WM / 16, CW = BN / WN, NT = CW / 16, ES = (int)sizeof(T), kStep = 128 / ES;
     char *const sa0 = lds.a[0], *const sb0 = lds.b[0], *const sa1 = lds.a[1], *const sb1 = lds.b[1];
+    auto buffer = [&](int i) {
+        if constexpr (NB == 4) if (i >= 4) return i == 4 ? lds.a[2] : i == 5 ? lds.b[2] : i == 6 ? lds.a[3] : lds.b[3];
+        return i == 0 ? sa0 : i == 1 ? sb0 : i == 2 ? sa1 : sb1;
+    };
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * CW;
+    const int half = wave / (WM * WN), at_block = wave % (WM * WN);   // (NB == 4: half of a step; 0)
+    const int wm = (at_block / WN) * (BM / WM), wn = (at_block % WN) * CW;
     constexpr int kCols = EPI == kGate ? BN / 2 : BN;      // columns of C a tile covers
     const int64_t m0 = w.m0, n0 = (int64_t)w.tn * kCols;
 
@@ -397,13 +409,14 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, cons
             if (plain < n) step(plain & 1 ? sa1 : sa0, plain & 1 ? sb1 : sb0, sa0, sb0, false, Flag<true>());
     } else {
         s16x8 fa[2][MT], fb[2][NT];
-        auto read = [&](const char* a, const char* b, int kk, int s) {
+        // half kk of step s into the registers' half `to`
+        auto read = [&](const char* a, const char* b, int kk, int s, int to) {
             int oa = base_a, ob = base_b;   // (as above)
             asm volatile("" : "+v"(oa), "+v"(ob));
 #pragma unroll
-            for (int j = 0; j < NT; ++j) fb[kk][j] = Fragments<2, BN, BC>::get(b, ob, j, kk);
+            for (int j = 0; j < NT; ++j) fb[to][j] = Fragments<2, BN, BC>::get(b, ob, j, kk);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) fa[kk][i] = Fragments<2, BM, AC>::get(a, oa, i, kk);
+            for (int i = 0; i < MT; ++i) fa[to][i] = Fragments<2, BM, AC>::get(a, oa, i, kk);
             if constexpr (EXACT && (!AC || !BC))
                 if (s == clean) {
                     s16x8 keep;
@@ -411,10 +424,10 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, cons
                     for (int e = 0; e < 8; ++e) keep[e] = 32 * kk + 8 * (lane >> 4) + e < rest ? -1 : 0;
                     if constexpr (!BC)
 #pragma unroll
-                        for (int j = 0; j < NT; ++j) fb[kk][j] &= keep;
+                        for (int j = 0; j < NT; ++j) fb[to][j] &= keep;
                     if constexpr (!AC)
 #pragma unroll
-                        for (int i = 0; i < MT; ++i) fa[kk][i] &= keep;
+                        for (int i = 0; i < MT; ++i) fa[to][i] &= keep;
                 }
         };
         auto multiply = [&](int kk) {
@@ -423,7 +436,60 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, cons
 #pragma unroll
                 for (int j = 0; j < NT; ++j) acc[i][j] = mfma16(fb[kk][j], fa[kk][i], acc[i][j], T());
         };
-        if constexpr (NW == 8) {
+        if constexpr (NB == 4) {
+            // While a wave multiplies its half of a step, it reads that of the next.  Between steps all waves meet: by then
+            // each has read its part of this step's buffer, which takes the step NB further on, and the next step's data,
+            // asked for NB - 1 steps earlier, is there.
+            constexpr int kIssued = (BM + BN) * 128 / 1024 / NW;   // a wave's direct loads a step
+            static_assert(KS == 2 && kIssued == 4 && MT % 4 == 0, "the waits below; what the waves exchange");
+            // Own LDS reads are done, and of the direct loads those of steps later than s, of which `ahead` at the most
+            // have been asked for, may be in flight.
+            auto arrived = [&](int s, int ahead) {
+                const int later = n - 1 - s < ahead ? n - 1 - s : ahead;
+                if (later >= 3) __builtin_amdgcn_s_waitcnt(0x007C);        // 12 loads
+                else if (later == 2) __builtin_amdgcn_s_waitcnt(0x0078);   // 8
+                else if (later == 1) __builtin_amdgcn_s_waitcnt(0x0074);   // 4
+                else __builtin_amdgcn_s_waitcnt(0x0070);
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");   // (no read moves up)
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            auto step = [&](int at, int s) {
+                const int next = (at + 1) % NB;
+                arrived(s + 1, NB - 2);
+                read(lds.a[next], lds.b[next], half, s + 1, next & 1);
+                if (s + NB < n) issue(lds.a[at], lds.b[at]);
+                multiply(at & 1);
+            };
+#pragma unroll
+            for (int k = 0; k < NB; ++k)
+                if (n > k) issue(lds.a[k], lds.b[k]);
+            arrived(0, NB - 1);
+            read(sa0, sb0, half, 0, 0);
+            int s = 0;
+            for (; s + NB <= n; s += NB)
+#pragma unroll
+                for (int k = 0; k < NB; ++k) step(k, s + k);
+#pragma unroll
+            for (int k = 0; k < NB - 1; ++k)
+                if (s + k < n) step(k, s + k);
+            // both halves' sums: each wave finishes one half of the rows
+            __syncthreads();
+            constexpr int kSwap = MT / 2 * NT;
+            f32x4* const box = (f32x4*)buffer(wave);
+            static_assert(kSwap * 1024 <= BM * 128, "the box");
+#pragma unroll
+            for (int i = 0; i < MT / 2; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) box[(i * NT + j) * 64 + lane] = half ? acc[i][j] : acc[i + MT / 2][j];
+            __syncthreads();
+            const f32x4* const theirs = (const f32x4*)buffer(wave ^ 4);
+#pragma unroll
+            for (int i = 0; i < MT / 2; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = (half ? acc[i + MT / 2][j] : acc[i][j]) + theirs[(i * NT + j) * 64 + lane];
+        } else if constexpr (NW == 8) {
             // Two waves a SIMD, of which one reads fragments while the other multiplies: waves 4 - 7 run one phase behind.
             // (8192 x 4096 x 16384, bf16, down projection: 1.31 PFLOP/s; with all waves in step 1.20.)
             auto meet = [] {
@@ -433,14 +499,14 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, cons
             };
             auto phases = [&](char* a, char* b, char* an, char* bn, int s, bool more) {
                 if (more) issue(an, bn);
-                read(a, b, 0, s);
+                read(a, b, 0, s, 0);
                 __builtin_amdgcn_s_waitcnt(0xC07F);     // own LDS reads done
                 meet();
                 __builtin_amdgcn_s_setprio(1);
                 multiply(0);
                 __builtin_amdgcn_s_setprio(0);
                 meet();
-                read(a, b, 1, s);
+                read(a, b, 1, s, 1);
                 __builtin_amdgcn_s_waitcnt(0x0070);     // own LDS reads done, own direct loads landed
                 meet();
                 __builtin_amdgcn_s_setprio(1);
@@ -460,48 +526,26 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, cons
             if (wave < 4) meet();
         } else {
             // While the matrix instructions of one half of a step run, the fragments of the next half are read.  Between
-            // the halves all waves meet: by then each has read the last of this step's buffer, which takes the step NB
-            // further on from memory, and the next step's data, asked for NB - 1 steps earlier, is there.
-            constexpr int kIssued = (BM + BN) * 128 / 1024 / NW;   // a wave's direct loads a step
-            static_assert(NB == 2 || (NB == 4 && kIssued == 8), "the waits below");
-            // All waves, with step s's data: own LDS reads are done, and of the direct loads those of later steps, of which
-            // `ahead` at the most have been asked for, may be in flight.
-            auto arrived = [&](int s, int ahead) {
-                if constexpr (NB == 2) {
-                    landed();
-                } else {
-                    const int later = n - 1 - s < ahead ? n - 1 - s : ahead;
-                    if (later >= 3) __builtin_amdgcn_s_waitcnt(0x4078);        // 24 loads
-                    else if (later == 2) __builtin_amdgcn_s_waitcnt(0x4070);   // 16
-                    else if (later == 1) __builtin_amdgcn_s_waitcnt(0x0078);   // 8
-                    else __builtin_amdgcn_s_waitcnt(0x0070);
-                    __builtin_amdgcn_sched_barrier(0);
-                    __builtin_amdgcn_s_barrier();
-                    asm volatile("" ::: "memory");   // (no read moves up)
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            };
+            // the halves all waves meet: by then each has read the last of this step's buffer, which takes the step after
+            // the next from memory, and the next step's data is there.
             auto step = [&](int at, int s) {
-                const int next = (at + 1) % NB;
-                read(lds.a[at], lds.b[at], 1, s);
+                read(lds.a[at], lds.b[at], 1, s, 1);
                 multiply(0);
-                arrived(s + 1, NB - 2);
-                if (s + NB < n) issue(lds.a[at], lds.b[at]);
-                read(lds.a[next], lds.b[next], 0, s + 1);
+                landed();
+                read(lds.a[at ^ 1], lds.b[at ^ 1], 0, s + 1, 0);
+                if (s + 2 < n) issue(lds.a[at], lds.b[at]);
                 multiply(1);
             };
-#pragma unroll
-            for (int k = 0; k < NB; ++k)
-                if (n > k) issue(lds.a[k], lds.b[k]);
-            arrived(0, NB - 1);
-            read(sa0, sb0, 0, 0);
+            if (n > 0) issue(sa0, sb0);
+            if (n > 1) issue(sa1, sb1);
+            landed();
+            read(sa0, sb0, 0, 0, 0);
             int s = 0;
-            for (; s + NB <= n; s += NB)
-#pragma unroll
-                for (int k = 0; k < NB; ++k) step(k, s + k);
-#pragma unroll
-            for (int k = 0; k < NB - 1; ++k)
-                if (s + k < n) step(k, s + k);
+            for (; s + 2 <= n; s += 2) {
+                step(0, s);
+                step(1, s + 1);
+            }
+            if (s < n) step(0, s);
         }
     }
 
@@ -510,8 +554,8 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, cons
     __syncthreads();
     constexpr int kRow = CW + 4, kTurn = 32 * kRow * 4;    // floats a row (four more than it holds: no bank twice)
     constexpr int kFit = (BM < BN ? BM : BN) * 128 / kTurn;
-    static_assert(kFit >= 1 && 4 * kFit >= NW, "a turn buffer for every wave");
-    float* turn = (float*)((wave / kFit == 0 ? sa0 : wave / kFit == 1 ? sb0 : wave / kFit == 2 ? sa1 : sb1) + wave % kFit * kTurn);
+    static_assert(kFit >= 1 && 2 * NB * kFit >= NW, "a turn buffer for every wave");
+    float* turn = (float*)(buffer(wave / kFit) + wave % kFit * kTurn);
     constexpr int kLanes = EPI == kGate ? CW / 8 : CW / 4, kTake = 64 / kLanes;      // lanes a row, rows a turn
     const int tr = lane / kLanes, tc = (lane % kLanes) * 4;
     // this wave's first column, and whether it and the ones behind it are all inside, with nothing to be written behind the
@@ -520,8 +564,8 @@ __device__ __forceinline__ void tile_body(const TileArgs& p, const Work& w, cons
     const int64_t pad = EXACT ? 0 : EPI == kGate ? p.ldc : EPI == kGateGrad ? (p.ldc > 2 * p.N || p.ldh > p.N ? p.N + 1 : 0) : 0;
     const bool whole = past < p.N || (past == p.N && pad <= p.N);
 #pragma unroll
-    for (int i = 0; i < MT; i += 2) {
-        const int64_t mb = m0 + wm + i * 16, n = nb + tc;
+    for (int i = 0; i < MT / KS; i += 2) {
+        const int64_t mb = m0 + wm + half * (MT / 2 * 16) + i * 16, n = nb + tc;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
