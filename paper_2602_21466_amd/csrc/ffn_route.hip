@@ -127,26 +127,36 @@ __global__ __launch_bounds__(kSort) void sort_place_kernel(SortArgs a) {
 
 // ---------------------------------------------------------------- rows
 //
-// TPR threads take a row, two chunks of eight values a thread and turn: x's rows (grad_y's) are read once for all of their
-// choices, and the loads of two chunks of four choices are in flight together.
+// TPR threads take a row, 16 values a thread and turn in chunks of 16 bytes, side by side over the threads: x's rows
+// (grad_y's) are read once for all of their choices, and the loads of four choices are in flight together.
 
-template <typename T> struct Chunk { typedef T V __attribute__((ext_vector_type(8))); };
+template <typename T> struct Chunk {
+    static constexpr int kVals = 16 / sizeof(T), kTurn = 16 / kVals;   // values, chunks a turn
+    typedef T V __attribute__((ext_vector_type(kVals)));
+};
 template <typename T> __device__ __forceinline__ typename Chunk<T>::V load_chunk(const T* row, int64_t c, int64_t D) {
+    constexpr int kVals = Chunk<T>::kVals;
     typename Chunk<T>::V v;
-    if (c + 8 <= D) {
+    if (c + kVals <= D) {
         __builtin_memcpy(&v, row + c, sizeof(v));
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c + j < D ? row[c + j] : (T)0.0f;
+        for (int j = 0; j < kVals; ++j) v[j] = c + j < D ? row[c + j] : (T)0.0f;
     }
     return v;
 }
+// Chunk i of a turn: those beyond the row repeat the turn's first, in whose branch they are read with it.
+template <typename T, int TPR> __device__ __forceinline__ typename Chunk<T>::V load_turn(const T* row, int64_t c, int i, int64_t D) {
+    const int64_t at = c + i * TPR * Chunk<T>::kVals;
+    return load_chunk(row, i == 0 || at < D ? at : c, D);
+}
 template <typename T> __device__ __forceinline__ void store_chunk(T* row, int64_t c, int64_t D, typename Chunk<T>::V v) {
-    if (c + 8 <= D) {
+    constexpr int kVals = Chunk<T>::kVals;
+    if (c + kVals <= D) {
         __builtin_memcpy(row + c, &v, sizeof(v));
-    } else {
+    } else if (c < D) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < kVals; ++j)
             if (c + j < D) row[c + j] = v[j];
     }
 }
@@ -156,7 +166,7 @@ template <typename T> __device__ __forceinline__ void store_chunk(T* row, int64_
 // 366 with all kept, 366 with gather's alone kept; rows of 4001 x 1089 in fp32 85 and 93).
 template <typename T> __device__ __forceinline__ void put_chunk(T* row, int64_t c, int64_t D, typename Chunk<T>::V v, bool past) {
     typedef typename Chunk<T>::V U __attribute__((aligned(sizeof(T))));
-    if (past && c + 8 <= D) __builtin_nontemporal_store(v, (U*)(row + c));
+    if (past && c + Chunk<T>::kVals <= D) __builtin_nontemporal_store(v, (U*)(row + c));
     else store_chunk(row, c, D, v);
 }
 template <typename T> __device__ __forceinline__ bool large(const RouteArgs& p) { return p.slots * p.width * (int64_t)sizeof(T) >= 16 << 20; }
@@ -185,8 +195,9 @@ template <typename T> __device__ __forceinline__ void zero_behind(const RouteArg
     int64_t held = p.offsets[p.experts];
     held = held < 0 ? 0 : held < p.slots ? held : p.slots;
     const typename Chunk<T>::V zero = {};
-    for (Chunks k(p.slots - held, (p.ld_sorted + 7) >> 3, blockIdx.x - (gridDim.x - kZeroGroups), kZeroGroups); k.more(); k.next())
-        store_chunk((T*)p.out_sorted + (held + k.row) * p.ld_sorted, k.at * 8, p.ld_sorted, zero);
+    constexpr int kVals = Chunk<T>::kVals;
+    for (Chunks k(p.slots - held, (p.ld_sorted + kVals - 1) / kVals, blockIdx.x - (gridDim.x - kZeroGroups), kZeroGroups); k.more(); k.next())
+        store_chunk((T*)p.out_sorted + (held + k.row) * p.ld_sorted, k.at * kVals, p.ld_sorted, zero);
 }
 
 // This thread's first row, its place among the row's threads, and from a row to its next one (of `groups` work-groups).
@@ -200,21 +211,23 @@ template <int TPR> __device__ __forceinline__ int64_t row_step(unsigned groups) 
 template <typename T, int TPR>
 __global__ __launch_bounds__(kThreads) void gather_kernel(RouteArgs p) {
     if (p.offsets && blockIdx.x >= gridDim.x - kZeroGroups) return zero_behind<T>(p);
+    constexpr int kVals = Chunk<T>::kVals, kTurn = Chunk<T>::kTurn;
     int t;
     const int64_t D = p.width;
     const bool past = large<T>(p);
     for (int64_t n = own_row<TPR>(t); n < p.N; n += row_step<TPR>(gridDim.x - (p.offsets ? kZeroGroups : 0))) {
         const T* row = (const T*)p.rows + n * p.ld;
         const int32_t* place = p.place + n * p.per_row;
-        for (int64_t c = t * 8; c < D; c += TPR * 16) {
-            const int64_t c2 = c + TPR * 8;
-            const auto v = load_chunk(row, c, D), v2 = load_chunk(row, c2 < D ? c2 : c, D);
+        for (int64_t c = t * kVals; c < D; c += TPR * 16) {
+            typename Chunk<T>::V v[kTurn];
+#pragma unroll
+            for (int i = 0; i < kTurn; ++i) v[i] = load_turn<T, TPR>(row, c, i, D);
             for (int j = 0; j < p.per_row; ++j) {
                 const uint32_t to = (uint32_t)place[j];
                 if (to >= (uint64_t)p.slots) continue;
                 T* out = (T*)p.out_sorted + (int64_t)to * p.ld_sorted;
-                put_chunk(out, c, p.ld_sorted, v, past);
-                if (c2 < D) put_chunk(out, c2, p.ld_sorted, v2, past);
+#pragma unroll
+                for (int i = 0; i < kTurn; ++i) put_chunk(out, c + i * TPR * kVals, p.ld_sorted, v[i], past);
             }
         }
     }
@@ -222,17 +235,17 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(RouteArgs p) {
 
 template <typename T, int TPR>
 __global__ __launch_bounds__(kThreads) void combine_kernel(RouteArgs p) {
+    constexpr int kVals = Chunk<T>::kVals, kTurn = Chunk<T>::kTurn;
     int t;
     const int64_t D = p.width;
     const bool past = large<T>(p);
     for (int64_t n = own_row<TPR>(t); n < p.N; n += row_step<TPR>(gridDim.x)) {
         const int32_t* place = p.place + n * p.per_row;
         const float* weights = p.weights ? p.weights + n * p.per_row : nullptr;
-        for (int64_t c = t * 8; c < D; c += TPR * 16) {
-            const int64_t c2 = c + TPR * 8;
-            float sum[2][8] = {};
+        for (int64_t c = t * kVals; c < D; c += TPR * 16) {
+            float sum[kTurn][kVals] = {};
             for (int k = 0; k < p.per_row; k += 4) {
-                typename Chunk<T>::V v[4][2] = {};
+                typename Chunk<T>::V v[4][kTurn] = {};
                 float w[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -241,24 +254,22 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(RouteArgs p) {
                     if (from >= (uint64_t)p.slots) continue;
                     w[j] = weights ? weights[k + j] : 1.0f;
                     const T* row = (const T*)p.sorted + (int64_t)from * D;
-                    v[j][0] = load_chunk(row, c, D);
-                    v[j][1] = load_chunk(row, c2 < D ? c2 : c, D);
+#pragma unroll
+                    for (int i = 0; i < kTurn; ++i) v[j][i] = load_turn<T, TPR>(row, c, i, D);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        sum[0][e] += w[j] * to_f32(v[j][0][e]);
-                        sum[1][e] += w[j] * to_f32(v[j][1][e]);
-                    }
+                    for (int i = 0; i < kTurn; ++i)
+#pragma unroll
+                        for (int e = 0; e < kVals; ++e) sum[i][e] += w[j] * to_f32(v[j][i][e]);
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < kTurn; ++i) {
                 typename Chunk<T>::V o;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = (T)sum[i][e];
-                if (i && c2 >= D) continue;
-                put_chunk((T*)p.out_rows + n * p.ld_out, i ? c2 : c, D, o, past);
+                for (int e = 0; e < kVals; ++e) o[e] = (T)sum[i][e];
+                put_chunk((T*)p.out_rows + n * p.ld_out, c + i * TPR * kVals, D, o, past);
             }
         }
     }
@@ -288,6 +299,7 @@ template <typename T, int TPR>
 __global__ __launch_bounds__(kThreads) void combine_backward_kernel(RouteArgs p) {
     if (p.out_sorted && blockIdx.x >= gridDim.x - kZeroGroups) return zero_behind<T>(p);
     __shared__ float s[4 * (kThreads / 64)];
+    constexpr int kVals = Chunk<T>::kVals, kTurn = Chunk<T>::kTurn / 2;   // (eight values a turn)
     int t;
     const int64_t D = p.width, first = own_row<TPR>(t), step = row_step<TPR>(gridDim.x - (p.out_sorted ? kZeroGroups : 0));
     const bool past = large<T>(p);
@@ -303,26 +315,37 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(RouteArgs p)
                 at[j] = k0 + j < p.per_row && mine ? (uint32_t)p.place[n * p.per_row + k0 + j] : ~0u;
                 w[j] = k0 + j < p.per_row && p.weights ? p.weights[n * p.per_row + k0 + j] : 1.0f;
             }
-            for (int64_t c = t * 8; c < D; c += TPR * 8) {
-                const auto g = load_chunk(gy, c, D);
-                typename Chunk<T>::V v[4] = {};
+            for (int64_t c = t * kVals; c < D; c += TPR * 8) {
+                typename Chunk<T>::V g[kTurn], v[4][kTurn] = {};
+#pragma unroll
+                for (int i = 0; i < kTurn; ++i) g[i] = load_turn<T, TPR>(gy, c, i, D);
                 if (p.grad_weights) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (at[j] < (uint64_t)p.slots) v[j] = load_chunk((const T*)p.sorted + (int64_t)at[j] * D, c, D);
+#pragma unroll
+                        for (int i = 0; i < kTurn; ++i)
+                            if (at[j] < (uint64_t)p.slots) v[j][i] = load_turn<T, TPR>((const T*)p.sorted + (int64_t)at[j] * D, c, i, D);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (at[j] >= (uint64_t)p.slots) continue;
                     if (p.grad_weights) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) dot[j] += to_f32(g[e]) * to_f32(v[j][e]);   // (zeros beyond the rows)
+                        for (int i = 0; i < kTurn; ++i) {
+                            float sum = dot[j];
+#pragma unroll
+                            for (int e = 0; e < kVals; ++e) sum += to_f32(g[i][e]) * to_f32(v[j][i][e]);   // (zeros beyond the rows)
+                            if (i == 0 || c + i * TPR * kVals < D) dot[j] = sum;
+                        }
                     }
                     if (p.out_sorted) {
-                        typename Chunk<T>::V o;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) o[e] = (T)(w[j] * to_f32(g[e]));
-                        put_chunk((T*)p.out_sorted + (int64_t)at[j] * p.ld_sorted, c, p.ld_sorted, o, past);
+                        for (int i = 0; i < kTurn; ++i) {
+                            typename Chunk<T>::V o;
+#pragma unroll
+                            for (int e = 0; e < kVals; ++e) o[e] = (T)(w[j] * to_f32(g[i][e]));
+                            put_chunk((T*)p.out_sorted + (int64_t)at[j] * p.ld_sorted, c + i * TPR * kVals, p.ld_sorted, o, past);
+                        }
                     }
                 }
             }
