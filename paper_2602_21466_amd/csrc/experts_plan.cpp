@@ -51,9 +51,9 @@ Cost cost_of(int32_t tile, bool wide) { return wide ? (tile == 256 ? Cost{4.9, 2
 
 // The shortest by a count of those, as a single block's products are cut (ffn_plan.cpp), with what the host knows:
 // `groups(tile)` work-groups by the mean, of `steps` steps of k each.  256 of 256-wide tiles or 512 of 128-wide ones run at
-// one time, and one 128-wide tile alone takes three quarters of what two take.  Parts of k cost a launch, a tenth of a
-// microsecond a part and their sums, written and read once at 4 TB/s; the gate's gradient in the tiles' own epilogue costs
-// ten where they are few.
+// one time, and one 128-wide tile alone takes three quarters of what two take; of 16-bit arrays, what is beyond whole rounds
+// of 256-wide tiles is cut into 128-wide ones (ffn_experts.h).  Parts of k cost a launch, a tenth of a microsecond a part and
+// their sums, written and read once at 4 TB/s; the gate's gradient in the tiles' own epilogue costs ten where they are few.
 template <typename Groups> Cut shortest(Groups groups, int64_t steps, double outputs, bool wide, bool gate_grad) {
     Cut best = {128, 1, false};
     double least = 1e300;
@@ -62,7 +62,8 @@ template <typename Groups> Cut shortest(Groups groups, int64_t steps, double out
         const Cost cost = cost_of(tile, wide);
         for (int32_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); ++s) {
             const double n = all * s / slots, full = std::floor(n), rest = n - full;
-            const double rounds = full + (rest == 0.0 ? 0.0 : tile == 128 && rest <= 0.5 ? 0.75 : 1.0);
+            const bool cut = tile == 256 && !wide && s == 1 && full > 0.0;
+            const double rounds = full + (rest == 0.0 ? 0.0 : tile == 128 && rest <= 0.5 ? 0.75 : cut && rest <= 0.25 ? 0.45 : cut && rest <= 0.5 ? 0.9 : 1.0);
             const double t = rounds * ((double)tiles(steps, s) + cost.ends) * cost.step;
             const double join = 3.0 + 0.1 * s + outputs * s * 8.0 / 4e6, own = gate_grad ? 10.0 : 0.0;
             const bool joined = s > 1 || own > join;

@@ -11,31 +11,49 @@
 namespace ffn {
 namespace dev {
 
-// Work-group `block` of C = A B^T by expert.
-template <typename T, int BM, bool BC, int EPI, int NB>
+// Tiles of 256 that run at one time, and how many beyond a multiple of them are cut into four of 128 each: one of those alone
+// takes 0.45 of a tile's time, so that up to 64 tiles take that and up to 128 twice that (16384 rows over 16 experts, 4096
+// values to 2048, bf16: 290 us, 337 without).
+constexpr int kRound = 256, kCutTiles = 128;
+
+// Work-group `block` of C = A B^T by expert.  CUT: see above.
+template <typename T, int BM, bool BC, int EPI, bool CUT, int NB>
 __device__ __forceinline__ void rows_group(const TileArgs& p, const Groups& g, int block, const TileLds<NB>& lds) {
     constexpr int WM = 2, WN = BM == 256 ? 4 : 2;
     const int lane = threadIdx.x & 63;
     Scan first;
-    const int total = count_tiles(g, lane, BM, 0, first);
-    if ((int64_t)block >= (int64_t)total * p.tiles_n * p.splits) return;
+    const int total = count_tiles(g, lane, BM, 0, first), tiles = total * p.tiles_n;
+    // (the whole rounds' tiles are dealt to the dies apart from what is cut)
+    const int over = tiles % kRound, rest = CUT && p.splits == 1 && tiles > kRound && over <= kCutTiles ? over : 0, whole = tiles - rest;
+    if ((int64_t)block >= (int64_t)whole * p.splits + 4 * rest) return;
     // as place() does, but expert by expert, so that tiles side by side share an expert's B (16384 rows over 16 experts of 2048 x
     // 4096, a training step in bf16: 2.87 ms, 2.91 by rows of tiles across experts)
-    int t = by_die(block, total * p.tiles_n * p.splits), tm, tn;
-    const int split = t / (total * p.tiles_n);
-    t -= split * total * p.tiles_n;
+    const bool quarter = block >= whole * p.splits;
+    int t = quarter ? by_die(block - whole, 4 * rest) : by_die(block, whole * p.splits), tm, tn;
+    const int q = t & 3, split = quarter ? 0 : t / whole;
+    t = quarter ? whole + (t >> 2) : t - split * whole;
     Run r = find_tile(g, lane, BM, 0, first, t / p.tiles_n);
     const int its = Scan::tiles_of(r.end - r.begin, BM, 0), bands = (its + 7) >> 3;
     walk(t % p.tiles_n + r.tile * p.tiles_n, its, p.tiles_n, (its + bands - 1) / bands, tm, tn);
-    r.tile = tm;
     const Exact xa = {(const char*)g.a_end, g.source, (uint32_t)g.per_row, (uint32_t)g.rows}, xb = {(const char*)g.b_end, nullptr, 1, 0};
-    tile_body<T, BM, BM, WM, WN, false, BC, EPI, true, NB>(p, Work{p.a, (const char*)p.b + r.expert * g.b_step, (int64_t)r.begin + (int64_t)r.tile * BM, r.end, p.K, 0, p.M,
-                                                              tn, split, xa, xb, nullptr}, lds);
+    Work w = {p.a, (const char*)p.b + r.expert * g.b_step, (int64_t)r.begin + (int64_t)tm * BM, r.end, p.K, 0, p.M, tn, split, xa, xb, nullptr};
+    if constexpr (CUT) {
+        if (quarter) {
+            static_assert(BM == 256 && NB == 2, "a step's buffers of the smaller tiles in each of the larger's");
+            w.m0 += (q >> 1) * 128;
+            w.tn = tn * 2 + (q & 1);
+            if (w.m0 >= r.end || (int64_t)w.tn * (EPI == kGate ? 64 : 128) >= p.N) return;
+            const TileLds<4> four = {{lds.a[0], lds.b[0], lds.a[1], lds.b[1]}, {lds.a[0] + 16384, lds.b[0] + 16384, lds.a[1] + 16384, lds.b[1] + 16384}};
+            tile_body<T, 128, 128, 2, 2, false, BC, EPI, true, 4>(p, w, four);
+            return;
+        }
+    }
+    tile_body<T, BM, BM, WM, WN, false, BC, EPI, true, NB>(p, w, lds);
 }
 template <typename T, int BM, bool BC, int EPI>
 __global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_rows_kernel(TileArgs p, Groups g) {
     FFN_TILE_LDS(BM, BM);
-    rows_group<T, BM, BC, EPI>(p, g, blockIdx.x, lds);
+    rows_group<T, BM, BC, EPI, BM == 256 && sizeof(T) == 2>(p, g, blockIdx.x, lds);
 }
 // The same for launches of no more tiles than compute units, where a step waits for memory and for the steps of its own
 // work: deeper buffers, and two waves a SIMD (2002 rows of 1089 values over 6 experts to 2 x 725 gated columns and back to
@@ -43,7 +61,7 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_rows_kernel(Tile
 template <typename T, bool BC, int EPI>
 __global__ __launch_bounds__(512) void expert_rows_deep_kernel(TileArgs p, Groups g) {
     FFN_TILE_LDS4(128, 128);
-    rows_group<T, 128, BC, EPI>(p, g, blockIdx.x, lds);
+    rows_group<T, 128, BC, EPI, false>(p, g, blockIdx.x, lds);
 }
 
 constexpr int kManyTiles = 64;
@@ -91,12 +109,12 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_grads_kernel(Exp
     FFN_TILE_LDS(BM, BM);
     const int at = (int)blockIdx.x < a.end[0] ? 0 : (int)blockIdx.x < a.end[1] ? 1 : 2, k = a.order[at];
     const int block = at ? blockIdx.x - a.end[at - 1] : blockIdx.x;
-    if (k == 0) rows_group<T, BM, true, kPartial>(a.t[0], a.g[0], block, lds);
+    if (k == 0) rows_group<T, BM, true, kPartial, false>(a.t[0], a.g[0], block, lds);
     else sums_group<T, BM>(a.t[k], a.g[k], a.partial[k - 1], block, lds);
 }
 
 template <typename T, int BM, bool BC, int EPI> int run_rows(const TileArgs& p, const Groups& g, hipStream_t s) {
-    const dim3 grid((unsigned)(p.tiles_m * p.tiles_n * p.splits));
+    const dim3 grid((unsigned)(p.tiles_m * p.tiles_n * p.splits + (BM == 256 && sizeof(T) == 2 ? 3 * kCutTiles : 0)));
     if constexpr (BM == 128 && sizeof(T) == 2)
         if (g.deep) {
             expert_rows_deep_kernel<T, BC, EPI><<<grid, 512, 0, s>>>(p, g);

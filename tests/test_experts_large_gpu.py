@@ -16,10 +16,12 @@ def _randn(torch, t, *shape, scale=1.0, seed=0):
     return torch.empty(*shape, dtype=t, device="cuda").normal_(0.0, scale, generator=g)
 
 
-# x past 2^31 bytes, x's sorted rows past 2^31 values; and H, dG, dU past 2^32 bytes, saved past 2^32 values
+# x past 2^31 bytes, x's sorted rows past 2^31 values; H, dG, dU past 2^32 bytes, saved past 2^32 values; and each product in
+# more than a round of 256-wide tiles, of which those beyond it are cut
 @pytest.mark.parametrize("N,K,E,di,df,do,dtype", [(66001, 2, 3, 16384, 8, 8, "bf16"), (40003, 1, 2, 16385, 4, 12, "fp32"),
-                                                  (100003, 2, 3, 64, 16400, 40, "bf16")])
-def test_offsets_past_32_bits(N, K, E, di, df, do, dtype):
+                                                  (100003, 2, 3, 64, 16400, 40, "bf16"), (3200, 1, 2, 520, 7399, 7402, "bf16"),
+                                                  (3200, 1, 2, 519, 7402, 7399, "fp16")])
+def test_long_and_wide(N, K, E, di, df, do, dtype):
     torch, lib = _setup()
     t = _dt(torch, dtype)
     rng = np.random.default_rng(N)
