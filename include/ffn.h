@@ -3,8 +3,8 @@
  * tensor products, on MI355X (gfx950): the gated feed-forward block (the
  * network that makes per-pair path weights for cgtp_forward_weighted, or mixes
  * scalar channels), the norms before and after a block fused with its gate and
- * residual scale, and dropout from a counter-based generator.  Each has its
- * gradients.
+ * residual scale, the layer norm, and dropout from a counter-based generator.
+ * Each has its gradients.
  *
  * Arrays are row-major device arrays of one type:
  *   FFN_FP32, FFN_BF16 or FFN_FP16.

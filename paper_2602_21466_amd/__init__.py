@@ -10,8 +10,9 @@ There is no CPU fallback: if the shared library is missing or the GPU is
 absent, the calls raise.
 
 The functions carry the C names (``cgtp_plan``, ``cgtp_forward``,
-``istp_plan``, ``ffn_plan``, ...); ``Plan``, ``IstpPlan``, ``FfnPlan`` and
-``NormPlan`` are small convenience wrappers around them.
+``istp_plan``, ``ffn_plan``, ...); ``Plan``, ``IstpPlan``, ``FfnPlan``,
+``NormPlan``, ``LayerNormPlan``, ``Routes`` and ``ExpertsPlan`` are small
+convenience wrappers around them.
 """
 from __future__ import annotations
 
