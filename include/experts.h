@@ -12,8 +12,9 @@
  *
  * Arrays, types, alignment, overlaps, streams, workspaces, graphs and status codes
  * are as in ffn.h.  N == 0 returns CGTP_OK; what sums over rows is then zero.
- * place, source and offsets are device arrays that ffn_route wrote; entries out of
- * their range read and write nothing out of bounds, but give other results.
+ * place, source and offsets are device arrays that ffn_route wrote, for as many
+ * rows, choices and experts; entries out of their range read and write nothing out
+ * of bounds, but give other results.
  */
 #ifndef EXPERTS_H
 #define EXPERTS_H

@@ -116,7 +116,8 @@ class Routes:
         place (like index)     the sorted row of each choice, -1 where it chose none
         source [S]             the choice n * per_row + k of each sorted row, -1 from offsets[experts] on
 
-    All three are int32 tensors on the GPU; nothing is copied to the host."""
+    All three are int32 tensors on the GPU; nothing is copied to the host.  They are memory of the stream that they were
+    made on: where another uses them, keep them until it is done."""
 
     def __init__(self, index, experts: int, stream=None):
         if not index.is_cuda or index.dim() not in (1, 2) or not index.is_contiguous() or \

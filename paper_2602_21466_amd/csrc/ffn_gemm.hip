@@ -124,6 +124,7 @@ __global__ __launch_bounds__(kThreads) void join_sums_kernel(ExpertGrads a) {
         first += __builtin_amdgcn_readlane(s.upto, e - e0) - parts;
     }
     if (parts == 1) return;
+    if (parts > p.splits - first) parts = p.splits - first;   // (of offsets that ffn_route wrote there are no more)
     const int64_t ld = (p.N + 3) & ~3LL, quads = ld >> 2, total = p.M * quads, part = p.M * ld;
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
         const int64_t row = i / quads, c = (i - row * quads) * 4;

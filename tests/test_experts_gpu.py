@@ -402,6 +402,37 @@ def test_mixture_captured_and_replayed(N, dtype):
         assert all(torch.equal(a, b) for a, b in zip(got, want)), s
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("N", [6, 500])
+def test_entries_out_of_range_stay_inside(N, dtype):
+    """An order with entries far out of their range: other results, but nothing is written outside the outputs, and rows
+    that no such entry is about keep theirs."""
+    torch, lib = _setup()
+    K, E, di, df, do = 2, 3, 40, 56, 24
+    index, x, wi, wo, gy = (t.cuda() if torch.is_tensor(t) else t for t in _case(torch, N, K, E, di, df, do, dtype, "even"))
+    plan = lib.ExpertsPlan(E, di, df, do, dtype=dtype)
+    good = lib.Routes(torch.from_numpy(index).cuda(), E)
+    want, saved = plan.forward(x, good, wi, wo, save=True)
+    want_y = good.combine(want)
+    S, far = N * K, torch.tensor([-2 ** 31, 2 ** 31 - 1, N * K, -7], dtype=torch.int32, device="cuda")
+    bad = lib.Routes(torch.from_numpy(index).cuda(), E)
+    bad.place[1], bad.source[3:5] = far[:2], far[1:3]
+    room = torch.full((S + 64, do), 7.0, dtype=x.dtype, device="cuda")
+    out = plan.forward(x, bad, wi, wo, out=room[32:32 + S])
+    keep = [p for p in range(S) if p not in (3, 4)]
+    assert torch.equal(out[keep], want[keep]) and (room[:32] == 7).all() and (room[32 + S:] == 7).all()
+    rows = [n for n in range(N) if n != 1]
+    assert torch.equal(bad.combine(want)[rows], want_y[rows]) and not bad.combine(want)[1].any()
+    bad.offsets[0], bad.offsets[E] = far[0], far[1]
+    xs = torch.full((S + 64, di), 7.0, dtype=x.dtype, device="cuda")
+    bad.gather(x, out=xs[32:32 + S])
+    out = plan.forward(x, bad, wi, wo, out=room[32:32 + S])
+    assert (room[:32] == 7).all() and (room[32 + S:] == 7).all() and (xs[:32] == 7).all() and (xs[32 + S:] == 7).all()
+    grads = plan.backward(x, bad, wi, wo, saved, gy)
+    gys, gw = bad.combine_backward(want, torch.ones(N, K, device="cuda"), want_y)
+    assert all(bool(t.isfinite().all()) for t in (*grads, gw)) and not gw[1].any()
+
+
 def test_refusals():
     torch, lib = _setup()
     plan = lib.ExpertsPlan(3, 16, 24, 8)
