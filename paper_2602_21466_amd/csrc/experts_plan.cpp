@@ -177,28 +177,37 @@ int rows_product(ffn::TileArgs t, ffn::Groups g, int32_t epilogue, bool bc, int3
 }
 
 // The forward products for few rows an expert, where reading the weights is the time: tiles of 16, 32 or 64 rows, so that
-// most experts have one; weight rows a work-group and waves as for a single block (ffn_plan.cpp), the work-groups being
-// those of all experts with a row.
+// most experts have one; the work-groups are those of all experts with a row.  What a work-group reads of x beside its weight
+// rows comes from the L2: 16 weight rows read as much as 16 of x, 32 half of it a weight (64 rows over 16 experts of 4096 values to
+// 2048 in bf16: 61 us by 32 weight rows, 79 by 16; 16 rows, 41 by 16 and 63 by 8).  The gate's products hold two of each.
 struct Few { int32_t rows, nr, waves; };
 Few few_cut(const Shape& s, bool gate, int32_t dtype) {
+    const bool wide = dtype == FFN_FP32;
     const int64_t with = s.E < s.R ? s.E : s.R, mean = tiles(s.R, with), all = with * s.N;
     Few c;
     // 64 rows, two of 16 experts each, 2048 x 4096: bf16 168 us by tiles of 32 rows and 198 of 16; fp32 332 by 16, 399 by 32
-    c.rows = mean <= (dtype == FFN_FP32 ? 10 : 6) ? 16 : mean <= 24 ? 32 : 64;
-    c.nr = (c.rows == 16 && dtype != FFN_FP32) || all < 16 * 192 ? 8 : gate && c.rows > 16 && all >= 32 * 512 ? 32 : 16;
+    c.rows = mean <= (wide ? 10 : 6) ? 16 : mean <= 24 || wide ? 32 : 64;
+    if (all < 16 * 192 || (gate && c.rows == 16 && !wide)) c.nr = 8;
+    else c.nr = all >= 32 * 256 && c.rows > 16 ? 32 : 16;
     const int32_t per = (c.nr > 16 ? 2 : 1) * (gate ? 2 : 1) * (c.rows / 16);
-    const int64_t blocks = tiles(s.K, dtype == FFN_FP32 ? 64 : 128), groups = tiles(all, c.nr);
-    c.waves = 8;
+    const int64_t blocks = tiles(s.K, wide ? 64 : 128), groups = tiles(all, c.nr);
+    // (gated, 64 rows over 8 experts of 1024 x 2048 in bf16: 15.3 us by four waves, 17.3 by eight)
+    c.waves = gate && c.nr == 32 ? 4 : 8;
     while (c.waves > 1 && (c.waves * per > 64 || c.waves > 2 * blocks || (c.waves * 4 > blocks && groups * c.waves > 4096))) c.waves /= 2;
     return c;
 }
-// Whether these kernels are the faster ones: against tiles, 16 experts of 2048 x 4096 in bf16 take 28 us for one row (47), 168
-// for 8 rows an expert (190), 198 for 16 (196); in fp32 473 for 16 (618) and 728 for 32 (617); small weights, which are read
-// from the caches, 19.6 for 32 rows an expert (27.5; 8 experts, 512 x 1024, bf16).
-bool few_rows(int64_t R, const ffn_experts_s* p) {
+// Whether these kernels are the faster ones, by the mean of an expert's rows.  Against tiles (both products), 16 experts of
+// 2048 x 4096 in bf16 take 24 us for one row (47), 173 for 12 rows an expert (212), 201 for 24 (216), 231 for 32 (218); 8 of
+// 512 x 1024, whose weights the caches hold, 17.6 for 40 (25.7), 27 for 64 (26).  Their 16-byte loads to registers take longer
+// where 16-bit rows start on 4 bytes (8 experts of 510 x 1022: 21.7 for 24, 26.1 by tiles; 28.9 and 26.8 for 32; 16 of 2046 x
+// 4094: 211 and 214 for 8, 224 and 220 for 16) and twice as long on 2 (511 x 1023: 28.4 and 29.7 for 24; 8 of 1023 x 2047: 45
+// and 41 for one, 71 and 40 for 16), where tiles' direct loads hardly do; so each product goes by the alignment of its own
+// rows, of K values.  In fp32 8 of 1024 x 2048 take 69 for 24 (115), 100 for 32 (115), 149 for 64 (118).
+bool few_rows(int64_t R, const ffn_experts_s* p, int64_t K) {
     const int64_t with = p->experts < R ? p->experts : R, mean = tiles(R, with);
-    const int64_t bytes = with * p->d_ff * (2 * p->d_in + p->d_out) * size_of(p->dtype);
-    return mean <= (p->dtype == FFN_FP32 ? 24 : bytes <= (1 << 25) ? 30 : 16);
+    const bool small = with * p->d_ff * (2 * p->d_in + p->d_out) * size_of(p->dtype) <= (1 << 25);
+    if (p->dtype == FFN_FP32) return mean <= 28;
+    return mean <= (K % 4 == 0 ? (small ? 48 : 24) : K % 2 == 0 ? (small ? 24 : 10) : small ? 24 : 0);
 }
 int few_product(ffn::FewArgs p, const ffn::Groups& g, int32_t epilogue, int32_t dtype, void* stream) {
     const bool gate = epilogue == ffn::kGate;
@@ -421,43 +430,50 @@ int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const in
     rc = current_device_is(plan->device);
     if (rc != CGTP_OK) return rc;
     char* ws = (char*)workspace;
-    if (few_rows(R, plan)) {
+    const bool few_gate = few_rows(R, plan, di), few_down = few_rows(R, plan, df);
+    ffn::PackJobs jobs = {};
+    Matrix Wi = {}, Wo = {};
+    if (!few_gate) Wi = readable(w_in, E * 2 * df, di, dt, ws + l.w_in, &jobs);
+    if (!few_down) Wo = readable(w_out, E * d_o, df, dt, ws + l.w_out, &jobs);
+    if (jobs.n) rc = status(ffn::launch_pack(jobs, dt, hip_stream));
+    if (rc != CGTP_OK) return rc;
+    const Matrix H = matrix(ws + l.h, R, up8(df), df, e);
+    if (few_gate) {
         ffn::FewArgs f = {};
         f.x = x; f.ldx = ldx; f.w = w_in; f.ldw = di;
         f.N = df; f.K = di;
-        f.c = ws + l.h; f.ldc = up8(df);
+        f.c = ws + l.h; f.ldc = H.ld;
         f.saved = (float*)saved; f.act = plan->act;
         rc = few_product(f, {offsets, plan->experts, R, 2 * df * di * e, nullptr, nullptr, 0, source, per_row}, ffn::kGate, dt, hip_stream);
+    } else {
+        // x's rows where they are, by 32-bit offsets, or copied in the sorted order
+        const bool there = direct(x, N, ldx, di, e) && ((N - 1) * ldx + di) * e < (1LL << 31) - 256;
+        if (!there) rc = gather(plan, x, ldx, place, ws + l.x, N, per_row, hip_stream);
         if (rc != CGTP_OK) return rc;
-        f.x = ws + l.h; f.ldx = up8(df); f.w = w_out; f.ldw = df;
+        const Matrix X = there ? matrix(x, N, ldx, di, e) : matrix(ws + l.x, R, up8(di), di, e);
+        ffn::TileArgs t = {};
+        t.a = X.p; t.lda = X.ld;
+        t.b = Wi.p; t.ldb = Wi.ld;
+        t.M = R; t.N = df; t.K = di;
+        t.c = ws + l.h; t.ldc = H.ld;
+        t.act = plan->act; t.saved = (float*)saved;
+        const ffn::Groups g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, X.end, Wi.end, 0, there ? source : nullptr, per_row};
+        rc = rows_product(t, g, ffn::kGate, false, dt, ws + l.partial, hip_stream);
+    }
+    if (rc != CGTP_OK) return rc;
+    if (few_down) {
+        ffn::FewArgs f = {};
+        f.x = ws + l.h; f.ldx = H.ld; f.w = w_out; f.ldw = df;
         f.N = d_o; f.K = df;
-        f.c = y; f.ldc = d_o; f.saved = nullptr;
+        f.c = y; f.ldc = d_o;
         return few_product(f, {offsets, plan->experts, R, d_o * df * e, nullptr, nullptr, 0, nullptr, 1}, ffn::kStore, dt, hip_stream);
     }
-    ffn::PackJobs jobs = {};
-    const Matrix Wi = readable(w_in, E * 2 * df, di, dt, ws + l.w_in, &jobs), Wo = readable(w_out, E * d_o, df, dt, ws + l.w_out, &jobs);
-    rc = status(ffn::launch_pack(jobs, dt, hip_stream));
-    // x's rows where they are, by 32-bit offsets, or copied in the sorted order
-    const bool there = direct(x, N, ldx, di, e) && ((N - 1) * ldx + di) * e < (1LL << 31) - 256;
-    if (rc == CGTP_OK && !there) rc = gather(plan, x, ldx, place, ws + l.x, N, per_row, hip_stream);
-    if (rc != CGTP_OK) return rc;
-    const Matrix X = there ? matrix(x, N, ldx, di, e) : matrix(ws + l.x, R, up8(di), di, e), H = matrix(ws + l.h, R, up8(df), df, e);
-    ffn::TileArgs t = {};
-    t.a = X.p; t.lda = X.ld;
-    t.b = Wi.p; t.ldb = Wi.ld;
-    t.M = R; t.N = df; t.K = di;
-    t.c = ws + l.h; t.ldc = H.ld;
-    t.act = plan->act; t.saved = (float*)saved;
-    ffn::Groups g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, X.end, Wi.end, 0, there ? source : nullptr, per_row};
-    rc = rows_product(t, g, ffn::kGate, false, dt, ws + l.partial, hip_stream);
-    if (rc != CGTP_OK) return rc;
     ffn::TileArgs o = {};
     o.a = H.p; o.lda = H.ld;
     o.b = Wo.p; o.ldb = Wo.ld;
     o.M = R; o.N = d_o; o.K = df;
     o.c = y; o.ldc = d_o;
-    g = {offsets, plan->experts, R, d_o * Wo.ld * e, H.end, Wo.end, 0, nullptr, 1};
-    return rows_product(o, g, ffn::kStore, false, dt, ws + l.partial, hip_stream);
+    return rows_product(o, {offsets, plan->experts, R, d_o * Wo.ld * e, H.end, Wo.end, 0, nullptr, 1}, ffn::kStore, false, dt, ws + l.partial, hip_stream);
 }
 
 int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const int32_t* place, const int32_t* source,

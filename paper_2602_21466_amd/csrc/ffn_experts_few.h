@@ -24,7 +24,7 @@ template <typename T, int MT, int EPI> int run_expert_few(const FewArgs& p, cons
     const int lds = waves * (nr > 16 ? 2 : 1) * (EPI == kGate ? 2 : 1) * MT * 1024;
     if (lds > 64 * 1024 || most > 65535) return (int)hipErrorInvalidValue;
     // (those that few_cut() asks for)
-    constexpr bool k16 = MT > 1 || sizeof(T) == 4, k32 = MT > 1 && EPI == kGate;
+    constexpr bool k16 = MT > 1 || EPI == kStore || sizeof(T) == 4, k32 = MT > 1;
     if (nr == 8) {
         expert_few_kernel<T, MT, 8, EPI><<<grid, waves * 64, lds, s>>>(p, g);
         return (int)hipGetLastError();

@@ -126,7 +126,7 @@ template <typename T> int few_launch(const ffn::FewArgs& p, const ffn::Groups& g
     const bool gate = epi == ffn::kGate;
     const int mt = rows / 16;
     EXPECT((rows == 16 || rows == 32 || (rows == 64 && T::size == 2)) && (epi == ffn::kStore || gate));
-    EXPECT(nr == 8 || (nr == 16 && (mt > 1 || T::size == 4)) || (nr == 32 && mt > 1 && gate));
+    EXPECT(nr == 8 || (nr == 16 && (mt > 1 || T::size == 4 || !gate)) || (nr == 32 && mt > 1));
     EXPECT(waves >= 1 && waves <= 8 && waves * (nr > 16 ? 2 : 1) * (gate ? 2 : 1) * mt <= 64 && most <= 65535);
     int64_t tiles = 0;
     for (int e = 0; e < g.experts; ++e) tiles += (g.offsets[e + 1] - g.offsets[e] + rows - 1) / rows;

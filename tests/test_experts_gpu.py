@@ -120,11 +120,13 @@ def _check(got, pair, what):
     assert not over.numel() or float(over.max()) <= 0.0, (what, float(over.max()))
 
 
-# rows, choices, experts and sizes: one row, few rows, runs that end inside tiles, odd strides, long sums, wide outputs
+# rows, choices, experts and sizes: one row, few rows, runs that end inside tiles, odd strides, long sums, wide outputs, one
+# product by the kernels for few rows and the other by tiles, both ways
 SIZES = [(1, 1, 1, 1, 1, 1), (1, 2, 8, 64, 128, 64), (1, 1, 3, 81, 324, 489), (3, 2, 4, 17, 5, 31), (16, 4, 6, 256, 64, 256),
          (17, 1, 2, 96, 200, 40), (64, 2, 3, 128, 64, 8), (100, 3, 5, 75, 130, 77), (200, 2, 65, 40, 72, 24),
          (300, 2, 3, 264, 72, 129), (257, 1, 1, 520, 264, 136), (500, 4, 4, 64, 256, 320), (1000, 1, 7, 32, 48, 56),
-         (90, 2, 200, 24, 16, 9), (33, 2, 2, 1000, 2056, 8), (600, 1, 2, 8, 8, 2000)]
+         (90, 2, 200, 24, 16, 9), (33, 2, 2, 1000, 2056, 8), (600, 1, 2, 8, 8, 2000), (40, 1, 1, 64, 61, 24),
+         (80, 1, 2, 61, 64, 24), (16, 1, 4, 2000, 2056, 1032)]
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
