@@ -25,11 +25,13 @@ struct Scan {
         end = end < begin ? begin : end < R ? end : R;
         upto = tiles_of(end - begin, side, least);
         if (e >= g.experts) upto = 0;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int v = __shfl_up(upto, o, 64);
-            if (lane >= o) upto += v;
-        }
+        // within 16 lanes, then the rows' sums to the rows behind them
+        upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xf, 0xf, false);   // one lane up
+        upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xf, 0xf, false);
+        upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xf, 0xf, false);
+        upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xf, 0xf, false);
+        upto += __builtin_amdgcn_update_dpp(0, upto, 0x142, 0xa, 0xf, false);   // a row's last lane to the next row
+        upto += __builtin_amdgcn_update_dpp(0, upto, 0x143, 0xc, 0xf, false);   // lane 31 to the last two
     }
     static __device__ __forceinline__ int tiles_of(int rows, int side, int least) {
         const int n = (int)((uint32_t)(rows + side - 1) / (uint32_t)side);
