@@ -13,10 +13,10 @@ def test_kernels_for_few_rows_are_those_a_call_can_reach():
         wide = dtype == "f"
         for gate in (0, 1):
             for mean in range(1, 29 if wide else 49):
-                for n in (8, 16 * 192 - 1, 16 * 192, 32 * 256 - 1, 32 * 256, 1 << 20):
+                for n in (8, 16 * 200 - 1, 16 * 200, 32 * 256 - 1, 32 * 256, 1 << 20):
                     rows = 16 if mean <= (10 if wide else 6) else 32 if mean <= 24 or wide else 64
                     nr = 32 if n >= 32 * 256 and rows > 16 else 16
-                    if n < 16 * 192 or (gate and rows == 16 and not wide):
+                    if n < 16 * 200 or (gate and rows == 16 and not wide):
                         nr = 8
                     want.add((dtype, rows // 16, nr, gate))
     found = re.findall(r"17expert_few_kernelI(f|DF16b|DF16_)Li(\d+)ELi(\d+)ELi(\d+)EE", _symbols("-D"))
