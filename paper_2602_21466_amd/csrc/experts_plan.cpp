@@ -96,8 +96,8 @@ Cut cut_rows(const Shape& s, int32_t dtype, int32_t epilogue) {
 
 // The gradients' products of one launch: the rows' [R, d_in], whose k is in `splits` parts, and the weights', sums over each
 // expert's rows in parts of `chunk` of them (0: one part an expert).  Counted like shortest(): all work-groups' steps over
-// those that run at one time, then half of one that comes late, of the shorter kind; a few experts may have three times the
-// mean.
+// those that run at one time, then half of one that comes late, of the shorter kind where these fill what the longer leave;
+// a few experts may have three times the mean.
 struct GradCut { int32_t tile, splits, chunk; bool sums_first; };
 GradCut cut_grads(const ffn_experts_s* p, int64_t R) {
     const bool wide = p->dtype == FFN_FP32;
@@ -112,11 +112,12 @@ GradCut cut_grads(const ffn_experts_s* p, int64_t R) {
         const double each = (double)(tiles(2 * df, tile) * tiles(di, tile) + tiles(d_o, tile) * tiles(df, tile));
         auto consider = [&](int32_t chunk) {
             const double parts = chunk ? (double)R / chunk + 0.5 * E : (double)E, sums = each * ((double)R / k + parts * ends);
-            const double one = (chunk ? (double)chunk : longest) / k + ends, join = chunk ? 4.0 + parts * outputs * 8.0 / 4e6 : 0.0;
+            const double one = (chunk ? (double)chunk : longest) / k + ends, join = chunk ? 4.0 + parts * outputs * 4.5 / 4e6 : 0.0;
             for (int32_t s = 1; s <= 64 && (s == 1 || steps / s >= 4); s += s < 4 ? 1 : s / 2) {
-                const double own = (double)tiles(steps, s) + ends, all = (rows * s * own + sums) / slots, late = rows * s + each * parts <= slots ? 0.0 : 0.5 * (own < one ? own : one);
-                const double longest_one = own > one ? own : one, run = all + late > longest_one ? all + late : longest_one;
-                const double t = step * run + join + 0.1 * s + (double)R * di * s * 8.0 / 4e6;
+                const double own = (double)tiles(steps, s) + ends, all = (rows * s * own + sums) / slots;
+                const double less = own < one ? own : one, more = own < one ? one : own, fill = (own < one ? rows * s * own : sums) / slots;
+                const double late = rows * s + each * parts <= slots ? 0.0 : 0.5 * more - fill > 0.5 * less ? 0.5 * more - fill : 0.5 * less;
+                const double t = step * (all + late > more ? all + late : more) + join + 0.1 * s + (double)R * di * s * 8.0 / 4e6;
                 if (t < least) { least = t; best = {tile, s, chunk, one > own}; }
             }
         };
