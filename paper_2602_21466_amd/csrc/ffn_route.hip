@@ -163,7 +163,7 @@ template <typename T> __device__ __forceinline__ void store_chunk(T* row, int64_
 
 // A result: past the caches where all of them are more than these hold, as what stays there is written to memory during
 // the next kernel (16384 x 4096 in bf16, two choices a row, gather and combine after each other and their gradients: 346 us;
-// 366 with all kept, 366 with gather's alone kept; rows of 4001 x 1089 in fp32 85 and 93).
+// 366 with all kept, 366 with gather's alone kept).
 template <typename T> __device__ __forceinline__ void put_chunk(T* row, int64_t c, int64_t D, typename Chunk<T>::V v, bool past) {
     typedef typename Chunk<T>::V U __attribute__((aligned(sizeof(T))));
     if (past && c + Chunk<T>::kVals <= D) __builtin_nontemporal_store(v, (U*)(row + c));
