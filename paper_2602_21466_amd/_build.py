@@ -1,6 +1,7 @@
 """Compiles the HIP library (libcgtp.so: full CGTP and the MIMO signal products) in-tree for gfx950 with hipcc."""
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import subprocess
 
@@ -25,15 +26,15 @@ FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
 
 
 def build(force: bool = True, extra=None) -> str:
-    """Compiles every source to an object in parallel (one hipcc each), then links the library."""
+    """Compiles every source to an object, as many at a time as there are processors, then links the library."""
     if not force and os.path.exists(LIB):
         return LIB
     tag = ".tmp%d" % os.getpid()
     objs = [os.path.join(HERE, "csrc", os.path.basename(src) + tag + ".o") for src in SOURCES]
     compile_flags = [f for f in FLAGS if f != "-shared"]
-    procs = [subprocess.Popen([HIPCC] + compile_flags + list(extra or []) + ["-c", src, "-o", obj])
-             for src, obj in zip(SOURCES, objs)]
-    failed = [src for src, p in zip(SOURCES, procs) if p.wait() != 0]
+    compile_one = lambda src, obj: subprocess.run([HIPCC] + compile_flags + list(extra or []) + ["-c", src, "-o", obj]).returncode
+    with concurrent.futures.ThreadPoolExecutor(min(os.cpu_count() or 1, 16)) as pool:
+        failed = [src for src, rc in zip(SOURCES, pool.map(compile_one, SOURCES, objs)) if rc != 0]
     try:
         if failed:
             raise subprocess.CalledProcessError(1, "hipcc", "failed: %s" % ", ".join(failed))
