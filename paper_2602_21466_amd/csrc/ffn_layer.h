@@ -213,8 +213,10 @@ __global__ __launch_bounds__(group_of(TPR), forward_waves(sizeof(T), TPR, I, fal
     }
 }
 
-// Waves a SIMD that the backward rows' registers are bounded for: two column sums a value live through the rows.
-constexpr int layer_backward_waves(int bytes, int tpr, int turns) { return turns == 1 || tpr == 1024 || bytes == 2 ? 4 : 3; }
+// Waves a SIMD that the backward rows' registers are bounded for: two column sums a value live through the rows.  Two turns of
+// 32-bit values take 180 registers, which is two waves (in fp32 16384 x 2500: 97 us; by three, with registers in scratch memory, 161,
+// and with w loaded twice a row instead 117; 8192 x 4096: 81, 103 and 90).
+constexpr int layer_backward_waves(int bytes, int tpr, int turns) { return turns == 1 || tpr == 1024 || bytes == 2 ? 4 : 2; }
 
 // One pass over the rows: gx, and each work-group's column sums, which stay in registers.  (16384 x 4096 in bf16: 88 us, 4.9
 // TB/s, and 7.5 for the joining of 1024 sets; 4001 x 1089 in fp16: 14.2 and 6.2.)
@@ -242,7 +244,9 @@ __global__ __launch_bounds__(group_of(TPR), layer_backward_waves(sizeof(T), TPR,
             gr[i] = row8<T>((const T*)p.gu + r * p.ldg, at8[i]);
         }
     };
-    constexpr bool kLean = TPR == 1024;
+    // (kAgain: nor is w held from the sums to gx, as 128 registers do not hold it beside 32-bit values; 4096 x 16384 in fp32: 175
+    // us, 210 with registers in scratch memory)
+    constexpr bool kLean = TPR == 1024, kAgain = kLean && sizeof(T) == 4;
     if constexpr (!kLean) {
         if (row < p.N) fetch(row);
 #pragma unroll
@@ -270,7 +274,7 @@ __global__ __launch_bounds__(group_of(TPR), layer_backward_waves(sizeof(T), TPR,
             }
             keep(x[i]);   // the next half starts from the loaded values
             keep(g[i]);
-            keep(w[i]);
+            if constexpr (!kAgain) keep(w[i]);
         }
         const int64_t at_row = row;
         row += workers;
@@ -280,6 +284,10 @@ __global__ __launch_bounds__(group_of(TPR), layer_backward_waves(sizeof(T), TPR,
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             if (at8[i].skip == 8) continue;
+            if constexpr (kAgain) {
+                asm volatile("" : "+v"(at8[i].c));
+                w[i] = ones8<T>(p.w, at8[i]);
+            }
             float gx[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
