@@ -192,7 +192,8 @@ int64_t ffn_norm_workspace_bytes(const ffn_norm *norm, int64_t N, int32_t residu
 /*
  * u = L(x; w, b) of N rows; x and u have row strides ldx and ldu.  w NULL: all
  * ones; b NULL: zeros.  stats: NULL, or [2, N] floats to receive m and then r of
- * the rows.  u == x with ldu == ldx is allowed.  Statuses as ffn_norm_forward.
+ * the rows.  u == x with ldu == ldx is allowed.  A row whose mean square deviation
+ * passes the range of 32 bits has r = 0.  Statuses as ffn_norm_forward.
  */
 int ffn_layer_forward(const ffn_norm *norm, const void *x, int64_t ldx, const void *w, const void *b, void *u,
                       int64_t ldu, float *stats, int64_t N, void *hip_stream);

@@ -23,6 +23,13 @@ template <typename T> __device__ __forceinline__ void offsets8(const void* p, in
     }
 }
 
+// r from the sum of the centred values' squares.  NaN stays NaN (fmaxf would drop it), and a variance past the range of 32 bits
+// infinite, r = 0, also where d^2 passes it.
+__device__ __forceinline__ float layer_r(float s2, float d, float D, float eps) {
+    const float v = s2 / D - fminf(d * d, 3.4028235e38f);
+    return 1.0f / sqrtf((v < 0.0f ? 0.0f : v) + eps);
+}
+
 // One row a work-group, eight columns a thread and turn, any width: a row is read three times, from the caches while it
 // fits them.
 template <typename T>
@@ -51,7 +58,7 @@ __global__ __launch_bounds__(kThreads) void layer_forward_kernel(LayerArgs p) {
             }
         }
         const float d = group_sum(s1, s) / (float)D;
-        const float r = 1.0f / sqrtf(fmaxf(group_sum(s2, s) / (float)D - d * d, 0.0f) + p.eps);
+        const float r = layer_r(group_sum(s2, s), d, (float)D, p.eps);
         if (p.stats && threadIdx.x == 0) {
             p.stats[row] = m + d;
             p.stats[p.N + row] = r;
@@ -197,7 +204,7 @@ __global__ __launch_bounds__(group_of(TPR), forward_waves(sizeof(T), TPR, I, fal
                 two[1] += c * c;
             }
         worker_sum<TPR, 2>(two, s, 1);
-        const float d = two[0] / (float)D, r = 1.0f / sqrtf(fmaxf(two[1] / (float)D - d * d, 0.0f) + p.eps);
+        const float d = two[0] / (float)D, r = layer_r(two[1], d, (float)D, p.eps);
         if (p.stats && t == 0) {
             p.stats[row] = m + d;
             p.stats[p.N + row] = r;
