@@ -73,6 +73,7 @@ struct Groups {
     int64_t rows;                         // sorted rows there may be
     int64_t b_step;                       // bytes from one expert's B to the next's
     const void *a_end, *b_end;            // behind the last bytes that may be read of either operand
+    int64_t b_shift;                      // bytes from where the last expert's B would be to where a copy of it is; 0: it is there
     int32_t chunk;                        // sums: rows of a part; 0: an expert's rows are one part
     const int32_t* source;                // rows of A are those of slots source[..] / per_row; NULL: they are in their order
     int32_t per_row;

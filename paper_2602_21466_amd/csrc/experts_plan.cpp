@@ -223,8 +223,9 @@ int few_product(ffn::FewArgs p, const ffn::Groups& g, int32_t epilogue, int32_t 
     }
 }
 
-// A matrix as a product reads it: where it is, and behind its last byte that may be read.
-struct Matrix { const void* p; int64_t ld; const void* end; };
+// A matrix as a product reads it: where it is, and behind its last byte that may be read; of the experts' weights, how far
+// from its place the last one's is, where that is a copy.
+struct Matrix { const void* p; int64_t ld; const void* end; int64_t shift; };
 
 // Direct loads take four bytes at a time: of 16-bit arrays two bytes more than the last value, which are in the array's own
 // four where its rows start on four bytes, and else on its page of memory unless the array ends with a page.
@@ -232,7 +233,7 @@ bool direct(const void* p, int64_t rows, int64_t ld, int64_t width, int64_t e) {
     return e == 4 || (((uintptr_t)p & 3) == 0 && (ld % 2 == 0 || rows == 1)) || (((uintptr_t)p + ((rows - 1) * ld + width) * e) & 4095) != 0;
 }
 Matrix matrix(const void* p, int64_t rows, int64_t ld, int64_t width, int64_t e) {
-    return {p, ld, (const char*)p + ((rows - 1) * ld + width) * e + (e == 2 ? 2 : 0)};
+    return {p, ld, (const char*)p + ((rows - 1) * ld + width) * e + (e == 2 ? 2 : 0), 0};
 }
 // It, or a copy of it in `scratch`.
 Matrix readable(const void* p, int64_t rows, int64_t width, int32_t dtype, void* scratch, ffn::PackJobs* jobs) {
@@ -241,8 +242,23 @@ Matrix readable(const void* p, int64_t rows, int64_t width, int32_t dtype, void*
     jobs->job[jobs->n++] = {p, scratch, width, rows, width, up8(width), 0};
     return matrix(scratch, rows, up8(width), width, e);
 }
+// The experts' weights, of `rows` rows each: only the last one's reach the end of the array, so these alone are copied, as they
+// lie, to scratch of weights_bytes().
+int64_t weights_bytes(int64_t rows, int64_t width, int32_t dtype) {
+    return dtype != FFN_FP32 && width % 2 ? packed_bytes(1, rows * width + 8, dtype) : 0;   // (what is read behind the last value)
+}
+Matrix weights(const void* p, int64_t E, int64_t rows, int64_t width, int32_t dtype, void* scratch, ffn::PackJobs* jobs) {
+    const int64_t e = size_of(dtype), each = rows * width;
+    Matrix m = matrix(p, E * rows, width, width, e);
+    if (direct(p, E * rows, width, width, e)) return m;
+    const char* last = (const char*)p + (E - 1) * each * e;
+    jobs->job[jobs->n++] = {last, scratch, each, 1, each, up8(each), 0};
+    m.shift = (int64_t)((uintptr_t)scratch - (uintptr_t)last);
+    return m;
+}
 
-// Byte offsets in the workspace: x's rows in the sorted order, intermediates, copies of operands, partial sums.
+// Byte offsets in the workspace: x's rows in the sorted order, intermediates, copies of operands, partial sums.  What a call
+// needs copied depends on where its arrays lie and on x's stride, which the query does not know.
 struct Layout { int64_t x, h, dgu, gy, w_in, w_out, partial, part_in, part_out, total; };
 Layout layout(const ffn_experts_s* p, int64_t R, bool backward) {
     const int64_t di = p->d_in, df = p->d_ff, d_o = p->d_out, E = p->experts;
@@ -251,10 +267,12 @@ Layout layout(const ffn_experts_s* p, int64_t R, bool backward) {
     Layout l = {};
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t o = at; at += bytes; return o; };
-    l.x = take(packed_bytes(R, di, t));
+    // (the kernels for few rows read everything where it is)
+    const bool tiled_gate = backward || (R > 0 && !few_rows(R, p, di)), tiled_down = backward || (R > 0 && !few_rows(R, p, df));
+    l.x = take(tiled_gate ? packed_bytes(R, di, t) : 0);
     l.h = take(packed_bytes(R, df, t));
-    l.w_in = take(narrow && di % 2 ? packed_bytes(E * 2 * df, di, t) : 0);
-    l.w_out = take(narrow && df % 2 ? packed_bytes(E * d_o, df, t) : 0);
+    l.w_in = take(tiled_gate ? weights_bytes(2 * df, di, t) : 0);
+    l.w_out = take(tiled_down ? weights_bytes(d_o, df, t) : 0);
     int64_t partial = 0;
     auto also = [&](int64_t bytes) { partial = bytes > partial ? bytes : partial; };
     if (backward) {
@@ -268,8 +286,8 @@ Layout layout(const ffn_experts_s* p, int64_t R, bool backward) {
             l.part_out = take(aligned(most_parts(R, E, c) * d_o * up4(df) * 4));
         }
     } else {
-        also(rows_partial({R, E, 2 * df, di}, t, ffn::kGate));
-        also(rows_partial({R, E, d_o, df}, t, ffn::kStore));
+        if (tiled_gate) also(rows_partial({R, E, 2 * df, di}, t, ffn::kGate));
+        if (tiled_down) also(rows_partial({R, E, d_o, df}, t, ffn::kStore));
     }
     l.partial = take(partial);
     l.total = at;
@@ -435,8 +453,8 @@ int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const in
     const bool few_gate = few_rows(R, plan, di), few_down = few_rows(R, plan, df);
     ffn::PackJobs jobs = {};
     Matrix Wi = {}, Wo = {};
-    if (!few_gate) Wi = readable(w_in, E * 2 * df, di, dt, ws + l.w_in, &jobs);
-    if (!few_down) Wo = readable(w_out, E * d_o, df, dt, ws + l.w_out, &jobs);
+    if (!few_gate) Wi = weights(w_in, E, 2 * df, di, dt, ws + l.w_in, &jobs);
+    if (!few_down) Wo = weights(w_out, E, d_o, df, dt, ws + l.w_out, &jobs);
     if (jobs.n) rc = status(ffn::launch_pack(jobs, dt, hip_stream));
     if (rc != CGTP_OK) return rc;
     const Matrix H = matrix(ws + l.h, R, up8(df), df, e);
@@ -446,7 +464,7 @@ int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const in
         f.N = df; f.K = di;
         f.c = ws + l.h; f.ldc = H.ld;
         f.saved = (float*)saved; f.act = plan->act;
-        rc = few_product(f, {offsets, plan->experts, R, 2 * df * di * e, nullptr, nullptr, 0, source, per_row}, ffn::kGate, dt, hip_stream);
+        rc = few_product(f, {offsets, plan->experts, R, 2 * df * di * e, nullptr, nullptr, 0, 0, source, per_row}, ffn::kGate, dt, hip_stream);
     } else {
         // x's rows where they are, by 32-bit offsets, or copied in the sorted order
         const bool there = direct(x, N, ldx, di, e) && ((N - 1) * ldx + di) * e < (1LL << 31) - 256;
@@ -459,7 +477,7 @@ int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const in
         t.M = R; t.N = df; t.K = di;
         t.c = ws + l.h; t.ldc = H.ld;
         t.act = plan->act; t.saved = (float*)saved;
-        const ffn::Groups g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, X.end, Wi.end, 0, there ? source : nullptr, per_row};
+        const ffn::Groups g = {offsets, plan->experts, R, 2 * df * Wi.ld * e, X.end, Wi.end, Wi.shift, 0, there ? source : nullptr, per_row};
         rc = rows_product(t, g, ffn::kGate, false, dt, ws + l.partial, hip_stream);
     }
     if (rc != CGTP_OK) return rc;
@@ -468,14 +486,14 @@ int ffn_experts_forward(ffn_experts_t plan, const void* x, int64_t ldx, const in
         f.x = ws + l.h; f.ldx = H.ld; f.w = w_out; f.ldw = df;
         f.N = d_o; f.K = df;
         f.c = y; f.ldc = d_o;
-        return few_product(f, {offsets, plan->experts, R, d_o * df * e, nullptr, nullptr, 0, nullptr, 1}, ffn::kStore, dt, hip_stream);
+        return few_product(f, {offsets, plan->experts, R, d_o * df * e, nullptr, nullptr, 0, 0, nullptr, 1}, ffn::kStore, dt, hip_stream);
     }
     ffn::TileArgs o = {};
     o.a = H.p; o.lda = H.ld;
     o.b = Wo.p; o.ldb = Wo.ld;
     o.M = R; o.N = d_o; o.K = df;
     o.c = y; o.ldc = d_o;
-    return rows_product(o, {offsets, plan->experts, R, d_o * Wo.ld * e, H.end, Wo.end, 0, nullptr, 1}, ffn::kStore, false, dt, ws + l.partial, hip_stream);
+    return rows_product(o, {offsets, plan->experts, R, d_o * Wo.ld * e, H.end, Wo.end, Wo.shift, 0, nullptr, 1}, ffn::kStore, false, dt, ws + l.partial, hip_stream);
 }
 
 int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const int32_t* place, const int32_t* source,
@@ -512,14 +530,14 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
     }
     char* ws = (char*)workspace;
     ffn::PackJobs jobs = {};
-    const Matrix Gy = readable(grad_y, R, d_o, dt, ws + l.gy, &jobs), Wo = readable(w_out, E * d_o, df, dt, ws + l.w_out, &jobs);
+    const Matrix Gy = readable(grad_y, R, d_o, dt, ws + l.gy, &jobs), Wo = weights(w_out, E, d_o, df, dt, ws + l.w_out, &jobs);
     Matrix Wi = {};
-    if (grad_x) Wi = readable(w_in, E * 2 * df, di, dt, ws + l.w_in, &jobs);
+    if (grad_x) Wi = weights(w_in, E, 2 * df, di, dt, ws + l.w_in, &jobs);
     rc = status(ffn::launch_pack(jobs, dt, hip_stream));
     if (rc == CGTP_OK && grad_w_in) rc = gather(plan, x, ldx, place, ws + l.x, N, per_row, hip_stream);
     if (rc != CGTP_OK) return rc;
     const Matrix H = matrix(ws + l.h, R, up8(df), df, e), D = matrix(ws + l.dgu, R, up8(2 * df), 2 * df, e), X = matrix(ws + l.x, R, up8(di), di, e);
-    ffn::Groups g = {offsets, plan->experts, R, d_o * Wo.ld * e, Gy.end, Wo.end, 0, nullptr, 1};
+    ffn::Groups g = {offsets, plan->experts, R, d_o * Wo.ld * e, Gy.end, Wo.end, Wo.shift, 0, nullptr, 1};
     ffn::TileArgs t = {};
     t.a = Gy.p; t.lda = Gy.ld;
     t.b = Wo.p; t.ldb = Wo.ld;
@@ -528,7 +546,7 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
     t.h = ws + l.h; t.ldh = H.ld;
     t.act = plan->act; t.saved = (float*)const_cast<void*>(saved);
     rc = rows_product(t, g, ffn::kGateGrad, true, dt, ws + l.partial, hip_stream);
-    if (rc != CGTP_OK || (!grad_x && !grad_w_in && !grad_w_out)) return rc;
+    if (rc != CGTP_OK) return rc;
     const GradCut c = cut_grads(plan, R);
     ffn::ExpertGrads a = {};
     for (int k = 0; k < 3; ++k) a.order[k] = c.sums_first ? (k + 1) % 3 : k;
@@ -539,7 +557,7 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
         w.tiles_m = (int32_t)tiles(M, c.tile);
         w.tiles_n = (int32_t)tiles(columns, c.tile);
         w.splits = (int32_t)most_parts(R, E, c);
-        a.g[k] = {offsets, plan->experts, R, 0, A.end, B.end, c.chunk, nullptr, 1};
+        a.g[k] = {offsets, plan->experts, R, 0, A.end, B.end, 0, c.chunk, nullptr, 1};
         a.partial[k - 1] = (float*)(ws + part);
     };
     if (grad_x) {
@@ -551,7 +569,7 @@ int ffn_experts_backward(ffn_experts_t plan, const void* x, int64_t ldx, const i
         d.tiles_m = (int32_t)most_tiles({R, E, di, 0}, c.tile);
         d.tiles_n = (int32_t)tiles(di, c.tile);
         d.splits = c.splits;
-        a.g[0] = {offsets, plan->experts, R, 2 * df * Wi.ld * e, D.end, Wi.end, 0, nullptr, 1};
+        a.g[0] = {offsets, plan->experts, R, 2 * df * Wi.ld * e, D.end, Wi.end, Wi.shift, 0, nullptr, 1};
     }
     if (grad_w_in) sums(1, D, X, 2 * df, di, grad_w_in, l.part_in);
     if (grad_w_out) sums(2, Gy, H, d_o, df, grad_w_out, l.part_out);

@@ -35,8 +35,9 @@ __device__ __forceinline__ void rows_group(const TileArgs& p, const Groups& g, i
     Run r = find_tile(g, lane, BM, 0, first, t / p.tiles_n);
     const int its = Scan::tiles_of(r.end - r.begin, BM, 0), bands = (its + 7) >> 3;
     walk(t % p.tiles_n + r.tile * p.tiles_n, its, p.tiles_n, (its + bands - 1) / bands, tm, tn);
-    const Exact xa = {(const char*)g.a_end, g.source, (uint32_t)g.per_row, (uint32_t)g.rows}, xb = {(const char*)g.b_end, nullptr, 1, 0};
-    Work w = {p.a, (const char*)p.b + r.expert * g.b_step, (int64_t)r.begin + (int64_t)tm * BM, r.end, p.K, 0, p.M, tn, split, xa, xb, nullptr};
+    const int64_t shift = r.expert == g.experts - 1 ? g.b_shift : 0;
+    const Exact xa = {(const char*)g.a_end, g.source, (uint32_t)g.per_row, (uint32_t)g.rows}, xb = {(const char*)g.b_end + shift, nullptr, 1, 0};
+    Work w = {p.a, (const char*)p.b + r.expert * g.b_step + shift, (int64_t)r.begin + (int64_t)tm * BM, r.end, p.K, 0, p.M, tn, split, xa, xb, nullptr};
     if constexpr (CUT) {
         if (quarter) {
             static_assert(BM == 256 && NB == 2, "a step's buffers of the smaller tiles in each of the larger's");
