@@ -218,10 +218,13 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(RouteArgs p) {
     for (int64_t n = own_row<TPR>(t); n < p.N; n += row_step<TPR>(gridDim.x - (p.offsets ? kZeroGroups : 0))) {
         const T* row = (const T*)p.rows + n * p.ld;
         const int32_t* place = p.place + n * p.per_row;
-        for (int64_t c = t * kVals; c < D; c += TPR * 16) {
+        for (int64_t c = t * kVals; c < p.ld_sorted; c += TPR * 16) {
             typename Chunk<T>::V v[kTurn];
 #pragma unroll
-            for (int i = 0; i < kTurn; ++i) v[i] = load_turn<T, TPR>(row, c, i, D);
+            for (int i = 0; i < kTurn; ++i) {
+                v[i] = load_turn<T, TPR>(row, c, i, D);
+                if (i > 0 && c + i * TPR * kVals >= D) v[i] = {};   // (stored where rows have room behind D)
+            }
             for (int j = 0; j < p.per_row; ++j) {
                 const uint32_t to = (uint32_t)place[j];
                 if (to >= (uint64_t)p.slots) continue;

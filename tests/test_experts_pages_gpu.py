@@ -32,3 +32,20 @@ def test_arrays_that_end_with_a_page(E, di, df, do, N, kind, dtype):
         y, saved = plan.forward(a[0], routes, a[1], a[2], save=True)
         outs.append((y[:M], saved[:M]) + plan.backward(a[0], routes, a[1], a[2], saved, a[3]))
     assert all(bool(p.isfinite().all()) and torch.equal(p, q) for p, q in zip(*outs))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("di", [1, 3, 5, 8, 12, 61, 81, 130, 257, 1089, 2050])
+def test_rows_in_the_sorted_order_have_zeros_behind_them(di, dtype):
+    """The rows of x that the gradients' products read, first in the workspace, in rows of a multiple of eight values."""
+    torch, lib = _setup()
+    N, K, E = 70, 2, 3
+    index, x, wi, wo, gy = _case(torch, N, K, E, di, 16, 8, dtype, "even")
+    x, wi, wo, gy = (t.cuda() for t in (x, wi, wo, gy))
+    plan, routes = lib.ExpertsPlan(E, di, 16, 8, dtype=dtype), lib.Routes(torch.from_numpy(index).cuda(), E)
+    _, saved = plan.forward(x, routes, wi, wo, save=True)
+    ws = torch.full((lib.ffn_experts_backward_workspace_bytes(plan._h, N, K),), 0xFF, dtype=torch.uint8, device="cuda")
+    plan.backward(x, routes, wi, wo, saved, gy, False, True, False, workspace=ws)
+    M, ld = int(routes.offsets[E]), (di + 7) // 8 * 8
+    rows = ws[:N * K * ld * x.element_size()].view(x.dtype).view(N * K, ld)[:M]
+    assert torch.equal(rows[:, :di], routes.gather(x)[:M]) and bool((rows[:, di:] == 0).all())
