@@ -14,7 +14,9 @@
  * are as in ffn.h.  N == 0 returns CGTP_OK; what sums over rows is then zero.
  * place, source and offsets are device arrays that ffn_route wrote, for as many
  * rows, choices and experts; entries out of their range read and write nothing out
- * of bounds, but give other results.
+ * of bounds, but give other results.  Of a 16-bit array of the blocks whose rows do
+ * not all start on four bytes, the two bytes behind its last value may be read
+ * where they are on the same page of memory (4096 bytes); no result depends on them.
  */
 #ifndef EXPERTS_H
 #define EXPERTS_H

@@ -198,13 +198,18 @@ Few few_cut(const Shape& s, bool gate, int32_t dtype) {
     while (c.waves > 1 && (c.waves * per > 64 || c.waves > 2 * blocks || (c.waves * 4 > blocks && groups * c.waves > 4096))) c.waves /= 2;
     return c;
 }
-// Whether these kernels are the faster ones, by the mean of an expert's rows.  Against tiles (both products), 16 experts of
-// 2048 x 4096 in bf16 take 24 us for one row (47), 173 for 12 rows an expert (212), 201 for 24 (216), 231 for 32 (218); 8 of
-// 512 x 1024, whose weights the caches hold, 17.6 for 40 (25.7), 27 for 64 (26).  Their 16-byte loads to registers take longer
-// where 16-bit rows start on 4 bytes (8 experts of 510 x 1022: 21.7 for 24, 26.1 by tiles; 28.9 and 26.8 for 32; 16 of 2046 x
-// 4094: 211 and 214 for 8, 224 and 220 for 16) and twice as long on 2 (511 x 1023: 28.4 and 29.7 for 24; 8 of 1023 x 2047: 45
-// and 41 for one, 71 and 40 for 16), where tiles' direct loads hardly do; so each product goes by the alignment of its own
-// rows, of K values.  In fp32 8 of 1024 x 2048 take 69 for 24 (115), 100 for 32 (115), 149 for 64 (118).
+// Whether these kernels are the faster ones, by the mean of an expert's rows.  Against tiles (both products, experts chosen at
+// random), 16 experts of 2048 x 4096 in bf16 take 16 us for one choice (28), 159 for 12 rows an expert (207), 188 for 24 (209), 219
+// for 32 (209); 8 of 512 x 1024, whose weights the caches hold, 16 for 40 (23), 24 for 64 (24).  Their 16-byte loads to registers
+// take longer where 16-bit rows start on 4 bytes (8 experts of 510 x 1022: 17 and 24 by tiles for 24 rows of each, 26 and 24 at
+// random; 16 of 2046 x 4094: 165 and 170 for 2, 196 and 185 for 4, 210 and 187 for 10) and twice as long on 2 (511 x 1023: 25 and
+// 26 for 24 of each, 39 and 26 at random; 8 of 1023 x 2047: 48 and 38 for one, 68 and 36 for 16), where tiles' direct loads hardly do; so
+// each product goes by the alignment of its own rows, of K values.  In fp32 8 of 1024 x 2048 take 78 for 28 (81), 93 for 40 (83), 121
+// for 64 (94).
+// The mean does not tell how the rows lie.  With half of them on one expert these kernels stay ahead or within 3 % (16 of 2048 x 4096,
+// 24 rows an expert: 206 us and 266; 64 of 2048 x 2048: 391 and 380).  With all on one they read its weights again for each tile of
+// rows, from the caches, and tiles are ahead from 12 rows an expert on (67 and 66; 24: 113 and 69; of 64 experts 4: 98 and 64, 24:
+// 219 and 68).
 bool few_rows(int64_t R, const ffn_experts_s* p, int64_t K) {
     const int64_t with = p->experts < R ? p->experts : R, mean = tiles(R, with);
     const bool small = with * p->d_ff * (2 * p->d_in + p->d_out) * size_of(p->dtype) <= (1 << 25);

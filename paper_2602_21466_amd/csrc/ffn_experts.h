@@ -13,7 +13,7 @@ namespace dev {
 
 // Tiles of 256 that run at one time, and how many beyond a multiple of them are cut into four of 128 each: one of those alone
 // takes 0.45 of a tile's time, so that up to 64 tiles take that and up to 128 twice that (16384 rows over 16 experts, 4096
-// values to 2048, bf16: 290 us, 337 without).
+// values to 2048, bf16: a seventh less time with it).
 constexpr int kRound = 256, kCutTiles = 128;
 
 // Work-group `block` of C = A B^T by expert.  CUT: see above.
@@ -51,8 +51,8 @@ __device__ __forceinline__ void rows_group(const TileArgs& p, const Groups& g, i
     }
     tile_body<T, BM, BM, WM, WN, false, BC, EPI, true, NB>(p, w, lds);
 }
-// (16384 rows over 16 experts of 2048 x 4096 in bf16: the gated product with G and U kept 671 us, 0.82 PFLOP/s; 281 down, 0.98;
-// dG, dU and H 440, 0.62, where G and U are read.)
+// (16384 rows over 16 experts of 2048 x 4096 in bf16: the gated product with G and U kept 673 us, 0.82 PFLOP/s; 279 down, 0.98;
+// dG, dU and H 436, 0.63, where G and U are read.)
 template <typename T, int BM, bool BC, int EPI>
 __global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_rows_kernel(TileArgs p, Groups g) {
     FFN_TILE_LDS(BM, BM);
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_rows_kernel(Tile
 }
 // The same for launches of no more tiles than compute units, where a step waits for memory and for the steps of its own
 // work: deeper buffers, and two waves a SIMD (2002 rows of 1089 values over 6 experts to 2 x 725 gated columns and back to
-// 1089, fp16: 23.4 and 15.5 us; 27.2 and 18.4 with a wave a SIMD, which reads and multiplies in turn).
+// 1089, fp16: 22.7 and 15.0 us; 27.2 and 18.4 with a wave a SIMD, which reads and multiplies in turn).
 template <typename T, bool BC, int EPI>
 __global__ __launch_bounds__(512) void expert_rows_deep_kernel(TileArgs p, Groups g) {
     FFN_TILE_LDS4(128, 128);
@@ -105,8 +105,8 @@ __device__ __forceinline__ void sums_group(TileArgs p, const Groups& g, float* p
 }
 
 // The three products of the gradients that need dG, dU and H alone, in one launch, those of the longest sums first: the
-// others take the places that these leave.  (The same sizes: 1387 us, 0.99 PFLOP/s; a
-// training step took 3.05 ms, 3.21 with three launches.)
+// others take the places that these leave.  (The same sizes: 1374 us, 1.00 PFLOP/s; a
+// training step takes a twentieth less than with three launches.)
 template <typename T, int BM>
 __global__ __launch_bounds__(BM == 256 ? 512 : 256) void expert_grads_kernel(ExpertGrads a) {
     FFN_TILE_LDS(BM, BM);

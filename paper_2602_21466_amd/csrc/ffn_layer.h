@@ -221,7 +221,7 @@ __global__ __launch_bounds__(group_of(TPR), forward_waves(sizeof(T), TPR, I, fal
 }
 
 // Waves a SIMD that the backward rows' registers are bounded for: two column sums a value live through the rows.  Two turns of
-// 32-bit values take 180 registers, which is two waves (in fp32 16384 x 2500: 97 us; by three, with registers in scratch memory, 161,
+// 32-bit values take 173 registers, which is two waves (in fp32 16384 x 2500: 97 us; by three, with registers in scratch memory, 161,
 // and with w loaded twice a row instead 117; 8192 x 4096: 81, 103 and 90).
 constexpr int layer_backward_waves(int bytes, int tpr, int turns) { return turns == 1 || tpr == 1024 || bytes == 2 ? 4 : 2; }
 
