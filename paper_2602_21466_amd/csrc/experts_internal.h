@@ -66,6 +66,9 @@ int launch_combine_parts(const RouteArgs& a, int32_t splits, int32_t dtype, void
 
 // ---------------------------------------------------------------- the experts' products
 
+// Bytes that may be read behind the last expert's B where that is a copy.
+constexpr int64_t kCopyRoom = 2;
+
 // The runs of sorted rows that a launch's products are about.
 struct Groups {
     const int32_t* offsets;

@@ -259,6 +259,7 @@ Matrix weights(const void* p, int64_t E, int64_t rows, int64_t width, int32_t dt
     const char* last = (const char*)p + (E - 1) * each * e;
     jobs->job[jobs->n++] = {last, scratch, each, 1, each, up8(each), 0};
     m.shift = (int64_t)((uintptr_t)scratch - (uintptr_t)last);
+    m.end = (const char*)p + E * each * e;   // (rows of small experts before the last are read up to there)
     return m;
 }
 

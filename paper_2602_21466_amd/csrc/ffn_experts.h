@@ -35,8 +35,8 @@ __device__ __forceinline__ void rows_group(const TileArgs& p, const Groups& g, i
     Run r = find_tile(g, lane, BM, 0, first, t / p.tiles_n);
     const int its = Scan::tiles_of(r.end - r.begin, BM, 0), bands = (its + 7) >> 3;
     walk(t % p.tiles_n + r.tile * p.tiles_n, its, p.tiles_n, (its + bands - 1) / bands, tm, tn);
-    const int64_t shift = r.expert == g.experts - 1 ? g.b_shift : 0;
-    const Exact xa = {(const char*)g.a_end, g.source, (uint32_t)g.per_row, (uint32_t)g.rows}, xb = {(const char*)g.b_end + shift, nullptr, 1, 0};
+    const int64_t shift = r.expert == g.experts - 1 ? g.b_shift : 0, behind = shift ? shift + kCopyRoom : 0;
+    const Exact xa = {(const char*)g.a_end, g.source, (uint32_t)g.per_row, (uint32_t)g.rows}, xb = {(const char*)g.b_end + behind, nullptr, 1, 0};
     Work w = {p.a, (const char*)p.b + r.expert * g.b_step + shift, (int64_t)r.begin + (int64_t)tm * BM, r.end, p.K, 0, p.M, tn, split, xa, xb, nullptr};
     if constexpr (CUT) {
         if (quarter) {

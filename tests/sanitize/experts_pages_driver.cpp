@@ -32,27 +32,35 @@ static volatile unsigned char sink;
 static void read_all(const void* from, const void* end) {
     for (const char* p = (const char*)from; p < (const char*)end; ++p) sink = sink + (unsigned char)*p;
 }
-// Every byte that a product may read of B; the last expert's, where they are a copy, are its own values.
-static int rows_seen(const ffn::TileArgs& t, const ffn::Groups& g) {
+// Every byte that a product reads of B; the last expert's, where they are a copy, are its own values.
+static int rows_seen(const ffn::TileArgs& t, const ffn::Groups& g, int size, int epi, bool cols) {
     ++tiled;
-    // (four bytes at a time, where rows start on four: what is left of them is not read)
-    const char* end = (const char*)g.b_end;
-    read_all(t.b, g.b_shift ? end - 2 : t.ldb % 2 == 0 ? end - (end - (const char*)t.b) % 4 : end);
+    // as the loads go: 16 bytes of a row at a time, of which the words that are wholly before the end
+    const int64_t rows = cols ? t.K : epi == ffn::kGate ? 2 * t.N : t.N, width = (cols ? t.N : t.K) * size;
+    for (int e = 0; e < g.experts; ++e) {
+        const int64_t shift = e == g.experts - 1 ? g.b_shift : 0;
+        const uintptr_t base = (uintptr_t)t.b + e * g.b_step + shift, end = (uintptr_t)g.b_end + (shift ? shift + ffn::kCopyRoom : 0);
+        for (int64_t r = 0; r < rows; ++r)
+            for (int64_t at = 0; at < (width + 15) / 16 * 16; at += 4) {
+                const uintptr_t word = base + r * t.ldb * size + at;
+                if (word + 4 <= end) read_all((const void*)word, (const void*)(word + 4));
+            }
+    }
     if (g.b_shift == 0) return 0;
     ++copies;
     const char *b = (const char*)t.b + (g.experts - 1) * g.b_step, *last = (const char*)((uintptr_t)b + g.b_shift);
-    EXPECT(last >= ws_begin && last + g.b_step + 2 <= ws_end && (const char*)g.b_end == b + g.b_step + 2);
+    EXPECT(last >= ws_begin && last + g.b_step + 2 <= ws_end && (const char*)g.b_end == b + g.b_step + 2 - ffn::kCopyRoom);
     EXPECT(std::memcmp(last, b, g.b_step) == 0);
     return 0;
 }
 namespace ffn {
-#define BY_TYPE(NAME, PARAMS, RUN)      \
-    int NAME##_fp32 PARAMS { RUN; return 0; }  \
-    int NAME##_bf16 PARAMS { RUN; return 0; }  \
-    int NAME##_fp16 PARAMS { RUN; return 0; }
-BY_TYPE(launch_expert_rows, (const TileArgs& t, const Groups& g, int32_t, bool, int32_t, void*), rows_seen(t, g))
+#define BY_TYPE(NAME, PARAMS, RUN)                                     \
+    int NAME##_fp32 PARAMS { constexpr int kSize = 4; RUN; return kSize - 4; }  \
+    int NAME##_bf16 PARAMS { constexpr int kSize = 2; RUN; return kSize - 2; }  \
+    int NAME##_fp16 PARAMS { constexpr int kSize = 2; RUN; return kSize - 2; }
+BY_TYPE(launch_expert_rows, (const TileArgs& t, const Groups& g, int32_t epi, bool cols, int32_t, void*), rows_seen(t, g, kSize, epi, cols))
 BY_TYPE(launch_expert_few, (const FewArgs&, const Groups&, int32_t, int32_t, int32_t, int32_t, int64_t, void*), ++few)
-BY_TYPE(launch_expert_grads, (const ExpertGrads& a, int32_t, void*), if (a.t[0].a) rows_seen(a.t[0], a.g[0]))
+BY_TYPE(launch_expert_grads, (const ExpertGrads& a, int32_t, void*), if (a.t[0].a) rows_seen(a.t[0], a.g[0], kSize, kPartial, true))
 int launch_pack(PackJobs jobs, int32_t dtype, void*) {
     for (int k = 0; k < jobs.n; ++k)
         for (int64_t r = 0, e = dtype == FFN_FP32 ? 4 : 2; r < jobs.job[k].rows; ++r) {
@@ -125,6 +133,9 @@ int main() {
     page_ends(2, 8, 257, 64, 300);     // of w_out
     page_ends(4, 7, 9, 48, 1000);      // of both
     page_ends(1, 64, 64, 8, 300);      // of none
+    page_ends(8, 1, 1, 8, 1000);       // of experts whose weights are less than what is read at a time
+    page_ends(16, 3, 1, 1, 2000);
+    page_ends(8, 8, 3, 1, 1000);
     EXPECT(tiled > 0 && copies >= 8);
     if (fails) return 1;
     std::printf("workspaces OK\n");

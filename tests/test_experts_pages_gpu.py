@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("E,di,df,do,N", [(3, 9, 256, 8, 300), (2, 8, 257, 64, 300), (4, 7, 9, 48, 1000), (1, 9, 24, 8, 500),
-                                          (2, 1023, 1024, 520, 20000)])
+                                          (2, 1023, 1024, 520, 20000), (8, 1, 1, 8, 3000), (8, 8, 3, 1, 3000)])
 @pytest.mark.parametrize("kind", ["even", "one"])
 def test_arrays_that_end_with_a_page(E, di, df, do, N, kind, dtype):
     torch, lib = _setup()
